@@ -190,6 +190,168 @@ int adpsgd_step(float* theta, float* theta_peer, const float* const* grads, int3
                 float scale, int64_t n, float lr, uint32_t flags, void* theta_lp,
                 hipStream_t stream);
 
+/* ---------------------------------------------------------------------------
+ * Selective state space scan and its short causal convolution: the recurrence
+ * of a causal (streaming) acoustic model, where the LSTM stack above needs
+ * the whole chunk.  Frame-major as above, each activation tensor with a row
+ * pitch of its own: element (t, b, j) is at (t*B + b)*ld + j, so halves and
+ * columns of a wider projection are read and written where they lie.
+ * Activations hold the precision's type, parameters and their gradients are
+ * float32, the scan's state is float32, sums and states are float32 inside.
+ *   D channels in G groups of D/G adjacent ones, N states per channel
+ *   (1..64), W convolution taps (1..8), T frames, B sequences; T*B at most
+ *   2^24.
+ *   lens (NULL, or B int32 on the device): frames t >= lens[b] do not belong
+ *   to sequence b (values outside 0..T count as the nearer end).  Their inputs
+ *   are not read, outputs and gradients there are zero, and the state
+ *   behind the last frame is the one after frame lens[b] - 1.
+ * Outputs must not overlap each other or an input, except where said.
+ * ------------------------------------------------------------------------- */
+typedef struct ssm_dims {
+  int32_t T, B, D, N, G, W, precision;
+} ssm_dims;
+
+enum {
+  SSM_SOFTPLUS = 1u,   /* scan: step = softplus(dt + dt_bias), else dt + dt_bias */
+  SSM_SILU = 2u        /* convolution: y = silu(pre), else y = pre */
+};
+
+/* Sizes in bytes of caller-allocated buffers:
+ *   saved    -- states that ssm_scan_fwd keeps for ssm_scan_bwd
+ *   fwd, bwd -- scratch of ssm_scan_fwd and ssm_scan_bwd
+ *   conv_bwd -- scratch of ssm_conv_bwd
+ * A buffer belongs to one call (or one captured graph) at a time.  Any output
+ * pointer may be NULL.  Returns 0 or BLSTM_EINVAL/EUNSUPPORTED. */
+int ssm_workspace_bytes(const ssm_dims* dims, size_t* saved, size_t* fwd, size_t* bwd, size_t* conv_bwd);
+
+/* pre[t] = bias + sum_j w[j] x[t - W + 1 + j] per channel, y = silu(pre) or pre.
+ *   w [D][W] float32 (the last tap meets the current frame), bias [D] or NULL
+ *   state      [B][W-1][D] (precision's type): the W-1 inputs before frame 0,
+ *              oldest first; NULL for zeros
+ *   state_out  the same behind the last frame, or NULL; another buffer than state. */
+int ssm_conv_fwd(const ssm_dims* dims, const void* x, int64_t ldx, const float* w, const float* bias,
+                 const int32_t* lens, const void* state, void* y, int64_t ldy, void* state_out, uint32_t flags,
+                 hipStream_t stream);
+
+/* Gradients of ssm_conv_fwd: dx, dw [D][W], dbias [D] (or NULL) and dstate
+ * [B][W-1][D] (or NULL) given dy and, where the loss depends on state_out,
+ * dstate_out [B][W-1][D] (or NULL), both in the precision's type.  All are
+ * overwritten. */
+int ssm_conv_bwd(const ssm_dims* dims, const void* x, int64_t ldx, const float* w, const float* bias,
+                 const int32_t* lens, const void* state, const void* dy, int64_t lddy, const void* dstate_out,
+                 void* dx, int64_t lddx, float* dw, float* dbias, void* dstate, void* ws, uint32_t flags,
+                 hipStream_t stream);
+
+/* One frame (T = 1) of B streams.  state [n_slots][W-1][D] is updated in
+ * place; stream b's is row slots[b] (device int32), or row b where slots is
+ * NULL (n_slots >= B then).  A slot outside 0..n_slots-1 means no stream: its y is
+ * zero and no state changes.  Where several rows name one slot, the first of
+ * them is the stream and the others count as none. */
+int ssm_conv_step(const ssm_dims* dims, const void* x, int64_t ldx, const float* w, const float* bias,
+                  const int32_t* slots, int32_t n_slots, void* state, void* y, int64_t ldy, uint32_t flags,
+                  hipStream_t stream);
+
+/* The scan's inputs.  Per sequence, channel d of group g and state n:
+ *   s_t = softplus(dt_t + dt_bias) (SSM_SOFTPLUS) or dt_t + dt_bias
+ *   h_t[n] = exp(s_t A[d][n]) h_{t-1}[n] + s_t x_t B_t[g][n],   h_{-1} = h0 or 0
+ *   o_t = sum_n C_t[g][n] h_t[n] + Dskip[d] x_t
+ *   y_t = o_t silu(z_t)   (z given), else o_t
+ * x, dt, z [T][B][D]; Bm, Cm [T][B][G*N]; A [D][N]; Dskip, dt_bias [D];
+ * h0 [B][D][N].  z, Dskip, dt_bias, h0 and lens may be NULL. */
+typedef struct ssm_scan_in {
+  const void *x, *dt, *Bm, *Cm, *z;
+  int64_t ldx, lddt, ldb, ldc, ldz;
+  const float *A, *Dskip, *dt_bias, *h0;
+  const int32_t* lens;
+  uint32_t flags;
+} ssm_scan_in;
+
+/* y [T][B][D]; h_last [B][D][N] (or NULL; may equal h0): the state behind each sequence's last
+ * frame; saved: what ssm_scan_bwd reads, or NULL where there is no backward;
+ * ws: scratch. */
+int ssm_scan_fwd(const ssm_dims* dims, const ssm_scan_in* in, void* y, int64_t ldy, float* h_last, void* saved,
+                 void* ws, hipStream_t stream);
+
+/* Gradients of ssm_scan_fwd's inputs, all overwritten.  dx, ddt, dz [T][B][D]
+ * and dBm, dCm [T][B][G*N] in the precision's type, the others float32.
+ * dz is required with z; dDskip, ddt_bias and dh0 may be NULL.
+ * dh_last [B][D][N]: the loss gradient of h_last, NULL for zeros. */
+typedef struct ssm_scan_grads {
+  void *dx, *ddt, *dBm, *dCm, *dz;
+  int64_t lddx, ldddt, lddb, lddc, lddz;
+  float *dA, *dDskip, *ddt_bias, *dh0;
+} ssm_scan_grads;
+
+/* in: as given to that ssm_scan_fwd (h0 itself is not read again), saved: as
+ * it left it; dy [T][B][D] in the precision's type. */
+int ssm_scan_bwd(const ssm_dims* dims, const ssm_scan_in* in, const void* dy, int64_t lddy, const float* dh_last,
+                 const void* saved, const ssm_scan_grads* out, void* ws, hipStream_t stream);
+
+/* One frame (T = 1) of B streams; in->h0 and in->lens are ignored.  state
+ * [n_slots][D][N] float32 is updated in place; slots as in ssm_conv_step. */
+int ssm_scan_step(const ssm_dims* dims, const ssm_scan_in* in, const int32_t* slots, int32_t n_slots, float* state,
+                  void* y, int64_t ldy, hipStream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * Distillation: a student's head trained on a teacher's top logits.
+ * ------------------------------------------------------------------------- */
+#define SOFTMAX_MAX_TOP 256
+#define SOFTMAX_MAX_CLASSES (1 << 18)
+
+/* The k largest logits of every row and what the others weigh:
+ *   top  [M][k] float32, the logits themselves in descending order
+ *   idx  [M][k] int32, their classes; among equal logits the lower class first
+ *   rest [M] float32 (or NULL), log of the sum over the other classes of
+ *        exp(logit / temperature); -inf where there are none
+ * logits [M][K] of the precision's type, row pitch ld; 1 <= k <= K and
+ * k <= SOFTMAX_MAX_TOP, K <= SOFTMAX_MAX_CLASSES.  A NaN orders above +inf. */
+int softmax_topk_rows(const void* logits, int64_t ld, int64_t M, int32_t K, int32_t precision, int32_t k,
+                      float temperature, float* top, int32_t* idx, float* rest, hipStream_t stream);
+
+/* What a row is trained on.  With u = logits / temperature and the k listed
+ * classes' top / temperature and rest (NULL: -inf) normalised to
+ * probabilities p_i and r, the soft loss is the Kullback-Leibler divergence
+ * of the student's softmax(u) from them, the classes that are not listed as one
+ * bucket; the hard loss is the cross-entropy of softmax(logits) with labels:
+ *   row_loss = weight (soft temperature^2 KL + hard CE)
+ * An entry whose idx is outside 0..K-1 is absent; a class listed twice has
+ * both probabilities; a row without entries and rest has no soft loss.
+ * labels (NULL: none) outside 0..K-1: the row has no hard loss.
+ * weights [M] float32 (NULL: ones): a row of weight 0 has loss and gradient 0
+ * whatever it holds. */
+typedef struct softmax_teacher {
+  const float* top;       /* [M][k] */
+  const int32_t* idx;     /* [M][k] */
+  const float* rest;      /* [M] or NULL */
+  const int32_t* labels;  /* [M] or NULL */
+  const float* weights;   /* [M] or NULL */
+  int32_t k;              /* 1..SOFTMAX_MAX_TOP */
+  float temperature, soft, hard;
+} softmax_teacher;
+
+/* row_loss [M] float32 as above (without loss_scale) and dlogits [M][K] =
+ * loss_scale * d(sum of row losses)/dlogits in the precision's type, row pitch
+ * ldd.  dlogits may equal logits where ldd = ld. */
+int softmax_distill_rows(const void* logits, int64_t ld, int64_t M, int32_t K, int32_t precision,
+                         const softmax_teacher* teacher, float loss_scale, float* row_loss, void* dlogits,
+                         int64_t ldd, hipStream_t stream);
+
+/* The two on the acoustic model's head, from y_top, for dims as above (bf16:
+ * the logits are float32 throughout, as in softmax_ce_fwd_bwd).
+ * softmax_head_ws_bytes: size of ws for either. */
+int softmax_head_ws_bytes(const blstm_dims* dims, size_t* bytes);
+
+/* softmax_topk_rows of the head's logits for the T*B frames of y_top. */
+int softmax_topk(const blstm_dims* dims, const float* theta, const void* theta_lp, const void* y_top, int32_t k,
+                 float temperature, float* top, int32_t* idx, float* rest, void* ws, hipStream_t stream);
+
+/* softmax_ce_fwd_bwd with the teacher's loss in place of the cross-entropy:
+ * *loss = loss_scale * sum of the row losses, dy_top and the head slots of
+ * grad as there. */
+int softmax_distill_fwd_bwd(const blstm_dims* dims, const float* theta, const void* theta_lp, const void* y_top,
+                            const softmax_teacher* teacher, float loss_scale, float* loss, float* dy_top,
+                            float* grad, void* ws, hipStream_t stream);
+
 /* Message describing the last failure on the calling thread ("" if none). */
 const char* blstm_last_error(void);
 

@@ -23,11 +23,39 @@ HEAD_STATIC_SCRATCH_BYTES = 64 << 20   # the static head workspace (adpsgd_blstm
 
 EXPORTED = ("blstm_param_count", "blstm_workspace_bytes", "blstm_pack_params", "blstm_fwd",
             "softmax_ce_fwd_bwd", "softmax_ce_fwd_bwd_static", "blstm_bwd", "replica_grad_reduce", "adpsgd_step",
-            "blstm_recurrence_ok", "blstm_last_error", "blstm_timing_begin", "blstm_timing_end")
+            "blstm_recurrence_ok", "blstm_last_error", "blstm_timing_begin", "blstm_timing_end",
+            "ssm_workspace_bytes", "ssm_conv_fwd", "ssm_conv_bwd", "ssm_conv_step", "ssm_scan_fwd", "ssm_scan_bwd",
+            "ssm_scan_step", "softmax_topk_rows", "softmax_distill_rows", "softmax_head_ws_bytes", "softmax_topk",
+            "softmax_distill_fwd_bwd")
+SSM_SOFTPLUS = 1
+SSM_SILU = 2
+SOFTMAX_MAX_TOP = 256                  # most listed classes a row (adpsgd_blstm.h)
+SOFTMAX_MAX_CLASSES = 1 << 18
 
 
 class Dims(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("L", "D", "H", "P", "K", "T", "B", "precision")]
+
+
+class SsmDims(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("T", "B", "D", "N", "G", "W", "precision")]
+
+
+class SsmScanIn(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("x", "dt", "Bm", "Cm", "z")] +
+                [(n, ctypes.c_int64) for n in ("ldx", "lddt", "ldb", "ldc", "ldz")] +
+                [(n, ctypes.c_void_p) for n in ("A", "Dskip", "dt_bias", "h0", "lens")] + [("flags", ctypes.c_uint32)])
+
+
+class SsmScanGrads(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("dx", "ddt", "dBm", "dCm", "dz")] +
+                [(n, ctypes.c_int64) for n in ("lddx", "ldddt", "lddb", "lddc", "lddz")] +
+                [(n, ctypes.c_void_p) for n in ("dA", "dDskip", "ddt_bias", "dh0")])
+
+
+class SoftmaxTeacher(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("top", "idx", "rest", "labels", "weights")] +
+                [("k", ctypes.c_int32)] + [(n, ctypes.c_float) for n in ("temperature", "soft", "hard")])
 
 
 class KernelTime(ctypes.Structure):
@@ -71,6 +99,22 @@ def lib():
         L.blstm_timing_begin.argtypes = [ctypes.c_char_p]
         L.blstm_timing_end.argtypes = [ctypes.POINTER(KernelTime), ctypes.c_int32,
                                        ctypes.POINTER(ctypes.c_int32)]
+        I, I64, U, F = ctypes.c_int32, ctypes.c_int64, ctypes.c_uint32, ctypes.c_float
+        SD, SI, SG, ST = (ctypes.POINTER(c) for c in (SsmDims, SsmScanIn, SsmScanGrads, SoftmaxTeacher))
+        L.ssm_workspace_bytes.argtypes = [SD] + [ctypes.POINTER(S)] * 4
+        L.ssm_conv_fwd.argtypes = [SD, P, I64, P, P, P, P, P, I64, P, U, P]
+        L.ssm_conv_bwd.argtypes = [SD, P, I64, P, P, P, P, P, I64, P, P, I64, P, P, P, P, U, P]
+        L.ssm_conv_step.argtypes = [SD, P, I64, P, P, P, I, P, P, I64, U, P]
+        L.ssm_scan_fwd.argtypes = [SD, SI, P, I64, P, P, P, P]
+        L.ssm_scan_bwd.argtypes = [SD, SI, P, I64, P, P, SG, P, P]
+        L.ssm_scan_step.argtypes = [SD, SI, P, I, P, P, I64, P]
+        L.softmax_topk_rows.argtypes = [P, I64, I64, I, I, I, F, P, P, P, P]
+        L.softmax_distill_rows.argtypes = [P, I64, I64, I, I, ST, F, P, P, I64, P]
+        L.softmax_head_ws_bytes.argtypes = [DP, ctypes.POINTER(S)]
+        L.softmax_topk.argtypes = [DP, P, P, P, I, F, P, P, P, P, P]
+        L.softmax_distill_fwd_bwd.argtypes = [DP, P, P, P, ST, F, P, P, P, P, P]
+        for name in EXPORTED[-12:]:
+            getattr(L, name).restype = ctypes.c_int
         for name in ("blstm_workspace_bytes", "blstm_pack_params", "blstm_fwd", "softmax_ce_fwd_bwd",
                      "softmax_ce_fwd_bwd_static",
                      "blstm_bwd", "replica_grad_reduce", "adpsgd_step", "blstm_timing_begin",
@@ -181,3 +225,270 @@ def blstm_timing_end(cap: int = 64) -> dict:
     count = ctypes.c_int32()
     _check("blstm_timing_end", lib().blstm_timing_end(buf, cap, ctypes.byref(count)))
     return {buf[i].name.decode(): (buf[i].launches, buf[i].total_ms) for i in range(min(count.value, cap))}
+
+
+# ------------------------------------------------------- state space operators ---
+# Tensors are checked against the dims here, before their addresses are given
+# to the library: a ValueError names the argument.
+def _on(x):
+    """The device index the call runs on, from its first tensor."""
+    if not x.is_cuda:
+        raise ValueError("tensors must be on the GPU")
+    return x.device
+
+
+def _have(name, t, shape, dtype, device, optional=False):
+    """Address of a contiguous tensor of this shape and type (None for an optional one that is absent)."""
+    if t is None:
+        if optional:
+            return None
+        raise ValueError(f"{name} is required")
+    if t.dtype != dtype or t.device != device or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {shape} on {device}: got {t.dtype} "
+                         f"{tuple(t.shape)} with strides {t.stride()} on {t.device}")
+    return t.data_ptr()
+
+
+def _rows(name, t, shape, dtype, device, optional=False):
+    """(address, row pitch) of a tensor whose last axis is contiguous and whose leading axes are rows at one pitch."""
+    if t is None:
+        if optional:
+            return None, 0
+        raise ValueError(f"{name} is required")
+    ok = t.dtype == dtype and t.device == device and tuple(t.shape) == shape and (shape[-1] == 1 or t.stride(-1) == 1)
+    if ok and len(shape) == 1:
+        return t.data_ptr(), shape[0]
+    if ok:
+        # the pitch, from the innermost of the leading axes with more than one row
+        st, ld, n = t.stride(), 0, 1
+        for i in range(len(shape) - 2, -1, -1):
+            if shape[i] > 1:
+                if not ld:
+                    ld = st[i]
+                ok = ok and st[i] == ld * n
+                n *= shape[i]
+        if not ld:
+            ld = shape[-1]
+        if ok and ld >= shape[-1]:
+            return t.data_ptr(), ld
+    raise ValueError(f"{name} must be {dtype} rows of shape {shape} on {device}, adjacent elements along the last "
+                     f"axis and one pitch from row to row: got {t.dtype} {tuple(t.shape)} with strides {t.stride()} "
+                     f"on {t.device}")
+
+
+def _call(fn, device, stream, *args):
+    """Calls fn on `device` (made current for the launch if it is not) and `stream`."""
+    import torch
+    if device.index == torch.cuda.current_device():
+        return _check(fn, getattr(lib(), fn)(*args, _stream(stream)))
+    with torch.cuda.device(device):
+        return _check(fn, getattr(lib(), fn)(*args, _stream(stream)))
+
+
+def _bytes(name, t, n, device):
+    if n == 0:
+        return None
+    if t is None or not t.is_contiguous() or t.device != device or t.numel() * t.element_size() < n:
+        raise ValueError(f"{name} must be a contiguous buffer of at least {n} bytes on {device} (ssm_workspace_bytes)")
+    if t.data_ptr() % 16:
+        raise ValueError(f"{name} must be 16-byte aligned")
+    return t.data_ptr()
+
+
+def _elem(dims):
+    import torch
+    return torch.bfloat16 if dims.precision == BLSTM_BF16 else torch.float32
+
+
+def make_ssm_dims(T, B, D, N=1, G=1, W=1, precision="bf16"):
+    if isinstance(precision, str):
+        precision = {"fp32": BLSTM_FP32, "bf16": BLSTM_BF16}[precision]
+    return SsmDims(T, B, D, N, G, W, precision)
+
+
+def ssm_workspace_bytes(dims: SsmDims) -> dict:
+    vals = [ctypes.c_size_t() for _ in range(4)]
+    _check("ssm_workspace_bytes", lib().ssm_workspace_bytes(ctypes.byref(dims), *[ctypes.byref(v) for v in vals]))
+    return dict(zip(("saved", "fwd", "bwd", "conv_bwd"), (v.value for v in vals)))
+
+
+def _ssm_bytes(dims):
+    """ssm_workspace_bytes, looked up once per dims object and values."""
+    key = (dims.T, dims.B, dims.D, dims.N, dims.G, dims.W, dims.precision)
+    got = dims.__dict__.get("sizes")
+    if got is None or got[0] != key:
+        got = dims.__dict__["sizes"] = (key, ssm_workspace_bytes(dims))
+    return got[1]
+
+
+def ssm_conv_fwd(dims, x, w, bias, y, lens=None, state=None, state_out=None, silu=True, stream=None):
+    import torch
+    dev, e = _on(x), _elem(dims)
+    T, B, D, W = dims.T, dims.B, dims.D, dims.W
+    px, ldx = _rows("x", x, (T, B, D), e, dev)
+    py, ldy = _rows("y", y, (T, B, D), e, dev)
+    return _call("ssm_conv_fwd", dev, stream, ctypes.byref(dims), px, ldx,
+                 _have("w", w, (D, W), torch.float32, dev), _have("bias", bias, (D,), torch.float32, dev, True),
+                 _have("lens", lens, (B,), torch.int32, dev, True), _have("state", state, (B, W - 1, D), e, dev, True),
+                 py, ldy, _have("state_out", state_out, (B, W - 1, D), e, dev, True), SSM_SILU if silu else 0)
+
+
+def ssm_conv_bwd(dims, x, w, bias, dy, dx, dw, dbias, ws, lens=None, state=None, dstate=None, dstate_out=None,
+                 silu=True, stream=None):
+    import torch
+    dev, e, f = _on(x), _elem(dims), torch.float32
+    T, B, D, W = dims.T, dims.B, dims.D, dims.W
+    px, ldx = _rows("x", x, (T, B, D), e, dev)
+    pdy, lddy = _rows("dy", dy, (T, B, D), e, dev)
+    pdx, lddx = _rows("dx", dx, (T, B, D), e, dev)
+    return _call("ssm_conv_bwd", dev, stream, ctypes.byref(dims), px, ldx, _have("w", w, (D, W), f, dev),
+                 _have("bias", bias, (D,), f, dev, True), _have("lens", lens, (B,), torch.int32, dev, True),
+                 _have("state", state, (B, W - 1, D), e, dev, True), pdy, lddy,
+                 _have("dstate_out", dstate_out, (B, W - 1, D), e, dev, True), pdx, lddx,
+                 _have("dw", dw, (D, W), f, dev), _have("dbias", dbias, (D,), f, dev, True),
+                 _have("dstate", dstate, (B, W - 1, D), e, dev, True),
+                 _bytes("ws", ws, _ssm_bytes(dims)["conv_bwd"], dev), SSM_SILU if silu else 0)
+
+
+def _slots(state, slots, B, row, dtype, dev):
+    """(state's address, its rows, slots' address); state is [rows][*row]."""
+    import torch
+    if state is None or state.dim() != 1 + len(row):
+        raise ValueError(f"state must be a tensor of rows of shape {row}")
+    n = state.shape[0]
+    return (_have("state", state, (n, *row), dtype, dev), n,
+            _have("slots", slots, (B,), torch.int32, dev, True))
+
+
+def ssm_conv_step(dims, x, w, bias, state, y, slots=None, silu=True, stream=None):
+    import torch
+    dev, e = _on(x), _elem(dims)
+    B, D, W = dims.B, dims.D, dims.W
+    px, ldx = _rows("x", x, (B, D), e, dev)
+    py, ldy = _rows("y", y, (B, D), e, dev)
+    ps, n, psl = _slots(state, slots, B, (W - 1, D), e, dev)
+    return _call("ssm_conv_step", dev, stream, ctypes.byref(dims), px, ldx, _have("w", w, (D, W), torch.float32, dev),
+                 _have("bias", bias, (D,), torch.float32, dev, True), psl, n, ps, py, ldy, SSM_SILU if silu else 0)
+
+
+def _scan_in(dims, lead, dev, x, dt, A, Bm, Cm, Dskip, z, dt_bias, h0, lens, softplus):
+    import torch
+    e, f = _elem(dims), torch.float32
+    B, D, N, GN = dims.B, dims.D, dims.N, dims.G * dims.N
+    px, ldx = _rows("x", x, (*lead, D), e, dev)
+    pdt, lddt = _rows("dt", dt, (*lead, D), e, dev)
+    pb, ldb = _rows("Bm", Bm, (*lead, GN), e, dev)
+    pc, ldc = _rows("Cm", Cm, (*lead, GN), e, dev)
+    pz, ldz = _rows("z", z, (*lead, D), e, dev, True)
+    return SsmScanIn(px, pdt, pb, pc, pz, ldx, lddt, ldb, ldc, ldz, _have("A", A, (D, N), f, dev),
+                     _have("Dskip", Dskip, (D,), f, dev, True), _have("dt_bias", dt_bias, (D,), f, dev, True),
+                     _have("h0", h0, (B, D, N), f, dev, True), _have("lens", lens, (B,), torch.int32, dev, True),
+                     SSM_SOFTPLUS if softplus else 0)
+
+
+def ssm_scan_fwd(dims, x, dt, A, Bm, Cm, y, ws, Dskip=None, z=None, dt_bias=None, h0=None, h_last=None, lens=None,
+                 softplus=True, saved=None, stream=None):
+    import torch
+    dev = _on(x)
+    T, B, D, N = dims.T, dims.B, dims.D, dims.N
+    arg = _scan_in(dims, (T, B), dev, x, dt, A, Bm, Cm, Dskip, z, dt_bias, h0, lens, softplus)
+    py, ldy = _rows("y", y, (T, B, D), _elem(dims), dev)
+    n = _ssm_bytes(dims)
+    return _call("ssm_scan_fwd", dev, stream, ctypes.byref(dims), ctypes.byref(arg), py, ldy,
+                 _have("h_last", h_last, (B, D, N), torch.float32, dev, True),
+                 None if saved is None else _bytes("saved", saved, n["saved"], dev), _bytes("ws", ws, n["fwd"], dev))
+
+
+def ssm_scan_bwd(dims, x, dt, A, Bm, Cm, dy, saved, ws, dx, ddt, dA, dBm, dCm, Dskip=None, dDskip=None, z=None,
+                 dz=None, dt_bias=None, ddt_bias=None, dh_last=None, dh0=None, lens=None, softplus=True, stream=None):
+    import torch
+    dev, e, f = _on(x), _elem(dims), torch.float32
+    T, B, D, N, GN = dims.T, dims.B, dims.D, dims.N, dims.G * dims.N
+    arg = _scan_in(dims, (T, B), dev, x, dt, A, Bm, Cm, Dskip, z, dt_bias, None, lens, softplus)
+    pdy, lddy = _rows("dy", dy, (T, B, D), e, dev)
+    pdx, lddx = _rows("dx", dx, (T, B, D), e, dev)
+    pdt, ldddt = _rows("ddt", ddt, (T, B, D), e, dev)
+    pdb, lddb = _rows("dBm", dBm, (T, B, GN), e, dev)
+    pdc, lddc = _rows("dCm", dCm, (T, B, GN), e, dev)
+    pdz, lddz = _rows("dz", dz, (T, B, D), e, dev, z is None)
+    out = SsmScanGrads(pdx, pdt, pdb, pdc, pdz, lddx, ldddt, lddb, lddc, lddz, _have("dA", dA, (D, N), f, dev),
+                       _have("dDskip", dDskip, (D,), f, dev, True), _have("ddt_bias", ddt_bias, (D,), f, dev, True),
+                       _have("dh0", dh0, (B, D, N), f, dev, True))
+    n = _ssm_bytes(dims)
+    return _call("ssm_scan_bwd", dev, stream, ctypes.byref(dims), ctypes.byref(arg), pdy, lddy,
+                 _have("dh_last", dh_last, (B, D, N), f, dev, True), _bytes("saved", saved, n["saved"], dev),
+                 ctypes.byref(out), _bytes("ws", ws, n["bwd"], dev))
+
+
+def ssm_scan_step(dims, x, dt, A, Bm, Cm, state, y, Dskip=None, z=None, dt_bias=None, slots=None, softplus=True,
+                  stream=None):
+    import torch
+    dev = _on(x)
+    B, D, N = dims.B, dims.D, dims.N
+    arg = _scan_in(dims, (B,), dev, x, dt, A, Bm, Cm, Dskip, z, dt_bias, None, None, softplus)
+    py, ldy = _rows("y", y, (B, D), _elem(dims), dev)
+    ps, n, psl = _slots(state, slots, B, (D, N), torch.float32, dev)
+    return _call("ssm_scan_step", dev, stream, ctypes.byref(dims), ctypes.byref(arg), psl, n, ps, py, ldy)
+
+
+# ---------------------------------------------------------------- distillation ---
+def _logits(logits):
+    import torch
+    if logits.dim() != 2 or logits.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError(f"logits must be bfloat16 or float32 rows [M][K]: got {logits.dtype} {tuple(logits.shape)}")
+    M, K = logits.shape
+    p, ld = _rows("logits", logits, (M, K), logits.dtype, _on(logits))
+    return p, ld, M, K, BLSTM_BF16 if logits.dtype == torch.bfloat16 else BLSTM_FP32
+
+
+def softmax_topk_rows(logits, top, idx, rest=None, temperature=1.0, stream=None):
+    """k is top's width."""
+    import torch
+    p, ld, M, K, prec = _logits(logits)
+    dev, k = logits.device, top.shape[-1]
+    return _call("softmax_topk_rows", dev, stream, p, ld, M, K, prec, k, temperature,
+                 _have("top", top, (M, k), torch.float32, dev), _have("idx", idx, (M, k), torch.int32, dev),
+                 _have("rest", rest, (M,), torch.float32, dev, True))
+
+
+def _teacher(M, dev, top, idx, rest, labels, weights, temperature, soft, hard):
+    import torch
+    k = top.shape[-1]
+    return SoftmaxTeacher(_have("top", top, (M, k), torch.float32, dev), _have("idx", idx, (M, k), torch.int32, dev),
+                          _have("rest", rest, (M,), torch.float32, dev, True),
+                          _have("labels", labels, (M,), torch.int32, dev, True),
+                          _have("weights", weights, (M,), torch.float32, dev, True), k, temperature, soft, hard)
+
+
+def softmax_distill_rows(logits, top, idx, row_loss, dlogits, rest=None, labels=None, weights=None, temperature=1.0,
+                         soft=1.0, hard=0.0, loss_scale=1.0, stream=None):
+    import torch
+    p, ld, M, K, prec = _logits(logits)
+    dev = logits.device
+    t = _teacher(M, dev, top, idx, rest, labels, weights, temperature, soft, hard)
+    pd, ldd = _rows("dlogits", dlogits, (M, K), logits.dtype, dev)
+    return _call("softmax_distill_rows", dev, stream, p, ld, M, K, prec, ctypes.byref(t), loss_scale,
+                 _have("row_loss", row_loss, (M,), torch.float32, dev), pd, ldd)
+
+
+def softmax_head_ws_bytes(dims: Dims) -> int:
+    n = ctypes.c_size_t()
+    _check("softmax_head_ws_bytes", lib().softmax_head_ws_bytes(ctypes.byref(dims), ctypes.byref(n)))
+    return n.value
+
+
+def softmax_topk(dims, theta, theta_lp, y_top, top, idx, ws, rest=None, temperature=1.0, stream=None):
+    """top, idx [T*B][k], rest [T*B]; k is top's width."""
+    import torch
+    dev, M, k = _on(y_top), dims.T * dims.B, top.shape[-1]
+    return _call("softmax_topk", dev, stream, ctypes.byref(dims), _ptr(theta), _ptr(theta_lp), _ptr(y_top), k,
+                 temperature, _have("top", top, (M, k), torch.float32, dev), _have("idx", idx, (M, k), torch.int32, dev),
+                 _have("rest", rest, (M,), torch.float32, dev, True), _ptr(ws))
+
+
+def softmax_distill_fwd_bwd(dims, theta, theta_lp, y_top, top, idx, loss_scale, loss, dy_top, grad, ws, rest=None,
+                            labels=None, weights=None, temperature=1.0, soft=1.0, hard=0.0, stream=None):
+    dev, M = _on(y_top), dims.T * dims.B
+    t = _teacher(M, dev, top, idx, rest, labels, weights, temperature, soft, hard)
+    return _call("softmax_distill_fwd_bwd", dev, stream, ctypes.byref(dims), _ptr(theta), _ptr(theta_lp), _ptr(y_top),
+                 ctypes.byref(t), loss_scale, _ptr(loss), _ptr(dy_top), _ptr(grad), _ptr(ws))

@@ -16,6 +16,7 @@
 #include <type_traits>
 
 #include "common.hpp"
+#include "distill.hpp"
 #include "gemm_kc.hpp"
 #include "reduce.hpp"
 
@@ -983,23 +984,16 @@ static bool logits_block() {
 template <typename T> struct VecH { static constexpr int v = 8; };
 template <> struct VecH<float> { static constexpr int v = 4; };
 
+// z = y W_l^T + b_l.  bf16: split over k (only P/128 column blocks), the
+// fixed-order reduction adds b_l and writes the bf16 z (at 2688 frames the
+// unsplit product in 64-row blocks saves the reduction but gains nothing)
 template <typename T>
-static int head_impl(const Layout& lo, const float* theta, const T* W, const T* ytop,
-                     const int32_t* labels, float scale, float* loss, float* dytop, float* grad,
-                     char* hws, hipStream_t s) {
+static void head_z(const Layout& lo, const float* theta, const T* W, const T* ytop, char* hws, hipStream_t s) {
   constexpr int V = VecH<T>::v;
   const int64_t M = lo.M;
-  const int P = lo.P, K = lo.K, Kp = lo.Kp, H2 = 2 * lo.H;
+  const int P = lo.P, H2 = 2 * lo.H;
   T* Z = (T*)(hws + lo.Z);
-  float* RL = (float*)(hws + lo.RL);
-  float* DZ = (float*)(hws + lo.DZ);
-  T* DZT = (T*)(hws + lo.DZT);
-  float* csp = (float*)(hws + lo.HCSP);
   float* part = (float*)(hws + lo.HSKP);
-
-  // z = y W_l^T + b_l.  bf16: split over k (only P/128 column blocks), the
-  // fixed-order reduction adds b_l and writes the bf16 z (at 2688 frames the
-  // unsplit product in 64-row blocks saves the reduction but gains nothing)
   if (std::is_same<T, bf16>::value && lo.sp_z > 1) {
     gemm_launch<T, true, true, V, V>("gemm_z", s, opnd(ytop, H2, H2, M), opnd(W + lo.Wl, H2, H2, P), M, P, H2, 1,
                                      lo.sp_z, epi_store<float>(part, P, M, P, (int64_t)lo.sp_z * M * P, M * P));
@@ -1010,9 +1004,67 @@ static int head_impl(const Layout& lo, const float* theta, const T* W, const T* 
     gemm_launch<T, true, true, V, V>("gemm_z", s, opnd(ytop, H2, H2, M), opnd(W + lo.Wl, H2, H2, P), M,
                                      P, H2, 1, 1, epi_store<T>(Z, P, M, P, 0, 0, theta + lo.bl));
   }
+}
+
+// Rows of float32 logits that the bf16 head's distillation holds at a time:
+// at 32000 classes 131 MB, which the last-level cache keeps between the
+// product that writes them and the row pass that reads them.
+static constexpr int64_t HEAD_ROWS = 1024;
+// Behind head_ws, bf16: those logits, then column-sum partials of db_s.
+static size_t head_logits_bytes(const Layout& lo) {
+  return lo.es == 2 ? (size_t)std::min(lo.M, HEAD_ROWS) * lo.Kp * 4 : 0;
+}
+static size_t head_extra_bytes(const Layout& lo) {
+  return lo.es == 2 ? head_logits_bytes(lo) + (size_t)COLSUM_MAX_CHUNKS * lo.Kp * 4 : 0;
+}
+// float32 logits of rows [r0, r0 + n) of z (n <= HEAD_ROWS in bf16), row pitch Kp.
+template <typename T>
+static float* head_logits(const Layout& lo, const float* theta, const T* W, char* hws, int64_t r0, int64_t n,
+                          hipStream_t s) {
+  constexpr int V = VecH<T>::v;
+  const T* Z = (const T*)(hws + lo.Z) + r0 * lo.P;
+  float* S = std::is_same<T, bf16>::value ? (float*)(hws + lo.head_bytes) : (float*)(hws + lo.S) + r0 * lo.Kp;
+  gemm_launch<T, true, true, V, V>("gemm_logits", s, opnd(Z, lo.P, lo.P, n), opnd(W + lo.Ws, lo.P, lo.P, lo.K), n,
+                                   lo.K, lo.P, 1, 1, epi_store<float>(S, lo.Kp, n, lo.K, 0, 0, theta + lo.bs));
+  return S;
+}
+
+// The head forward and backward: against labels, or with `teacher` given
+// against a teacher's top logits.
+template <typename T>
+static int head_impl(const Layout& lo, const float* theta, const T* W, const T* ytop,
+                     const int32_t* labels, float scale, float* loss, float* dytop, float* grad,
+                     char* hws, hipStream_t s, const softmax_teacher* teacher = nullptr) {
+  constexpr int V = VecH<T>::v;
+  const int64_t M = lo.M;
+  const int P = lo.P, K = lo.K, Kp = lo.Kp, H2 = 2 * lo.H;
+  T* Z = (T*)(hws + lo.Z);
+  float* RL = (float*)(hws + lo.RL);
+  float* DZ = (float*)(hws + lo.DZ);
+  T* DZT = (T*)(hws + lo.DZT);
+  float* csp = (float*)(hws + lo.HCSP);
+  float* part = (float*)(hws + lo.HSKP);
+
+  head_z<T>(lo, theta, W, ytop, hws, s);
   constexpr bool lp = std::is_same<T, bf16>::value;
   T* DS = (T*)(hws + lo.S);
-  if constexpr (lp) {
+  if (teacher) {
+    // float32: every row's logits at once, overwritten by ds in place; bf16: HEAD_ROWS at a time
+    const int64_t step = lp ? std::min(M, HEAD_ROWS) : M;
+    for (int64_t r0 = 0; r0 < M; r0 += step) {
+      const int64_t n = std::min(step, M - r0);
+      const float* S = head_logits<T>(lo, theta, W, hws, r0, n, s);
+      softmax_teacher t = *teacher;
+      t.top += r0 * t.k;
+      t.idx += r0 * t.k;
+      if (t.rest) t.rest += r0;
+      if (t.labels) t.labels += r0;
+      if (t.weights) t.weights += r0;
+      const int rc = distill_rows<float, T>(S, Kp, n, K, &t, scale, RL + r0, DS + r0 * Kp, Kp, Kp - K, s);
+      if (rc) return rc;
+    }
+    BLSTM_LAUNCH("loss_sum", loss_sum_kernel, dim3(1), dim3(256), 0, s, RL, M, scale, loss);
+  } else if constexpr (lp) {
     // logits transposed (classes x frames) twice: strip statistics, then ds,
     // the frame losses and the db_s partials
     const Opnd Aw = opnd(W + lo.Ws, P, P, K), Bz = opnd(Z, P, P, M);
@@ -1129,8 +1181,15 @@ static int head_impl(const Layout& lo, const float* theta, const T* W, const T* 
     gemm_f32<T, true, false, V, V>("gemm_dz", s, Az, Bz2, M, P, K, 1, lo.sp_dz, DZ, P, 0, part, lp ? DZT : nullptr, P,
                                    lo.big_dz);
   }
-  // db_s and db_l, the sums over frames of ds and dz (bf16: already done)
-  if constexpr (!lp) {
+  // db_s and db_l, the sums over frames of ds and dz (bf16: already done,
+  // but not against a teacher: there of the ds that the products read)
+  if constexpr (lp) {
+    if (teacher) {
+      colsum<T>("colsum_dbs", s, DS, M, K, Kp, (float*)(hws + lo.head_bytes + head_logits_bytes(lo)), K, 0,
+                grad + lo.bs, nullptr);
+      colsum<float>("colsum_dbl", s, DZ, M, P, P, part, P, 0, grad + lo.bl, nullptr);
+    }
+  } else {
     float* csl = part;   // at most M row ranges of P columns: within dz's partials, summed by now
     if (K % 4 != 0 || !colsum2(s, DS, M, K, Kp, csp, grad + lo.bs, DZ, M, P, P, csl, grad + lo.bl)) {
       colsum<T>("colsum_dbs", s, DS, M, K, Kp, csp, K, 0, grad + lo.bs, nullptr);
@@ -1244,4 +1303,64 @@ extern "C" int softmax_ce_fwd_bwd_static(const blstm_dims* dims, const float* th
   }
   return head_impl<float>(lo, theta, theta, (const float*)y_top, labels, loss_scale, loss, dy_top, grad, (char*)ws,
                           stream);
+}
+
+// ---------------------------------------------------------------------------
+// Distillation on the head.
+// ---------------------------------------------------------------------------
+extern "C" int softmax_head_ws_bytes(const blstm_dims* dims, size_t* bytes) {
+  Layout lo;
+  const int rc = make_layout(dims, &lo);
+  if (rc) return rc;
+  if (bytes) *bytes = lo.head_bytes + head_extra_bytes(lo);
+  return BLSTM_OK;
+}
+
+template <typename T>
+static int topk_impl(const Layout& lo, const float* theta, const T* W, const T* ytop, int32_t k, float temperature,
+                     float* top, int32_t* idx, float* rest, char* ws, hipStream_t s) {
+  head_z<T>(lo, theta, W, ytop, ws, s);
+  const int64_t step = std::is_same<T, bf16>::value ? std::min(lo.M, HEAD_ROWS) : lo.M;
+  for (int64_t r0 = 0; r0 < lo.M; r0 += step) {
+    const int64_t n = std::min(step, lo.M - r0);
+    const float* S = head_logits<T>(lo, theta, W, ws, r0, n, s);
+    const int rc = topk_rows<float>(S, lo.Kp, n, lo.K, k, temperature, top + r0 * k, idx + r0 * k,
+                                    rest ? rest + r0 : nullptr, s);
+    if (rc) return rc;
+  }
+  return BLSTM_OK;
+}
+
+extern "C" int softmax_topk(const blstm_dims* dims, const float* theta, const void* theta_lp, const void* y_top,
+                            int32_t k, float temperature, float* top, int32_t* idx, float* rest, void* ws,
+                            hipStream_t stream) {
+  Layout lo;
+  int rc = make_layout(dims, &lo);
+  if (!rc) rc = check_top(k, lo.K, temperature, "softmax_topk");
+  if (rc) return rc;
+  if (!theta || !y_top || !top || !idx || !ws) return blstm_fail(BLSTM_EINVAL, "softmax_topk: NULL pointer");
+  if (lo.prec == BLSTM_BF16) {
+    if (!theta_lp) return blstm_fail(BLSTM_EINVAL, "softmax_topk: theta_lp is NULL (bf16)");
+    return topk_impl<bf16>(lo, theta, (const bf16*)theta_lp, (const bf16*)y_top, k, temperature, top, idx, rest,
+                           (char*)ws, stream);
+  }
+  return topk_impl<float>(lo, theta, theta, (const float*)y_top, k, temperature, top, idx, rest, (char*)ws, stream);
+}
+
+extern "C" int softmax_distill_fwd_bwd(const blstm_dims* dims, const float* theta, const void* theta_lp,
+                                       const void* y_top, const softmax_teacher* teacher, float loss_scale,
+                                       float* loss, float* dy_top, float* grad, void* ws, hipStream_t stream) {
+  Layout lo;
+  int rc = make_layout(dims, &lo);
+  if (!rc) rc = check_teacher(teacher, lo.K, "softmax_distill_fwd_bwd");
+  if (rc) return rc;
+  if (!theta || !y_top || !loss || !dy_top || !grad || !ws)
+    return blstm_fail(BLSTM_EINVAL, "softmax_distill_fwd_bwd: NULL pointer");
+  if (lo.prec == BLSTM_BF16) {
+    if (!theta_lp) return blstm_fail(BLSTM_EINVAL, "softmax_distill_fwd_bwd: theta_lp is NULL (bf16)");
+    return head_impl<bf16>(lo, theta, (const bf16*)theta_lp, (const bf16*)y_top, nullptr, loss_scale, loss, dy_top,
+                           grad, (char*)ws, stream, teacher);
+  }
+  return head_impl<float>(lo, theta, theta, (const float*)y_top, nullptr, loss_scale, loss, dy_top, grad, (char*)ws,
+                          stream, teacher);
 }

@@ -38,6 +38,7 @@ class LearnerStep:
         self.loss = torch.zeros(1, dtype=torch.float32, device=dev)
         self.act_ws = torch.empty(max(sizes["act_ws"], 1), dtype=torch.uint8, device=dev)
         self.head_ws = torch.empty(max(sizes["head_ws"], 1), dtype=torch.uint8, device=dev)
+        self.distill_ws = None   # on first use
         self.loss_scale = 1.0 / (T * B)
 
     # ---------------------------------------------------------------- data ---
@@ -62,13 +63,40 @@ class LearnerStep:
                               self.y_top if y_top is None else y_top, self.labels,
                               self.loss_scale, self.loss, self.dy_top, self.grad, self.head_ws)
 
+    def _distill_ws(self):
+        if self.distill_ws is None:
+            self.distill_ws = torch.empty(bd.softmax_head_ws_bytes(self.dims), dtype=torch.uint8, device=self.device)
+        return self.distill_ws
+
+    def top_logits(self, k, temperature=1.0):
+        """This learner as a teacher, after forward(): the k top logits of every
+        frame, their classes and the log-sum-exp of the other logits over the
+        temperature, as new tensors ([T*B][k], [T*B][k], [T*B])."""
+        M = self.shape["T"] * self.shape["B"]
+        top = torch.empty((M, k), dtype=torch.float32, device=self.device)
+        idx = torch.empty((M, k), dtype=torch.int32, device=self.device)
+        rest = torch.empty(M, dtype=torch.float32, device=self.device)
+        bd.softmax_topk(self.dims, self.theta, self.theta_lp, self.y_top, top, idx, self._distill_ws(), rest,
+                        temperature)
+        return top, idx, rest
+
+    def distill(self, top, idx, rest=None, weights=None, temperature=1.0, soft=1.0, hard=0.0):
+        """head() against a teacher's top logits, mixed with the labels' cross-entropy."""
+        bd.softmax_distill_fwd_bwd(self.dims, self.theta, self.theta_lp, self.y_top, top, idx, self.loss_scale,
+                                   self.loss, self.dy_top, self.grad, self._distill_ws(), rest,
+                                   self.labels.view(-1), weights, temperature, soft, hard)
+
     def backward(self, dy_top=None):
         bd.blstm_bwd(self.dims, self.theta, self.theta_lp, self.act_ws, self.y_top,
                      self.dy_top if dy_top is None else dy_top, self.grad)
 
-    def gradient(self):
+    def gradient(self, teacher=None):
+        """teacher: arguments of distill() in a dict, in place of the labels alone."""
         self.forward()
-        self.head()
+        if teacher is None:
+            self.head()
+        else:
+            self.distill(**teacher)
         self.backward()
 
     def check_recurrence(self):
@@ -80,16 +108,18 @@ class LearnerStep:
         bd.adpsgd_step(self.theta, self.peer, [self.grad] if grads is None else grads, scale, lr,
                        flags, self.theta_lp)
 
-    def step(self, lr, flags=0):
+    def step(self, lr, flags=0, teacher=None):
         """The whole learner step: gradient, then the fused update."""
-        self.gradient()
+        self.gradient(teacher)
         self.update(lr, flags)
 
-    def capture(self, lr, steps=1, flags=0):
+    def capture(self, lr, steps=1, flags=0, teacher=None):
         """Record `steps` learner steps into a HIP graph (replaying it runs
         them again on the current buffers, i.e. continues training)."""
+        if teacher is not None:
+            self._distill_ws()   # allocated outside the graph's memory
         graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(graph):
             for _ in range(steps):
-                self.step(lr, flags)
+                self.step(lr, flags, teacher)
         return graph

@@ -31,12 +31,17 @@ def lr_schedule(epoch: int, base_lr: float, base_batch: int, batch: int, warmup_
 
 
 class Trainer:
-    def __init__(self, step, batches, base_lr: float, base_batch: int, warmup_epochs: int = 10, flags: int = 0):
+    def __init__(self, step, batches, base_lr: float, base_batch: int, warmup_epochs: int = 10, flags: int = 0,
+                 teacher=None, top: int = 32, temperature: float = 1.0, soft: float = 1.0, hard: float = 0.0):
         """step: a LearnerStep with its weights (and peer) loaded; batches:
         list of (features [T][B][D], labels [T][B]) numpy arrays, kept on the
         device.  The batch size of the recipe is the step's B (sequences).
         flags: the update's flags (ADPSGD_WRITE_PEER keeps the peer equal to
-        the learner, which makes the update plain SGD at half the rate)."""
+        the learner, which makes the update plain SGD at half the rate).
+        teacher: a LearnerStep of the same T, B, D and K with its weights
+        loaded; the steps then distil from its `top` top logits, taken once
+        per batch here, at `temperature`, with `soft` and `hard` the weights
+        of its loss and the labels' cross-entropy."""
         self.step = step
         dev = step.device
         self.x = [torch.from_numpy(np.ascontiguousarray(x, dtype=np.float32)).to(dev) for x, _ in batches]
@@ -44,6 +49,15 @@ class Trainer:
         self.base_lr, self.base_batch, self.warmup = base_lr, base_batch, warmup_epochs
         self.batch = step.shape["B"]
         self.flags = flags
+        self.teacher = [None] * len(self.x)
+        if teacher is not None:
+            for i, x in enumerate(self.x):
+                teacher.x.copy_(x)
+                teacher.forward()
+                logits, idx, rest = teacher.top_logits(top, temperature)
+                self.teacher[i] = dict(top=logits, idx=idx, rest=rest, temperature=temperature, soft=soft, hard=hard)
+            torch.cuda.synchronize()
+            teacher.check_recurrence()
 
     def run(self, epochs: int):
         """Returns [(epoch, lr, mean loss of the epoch's steps)]."""
@@ -52,10 +66,10 @@ class Trainer:
         for e in range(1, epochs + 1):
             lr = lr_schedule(e, self.base_lr, self.base_batch, self.batch, self.warmup)
             acc.zero_()
-            for x, y in zip(self.x, self.lab):
+            for x, y, teacher in zip(self.x, self.lab, self.teacher):
                 self.step.x.copy_(x)
                 self.step.labels.copy_(y)
-                self.step.step(lr, self.flags)
+                self.step.step(lr, self.flags, teacher)
                 acc += self.step.loss
             torch.cuda.synchronize()
             self.step.check_recurrence()

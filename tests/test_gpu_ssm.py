@@ -1,0 +1,399 @@
+"""GPU: the selective scan and its short convolution against float64 forms
+(tests/operator_models.py; gradients by autograd), over lane counts, groups,
+lengths, empty sequences, pitches and alignments, states in and out, slots.
+
+Tolerances, relative to a value and beside it to the root mean square of its
+tensor (om.far): half a step of the output's type, and for the float32 work
+inside (40 + 16 T) 2^-24.  A state is a product of up to T decays, each of three
+roundings (the step, its product, the exponential, which doubles them at
+exponents near 1), and a sum of T terms; what a frame adds to them (softplus, silu: about ten
+roundings; a sum over channels or states, in a tree or in order, on the
+order of its square root) is in the 40.  Parameter gradients are sums over
+T * B frames whose errors are those of the terms: the same bound."""
+
+import os
+import sys
+
+import pytest
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
+import operator_models as om  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+TYPES = {"bf16": torch.bfloat16, "fp32": torch.float32}
+
+
+def tol(T):
+    return (40 + 16 * T) * 2.0 ** -24
+
+
+def rows(t, dtype, odd):
+    """t on the GPU as columns of a wider tensor: from an odd column (nothing
+    aligned) or from one that four elements divide; the columns around it hold NaN."""
+    off = 1 if odd else 4
+    W = t.shape[-1] + (7 if odd else 8 + (-t.shape[-1]) % 4)
+    wide = torch.full((*t.shape[:-1], W), float("nan"), dtype=dtype, device="cuda")
+    wide[..., off:off + t.shape[-1]] = t.to(dtype).cuda()
+    return wide[..., off:off + t.shape[-1]]
+
+
+def untouched(view):
+    """The columns around a view of rows() still hold NaN."""
+    n = int(torch.isnan(view._base.float()).sum())
+    return n == view._base.numel() - view.numel()
+
+
+class Case:
+    """Inputs as the GPU sees them (rounded to the type) and in float64."""
+
+    def __init__(self, T, B, D, N, G=1, precision="bf16", gate=True, lens=None, state=True, softplus=True, odd=False,
+                 extras=True, seed=0):
+        from paper_1907_05701_amd import binding as bd
+        g = torch.Generator().manual_seed(seed * 1000 + T * 7 + D)
+        self.bd, self.T, self.B, self.D, self.N, self.G = bd, T, B, D, N, G
+        self.t, self.odd, self.lens, self.softplus = TYPES[precision], odd, lens, softplus
+        self.dims = bd.make_ssm_dims(T=T, B=B, D=D, N=N, G=G, W=1, precision=precision)
+
+        def r(*shape):
+            return torch.randn(shape, generator=g, dtype=torch.float64)
+
+        a = dict(x=r(T, B, D), dt=r(T, B, D), Bm=r(T, B, G * N), Cm=r(T, B, G * N))
+        if not softplus:
+            a["dt"] = a["dt"].abs() * 0.2
+        if gate:
+            a["z"] = r(T, B, D)
+        self.act = {k: v.to(self.t).double() for k, v in a.items()}
+        p = dict(A=-torch.exp(r(D, N) * 0.5))
+        if extras:
+            p.update(Dskip=r(D), dt_bias=r(D) * 0.5 - (2 if softplus else 0))
+            if not softplus:
+                p["dt_bias"] = p["dt_bias"].abs() * 0.1
+        if state:
+            p["h0"] = r(B, D, N)
+        self.par = {k: v.float().double() for k, v in p.items()}
+        self.dy = r(T, B, D).to(self.t).double()
+        self.dhl = r(B, D, N).float().double()
+        n = bd.ssm_workspace_bytes(self.dims)
+        self.ws = {k: torch.full((max(v, 1),), 255, dtype=torch.uint8, device="cuda") for k, v in n.items()}
+
+        def spoil(v):   # what lies behind a sequence's end is never read
+            v = v.clone()
+            for b, e in enumerate(om.lengths(lens, T, B)):
+                v[e:, b] = float("nan")
+            return v
+
+        self.gpu = {k: rows(spoil(v), self.t, odd) for k, v in self.act.items()}
+        self.gdy = rows(spoil(self.dy), self.t, odd)
+        self.gpar = {k: v.float().cuda() for k, v in self.par.items()}
+        self.glens = None if lens is None else torch.tensor(lens, dtype=torch.int32, device="cuda")
+
+    def out(self, *shape):
+        return rows(torch.zeros(shape), self.t, self.odd)
+
+    def forward(self, saved=True, **over):
+        y = self.out(self.T, self.B, self.D)
+        h = torch.full((self.B, self.D, self.N), float("nan"), device="cuda")
+        a = {**self.gpu, **self.gpar, **over}
+        self.bd.ssm_scan_fwd(self.dims, a["x"], a["dt"], a["A"], a["Bm"], a["Cm"], y, self.ws["fwd"],
+                             Dskip=a.get("Dskip"), z=a.get("z"), dt_bias=a.get("dt_bias"), h0=a.get("h0"), h_last=h,
+                             lens=self.glens, softplus=self.softplus, saved=self.ws["saved"] if saved else None)
+        return y, h
+
+    def backward(self):
+        o = dict(dx=self.out(self.T, self.B, self.D), ddt=self.out(self.T, self.B, self.D),
+                 dBm=self.out(self.T, self.B, self.G * self.N), dCm=self.out(self.T, self.B, self.G * self.N))
+        f = {k: torch.full(v.shape, float("nan"), device="cuda") for k, v in self.par.items()}
+        if "z" in self.gpu:
+            o["dz"] = self.out(self.T, self.B, self.D)
+        a = dict(self.gpu, **self.gpar)
+        self.bd.ssm_scan_bwd(self.dims, a["x"], a["dt"], a["A"], a["Bm"], a["Cm"], self.gdy, self.ws["saved"],
+                             self.ws["bwd"], o["dx"], o["ddt"], f["A"], o["dBm"], o["dCm"], Dskip=a.get("Dskip"),
+                             dDskip=f.get("Dskip"), z=a.get("z"), dz=o.get("dz"), dt_bias=a.get("dt_bias"),
+                             ddt_bias=f.get("dt_bias"), dh_last=self.dhl.float().cuda(), dh0=f.get("h0"),
+                             lens=self.glens, softplus=self.softplus)
+        return {k[1:]: v for k, v in o.items()}, f
+
+    def model(self):
+        leaves = {k: v.clone().requires_grad_() for k, v in {**self.act, **self.par}.items()}
+        y, h = om.scan(**leaves, lens=self.lens, softplus_on=self.softplus)
+        loss = (y * self.dy).sum() + (h * self.dhl).sum()
+        grads = torch.autograd.grad(loss, list(leaves.values()), allow_unused=True)
+        return y, h, {k: torch.zeros_like(v) if g is None else g for (k, v), g in zip(leaves.items(), grads)}
+
+
+def check(c):
+    y, h = c.forward()
+    act, par = c.backward()
+    torch.cuda.synchronize()
+    wy, wh, g = c.model()
+    t = tol(c.T)
+    got = {"y": om.far(y, wy, t), "h_last": om.far(h, wh, t)}
+    got.update({k: om.far(v, g[k], t) for k, v in {**act, **par}.items()})
+    print("[scan]", {k: f"{v:.2f}" for k, v in got.items()}, flush=True)
+    assert max(got.values()) <= 1.0, got
+    for v in (y, *act.values()):
+        assert untouched(v)
+
+
+@pytest.mark.parametrize("precision", ["fp32", "bf16"])
+@pytest.mark.parametrize("T,B,D,N,G", [
+    (1, 1, 1, 1, 1), (2, 1, 5, 2, 1), (16, 2, 64, 16, 1), (17, 3, 70, 16, 1), (33, 2, 130, 10, 2), (50, 2, 24, 3, 3),
+    (40, 2, 36, 8, 2), (23, 2, 40, 32, 1), (19, 2, 66, 29, 1), (18, 2, 44, 64, 1), (21, 2, 100, 50, 4), (5, 2, 256, 16, 2),
+], ids=str)
+def test_scan(gpu_lib, T, B, D, N, G, precision):
+    check(Case(T, B, D, N, G, precision))
+
+
+@pytest.mark.parametrize("precision", ["fp32", "bf16"])
+@pytest.mark.parametrize("lens", [[40, 0, 1, 17, 32], [3, 40, -2, 99, 16], [0, 0, 0, 0, 0]], ids=str)
+def test_scan_of_padded_batches(gpu_lib, lens, precision):
+    check(Case(40, 5, 68, 16, 1, precision, lens=lens))
+
+
+@pytest.mark.parametrize("precision", ["fp32", "bf16"])
+def test_scan_without_the_optional_inputs(gpu_lib, precision):
+    check(Case(20, 2, 48, 16, 1, precision, gate=False, state=False, extras=False))
+
+
+@pytest.mark.parametrize("precision", ["fp32", "bf16"])
+def test_scan_of_plain_steps(gpu_lib, precision):
+    check(Case(20, 2, 48, 16, 1, precision, softplus=False))
+
+
+@pytest.mark.parametrize("precision", ["fp32", "bf16"])
+@pytest.mark.parametrize("D,N,G", [(70, 16, 1), (45, 5, 3)])
+def test_scan_of_unaligned_rows(gpu_lib, D, N, G, precision):
+    check(Case(18, 2, D, N, G, precision, odd=True))
+
+
+@pytest.mark.parametrize("T,B,D,N", [(300, 1, 64, 16), (200, 3, 20, 4), (530, 2, 8, 24)])
+def test_scan_of_long_sequences(gpu_lib, T, B, D, N):
+    check(Case(T, B, D, N, 1, "fp32", lens=[T, T // 2, 0][:B]))
+
+
+def test_a_scan_in_pieces_is_the_whole(gpu_lib):
+    """h_last of one call as h0 of the next (in place, too); no saved states."""
+    c = Case(48, 2, 64, 16, precision="fp32")
+    y, h = c.forward()
+    state = c.gpar["h0"].clone()
+    for t0, t1 in ((0, 7), (7, 8), (8, 48)):
+        d = c.bd.make_ssm_dims(T=t1 - t0, B=2, D=64, N=16, precision="fp32")
+        piece = {k: v[t0:t1] for k, v in c.gpu.items()}
+        out = c.out(t1 - t0, 2, 64)
+        ws = torch.empty(max(1, c.bd.ssm_workspace_bytes(d)["fwd"]), dtype=torch.uint8, device="cuda")
+        c.bd.ssm_scan_fwd(d, piece["x"], piece["dt"], c.gpar["A"], piece["Bm"], piece["Cm"], out, ws,
+                          Dskip=c.gpar["Dskip"], z=piece["z"], dt_bias=c.gpar["dt_bias"], h0=state, h_last=state)
+        assert om.far(out, y[t0:t1].double().cpu(), tol(48)) <= 1.0
+    assert om.far(state, h.double().cpu(), tol(48)) <= 1.0
+
+
+@pytest.mark.parametrize("precision", ["fp32", "bf16"])
+@pytest.mark.parametrize("N,G", [(1, 1), (7, 2), (16, 1), (40, 1), (64, 2)])
+def test_scan_frame_by_frame(gpu_lib, N, G, precision):
+    c = Case(6, 3, 70, N, G, precision, odd=N == 7)
+    d = c.bd.make_ssm_dims(T=1, B=3, D=70, N=N, G=G, precision=precision)
+    wy, wh = om.scan(**c.act, **c.par)
+    state = torch.full((5, 70, N), 7.0, device="cuda")
+    state[[4, 0, 2]] = c.gpar["h0"]
+    slots = torch.tensor([4, 0, 2], dtype=torch.int32, device="cuda")
+    for t in range(6):
+        y = c.out(3, 70)
+        a = {k: v[t] for k, v in c.gpu.items()}
+        c.bd.ssm_scan_step(d, a["x"], a["dt"], c.gpar["A"], a["Bm"], a["Cm"], state, y, Dskip=c.gpar["Dskip"],
+                           z=a["z"], dt_bias=c.gpar["dt_bias"], slots=slots)
+        assert om.far(y, wy[t], tol(6)) <= 1.0
+        assert untouched(y)
+    assert om.far(state[[4, 0, 2]], wh, tol(6)) <= 1.0
+    assert bool((state[[1, 3]] == 7).all())
+
+
+def test_slots_that_name_no_stream(gpu_lib):
+    """Out of range, and a slot that an earlier row has: y is zero and no state changes."""
+    c = Case(1, 6, 20, 16, precision="fp32")
+    n, W = 4, 3
+    slots = torch.tensor([2, -1, 2, 4, 0, 2], dtype=torch.int32, device="cuda")
+    state = torch.randn(n, 20, 16, device="cuda")
+    was, y = state.clone(), torch.full((6, 20), 5.0, device="cuda")
+    a = {k: v[0] for k, v in c.gpu.items()}
+    c.bd.ssm_scan_step(c.dims, a["x"], a["dt"], c.gpar["A"], a["Bm"], a["Cm"], state, y, z=a["z"], slots=slots)
+    assert bool((y[[1, 2, 3, 5]] == 0).all()) and bool((y[[0, 4]] != 0).any(1).all())
+    assert torch.equal(state[[1, 3]], was[[1, 3]]) and not torch.equal(state[2], was[2])
+    wy, wh = om.scan(**{k: v[:, [0, 4]] for k, v in c.act.items()}, A=c.par["A"], h0=was[[2, 0]].double().cpu())
+    assert om.far(y[[0, 4]], wy[0], tol(1)) <= 1.0 and om.far(state[[2, 0]], wh, tol(1)) <= 1.0
+    d = c.bd.make_ssm_dims(T=1, B=6, D=20, W=W, precision="fp32")
+    cs = torch.randn(n, W - 1, 20, device="cuda")
+    cwas, w = cs.clone(), torch.randn(20, W, device="cuda")
+    y.fill_(5.0)
+    c.bd.ssm_conv_step(d, a["x"], w, None, cs, y, slots=slots)
+    assert bool((y[[1, 2, 3, 5]] == 0).all()) and torch.equal(cs[[1, 3]], cwas[[1, 3]])
+    wy, wh = om.conv(c.act["x"][:, [0, 4]], w.double().cpu(), None, cwas[[2, 0]].double().cpu())
+    assert om.far(y[[0, 4]], wy[0], tol(1)) <= 1.0 and torch.equal(cs[[2, 0]].double().cpu(), wh)
+
+
+def conv_case(T, B, D, W, precision, lens, state, bias, act, odd, dst):
+    from paper_1907_05701_amd import binding as bd
+    g = torch.Generator().manual_seed(T * 31 + D)
+    t = TYPES[precision]
+
+    def r(*shape, dtype=t):
+        return torch.randn(shape, generator=g, dtype=torch.float64).to(dtype).double()
+
+    f = torch.float32
+    v = dict(x=r(T, B, D), w=r(D, W, dtype=f))
+    if bias:
+        v["bias"] = r(D, dtype=f)
+    if state:
+        v["state"] = r(B, W - 1, D)
+    dy, de = r(T, B, D), r(B, W - 1, D)
+    d = bd.make_ssm_dims(T=T, B=B, D=D, W=W, precision=precision)
+    leaves = {k: a.clone().requires_grad_() for k, a in v.items()}
+    wy, we = om.conv(leaves["x"], leaves["w"], leaves.get("bias"), leaves.get("state"), lens, act)
+    loss = (wy * dy).sum() + ((we * de).sum() if dst else 0)
+    grads = torch.autograd.grad(loss, list(leaves.values()), allow_unused=True)
+    want = {k: torch.zeros_like(a) if q is None else q for (k, a), q in zip(leaves.items(), grads)}
+
+    def spoil(a):
+        a = a.clone()
+        for b, e in enumerate(om.lengths(lens, T, B)):
+            a[e:, b] = float("nan")
+        return a
+
+    x, gdy = rows(spoil(v["x"]), t, odd), rows(spoil(dy), t, odd)
+    w, b = v["w"].float().cuda(), v["bias"].float().cuda() if bias else None
+    st = v["state"].to(t).cuda() if state else None
+    n = None if lens is None else torch.tensor(lens, dtype=torch.int32, device="cuda")
+    y, so = rows(torch.zeros(T, B, D), t, odd), torch.full((B, W - 1, D), float("nan"), dtype=t, device="cuda")
+    bd.ssm_conv_fwd(d, x, w, b, y, lens=n, state=st, state_out=so, silu=act)
+    dx = rows(torch.zeros(T, B, D), t, odd)
+    got = {"w": torch.full((D, W), float("nan"), device="cuda")}
+    got["bias"] = torch.full((D,), float("nan"), device="cuda") if bias else None
+    got["state"] = torch.full((B, W - 1, D), float("nan"), dtype=t, device="cuda") if state else None
+    ws = torch.full((bd.ssm_workspace_bytes(d)["conv_bwd"],), 255, dtype=torch.uint8, device="cuda")
+    bd.ssm_conv_bwd(d, x, w, b, gdy, dx, got["w"], got["bias"], ws, lens=n, state=st, dstate=got["state"],
+                    dstate_out=de.to(t).cuda() if dst else None, silu=act)
+    got["x"] = dx
+    # a frame's sum of W products, silu; a parameter's sum of T * B of those
+    e = (40 + 4 * W) * 2.0 ** -24
+    far = {k: om.far(a, want[k], e) for k, a in got.items() if a is not None}
+    far["y"] = om.far(y, wy, e)
+    print("[conv]", {k: f"{a:.2f}" for k, a in far.items()}, flush=True)
+    assert max(far.values()) <= 1.0, far
+    assert torch.equal(so.double().cpu(), we.detach())
+    assert untouched(y) and untouched(dx)
+
+
+@pytest.mark.parametrize("precision", ["fp32", "bf16"])
+@pytest.mark.parametrize("T,B,D,W", [(1, 1, 1, 1), (1, 2, 9, 4), (3, 2, 64, 8), (21, 5, 260, 4), (50, 3, 33, 3), (130, 2, 12, 2),
+                                     (9, 40, 516, 4)], ids=str)
+def test_conv(gpu_lib, T, B, D, W, precision):
+    conv_case(T, B, D, W, precision, None, True, True, True, False, True)
+
+
+@pytest.mark.parametrize("lens", [None, [20, 0, 1, 2, 9], [3, 99, -4, 20, 19]], ids=str)
+@pytest.mark.parametrize("state,bias,act,odd,dst", [(True, True, True, True, True), (False, False, True, False, False),
+                                                    (True, False, False, False, True), (False, True, False, True, True)])
+def test_conv_of_padded_batches(gpu_lib, lens, state, bias, act, odd, dst):
+    for precision in ("fp32", "bf16"):
+        conv_case(20, 5, 24, 4, precision, lens, state, bias, act, odd, dst)
+
+
+@pytest.mark.parametrize("W", [1, 2, 4, 8])
+@pytest.mark.parametrize("precision", ["fp32", "bf16"])
+def test_conv_frame_by_frame(gpu_lib, W, precision):
+    from paper_1907_05701_amd import binding as bd
+    t = TYPES[precision]
+    g = torch.Generator().manual_seed(W)
+    T, B, D = 11, 3, 70
+    x = torch.randn(T, B, D, generator=g).to(t)
+    w, bias = torch.randn(D, W, generator=g), torch.randn(D, generator=g)
+    st = torch.randn(B, W - 1, D, generator=g).to(t)
+    wy, we = om.conv(x.double(), w.double(), bias.double(), st.double())
+    d = bd.make_ssm_dims(T=1, B=B, D=D, W=W, precision=precision)
+    gx, gs, y = x.cuda(), st.cuda(), torch.empty(B, D, dtype=t, device="cuda")
+    for i in range(T):
+        bd.ssm_conv_step(d, gx[i], w.cuda(), bias.cuda(), gs, y)
+        assert om.far(y, wy[i], (40 + 4 * W) * 2.0 ** -24) <= 1.0
+    assert torch.equal(gs.double().cpu(), we)
+
+
+def test_rows_past_32_bits(gpu_lib):
+    """A row pitch that puts the last frames behind 2^32 elements' worth of bytes."""
+    from paper_1907_05701_amd import binding as bd
+    T, D, N, ld = 20, 8, 4, 1 << 27
+    g = torch.Generator(device="cuda").manual_seed(3)
+    big = torch.empty(T * ld, dtype=torch.bfloat16, device="cuda")
+    x = torch.as_strided(big, (T, 1, D), (ld, ld, 1))
+    y = torch.as_strided(big, (T, 1, D), (ld, ld, 1), 64)
+    x.copy_(torch.randn(T, 1, D, generator=g, device="cuda"))
+    bc = torch.randn(T, 1, 2 * N, generator=g, device="cuda").bfloat16()
+    A = -torch.rand(D, N, generator=g, device="cuda")
+    d = bd.make_ssm_dims(T=T, B=1, D=D, N=N, W=4, precision="bf16")
+    ws = torch.empty(max(1, bd.ssm_workspace_bytes(d)["fwd"]), dtype=torch.uint8, device="cuda")
+    bd.ssm_scan_fwd(d, x, x, A, bc[..., :N], bc[..., N:], y, ws)
+    xd, bcd = x.double().cpu(), bc.double().cpu()
+    wy, _ = om.scan(xd, xd, A.double().cpu(), bcd[..., :N], bcd[..., N:])
+    assert om.far(y, wy, tol(T)) <= 1.0
+    w = torch.randn(D, 4, generator=g, device="cuda")
+    bd.ssm_conv_fwd(d, x, w, None, y)
+    assert om.far(y, om.conv(xd, w.double().cpu(), None)[0], tol(4)) <= 1.0
+
+
+def test_captured_passes_on_another_stream(gpu_lib):
+    """A graph of the convolution, the scan and their backward, replayed between
+    eager passes on other inputs, gives what eager calls give, bit for bit."""
+    bd_case = Case(40, 3, 96, 16, precision="bf16", lens=[40, 11, 0])
+    bd = bd_case.bd
+    d = bd.make_ssm_dims(T=40, B=3, D=96, N=16, W=4, precision="bf16")
+    n = bd.ssm_workspace_bytes(d)
+    ws = {k: torch.empty(max(v, 1), dtype=torch.uint8, device="cuda") for k, v in n.items()}
+    f, t = torch.float32, torch.bfloat16
+    x0, dy = torch.randn(40, 3, 96, device="cuda").to(t), torch.randn(40, 3, 96, device="cuda").to(t)
+    w = torch.randn(96, 4, device="cuda")
+    o = {k: torch.zeros(40, 3, m, dtype=t, device="cuda") for k, m in
+         dict(xc=96, y=96, dxc=96, ddt=96, dz=96, dB=16, dC=16, dx=96).items()}
+    o.update(dA=torch.zeros(96, 16, device="cuda"), dw=torch.zeros(96, 4, device="cuda"),
+             h=torch.zeros(3, 96, 16, device="cuda"))
+    a, p = bd_case.gpu, bd_case.gpar
+
+    def run():
+        bd.ssm_conv_fwd(d, x0, w, None, o["xc"], lens=bd_case.glens)
+        bd.ssm_scan_fwd(d, o["xc"], a["dt"], p["A"], a["Bm"], a["Cm"], o["y"], ws["fwd"], z=a["z"], h_last=o["h"],
+                        lens=bd_case.glens, saved=ws["saved"])
+        bd.ssm_scan_bwd(d, o["xc"], a["dt"], p["A"], a["Bm"], a["Cm"], dy, ws["saved"], ws["bwd"], o["dxc"], o["ddt"],
+                        o["dA"], o["dB"], o["dC"], z=a["z"], dz=o["dz"], lens=bd_case.glens)
+        bd.ssm_conv_bwd(d, x0, w, None, o["dxc"], o["dx"], o["dw"], None, ws["conv_bwd"], lens=bd_case.glens)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        run()
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        run()
+    for i in range(3):
+        x0.copy_(torch.randn(40, 3, 96, device="cuda"))
+        run()
+        torch.cuda.synchronize()
+        want = {k: v.clone() for k, v in o.items()}
+        for v in o.values():
+            v.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for k, v in o.items():
+            assert torch.equal(v, want[k]), (i, k)
+
+
+def test_the_binding_refuses_wrong_tensors(gpu_lib):
+    c = Case(4, 2, 16, 4, precision="bf16")
+    with pytest.raises(ValueError, match="x"):
+        c.forward(x=c.gpu["x"].float())
+    with pytest.raises(ValueError, match="A"):
+        c.forward(A=c.gpar["A"].t().contiguous())
+    with pytest.raises(ValueError, match="Bm"):
+        c.forward(Bm=c.gpu["Bm"].transpose(0, 1))
+    with pytest.raises(ValueError, match="dt"):
+        c.forward(dt=c.gpu["dt"][:3])
+    with pytest.raises(ValueError, match="h0"):
+        c.forward(h0=c.gpar["h0"].cpu())

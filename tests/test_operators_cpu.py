@@ -1,0 +1,142 @@
+"""Host-side checks of the state space and distillation entry points: bad
+arguments are refused, with a message, before anything is launched."""
+
+import ctypes
+
+import pytest
+
+from paper_1907_05701_amd import binding as bd
+
+PTR = ctypes.c_void_p(256)   # never read: every call here is refused on the host
+
+
+def _dims(**over):
+    return bd.make_ssm_dims(**dict(dict(T=5, B=3, D=12, N=4, G=2, W=4, precision="bf16"), **over))
+
+
+def _scan_in(dims, **over):
+    a = bd.SsmScanIn(256, 256, 256, 256, 256, dims.D, dims.D, dims.G * dims.N, dims.G * dims.N, dims.D, 256, 256, 256,
+                     256, None, bd.SSM_SOFTPLUS)
+    for k, v in over.items():
+        setattr(a, k, v)
+    return a
+
+
+def _refused(rc, code):
+    assert rc == code
+    assert len(bd.lib().blstm_last_error()) > 10
+
+
+@pytest.mark.parametrize("over,code", [
+    (dict(T=0), -1), (dict(B=-1), -1), (dict(N=0), -1), (dict(W=0), -1), (dict(G=5), -1), (dict(N=65), -2),
+    (dict(W=9), -2), (dict(T=1 << 13, B=1 << 12), -2), (dict(D=(1 << 20) + 2), -2), (dict(precision=3), -1)])
+def test_bad_ssm_dims(over, code):
+    with pytest.raises(bd.BlstmError) as e:
+        bd.ssm_workspace_bytes(_dims(**over))
+    assert e.value.code == code
+    L, d = bd.lib(), _dims(**over)
+    ok = _dims()
+    _refused(L.ssm_scan_fwd(ctypes.byref(d), ctypes.byref(_scan_in(ok)), PTR, 1 << 30, None, None, PTR, None), code)
+    _refused(L.ssm_conv_fwd(ctypes.byref(d), PTR, 1 << 30, PTR, None, None, None, PTR, 1 << 30, None, 0, None), code)
+
+
+def test_workspaces_hold_a_state_for_every_sixteen_frames():
+    a = bd.ssm_workspace_bytes(_dims(T=16, N=16))
+    b = bd.ssm_workspace_bytes(_dims(T=17, N=16))
+    assert a["saved"] == 3 * 12 * 16 * 4 and b["saved"] == 2 * a["saved"]
+    # states are held in whole lanes of four
+    assert bd.ssm_workspace_bytes(_dims(T=16, N=13))["saved"] == a["saved"]
+
+
+@pytest.mark.parametrize("field", ["x", "dt", "Bm", "Cm", "A"])
+def test_scan_needs_its_inputs(field):
+    L, d = bd.lib(), _dims()
+    bad = _scan_in(d, **{field: None})
+    _refused(L.ssm_scan_fwd(ctypes.byref(d), ctypes.byref(bad), PTR, 12, None, None, PTR, None), bd.BLSTM_EINVAL)
+    one = _dims(T=1)
+    _refused(L.ssm_scan_step(ctypes.byref(one), ctypes.byref(bad), None, 3, PTR, PTR, 12, None), bd.BLSTM_EINVAL)
+
+
+@pytest.mark.parametrize("field", ["ldx", "lddt", "ldb", "ldc", "ldz"])
+def test_scan_refuses_short_pitches(field):
+    L, d = bd.lib(), _dims()
+    bad = _scan_in(d, **{field: 7})
+    _refused(L.ssm_scan_fwd(ctypes.byref(d), ctypes.byref(bad), PTR, 12, None, None, PTR, None), bd.BLSTM_EINVAL)
+
+
+def test_scan_refusals():
+    L, d, one = bd.lib(), _dims(), _dims(T=1)
+    i = _scan_in(d)
+    _refused(L.ssm_scan_fwd(ctypes.byref(d), ctypes.byref(i), None, 12, None, None, PTR, None), bd.BLSTM_EINVAL)
+    _refused(L.ssm_scan_fwd(ctypes.byref(d), ctypes.byref(i), PTR, 11, None, None, PTR, None), bd.BLSTM_EINVAL)
+    _refused(L.ssm_scan_fwd(ctypes.byref(d), ctypes.byref(_scan_in(d, flags=4)), PTR, 12, None, None, PTR, None),
+             bd.BLSTM_EINVAL)
+    _refused(L.ssm_scan_step(ctypes.byref(d), ctypes.byref(i), None, 3, PTR, PTR, 12, None), bd.BLSTM_EINVAL)   # T
+    _refused(L.ssm_scan_step(ctypes.byref(one), ctypes.byref(i), None, 2, PTR, PTR, 12, None), bd.BLSTM_EINVAL)
+    _refused(L.ssm_scan_step(ctypes.byref(one), ctypes.byref(i), PTR, 0, PTR, PTR, 12, None), bd.BLSTM_EINVAL)
+    g = bd.SsmScanGrads(256, 256, 256, 256, None, 12, 12, 8, 8, 12, 256, None, None, None)   # z given, dz not
+    _refused(L.ssm_scan_bwd(ctypes.byref(d), ctypes.byref(i), PTR, 12, None, PTR, ctypes.byref(g), PTR, None),
+             bd.BLSTM_EINVAL)
+    g.dz, g.lddb = 256, 3
+    _refused(L.ssm_scan_bwd(ctypes.byref(d), ctypes.byref(i), PTR, 12, None, PTR, ctypes.byref(g), PTR, None),
+             bd.BLSTM_EINVAL)
+
+
+def test_conv_refusals():
+    L, d, one = bd.lib(), _dims(), _dims(T=1)
+    r = ctypes.byref(d)
+    _refused(L.ssm_conv_fwd(r, None, 12, PTR, None, None, None, PTR, 12, None, 0, None), bd.BLSTM_EINVAL)
+    _refused(L.ssm_conv_fwd(r, PTR, 11, PTR, None, None, None, PTR, 12, None, 0, None), bd.BLSTM_EINVAL)
+    _refused(L.ssm_conv_fwd(r, PTR, 12, PTR, None, None, PTR, PTR, 12, PTR, 0, None), bd.BLSTM_EINVAL)   # state_out is state
+    _refused(L.ssm_conv_fwd(r, PTR, 12, PTR, None, None, None, PTR, 12, None, 1, None), bd.BLSTM_EINVAL)   # flags
+    _refused(L.ssm_conv_bwd(r, PTR, 12, PTR, None, None, None, PTR, 12, None, PTR, 12, None, None, None, PTR, 0, None),
+             bd.BLSTM_EINVAL)
+    _refused(L.ssm_conv_step(r, PTR, 12, PTR, None, None, 3, PTR, PTR, 12, 0, None), bd.BLSTM_EINVAL)
+    _refused(L.ssm_conv_step(ctypes.byref(one), PTR, 12, PTR, None, None, 2, PTR, PTR, 12, 0, None), bd.BLSTM_EINVAL)
+    _refused(L.ssm_conv_step(ctypes.byref(one), PTR, 12, PTR, None, None, 3, None, PTR, 12, 0, None), bd.BLSTM_EINVAL)
+
+
+def _topk(M=4, K=10, ld=10, prec=1, k=3, tau=1.0, top=PTR):
+    return bd.lib().softmax_topk_rows(PTR, ld, M, K, prec, k, ctypes.c_float(tau), top, PTR, None, None)
+
+
+@pytest.mark.parametrize("over,code", [
+    (dict(M=0), -1), (dict(K=0), -1), (dict(ld=9), -1), (dict(prec=2), -1), (dict(k=0), -1), (dict(k=11), -1),
+    (dict(k=257, K=300, ld=300), -2), (dict(K=(1 << 18) + 1, ld=1 << 19), -2), (dict(tau=0.0), -1),
+    (dict(tau=float("nan")), -1), (dict(tau=float("inf")), -1), (dict(tau=-1.0), -1), (dict(top=None), -1)])
+def test_topk_refusals(over, code):
+    _refused(_topk(**over), code)
+
+
+@pytest.mark.parametrize("over,code", [
+    (dict(top=None), -1), (dict(idx=None), -1), (dict(k=0), -1), (dict(k=300), -2), (dict(temperature=0.0), -1),
+    (dict(soft=float("inf")), -1), (dict(hard=float("nan")), -1)])
+def test_distill_refusals(over, code):
+    t = bd.SoftmaxTeacher(256, 256, None, None, None, 3, 1.0, 1.0, 0.0)
+    for k, v in over.items():
+        setattr(t, k, v)
+    L, F = bd.lib(), ctypes.c_float(1.0)
+    _refused(L.softmax_distill_rows(PTR, 10, 4, 10, 1, ctypes.byref(t), F, PTR, ctypes.c_void_p(512), 10, None), code)
+    d = bd.make_dims(1, 8, 64, 8, 10, 2, 2, "fp32")
+    _refused(L.softmax_distill_fwd_bwd(ctypes.byref(d), PTR, None, PTR, ctypes.byref(t), F, PTR, PTR, PTR, PTR, None), code)
+
+
+def test_distill_buffers():
+    t = bd.SoftmaxTeacher(256, 256, None, None, None, 3, 1.0, 1.0, 0.0)
+    L, F, other = bd.lib(), ctypes.c_float(1.0), ctypes.c_void_p(512)
+    _refused(L.softmax_distill_rows(PTR, 10, 4, 10, 1, ctypes.byref(t), F, None, other, 10, None), -1)
+    _refused(L.softmax_distill_rows(PTR, 10, 4, 10, 1, ctypes.byref(t), F, PTR, other, 9, None), -1)
+    _refused(L.softmax_distill_rows(PTR, 10, 4, 10, 1, ctypes.byref(t), F, other, PTR, 12, None), -1)   # in place, other pitch
+    d = bd.make_dims(1, 8, 64, 8, 10, 2, 2, "bf16")
+    _refused(L.softmax_topk(ctypes.byref(d), PTR, None, PTR, 3, F, PTR, PTR, None, PTR, None), -1)      # no theta_lp
+    _refused(L.softmax_topk(ctypes.byref(d), PTR, PTR, PTR, 11, F, PTR, PTR, None, PTR, None), -1)
+
+
+def test_the_binding_refuses_host_tensors():
+    import torch
+    d = bd.make_ssm_dims(T=1, B=1, D=4, N=1, precision="fp32")
+    x = torch.zeros(1, 1, 4)
+    with pytest.raises(ValueError):
+        bd.ssm_conv_fwd(d, x, x, None, x)
+    with pytest.raises(ValueError):
+        bd.softmax_topk_rows(torch.zeros(2, 4), torch.zeros(2, 1), torch.zeros(2, 1, dtype=torch.int32))
