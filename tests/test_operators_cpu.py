@@ -40,12 +40,12 @@ def test_bad_ssm_dims(over, code):
     _refused(L.ssm_conv_fwd(ctypes.byref(d), PTR, 1 << 30, PTR, None, None, None, PTR, 1 << 30, None, 0, None), code)
 
 
-def test_workspaces_hold_a_state_for_every_sixteen_frames():
-    a = bd.ssm_workspace_bytes(_dims(T=16, N=16))
-    b = bd.ssm_workspace_bytes(_dims(T=17, N=16))
+def test_workspaces_hold_a_state_for_every_eight_frames():
+    a = bd.ssm_workspace_bytes(_dims(T=8, N=16))
+    b = bd.ssm_workspace_bytes(_dims(T=9, N=16))
     assert a["saved"] == 3 * 12 * 16 * 4 and b["saved"] == 2 * a["saved"]
-    # states are held in whole lanes of four
-    assert bd.ssm_workspace_bytes(_dims(T=16, N=13))["saved"] == a["saved"]
+    # states are held in whole lanes of eight
+    assert bd.ssm_workspace_bytes(_dims(T=8, N=9))["saved"] == a["saved"]
 
 
 @pytest.mark.parametrize("field", ["x", "dt", "Bm", "Cm", "A"])
