@@ -8,6 +8,9 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
+
+import torch
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libadpsgd_blstm.so")
@@ -100,14 +103,15 @@ def lib():
         L.blstm_timing_end.argtypes = [ctypes.POINTER(KernelTime), ctypes.c_int32,
                                        ctypes.POINTER(ctypes.c_int32)]
         I, I64, U, F = ctypes.c_int32, ctypes.c_int64, ctypes.c_uint32, ctypes.c_float
-        SD, SI, SG, ST = (ctypes.POINTER(c) for c in (SsmDims, SsmScanIn, SsmScanGrads, SoftmaxTeacher))
+        SD, SG, ST = (ctypes.POINTER(c) for c in (SsmDims, SsmScanGrads, SoftmaxTeacher))
         L.ssm_workspace_bytes.argtypes = [SD] + [ctypes.POINTER(S)] * 4
         L.ssm_conv_fwd.argtypes = [SD, P, I64, P, P, P, P, P, I64, P, U, P]
         L.ssm_conv_bwd.argtypes = [SD, P, I64, P, P, P, P, P, I64, P, P, I64, P, P, P, P, U, P]
         L.ssm_conv_step.argtypes = [SD, P, I64, P, P, P, I, P, P, I64, U, P]
-        L.ssm_scan_fwd.argtypes = [SD, SI, P, I64, P, P, P, P]
-        L.ssm_scan_bwd.argtypes = [SD, SI, P, I64, P, P, SG, P, P]
-        L.ssm_scan_step.argtypes = [SD, SI, P, I, P, P, I64, P]
+        # ssm_scan_in by its bytes
+        L.ssm_scan_fwd.argtypes = [SD, P, P, I64, P, P, P, P]
+        L.ssm_scan_bwd.argtypes = [SD, P, P, I64, P, P, SG, P, P]
+        L.ssm_scan_step.argtypes = [SD, P, P, I, P, P, I64, P]
         L.softmax_topk_rows.argtypes = [P, I64, I64, I, I, I, F, P, P, P, P]
         L.softmax_distill_rows.argtypes = [P, I64, I64, I, I, ST, F, P, P, I64, P]
         L.softmax_head_ws_bytes.argtypes = [DP, ctypes.POINTER(S)]
@@ -142,7 +146,6 @@ def _ptr(t):
 
 def _stream(stream):
     if stream is None:
-        import torch
         stream = torch.cuda.current_stream()
     return ctypes.c_void_p(stream.cuda_stream)
 
@@ -232,71 +235,75 @@ def blstm_timing_end(cap: int = 64) -> dict:
 # to the library: a ValueError names the argument.
 def _on(x):
     """The device index the call runs on, from its first tensor."""
-    if not x.is_cuda:
+    dev = x.get_device()
+    if dev < 0:
         raise ValueError("tensors must be on the GPU")
-    return x.device
+    return dev
 
 
-def _have(name, t, shape, dtype, device, optional=False):
+def _wrong(name, want, t, dev):
+    return ValueError(f"{name} must be {want} on cuda:{dev}: got {t.dtype} {tuple(t.shape)} with strides {t.stride()} "
+                      f"on {t.device}")
+
+
+def _have(name, t, shape, dtype, dev, optional=False):
     """Address of a contiguous tensor of this shape and type (None for an optional one that is absent)."""
     if t is None:
         if optional:
             return None
         raise ValueError(f"{name} is required")
-    if t.dtype != dtype or t.device != device or tuple(t.shape) != shape or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {shape} on {device}: got {t.dtype} "
-                         f"{tuple(t.shape)} with strides {t.stride()} on {t.device}")
+    if t.shape != shape or t.dtype != dtype or t.get_device() != dev or not t.is_contiguous():
+        raise _wrong(name, f"a contiguous {dtype} tensor of shape {shape}", t, dev)
     return t.data_ptr()
 
 
-def _rows(name, t, shape, dtype, device, optional=False):
-    """(address, row pitch) of a tensor whose last axis is contiguous and whose leading axes are rows at one pitch."""
+def _rows(name, t, shape, dtype, dev, optional=False):
+    """(address, row pitch) of a tensor [rows][W] or [T][B][W] whose last axis
+    is contiguous and whose leading axes are rows at one pitch."""
     if t is None:
         if optional:
             return None, 0
         raise ValueError(f"{name} is required")
-    ok = t.dtype == dtype and t.device == device and tuple(t.shape) == shape and (shape[-1] == 1 or t.stride(-1) == 1)
-    if ok and len(shape) == 1:
-        return t.data_ptr(), shape[0]
-    if ok:
-        # the pitch, from the innermost of the leading axes with more than one row
-        st, ld, n = t.stride(), 0, 1
-        for i in range(len(shape) - 2, -1, -1):
-            if shape[i] > 1:
-                if not ld:
-                    ld = st[i]
-                ok = ok and st[i] == ld * n
-                n *= shape[i]
-        if not ld:
-            ld = shape[-1]
-        if ok and ld >= shape[-1]:
+    if t.shape == shape and t.dtype == dtype and t.get_device() == dev:
+        st, W = t.stride(), shape[-1]
+        ld = st[-2]
+        if len(shape) == 3:
+            if shape[1] == 1:
+                ld = st[0]
+            elif shape[0] > 1 and st[0] != ld * shape[1]:
+                ld = -1
+        if ld < W and t.numel() == W:
+            ld = W   # one row: its pitch says nothing
+        if ld >= W and (st[-1] == 1 or W == 1):
             return t.data_ptr(), ld
-    raise ValueError(f"{name} must be {dtype} rows of shape {shape} on {device}, adjacent elements along the last "
-                     f"axis and one pitch from row to row: got {t.dtype} {tuple(t.shape)} with strides {t.stride()} "
-                     f"on {t.device}")
+    raise _wrong(name, f"{dtype} rows of shape {shape}, adjacent elements along the last axis and one pitch from row "
+                       "to row,", t, dev)
 
 
-def _call(fn, device, stream, *args):
-    """Calls fn on `device` (made current for the launch if it is not) and `stream`."""
-    import torch
-    if device.index == torch.cuda.current_device():
-        return _check(fn, getattr(lib(), fn)(*args, _stream(stream)))
-    with torch.cuda.device(device):
-        return _check(fn, getattr(lib(), fn)(*args, _stream(stream)))
+def _call(fn, dev, stream, *args):
+    """Calls fn on device `dev` (made current for the launch if it is not) and
+    `stream`, by default the device's current one."""
+    if dev != torch.cuda.current_device():
+        with torch.cuda.device(dev):
+            return _call(fn, dev, stream, *args)
+    # the handle alone: a Stream object costs more than the launch's other arguments together
+    s = torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+    rc = getattr(_lib or lib(), fn)(*args, s)
+    return _check(fn, rc) if rc else rc
 
 
-def _bytes(name, t, n, device):
+def _bytes(name, t, n, dev):
     if n == 0:
         return None
-    if t is None or not t.is_contiguous() or t.device != device or t.numel() * t.element_size() < n:
-        raise ValueError(f"{name} must be a contiguous buffer of at least {n} bytes on {device} (ssm_workspace_bytes)")
-    if t.data_ptr() % 16:
+    if t is None or not t.is_contiguous() or t.get_device() != dev or t.numel() * t.element_size() < n:
+        raise ValueError(f"{name} must be a contiguous buffer of at least {n} bytes on cuda:{dev} (ssm_workspace_bytes)")
+    p = t.data_ptr()
+    if p % 16:
         raise ValueError(f"{name} must be 16-byte aligned")
-    return t.data_ptr()
+    return p
 
 
 def _elem(dims):
-    import torch
     return torch.bfloat16 if dims.precision == BLSTM_BF16 else torch.float32
 
 
@@ -322,7 +329,6 @@ def _ssm_bytes(dims):
 
 
 def ssm_conv_fwd(dims, x, w, bias, y, lens=None, state=None, state_out=None, silu=True, stream=None):
-    import torch
     dev, e = _on(x), _elem(dims)
     T, B, D, W = dims.T, dims.B, dims.D, dims.W
     px, ldx = _rows("x", x, (T, B, D), e, dev)
@@ -335,7 +341,6 @@ def ssm_conv_fwd(dims, x, w, bias, y, lens=None, state=None, state_out=None, sil
 
 def ssm_conv_bwd(dims, x, w, bias, dy, dx, dw, dbias, ws, lens=None, state=None, dstate=None, dstate_out=None,
                  silu=True, stream=None):
-    import torch
     dev, e, f = _on(x), _elem(dims), torch.float32
     T, B, D, W = dims.T, dims.B, dims.D, dims.W
     px, ldx = _rows("x", x, (T, B, D), e, dev)
@@ -352,7 +357,6 @@ def ssm_conv_bwd(dims, x, w, bias, dy, dx, dw, dbias, ws, lens=None, state=None,
 
 def _slots(state, slots, B, row, dtype, dev):
     """(state's address, its rows, slots' address); state is [rows][*row]."""
-    import torch
     if state is None or state.dim() != 1 + len(row):
         raise ValueError(f"state must be a tensor of rows of shape {row}")
     n = state.shape[0]
@@ -361,7 +365,6 @@ def _slots(state, slots, B, row, dtype, dev):
 
 
 def ssm_conv_step(dims, x, w, bias, state, y, slots=None, silu=True, stream=None):
-    import torch
     dev, e = _on(x), _elem(dims)
     B, D, W = dims.B, dims.D, dims.W
     px, ldx = _rows("x", x, (B, D), e, dev)
@@ -371,8 +374,11 @@ def ssm_conv_step(dims, x, w, bias, state, y, slots=None, silu=True, stream=None
                  _have("bias", bias, (D,), torch.float32, dev, True), psl, n, ps, py, ldy, SSM_SILU if silu else 0)
 
 
+_SCAN_IN = struct.Struct("@5P5q5PI4x")
+assert _SCAN_IN.size == ctypes.sizeof(SsmScanIn)
+
+
 def _scan_in(dims, lead, dev, x, dt, A, Bm, Cm, Dskip, z, dt_bias, h0, lens, softplus):
-    import torch
     e, f = _elem(dims), torch.float32
     B, D, N, GN = dims.B, dims.D, dims.N, dims.G * dims.N
     px, ldx = _rows("x", x, (*lead, D), e, dev)
@@ -380,28 +386,28 @@ def _scan_in(dims, lead, dev, x, dt, A, Bm, Cm, Dskip, z, dt_bias, h0, lens, sof
     pb, ldb = _rows("Bm", Bm, (*lead, GN), e, dev)
     pc, ldc = _rows("Cm", Cm, (*lead, GN), e, dev)
     pz, ldz = _rows("z", z, (*lead, D), e, dev, True)
-    return SsmScanIn(px, pdt, pb, pc, pz, ldx, lddt, ldb, ldc, ldz, _have("A", A, (D, N), f, dev),
-                     _have("Dskip", Dskip, (D,), f, dev, True), _have("dt_bias", dt_bias, (D,), f, dev, True),
-                     _have("h0", h0, (B, D, N), f, dev, True), _have("lens", lens, (B,), torch.int32, dev, True),
-                     SSM_SOFTPLUS if softplus else 0)
+    # SsmScanIn's bytes (filling the ctypes structure field by field takes longer than the launch)
+    return _SCAN_IN.pack(px, pdt, pb, pc, pz or 0, ldx, lddt, ldb, ldc, ldz, _have("A", A, (D, N), f, dev),
+                         _have("Dskip", Dskip, (D,), f, dev, True) or 0,
+                         _have("dt_bias", dt_bias, (D,), f, dev, True) or 0,
+                         _have("h0", h0, (B, D, N), f, dev, True) or 0,
+                         _have("lens", lens, (B,), torch.int32, dev, True) or 0, SSM_SOFTPLUS if softplus else 0)
 
 
 def ssm_scan_fwd(dims, x, dt, A, Bm, Cm, y, ws, Dskip=None, z=None, dt_bias=None, h0=None, h_last=None, lens=None,
                  softplus=True, saved=None, stream=None):
-    import torch
     dev = _on(x)
     T, B, D, N = dims.T, dims.B, dims.D, dims.N
     arg = _scan_in(dims, (T, B), dev, x, dt, A, Bm, Cm, Dskip, z, dt_bias, h0, lens, softplus)
     py, ldy = _rows("y", y, (T, B, D), _elem(dims), dev)
     n = _ssm_bytes(dims)
-    return _call("ssm_scan_fwd", dev, stream, ctypes.byref(dims), ctypes.byref(arg), py, ldy,
+    return _call("ssm_scan_fwd", dev, stream, ctypes.byref(dims), arg, py, ldy,
                  _have("h_last", h_last, (B, D, N), torch.float32, dev, True),
                  None if saved is None else _bytes("saved", saved, n["saved"], dev), _bytes("ws", ws, n["fwd"], dev))
 
 
 def ssm_scan_bwd(dims, x, dt, A, Bm, Cm, dy, saved, ws, dx, ddt, dA, dBm, dCm, Dskip=None, dDskip=None, z=None,
                  dz=None, dt_bias=None, ddt_bias=None, dh_last=None, dh0=None, lens=None, softplus=True, stream=None):
-    import torch
     dev, e, f = _on(x), _elem(dims), torch.float32
     T, B, D, N, GN = dims.T, dims.B, dims.D, dims.N, dims.G * dims.N
     arg = _scan_in(dims, (T, B), dev, x, dt, A, Bm, Cm, Dskip, z, dt_bias, None, lens, softplus)
@@ -415,25 +421,23 @@ def ssm_scan_bwd(dims, x, dt, A, Bm, Cm, dy, saved, ws, dx, ddt, dA, dBm, dCm, D
                        _have("dDskip", dDskip, (D,), f, dev, True), _have("ddt_bias", ddt_bias, (D,), f, dev, True),
                        _have("dh0", dh0, (B, D, N), f, dev, True))
     n = _ssm_bytes(dims)
-    return _call("ssm_scan_bwd", dev, stream, ctypes.byref(dims), ctypes.byref(arg), pdy, lddy,
+    return _call("ssm_scan_bwd", dev, stream, ctypes.byref(dims), arg, pdy, lddy,
                  _have("dh_last", dh_last, (B, D, N), f, dev, True), _bytes("saved", saved, n["saved"], dev),
                  ctypes.byref(out), _bytes("ws", ws, n["bwd"], dev))
 
 
 def ssm_scan_step(dims, x, dt, A, Bm, Cm, state, y, Dskip=None, z=None, dt_bias=None, slots=None, softplus=True,
                   stream=None):
-    import torch
     dev = _on(x)
     B, D, N = dims.B, dims.D, dims.N
     arg = _scan_in(dims, (B,), dev, x, dt, A, Bm, Cm, Dskip, z, dt_bias, None, None, softplus)
     py, ldy = _rows("y", y, (B, D), _elem(dims), dev)
     ps, n, psl = _slots(state, slots, B, (D, N), torch.float32, dev)
-    return _call("ssm_scan_step", dev, stream, ctypes.byref(dims), ctypes.byref(arg), psl, n, ps, py, ldy)
+    return _call("ssm_scan_step", dev, stream, ctypes.byref(dims), arg, psl, n, ps, py, ldy)
 
 
 # ---------------------------------------------------------------- distillation ---
 def _logits(logits):
-    import torch
     if logits.dim() != 2 or logits.dtype not in (torch.bfloat16, torch.float32):
         raise ValueError(f"logits must be bfloat16 or float32 rows [M][K]: got {logits.dtype} {tuple(logits.shape)}")
     M, K = logits.shape
@@ -443,16 +447,14 @@ def _logits(logits):
 
 def softmax_topk_rows(logits, top, idx, rest=None, temperature=1.0, stream=None):
     """k is top's width."""
-    import torch
     p, ld, M, K, prec = _logits(logits)
-    dev, k = logits.device, top.shape[-1]
+    dev, k = logits.get_device(), top.shape[-1]
     return _call("softmax_topk_rows", dev, stream, p, ld, M, K, prec, k, temperature,
                  _have("top", top, (M, k), torch.float32, dev), _have("idx", idx, (M, k), torch.int32, dev),
                  _have("rest", rest, (M,), torch.float32, dev, True))
 
 
 def _teacher(M, dev, top, idx, rest, labels, weights, temperature, soft, hard):
-    import torch
     k = top.shape[-1]
     return SoftmaxTeacher(_have("top", top, (M, k), torch.float32, dev), _have("idx", idx, (M, k), torch.int32, dev),
                           _have("rest", rest, (M,), torch.float32, dev, True),
@@ -462,9 +464,8 @@ def _teacher(M, dev, top, idx, rest, labels, weights, temperature, soft, hard):
 
 def softmax_distill_rows(logits, top, idx, row_loss, dlogits, rest=None, labels=None, weights=None, temperature=1.0,
                          soft=1.0, hard=0.0, loss_scale=1.0, stream=None):
-    import torch
     p, ld, M, K, prec = _logits(logits)
-    dev = logits.device
+    dev = logits.get_device()
     t = _teacher(M, dev, top, idx, rest, labels, weights, temperature, soft, hard)
     pd, ldd = _rows("dlogits", dlogits, (M, K), logits.dtype, dev)
     return _call("softmax_distill_rows", dev, stream, p, ld, M, K, prec, ctypes.byref(t), loss_scale,
@@ -479,7 +480,6 @@ def softmax_head_ws_bytes(dims: Dims) -> int:
 
 def softmax_topk(dims, theta, theta_lp, y_top, top, idx, ws, rest=None, temperature=1.0, stream=None):
     """top, idx [T*B][k], rest [T*B]; k is top's width."""
-    import torch
     dev, M, k = _on(y_top), dims.T * dims.B, top.shape[-1]
     return _call("softmax_topk", dev, stream, ctypes.byref(dims), _ptr(theta), _ptr(theta_lp), _ptr(y_top), k,
                  temperature, _have("top", top, (M, k), torch.float32, dev), _have("idx", idx, (M, k), torch.int32, dev),

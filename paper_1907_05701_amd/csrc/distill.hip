@@ -6,6 +6,7 @@
 #include <math.h>
 
 #include <cmath>
+#include <type_traits>
 
 #include "common.hpp"
 #include "distill.hpp"
@@ -51,24 +52,82 @@ __device__ __forceinline__ float row_max(float v, float* buf) {
   return t;
 }
 
-// Calls f(column, value) for the thread's columns of a row.
+// Adjacent elements that a thread reads at once: 16 bytes.  Rows of any pitch
+// and start are read so (global memory takes 16-byte accesses at an element's alignment).
 template <typename TI> struct Wide;
 template <> struct Wide<float> { typedef f32x4 type; static constexpr int n = 4; };
 template <> struct Wide<bf16> { typedef bf16x8 type; static constexpr int n = 8; };
-template <typename TI, typename F>
-__device__ __forceinline__ void each(const TI* s, int K, bool vec, F f) {
-  constexpr int V = Wide<TI>::n;
-  typedef typename Wide<TI>::type W;
-  int done = 0;
-  if (vec) {
-    done = K / V * V;
-    for (int c = (int)threadIdx.x * V; c < done; c += RT * V) {
-      const W v = *(const W*)(s + c);
-#pragma unroll
-      for (int i = 0; i < V; ++i) f(c + i, (float)v[i]);
-    }
+
+// A row in registers: vector i of thread t holds columns (i RT + t) V and on, as
+// far as whole vectors go; the fewer than V columns behind them are one a
+// thread.  What does not exist is -inf.  bf16 pairs stay packed; again() between passes
+// keeps the compiler from carrying widened values and exponentials from one pass to the next.
+template <typename TI, int V, int NV, int RT> struct Row {
+  static constexpr bool PACKED = sizeof(TI) == 2 && V > 1;
+  static constexpr int W = PACKED ? V / 2 : V;   // words of a vector
+  uint32_t w[NV][W];
+  float tail;
+  static __device__ __forceinline__ int col(int i) { return (i * RT + (int)threadIdx.x) * V; }
+  static __device__ __forceinline__ int whole(int K) { return K / V * V; }
+  // vector i's address (a base that the workgroup shares and 32 bits of the
+  // thread's own), and whether it exists
+  template <typename P> static __device__ __forceinline__ P* at(P* s, int i) {
+    typedef typename std::conditional<std::is_const<P>::value, const char, char>::type C;
+    return (P*)((C*)(s + i * RT * V) + (uint32_t)(threadIdx.x * (V * sizeof(P))));
   }
-  for (int c = done + (int)threadIdx.x; c < K; c += RT) f(c, to_f32(s[c]));
+  static __device__ __forceinline__ bool has(int i, int n) { return (int)threadIdx.x * V < n - i * RT * V; }
+  // the thread's column behind the whole vectors (K or more: none)
+  static __device__ __forceinline__ int tail_col(int K) { return V == 1 ? K : whole(K) + (int)threadIdx.x; }
+  __device__ __forceinline__ float get(int i, int j) const {
+    if constexpr (!PACKED) return __uint_as_float(w[i][j]);
+    else return __uint_as_float(j & 1 ? w[i][j >> 1] & 0xffff0000u : w[i][j >> 1] << 16);
+  }
+  __device__ __forceinline__ void drop(int i, int j) {   // -inf
+    if constexpr (!PACKED) w[i][j] = 0xff800000u;
+    else w[i][j >> 1] = j & 1 ? (w[i][j >> 1] & 0xffffu) | 0xff800000u : (w[i][j >> 1] & 0xffff0000u) | 0xff80u;
+  }
+  __device__ __forceinline__ void again() {
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int j = 0; j < W; ++j) asm volatile("" : "+v"(w[i][j]));
+  }
+  __device__ __forceinline__ void load(const TI* s, int K) {
+    const int n = whole(K);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+#pragma unroll
+      for (int j = 0; j < W; ++j) w[i][j] = PACKED ? 0xff80ff80u : 0xff800000u;
+      if (has(i, n)) {
+        if constexpr (V == 1) w[i][0] = __float_as_uint(to_f32(*at(s, i)));
+        else __builtin_memcpy(w[i], at(s, i), V * sizeof(TI));
+      }
+    }
+    tail = tail_col(K) < K ? to_f32(s[tail_col(K)]) : -INFINITY;
+  }
+};
+
+// Rows longer than registers hold: calls f(column, value) for the thread's
+// columns, read from memory (the caches) by every pass.
+// ONE: element by element, in fewer registers.
+template <typename TI, int RT, bool ONE = false, typename F>
+__device__ __forceinline__ void each(const TI* s, int K, F f) {
+  if constexpr (ONE) {
+#pragma unroll 4
+    for (int c = (int)threadIdx.x; c < K; c += RT) f(c, to_f32(s[c]));
+    return;
+  }
+  constexpr int V = Wide<TI>::n;
+  const int done = K / V * V;
+#pragma unroll 1
+  for (int c = (int)threadIdx.x * V; c < done; c += RT * V) {
+    TI v[V];
+    __builtin_memcpy(v, s + c, V * sizeof(TI));
+#pragma unroll
+    for (int i = 0; i < V; ++i) f(c + i, to_f32(v[i]));
+  }
+  const int c = done + (int)threadIdx.x;
+  if (c < K) f(c, to_f32(s[c]));
 }
 
 // Order of logits as unsigned words: larger logit, larger word; both zeros
@@ -84,58 +143,89 @@ __device__ __forceinline__ float order_value(uint32_t w) {
 }
 
 // ---------------------------------------------------------------------------
-// The k largest of a row.  Each thread's maximum is one of RT; the k-th largest of
-// those is no larger than the row's k-th, and few logits lie above it
-// (about RT ln(RT / (RT - k)) of them in no particular order), so the logits
-// from there on are collected and ranked by counting.  Rows whose logits
-// bunch (ties, or all large ones in one thread's columns) can have more
-// than CAND candidates: their k-th logit, and the last class that ties with
-// it, are then found bit by bit.
+// The k largest of a row.  Each thread's maximum is one of RT; the k-th
+// largest of those is no larger than the row's k-th, and few logits lie above
+// it (about RT ln(RT / (RT - k)) of them in no particular order), so the
+// logits from there on are collected and ranked by counting.  Rows whose
+// logits bunch (ties, or all large ones in one thread's columns) can have
+// more than CAND candidates: their k-th logit, and the last class that ties
+// with it, are then found bit by bit.
 // ---------------------------------------------------------------------------
-template <typename TI>
-__global__ __launch_bounds__(RT) void topk_rows_kernel(const TI* __restrict__ logits, int64_t ld, int K, int k,
-                                                       float l2t, float* __restrict__ top, int32_t* __restrict__ idx,
-                                                       float* __restrict__ rest, bool vec) {
-  __shared__ uint32_t tmax[RT];
-  __shared__ uint64_t cand[CAND];
-  __shared__ uint32_t thr, count, cnt[2][RW];
-  __shared__ uint64_t kth;
-  __shared__ float buf[RW];
-  const int64_t m = blockIdx.x;
-  const TI* s = logits + m * ld;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  uint32_t mx = 0;
-  each(s, K, vec, [&](int, float v) { mx = max(mx, order_word(v)); });
-  tmax[tid] = mx;
-  if (tid == 0) count = 0;
+struct TopkLds {
+  uint32_t tmax[RT];
+  uint64_t cand[CAND];   // order word, complement of the class
+  uint32_t thr, count, cnt[2][RW], flag;
+  uint64_t kth;
+  float buf[RW];
+};
+struct TopkP {
+  int64_t ld;
+  int K, k;
+  float l2t;   // log2 e / temperature
+  float *top, *rest;
+  int32_t* idx;
+};
+
+// The k-th largest of the threads' maxima (order words), down to its bits from LOW on.
+template <int LOW>
+__device__ __forceinline__ uint32_t kth_max(TopkLds& l, int k) {
+  const int lane = threadIdx.x & 63;
   __syncthreads();
-  if (wave == 0) {
+  if (threadIdx.x < 64) {
     uint32_t w[RW], t = 0;
 #pragma unroll
-    for (int i = 0; i < RW; ++i) w[i] = tmax[i * 64 + lane];
-    for (int bit = 31; bit >= 0; --bit) {
+    for (int i = 0; i < RW; ++i) w[i] = l.tmax[i * 64 + lane];
+    for (int bit = 31; bit >= LOW; --bit) {
       const uint32_t c = t | (1u << bit);
       int n = 0;
 #pragma unroll
       for (int i = 0; i < RW; ++i) n += __popcll(__ballot(w[i] >= c));
       if (n >= k) t = c;
     }
-    if (lane == 0) thr = t;
+    if (lane == 0) l.thr = t;
   }
   __syncthreads();
-  const uint32_t th = thr;
-  each(s, K, vec, [&](int c, float v) {
-    const uint32_t w = order_word(v);
-    if (w >= th) {
-      const uint32_t at = atomicAdd(&count, 1u);
-      if (at < (uint32_t)CAND) cand[at] = ((uint64_t)w << 32) | (uint32_t)~c;
+  return l.thr;
+}
+__device__ __forceinline__ void push(TopkLds& l, float v, int c) {
+  const uint32_t at = atomicAdd(&l.count, 1u);
+  if (at < (uint32_t)CAND) l.cand[at] = ((uint64_t)order_word(v) << 32) | (uint32_t)~c;
+}
+// Writes the k largest of n candidates; f(candidate, rank) for every candidate.
+template <typename F>
+__device__ __forceinline__ void rank(TopkLds& l, int n, int64_t m, const TopkP& p, F f) {
+  for (int i = threadIdx.x; i < n; i += RT) {
+    const uint64_t w = l.cand[i];
+    int r = 0;
+#pragma unroll 8
+    for (int j = 0; j < n; ++j) r += l.cand[j] > w;
+    if (r < p.k) {
+      p.top[m * p.k + r] = order_value((uint32_t)(w >> 32));
+      p.idx[m * p.k + r] = (int32_t)~(uint32_t)w;
+      if (r == p.k - 1) l.kth = w;
     }
+    f(w, r);
+  }
+}
+
+// Any row, from memory.
+template <typename TI, bool ONE>
+__device__ __forceinline__ void topk_any(TopkLds& l, const TI* s, int64_t m, const TopkP& p) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, K = p.K;
+  uint32_t mx = 0;
+  each<TI, RT, ONE>(s, K, [&](int, float v) { mx = max(mx, order_word(v)); });
+  __syncthreads();
+  l.tmax[tid] = mx;
+  if (tid == 0) l.count = 0;
+  const uint32_t th = kth_max<0>(l, p.k);
+  each<TI, RT, ONE>(s, K, [&](int c, float v) {
+    if (order_word(v) >= th) push(l, v, c);
   });
   __syncthreads();
-  int n = (int)min(count, (uint32_t)CAND);
-  if (count > (uint32_t)CAND) {
-    // the k-th word: the largest with at least k words from it on
-    uint64_t t = 0;   // word, then ~class: the same order as the candidates'
+  int n = (int)min(l.count, (uint32_t)CAND);
+  if (l.count > (uint32_t)CAND) {
+    // the k-th: the largest word (and complement of the class) with k of them from it on
+    uint64_t t = 0;
     int par = 0;
     for (int bit = 63; bit >= 0; --bit) {
       const uint64_t c = t | (1ull << bit);
@@ -144,55 +234,166 @@ __global__ __launch_bounds__(RT) void topk_rows_kernel(const TI* __restrict__ lo
         continue;
       }
       uint32_t mine = 0;
-      each(s, K, vec, [&](int col, float v) {
+      each<TI, RT, ONE>(s, K, [&](int col, float v) {
         mine += ((((uint64_t)order_word(v)) << 32) | (uint32_t)~col) >= c;
       });
 #pragma unroll
       for (int o = 32; o > 0; o >>= 1) mine += __shfl_xor(mine, o);
-      if (lane == 0) cnt[par][wave] = mine;
+      if (lane == 0) l.cnt[par][wave] = mine;
       __syncthreads();
       uint32_t all = 0;
 #pragma unroll
-      for (int i = 0; i < RW; ++i) all += cnt[par][i];
-      if (all >= (uint32_t)k) t = c;
+      for (int i = 0; i < RW; ++i) all += l.cnt[par][i];
+      if (all >= (uint32_t)p.k) t = c;
       par ^= 1;
     }
-    if (tid == 0) count = 0;
+    if (tid == 0) l.count = 0;
     __syncthreads();
-    each(s, K, vec, [&](int c, float v) {
-      const uint64_t w = ((uint64_t)order_word(v) << 32) | (uint32_t)~c;
-      if (w >= t) cand[atomicAdd(&count, 1u)] = w;   // exactly k
+    each<TI, RT, ONE>(s, K, [&](int c, float v) {
+      if ((((uint64_t)order_word(v) << 32) | (uint32_t)~c) >= t) push(l, v, c);   // exactly k
     });
     __syncthreads();
-    n = k;
+    n = p.k;
   }
-  for (int i = tid; i < n; i += RT) {
-    const uint64_t w = cand[i];
-    int r = 0;
-    for (int j = 0; j < n; ++j) r += cand[j] > w;
-    if (r < k) {
-      top[m * k + r] = order_value((uint32_t)(w >> 32));
-      idx[m * k + r] = (int32_t)~(uint32_t)w;
-      if (r == k - 1) kth = w;
-    }
-  }
-  if (!rest) return;
+  rank(l, n, m, p, [](uint64_t, int) {});
+  if (!p.rest) return;
   __syncthreads();
-  const uint64_t last = kth;
+  const uint64_t last = l.kth;
   float rm = -INFINITY;
-  each(s, K, vec, [&](int c, float v) {
+  each<TI, RT, ONE>(s, K, [&](int c, float v) {
     if ((((uint64_t)order_word(v) << 32) | (uint32_t)~c) < last) rm = max_nan(rm, v);
   });
-  rm = row_max(rm, buf);
+  rm = row_max(rm, l.buf);
   float sum = 0.f;
   if (fabsf(rm) < INFINITY) {
-    each(s, K, vec, [&](int c, float v) {
-      if ((((uint64_t)order_word(v) << 32) | (uint32_t)~c) < last) sum += exp2_((v - rm) * l2t);
+    each<TI, RT, ONE>(s, K, [&](int c, float v) {
+      if ((((uint64_t)order_word(v) << 32) | (uint32_t)~c) < last) sum += exp2_((v - rm) * p.l2t);
     });
   }
-  sum = row_sum(sum, buf);
+  sum = row_sum(sum, l.buf);
   // the others' largest logit alone where it is infinite or a NaN, or there is none
-  if (tid == 0) rest[m] = fabsf(rm) < INFINITY ? rm * (l2t * LN2_F) + log2f(sum) * LN2_F : rm;
+  if (tid == 0) p.rest[m] = fabsf(rm) < INFINITY ? rm * (p.l2t * LN2_F) + log2f(sum) * LN2_F : rm;
+}
+
+template <typename TI>
+__global__ __launch_bounds__(RT) void topk_any_kernel(const TI* __restrict__ logits, const TopkP p) {
+  __shared__ TopkLds l;
+  topk_any<TI, false>(l, logits + (int64_t)blockIdx.x * p.ld, blockIdx.x, p);
+}
+
+// A row in registers, read once.  Candidates leave the registers (-inf in
+// their place), so that what stays is of the others; their sum is taken from the threshold,
+// which no other exceeds, and again from their own maximum where that leaves
+// nothing.  Rows with a NaN, and rows with too many candidates, go the way of any row.
+template <typename TI, int V, int NV>
+__global__ __launch_bounds__(RT, 4) void topk_rows_kernel(const TI* __restrict__ logits, const TopkP p) {
+  __shared__ TopkLds l;
+  const int64_t m = blockIdx.x;
+  const TI* s = logits + m * p.ld;
+  const int tid = threadIdx.x;
+  Row<TI, V, NV, RT> row;
+  row.load(s, p.K);
+  if (tid == 0) {
+    l.count = 0;
+    l.flag = 0;
+  }
+  __syncthreads();
+  float vm[NV], mx = -INFINITY;
+  bool nan = false;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    vm[i] = row.get(i, 0);
+#pragma unroll
+    for (int j = 1; j < V; ++j) vm[i] = fmaxf(vm[i], row.get(i, j));
+    if constexpr (V == 1) nan |= vm[i] != vm[i];
+    else {
+#pragma unroll
+      for (int j = 0; j < V; j += 2) nan |= __builtin_isunordered(row.get(i, j), row.get(i, j + 1));
+    }
+    mx = fmaxf(mx, vm[i]);
+  }
+  mx = fmaxf(mx, row.tail);
+  nan |= row.tail != row.tail;
+  if (nan) l.flag = 1;
+  l.tmax[tid] = order_word(mx);
+  // bf16: the lower 16 bits of all order words are alike; float32: a threshold
+  // rounded down to 11 bits lets a few more pass and takes a third fewer steps
+  constexpr uint32_t LOWEST = 0x007fffffu;   // of -inf
+  const uint32_t tw = max(kth_max<std::is_same<TI, bf16>::value ? 16 : 12>(l, p.k), LOWEST);
+  const float thr = order_value(tw);
+  row.again();
+  if (l.flag) {
+    topk_any<TI, true>(l, s, m, p);
+    return;
+  }
+  const int whole = row.whole(p.K);
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    if (vm[i] >= thr && row.has(i, whole)) {
+      // few vectors come here, and fewer of their values: those are read
+      // again, so that this is one loop and not a branch per value
+      uint32_t bits = 0;
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const bool in = row.get(i, j) >= thr;
+        bits |= in ? 1u << j : 0u;
+        if (in) row.drop(i, j);
+      }
+      for (; bits; bits &= bits - 1) {
+        const int c = row.col(i) + __builtin_ctz(bits);
+        push(l, to_f32(s[c]), c);
+      }
+    }
+  }
+  if (row.tail >= thr && row.tail_col(p.K) < p.K) {
+    push(l, row.tail, row.tail_col(p.K));
+    row.tail = -INFINITY;
+  }
+  __syncthreads();
+  const int n = (int)l.count;
+  if (n > CAND) {
+    topk_any<TI, true>(l, s, m, p);
+    return;
+  }
+  const float ref = fabsf(thr) < INFINITY ? thr * p.l2t : 0.f;
+  float sum = 0.f, rm = -INFINITY;
+  rank(l, n, m, p, [&](uint64_t w, int r) {
+    if (r < p.k) return;
+    const float v = order_value((uint32_t)(w >> 32));
+    sum += exp2_(v * p.l2t - ref);
+    rm = fmaxf(rm, v);
+  });
+  if (!p.rest) return;
+  row.again();
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+#pragma unroll
+    for (int j = 0; j < V; ++j) sum += exp2_(row.get(i, j) * p.l2t - ref);
+  sum += exp2_(row.tail * p.l2t - ref);
+  sum = row_sum(sum, l.buf);
+  if (sum > 1e-20f && sum < 1e30f) {
+    if (tid == 0) p.rest[m] = (ref + log2f(sum)) * LN2_F;
+    return;
+  }
+  // far below the threshold, or infinite
+  row.again();
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+#pragma unroll
+    for (int j = 0; j < V; ++j) rm = fmaxf(rm, row.get(i, j));
+  rm = row_max(fmaxf(rm, row.tail), l.buf);
+  sum = 0.f;
+  if (fabsf(rm) < INFINITY) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int j = 0; j < V; ++j) sum += exp2_((row.get(i, j) - rm) * p.l2t);
+    sum += exp2_((row.tail - rm) * p.l2t);
+    for (int i = tid; i < n; i += RT)
+      if (l.cand[i] < l.kth) sum += exp2_((order_value((uint32_t)(l.cand[i] >> 32)) - rm) * p.l2t);
+  }
+  sum = row_sum(sum, l.buf);
+  if (tid == 0) p.rest[m] = fabsf(rm) < INFINITY ? rm * (p.l2t * LN2_F) + log2f(sum) * LN2_F : rm;
 }
 
 // ---------------------------------------------------------------------------
@@ -211,152 +412,254 @@ struct DistillP {
   float* row_loss;
   int K, k, pad;
   float it2, tau, soft, hard, scale;   // it2: log2 e / tau
-  bool vec, vecd;
+};
+// Threads of a row: 512 with 64 values each, two rows on a CU.  (2688 bf16 rows
+// of 32000, labels given / not: 100 / 70 us; 256 threads 99 / 74, but float32 279 against 79; 1024
+// threads 142 / 115.)
+static constexpr int DT = RT;
+static_assert(MAXK <= DT, "an entry a thread");
+struct DistillLds {
+  float pv[MAXK];
+  int32_t iv[MAXK];
+  float buf[8][DT / 64];
+  uint32_t dup;
 };
 
-template <typename TI, typename TO>
-__global__ __launch_bounds__(RT) void distill_rows_kernel(const TI* logits, TO* dlogits, const DistillP p) {
-  extern __shared__ uint32_t listed[];   // a bit per class
-  __shared__ float pv[MAXK], uv[MAXK];
-  __shared__ int32_t iv[MAXK];
-  __shared__ float buf[RW];
-  __shared__ uint32_t dup;
+// Joins a wave's values (0: sum, 1: maximum) into buf; after a barrier all_of adds the waves up.
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
+  return v;
+}
+__device__ __forceinline__ void put_wave(float* buf, float v) {
+  if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = v;
+}
+__device__ __forceinline__ float all_sum(const float* buf) {
+  float t = buf[0];
+#pragma unroll
+  for (int w = 1; w < DT / 64; ++w) t += buf[w];
+  return t;
+}
+__device__ __forceinline__ float all_max(const float* buf) {
+  float t = buf[0];
+#pragma unroll
+  for (int w = 1; w < DT / 64; ++w) t = fmaxf(t, buf[w]);
+  return t;
+}
+
+// A row's other classes (those that are not listed): in registers, or, NV = 0, read
+// from memory by each pass.  others(f) calls f(value) for each, the listed
+// ones and what lies behind K as -inf; write(f) stores f(value) in their place.
+template <typename TI, typename TO, int V, int NV> struct Others {
+  Row<TI, V, NV, DT> row;
+  __device__ __forceinline__ void load(const TI* s, int K) { row.load(s, K); }
+  __device__ __forceinline__ void mask(const uint32_t* listed, int K) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = row.col(i);
+      // V columns never straddle a word
+      const uint32_t bits = (listed[c >> 5] >> (c & 31)) & ((1u << V) - 1);
+      if (bits) {
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+          if ((bits >> j) & 1u) row.drop(i, j);
+      }
+    }
+    const int c = row.tail_col(K);
+    if (c < K && ((listed[c >> 5] >> (c & 31)) & 1u)) row.tail = -INFINITY;
+  }
+  template <typename F> __device__ __forceinline__ void others(const TI*, int, const uint32_t*, F f) {
+    row.again();
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) f(row.get(i, j));
+      if constexpr (V > 1) __builtin_amdgcn_sched_barrier(0);   // one vector at a time: fewer registers
+    }
+    if constexpr (V > 1) f(row.tail);
+  }
+  template <typename F> __device__ __forceinline__ void write(const TI*, TO* d, int K, const uint32_t*, F f) {
+    row.again();
+    const int n = row.whole(K);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      TO o[V];
+#pragma unroll
+      for (int j = 0; j < V; ++j) o[j] = from_f32<TO>(f(row.get(i, j)));
+      if (row.has(i, n)) __builtin_memcpy(row.at(d, i), o, V * sizeof(TO));
+      if constexpr (V > 1) __builtin_amdgcn_sched_barrier(0);
+    }
+    if (row.tail_col(K) < K) d[row.tail_col(K)] = from_f32<TO>(f(row.tail));
+  }
+};
+template <typename TI, typename TO, int V> struct Others<TI, TO, V, 0> {
+  __device__ __forceinline__ void load(const TI*, int) {}
+  __device__ __forceinline__ void mask(const uint32_t*, int) {}
+  static __device__ __forceinline__ float of(const uint32_t* listed, int c, float v) {
+    return ((listed[c >> 5] >> (c & 31)) & 1u) ? -INFINITY : v;
+  }
+  template <typename F> __device__ __forceinline__ void others(const TI* s, int K, const uint32_t* listed, F f) const {
+    each<TI, DT>(s, K, [&](int c, float v) { f(of(listed, c, v)); });
+  }
+  template <typename F>
+  __device__ __forceinline__ void write(const TI* s, TO* d, int K, const uint32_t* listed, F f) const {
+    // a thread writes only where it has read (d may be s)
+    const int done = K / V * V;
+    for (int c = (int)threadIdx.x * V; c < done; c += DT * V) {
+      TI v[V];
+      TO o[V];
+      __builtin_memcpy(v, s + c, V * sizeof(TI));
+#pragma unroll
+      for (int j = 0; j < V; ++j) o[j] = from_f32<TO>(f(of(listed, c + j, to_f32(v[j]))));
+      __builtin_memcpy(d + c, o, V * sizeof(TO));
+    }
+    const int c = done + (int)threadIdx.x;
+    if (c < K) d[c] = from_f32<TO>(f(of(listed, c, to_f32(s[c]))));
+  }
+};
+
+// HARD: with the labels' cross-entropy.
+template <typename TI, typename TO, int V, int NV, bool HARD>
+__global__ __launch_bounds__(DT, 4) void distill_rows_kernel(const TI* logits, TO* dlogits, const DistillP p) {
+  extern __shared__ uint32_t listed[];   // a bit per class, to the end of the registers' columns
+  __shared__ DistillLds l;
   const int64_t m = blockIdx.x;
   const TI* s = logits + m * p.ld;
   TO* d = dlogits + m * p.ldd;
   const int tid = threadIdx.x, K = p.K;
   const float weight = p.weights ? p.weights[m] : 1.f;
-  for (int c = K + tid; c < K + p.pad; c += RT) d[c] = from_f32<TO>(0.f);
+  for (int c = K + tid; c < K + p.pad; c += DT) d[c] = from_f32<TO>(0.f);
   if (weight == 0.f) {
-    for (int c = tid; c < K; c += RT) d[c] = from_f32<TO>(0.f);
+    for (int c = tid; c < K; c += DT) d[c] = from_f32<TO>(0.f);
     if (tid == 0) p.row_loss[m] = 0.f;
     return;
   }
-  const int words = (K + 31) / 32;
-  for (int i = tid; i < words; i += RT) listed[i] = 0;
-  if (tid == 0) dup = 0;
-  __syncthreads();
-  // the teacher's probabilities (base-2 exponents throughout)
+  Others<TI, TO, V, NV> row;
+  row.load(s, K);   // in flight while the teacher's part runs
+  const int words = (NV ? NV * V * DT : K + 31) / 32;
+  for (int i = tid; i < words; i += DT) listed[i] = 0;
+  if (tid == 0) l.dup = 0;
   int at = -1;
-  float t2 = -INFINITY;
+  float t2 = -INFINITY, sv = -INFINITY;   // the entry's teacher logit (times log2 e / tau), student logit
   if (tid < p.k) {
     at = p.idx[m * p.k + tid];
     if (at < 0 || at >= K) at = -1;
     else {
       t2 = p.top[m * p.k + tid] * p.it2;
-      if (atomicOr(&listed[at >> 5], 1u << (at & 31)) & (1u << (at & 31))) dup = 1;
+      sv = to_f32(s[at]);
     }
-    iv[tid] = at;
+    l.iv[tid] = at;
   }
   const float r2 = p.rest ? p.rest[m] * LOG2E_F : -INFINITY;
-  const float tm = row_max(max_nan(t2, r2), buf);
-  float prob = 0.f, r = 0.f, tz = 1.f;
-  const bool taught = !(tm == -INFINITY);
-  if (taught) {
-    prob = exp2_(t2 - tm);
-    r = exp2_(r2 - tm);
-  }
-  tz = row_sum(prob, buf) + r;
-  if (taught) { prob /= tz; r /= tz; }
-  float lp = taught ? t2 - tm - log2f(tz) : 0.f;   // log2 of it
-  const float lr = taught ? r2 - tm - log2f(tz) : 0.f;
-  float own = prob;       // of the entry's class
-  bool lead = at >= 0;    // the class's first entry
-  if (tid < p.k) pv[tid] = prob;
+  const int lab = HARD ? p.labels[m] : -1;
+  const bool marked = HARD && lab >= 0 && lab < K;
+  const float sl = marked ? to_f32(s[lab]) : 0.f;
   __syncthreads();
-  if (dup && at >= 0) {
+  if (at >= 0 && (atomicOr(&listed[at >> 5], 1u << (at & 31)) & (1u << (at & 31)))) l.dup = 1;
+  put_wave(l.buf[0], wave_max(t2));
+  put_wave(l.buf[1], wave_max(sv));
+  __syncthreads();
+  // the teacher's probabilities (base-2 exponents throughout)
+  const float tm = fmaxf(all_max(l.buf[0]), r2), lm = all_max(l.buf[1]);
+  const bool taught = !(tm == -INFINITY);
+  const float e = taught ? exp2_(t2 - tm) : 0.f, er = taught ? exp2_(r2 - tm) : 0.f;
+  if (tid < p.k) l.pv[tid] = e;
+  put_wave(l.buf[2], wave_sum(e));
+  row.mask(listed, K);
+  float rm = -INFINITY;
+  row.others(s, K, listed, [&](float v) { rm = fmaxf(rm, v); });
+  put_wave(l.buf[3], wave_max(rm));
+  __syncthreads();
+  const float tz = all_sum(l.buf[2]) + er, l2tz = taught ? tm + log2f(tz) : 0.f;
+  const float prob = taught ? e / tz : 0.f, r = taught ? er / tz : 0.f;
+  float lp = t2 - l2tz;     // log2 of the entry's probability
+  float own = prob;         // of its class
+  bool lead = at >= 0;      // the class's first entry
+  if (l.dup && at >= 0) {
     own = 0.f;
     for (int j = 0; j < p.k; ++j)
-      if (iv[j] == at) {
-        own += pv[j];
+      if (l.iv[j] == at) {
+        own += l.pv[j];
         if (j < tid) lead = false;
       }
+    own /= tz;
     lp = log2f(own);
   }
-  // the student's maxima: the others' (times log2 e / tau), the row's
-  float rm = -INFINITY, am = -INFINITY;
-  each(s, K, p.vec, [&](int c, float v) {
-    am = max_nan(am, v);
-    if (!((listed[c >> 5] >> (c & 31)) & 1u)) rm = max_nan(rm, v);
-  });
-  rm = row_max(rm, buf) * p.it2;
-  am = row_max(am, buf);
-  const float rref = rm == -INFINITY ? 0.f : rm, aref = am == -INFINITY ? 0.f : am;
+  // maxima: the others' (as an exponent), the row's
+  rm = all_max(l.buf[3]);
+  const float am = fmaxf(rm, lm), aref = am == -INFINITY ? 0.f : am;
+  const float rref = rm == -INFINITY ? 0.f : rm * p.it2, um = aref * p.it2;
+  const float eo = rm == -INFINITY ? 0.f : exp2_(rref - um);   // the others' sums, from the row's maximum
+  const float h2 = -aref * LOG2E_F;
   float zr = 0.f, z1 = 0.f;
-  each(s, K, p.vec, [&](int c, float v) {
-    if (!((listed[c >> 5] >> (c & 31)) & 1u)) zr += exp2_(v * p.it2 - rref);
-    if (p.labels) z1 += exp2_((v - aref) * LOG2E_F);
+  row.others(s, K, listed, [&](float v) {
+    zr += exp2_(v * p.it2 - rref);
+    if constexpr (HARD) z1 += exp2_(v * LOG2E_F + h2);
   });
-  zr = row_sum(zr, buf);
-  if (p.labels) z1 = row_sum(z1, buf);
-  // the listed logits, before any gradient is written over them
-  const float sv = at >= 0 ? to_f32(s[at]) : -INFINITY, u = sv * p.it2;
-  const float um = aref * p.it2;   // the row's maximum, as u
+  const float u = sv * p.it2;
   const float ez = lead ? exp2_(u - um) : 0.f;
-  const float eo = rm == -INFINITY ? 0.f : exp2_(rref - um);   // the others' sum in the same terms
-  const float z = row_sum(ez, buf) + zr * eo;
+  if (HARD && lead) z1 += exp2_(sv * LOG2E_F + h2);
+  put_wave(l.buf[4], wave_sum(zr));
+  put_wave(l.buf[5], wave_sum(ez));
+  if constexpr (HARD) put_wave(l.buf[6], wave_sum(z1));
+  __syncthreads();   // every listed logit and the label's have been read, too
+  zr = all_sum(l.buf[4]);
+  const float z = all_sum(l.buf[5]) + zr * eo;
+  if constexpr (HARD) z1 = all_sum(l.buf[6]);
   const float l2z = log2f(z);
-  float kl = 0.f;
-  if (at >= 0 && prob > 0.f) kl = prob * (lp - (u - um - l2z));
-  kl = row_sum(kl, buf);
-  if (r > 0.f) kl += r * (lr - (log2f(zr) + rref - um - l2z));
-  const int lab = p.labels ? p.labels[m] : -1;
-  const bool marked = lab >= 0 && lab < K;
-  const float sl = marked ? to_f32(s[lab]) : 0.f;
-  float loss = taught ? p.soft * p.tau * p.tau * kl * LN2_F : 0.f;
-  if (marked) loss += p.hard * (aref + log2f(z1) * LN2_F - sl);
-  if (tid == 0) p.row_loss[m] = weight * loss;
+  put_wave(l.buf[7], wave_sum(at >= 0 && prob > 0.f ? prob * (lp - (u - um - l2z)) : 0.f));
   const float ks = taught ? p.scale * weight * p.soft * p.tau : 0.f, kh = marked ? p.scale * weight * p.hard : 0.f;
   const float cr = ks * (eo / z - (r > 0.f && zr > 0.f ? r / zr : 0.f));   // of e^(u - rref) in the others
   const float ch = marked ? kh / z1 : 0.f;
-  __syncthreads();   // every listed logit and the label's have been read
-  {
-    // a class's dense part; the listed ones' soft part follows
-    auto grad = [&](int c, float v) {
-      float g = 0.f;
-      if (!((listed[c >> 5] >> (c & 31)) & 1u)) g = cr * exp2_(v * p.it2 - rref);
-      if (marked) {
-        g += ch * exp2_((v - aref) * LOG2E_F);
-        if (c == lab) g -= kh;
-      }
-      return g;
-    };
-    constexpr int V = Wide<TI>::n;
-    typedef typename Wide<TI>::type W;
-    int done = 0;
-    if (p.vec && p.vecd) {
-      done = K / V * V;
-      for (int c = tid * V; c < done; c += RT * V) {
-        const W v = *(const W*)(s + c);
-        TO o[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) o[i] = from_f32<TO>(grad(c + i, (float)v[i]));
-        __builtin_memcpy(__builtin_assume_aligned(d + c, V * sizeof(TO)), o, V * sizeof(TO));
-      }
-    }
-    for (int c = done + tid; c < K; c += RT) d[c] = from_f32<TO>(grad(c, to_f32(s[c])));
-  }
-  __syncthreads();   // the dense parts lie before the listed ones' values
+  row.write(s, d, K, listed, [&](float v) {
+    float g = cr * exp2_(v * p.it2 - rref);
+    if constexpr (HARD) g += ch * exp2_(v * LOG2E_F + h2);
+    return g;
+  });
+  __syncthreads();   // the others lie before what replaces the listed ones' and the label's values
   if (lead) {
     float g = ks * (ez / z - own);
-    if (marked) {
-      g += ch * exp2_((sv - aref) * LOG2E_F);
+    if constexpr (HARD) {
+      g += ch * exp2_(sv * LOG2E_F + h2);
       if (at == lab) g -= kh;
     }
     d[at] = from_f32<TO>(g);
   }
+  if (tid != 0) return;
+  if (marked && !((listed[lab >> 5] >> (lab & 31)) & 1u))
+    d[lab] = from_f32<TO>(cr * exp2_(sl * p.it2 - rref) + ch * exp2_(sl * LOG2E_F + h2) - kh);
+  float loss = 0.f;
+  if (taught) {
+    float kl = all_sum(l.buf[7]);
+    if (r > 0.f) kl += r * (r2 - l2tz - (log2f(zr) + rref - um - l2z));
+    loss = p.soft * p.tau * p.tau * kl * LN2_F;
+  }
+  if (marked) loss += p.hard * (aref + log2f(z1) * LN2_F - sl);
+  p.row_loss[m] = weight * loss;
 }
 
 // ---------------------------------------------------------------------------
 // Host side.
 // ---------------------------------------------------------------------------
+// Columns that a row in registers may have, element by element and 16 bytes at
+// a time.  Short rows go element by element: their few 16-byte pieces would
+// leave most threads without a maximum of their own.
+static constexpr int SHORT = 8 * RT;
+static constexpr int LONG = 64 * RT;
+template <typename TI, int T> struct Long { static constexpr int V = Wide<TI>::n, NV = LONG / T / V, K = LONG; };
+
 template <typename TI>
 int topk_rows(const TI* logits, int64_t ld, int64_t M, int32_t K, int32_t k, float temperature, float* top,
               int32_t* idx, float* rest, hipStream_t stream) {
-  constexpr int V = Wide<TI>::n;
-  const bool vec = ((uintptr_t)logits % 16) == 0 && ld % V == 0;
-  BLSTM_LAUNCH("softmax_topk_rows", topk_rows_kernel<TI>, dim3((unsigned)M), dim3(RT), 0, stream, logits, ld, K, k,
-               LOG2E_F / temperature, top, idx, rest, vec);
+  using L = Long<TI, RT>;
+  const TopkP p{ld, K, k, LOG2E_F / temperature, top, rest, idx};
+  const dim3 grid((unsigned)M), block(RT);
+  if (K <= SHORT)
+    BLSTM_LAUNCH("softmax_topk_rows", (topk_rows_kernel<TI, 1, 8>), grid, block, 0, stream, logits, p);
+  else if (K <= L::K)
+    BLSTM_LAUNCH("softmax_topk_rows", (topk_rows_kernel<TI, L::V, L::NV>), grid, block, 0, stream, logits, p);
+  else
+    BLSTM_LAUNCH("softmax_topk_rows", topk_any_kernel<TI>, grid, block, 0, stream, logits, p);
   return blstm_check_launch("softmax_topk_rows");
 }
 template int topk_rows<float>(const float*, int64_t, int64_t, int32_t, int32_t, float, float*, int32_t*, float*, hipStream_t);
@@ -365,16 +668,20 @@ template int topk_rows<bf16>(const bf16*, int64_t, int64_t, int32_t, int32_t, fl
 template <typename TI, typename TO>
 int distill_rows(const TI* logits, int64_t ld, int64_t M, int32_t K, const softmax_teacher* t, float loss_scale,
                  float* row_loss, TO* dlogits, int64_t ldd, int32_t pad, hipStream_t stream) {
-  constexpr int V = Wide<TI>::n;
+  using L = Long<TI, DT>;
   DistillP p{};
   p.ld = ld; p.ldd = ldd; p.top = t->top; p.rest = t->rest; p.weights = t->weights; p.idx = t->idx;
   p.labels = t->hard != 0.f ? t->labels : nullptr;
   p.row_loss = row_loss; p.K = K; p.k = t->k; p.pad = pad;
   p.it2 = LOG2E_F / t->temperature; p.tau = t->temperature; p.soft = t->soft; p.hard = t->hard; p.scale = loss_scale;
-  p.vec = ((uintptr_t)logits % 16) == 0 && ld % V == 0;
-  p.vecd = ((uintptr_t)dlogits % (V * sizeof(TO))) == 0 && ldd % V == 0;
-  BLSTM_LAUNCH("softmax_distill_rows", (distill_rows_kernel<TI, TO>), dim3((unsigned)M), dim3(RT),
-               (size_t)cdiv(K, 32) * 4, stream, logits, dlogits, p);
+#define ROWS(V, NV, HARD, BYTES)                                                                                      \
+  BLSTM_LAUNCH("softmax_distill_rows", (distill_rows_kernel<TI, TO, V, NV, HARD>), dim3((unsigned)M), dim3(DT), BYTES, \
+               stream, logits, dlogits, p)
+#define ROWS_BY_K(HARD)                                           \
+  if (K <= SHORT) ROWS(1, SHORT / DT, HARD, SHORT / 8);                    \
+  else if (K <= L::K) ROWS(L::V, L::NV, HARD, L::K / 8);          \
+  else ROWS(L::V, 0, HARD, (size_t)cdiv(K, 32) * 4);
+  if (p.labels) { ROWS_BY_K(true) } else { ROWS_BY_K(false) }
   return blstm_check_launch("softmax_distill_rows");
 }
 template int distill_rows<float, float>(const float*, int64_t, int64_t, int32_t, const softmax_teacher*, float, float*, float*, int64_t, int32_t, hipStream_t);

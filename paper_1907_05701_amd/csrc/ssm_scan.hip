@@ -726,13 +726,17 @@ __global__ __launch_bounds__(256) void ssm_scan_sum_kernel(const ScanSum p) {
 }
 
 // One frame of B streams: LPC lanes a channel, four states each; the state is
-// read and written once.
+// read and written once, which bounds the kernel.  A thread has CPT channels,
+// whose states it loads before it computes, and reads B and C once for them.
+static constexpr int CPT = 4;
 template <typename T, int LPC>
 __global__ __launch_bounds__(256) void ssm_scan_step_kernel(const ScanP p, const int32_t* __restrict__ slots,
                                                             int n_slots, float* state) {
-  constexpr int CH = 256 / LPC;   // channels of a workgroup
-  const int tiles = (p.D + CH - 1) / CH;
-  const int b = (int)(blockIdx.x / (unsigned)tiles), d = (int)(blockIdx.x % (unsigned)tiles) * CH + threadIdx.x / LPC;
+  constexpr int CH = 256 / LPC;   // channels that a workgroup has at a time
+  // workgroups do not cross groups: B and C are one row for all of its channels
+  const int per = p.tpg, tiles = p.G * per;
+  const int b = (int)(blockIdx.x / (unsigned)tiles), tile = (int)(blockIdx.x % (unsigned)tiles);
+  const int g = tile / per, c0 = tile % per * CH * CPT + threadIdx.x / LPC;   // within the group
   const int part = threadIdx.x % LPC;
   __shared__ int taken;
   int slot = b;
@@ -745,35 +749,51 @@ __global__ __launch_bounds__(256) void ssm_scan_step_kernel(const ScanP p, const
     __syncthreads();
     if (taken || slot < 0 || slot >= n_slots) slot = -1;
   }
-  if (d >= p.D) return;
-  float o = 0.f, xv = 0.f;
-  if (slot >= 0) {
-    const int g = d / p.Dg;
-    xv = to_f32(((const T*)p.x)[(int64_t)b * p.ldx + d]);
-    float s = to_f32(((const T*)p.dt)[(int64_t)b * p.lddt + d]) + (p.dtb ? p.dtb[d] : 0.f);
-    if (p.softplus) s = softplusf_(s);
-    const float u = s * xv;
-    const int64_t row = (int64_t)slot * p.D + d;
-    States<4> h = ld_states<4>(state, row, p.N, part * 4, true);
-    const States<4> A = ld_states<4>(p.A, d, p.N, part * 4, true);
-    const T* Bm = (const T*)p.Bm + (int64_t)b * p.ldb + g * p.N;
-    const T* Cm = (const T*)p.Cm + (int64_t)b * p.ldc + g * p.N;
+  T* y = (T*)p.y + (int64_t)b * p.ldy + g * p.Dg;
+  if (slot < 0) {
+    for (int i = 0; i < CPT; ++i)
+      if (part == 0 && c0 + i * CH < p.Dg) y[c0 + i * CH] = from_f32<T>(0.f);
+    return;
+  }
+  States<4> h[CPT], A[CPT];
+  float x[CPT], dt[CPT], z[CPT], skip[CPT];
+#pragma unroll
+  for (int i = 0; i < CPT; ++i) {
+    const int c = c0 + i * CH, d = g * p.Dg + c;
+    const bool on = c < p.Dg;
+    h[i] = ld_states<4>(state, (int64_t)slot * p.D + d, p.N, part * 4, on);
+    A[i] = ld_states<4>(p.A, d, p.N, part * 4, on);
+    x[i] = dt[i] = z[i] = skip[i] = 0.f;
+    if (on) {
+      x[i] = to_f32(((const T*)p.x)[(int64_t)b * p.ldx + d]);
+      dt[i] = to_f32(((const T*)p.dt)[(int64_t)b * p.lddt + d]) + (p.dtb ? p.dtb[d] : 0.f);
+      if (p.z) z[i] = to_f32(((const T*)p.z)[(int64_t)b * p.ldz + d]);
+      if (p.Dskip) skip[i] = p.Dskip[d];
+    }
+  }
+  const T* Bm = (const T*)p.Bm + (int64_t)b * p.ldb + g * p.N;
+  const T* Cm = (const T*)p.Cm + (int64_t)b * p.ldc + g * p.N;
+  float Bv[4], Cv[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int n = part * 4 + j;
+    Bv[j] = n < p.N ? to_f32(Bm[n]) : 0.f;
+    Cv[j] = n < p.N ? to_f32(Cm[n]) : 0.f;
+  }
+#pragma unroll
+  for (int i = 0; i < CPT; ++i) {
+    const int c = c0 + i * CH;
+    const float s = p.softplus ? softplusf_(dt[i]) : dt[i], u = s * x[i], s2 = s * LOG2E_F;
+    float o = 0.f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int n = part * 4 + j;
-      const float Bv = n < p.N ? to_f32(Bm[n]) : 0.f, Cv = n < p.N ? to_f32(Cm[n]) : 0.f;
-      h.v[j] = __builtin_amdgcn_exp2f(s * LOG2E_F * A.v[j]) * h.v[j] + u * Bv;
-      o += Cv * h.v[j];
+      h[i].v[j] = __builtin_amdgcn_exp2f(s2 * A[i].v[j]) * h[i].v[j] + u * Bv[j];
+      o += Cv[j] * h[i].v[j];
     }
-    st_states<4>(state, row, p.N, part * 4, true, h);
-  }
-  o = group_sum<LPC>(o);
-  if (part == 0) {
-    if (slot >= 0) {
-      if (p.Dskip) o += p.Dskip[d] * xv;
-      if (p.z) o *= siluf_(to_f32(((const T*)p.z)[(int64_t)b * p.ldz + d]));
-    }
-    ((T*)p.y)[(int64_t)b * p.ldy + d] = from_f32<T>(o);
+    st_states<4>(state, (int64_t)slot * p.D + g * p.Dg + c, p.N, part * 4, c < p.Dg, h[i]);
+    o = group_sum<LPC>(o) + skip[i] * x[i];
+    if (p.z) o *= siluf_(z[i]);
+    if (part == 0 && c < p.Dg) y[c] = from_f32<T>(o);
   }
 }
 
@@ -1004,7 +1024,8 @@ extern "C" int ssm_scan_step(const ssm_dims* dims, const ssm_scan_in* in, const 
   if (ldy < dims->D) return blstm_fail(BLSTM_EINVAL, "ssm_scan_step: a row pitch is below its row");
   p.y = y; p.ldy = ldy;
   const int lpc = lanes_of(dims->N, 4);
-  const int64_t blocks = (int64_t)dims->B * cdiv(dims->D, 256 / lpc);
+  p.tpg = (int)cdiv(p.Dg, 256 / lpc * CPT);
+  const int64_t blocks = (int64_t)dims->B * dims->G * p.tpg;
   if (blocks > 0x7fffffff) return blstm_fail(BLSTM_EUNSUPPORTED, "ssm_scan_step: B*D too large");
 #define STEP(T, L)                                                                                                \
   case L:                                                                                                         \
