@@ -19,7 +19,8 @@ struct ConvP {
   void *y, *sto, *dx, *dstate;
   float* part;   // [row blocks][W + 1][D]: dw by taps, then dbias
   int T, B, D, C4, nseg, silu;
-  bool vx, vdy, vy, vdx, vs;   // 4-wide accesses possible (vs: state rows)
+  bool vx, vdy, vy, vdx, vs, vw;   // 4-wide accesses possible (vs: state rows, vw: weights)
+  int tx, ncb;   // forward: threads along the channels, workgroups along them
 };
 
 __device__ __forceinline__ int conv_len(const ConvP& p, int b) {
@@ -38,6 +39,17 @@ __device__ __forceinline__ typename Vec4<T>::type conv_input(const ConvP& p, int
 template <int W>
 __device__ __forceinline__ void conv_weights(const ConvP& p, int c, int nv, f32x4* w, f32x4& bias) {
   bias = f32x4{0.f, 0.f, 0.f, 0.f};
+  if (p.vw && nv >= 4) {   // the four channels' taps are adjacent
+    f32x4 raw[W];
+#pragma unroll
+    for (int j = 0; j < W; ++j) raw[j] = *(const f32x4*)(p.w + (int64_t)c * W + 4 * j);
+    if (p.bias) bias = *(const f32x4*)(p.bias + c);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < W; ++j) w[j][i] = raw[(i * W + j) / 4][(i * W + j) % 4];
+    return;
+  }
 #pragma unroll
   for (int j = 0; j < W; ++j) w[j] = f32x4{0.f, 0.f, 0.f, 0.f};
   for (int i = 0; i < nv; ++i) {
@@ -49,14 +61,13 @@ __device__ __forceinline__ void conv_weights(const ConvP& p, int c, int nv, f32x
 
 template <typename T, int W>
 __global__ __launch_bounds__(256) void ssm_conv_fwd_kernel(const ConvP p) {
-  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int c = (int)(id % p.C4) * 4;
-  const int64_t r = id / p.C4;
-  const int b = (int)(r % p.B);
-  const int64_t sg = r / p.B;
-  if (sg >= p.nseg) return;
+  const unsigned tx = (unsigned)p.tx, ncb = (unsigned)p.ncb;   // tx: a power of two
+  const int c = (int)((blockIdx.x % ncb) * tx + (threadIdx.x & (tx - 1))) * 4;
+  const unsigned r = blockIdx.x / ncb * (256u / tx) + threadIdx.x / tx;   // at most T * B of them
+  const int b = (int)(r % (unsigned)p.B), sg = (int)(r / (unsigned)p.B);
+  if (sg >= p.nseg || c >= p.D) return;
   const int nv = min(4, p.D - c), len = conv_len(p, b);
-  const int t0 = (int)sg * SEG;
+  const int t0 = sg * SEG;
   typename Vec4<T>::type in[SEG + W - 1], last[W > 1 ? W - 1 : 1];
 #pragma unroll
   for (int j = 0; j < SEG + W - 1; ++j) in[j] = conv_input<T, W>(p, t0 - W + 1 + j, b, len, c, nv);
@@ -98,9 +109,9 @@ __global__ __launch_bounds__(256) void ssm_conv_bwd_kernel(const ConvP p) {
   conv_weights<W>(p, c, nv, w, bias);
 #pragma unroll
   for (int j = 0; j < W; ++j) dw[j] = db;
-  const int64_t items = (int64_t)p.nseg * p.B;
-  for (int64_t it = (int64_t)blockIdx.y * 4 + rl; it < items && nv > 0; it += (int64_t)gridDim.y * 4) {
-    const int b = (int)(it % p.B), t0 = (int)(it / p.B) * SEG, t1 = min(p.T, t0 + SEG);
+  const int items = p.nseg * p.B;   // at most T * B
+  for (int it = (int)blockIdx.y * 4 + rl; it < items && nv > 0; it += (int)gridDim.y * 4) {
+    const int b = (int)((unsigned)it % (unsigned)p.B), t0 = (int)((unsigned)it / (unsigned)p.B) * SEG, t1 = min(p.T, t0 + SEG);
     const int len = conv_len(p, b);
     // inputs t0 - W + 1 .. t0 + SEG + W - 2, gradients t0 .. t0 + SEG + W - 2
     typename Vec4<T>::type in[SEG + 2 * W - 2], gy[SEG + W - 1];
@@ -245,6 +256,7 @@ static int conv_args(const ssm_dims* d, const char* fn, const void* x, int64_t l
   p->T = d->T; p->B = d->B; p->D = d->D; p->C4 = (int)cdiv(d->D, 4);
   p->nseg = (int)cdiv(d->T, SEG);
   p->silu = flags & SSM_SILU;
+  p->vw = (uintptr_t)w % 16 == 0 && (uintptr_t)bias % 16 == 0;
   p->vx = four(x, ldx, es);
   p->vs = d->D % 4 == 0 && ((uintptr_t)state % (4 * es)) == 0;
   return BLSTM_OK;
@@ -278,7 +290,10 @@ extern "C" int ssm_conv_fwd(const ssm_dims* dims, const void* x, int64_t ldx, co
   p.y = y; p.ldy = ldy; p.sto = state_out;
   p.vy = four(y, ldy, es);
   p.vs = p.vs && ((uintptr_t)state_out % (4 * es)) == 0;
-  const int64_t blocks = cdiv((int64_t)p.C4 * p.B * p.nseg, 256);
+  p.tx = 1;
+  while (p.tx < 256 && p.tx < p.C4) p.tx *= 2;
+  p.ncb = (int)cdiv(p.C4, p.tx);
+  const int64_t blocks = cdiv((int64_t)p.B * p.nseg, 256 / p.tx) * p.ncb;
   if (blocks > 0x7fffffff) return blstm_fail(BLSTM_EUNSUPPORTED, "ssm_conv_fwd: T*B*D too large");
 #define FWD(T, W) \
   BLSTM_LAUNCH("ssm_conv_fwd", (ssm_conv_fwd_kernel<T, W>), dim3((unsigned)blocks), dim3(256), 0, stream, p)
