@@ -14,20 +14,20 @@
 #define LOG2E_F 1.4426950408889634f
 #define LN2_F 0.6931471805599453f
 static_assert(SOFTMAX_MAX_CLASSES == 1 << 18, "bits of a class");
-static constexpr int RT = 512;             // threads of a row
-static constexpr int RW = RT / 64;
+static constexpr int RT = 512;             // least threads of a row (T below: 512 or 1024)
 static constexpr int CAND = 1024;          // most candidates kept in LDS
 static constexpr int MAXK = SOFTMAX_MAX_TOP;
-static_assert(MAXK <= RT && MAXK <= CAND, "the k-th largest of the threads' maxima bounds the k-th logit");
+static_assert(MAXK <= RT && MAXK <= CAND, "an entry a thread; the k-th largest of the threads' maxima bounds the k-th logit");
 
 __device__ __forceinline__ float exp2_(float v) { return __builtin_amdgcn_exp2f(v); }
 
-// Sum and maximum over the workgroup, in lane and wave order; buf: RW floats.
+// Sum and maximum over the workgroup, in lane and wave order; buf: T / 64 floats.
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
   return v;
 }
+template <int T>
 __device__ __forceinline__ float row_sum(float v, float* buf) {
   v = wave_sum(v);
   __syncthreads();
@@ -35,11 +35,12 @@ __device__ __forceinline__ float row_sum(float v, float* buf) {
   __syncthreads();
   float t = buf[0];
 #pragma unroll
-  for (int w = 1; w < RW; ++w) t += buf[w];
+  for (int w = 1; w < T / 64; ++w) t += buf[w];
   return t;
 }
 // a NaN among the values is the maximum
 __device__ __forceinline__ float max_nan(float a, float b) { return (a > b || a != a) ? a : b; }
+template <int T>
 __device__ __forceinline__ float row_max(float v, float* buf) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v = max_nan(v, __shfl_xor(v, o));
@@ -48,7 +49,7 @@ __device__ __forceinline__ float row_max(float v, float* buf) {
   __syncthreads();
   float t = buf[0];
 #pragma unroll
-  for (int w = 1; w < RW; ++w) t = max_nan(t, buf[w]);
+  for (int w = 1; w < T / 64; ++w) t = max_nan(t, buf[w]);
   return t;
 }
 
@@ -58,24 +59,24 @@ template <typename TI> struct Wide;
 template <> struct Wide<float> { typedef f32x4 type; static constexpr int n = 4; };
 template <> struct Wide<bf16> { typedef bf16x8 type; static constexpr int n = 8; };
 
-// A row in registers: vector i of thread t holds columns (i RT + t) V and on, as
+// A row in registers: vector i of thread t holds columns (i T + t) V and on, as
 // far as whole vectors go; the fewer than V columns behind them are one a
 // thread.  What does not exist is -inf.  bf16 pairs stay packed; again() between passes
 // keeps the compiler from carrying widened values and exponentials from one pass to the next.
-template <typename TI, int V, int NV, int RT> struct Row {
+template <typename TI, int V, int NV, int T> struct Row {
   static constexpr bool PACKED = sizeof(TI) == 2 && V > 1;
   static constexpr int W = PACKED ? V / 2 : V;   // words of a vector
   uint32_t w[NV][W];
   float tail;
-  static __device__ __forceinline__ int col(int i) { return (i * RT + (int)threadIdx.x) * V; }
+  static __device__ __forceinline__ int col(int i) { return (i * T + (int)threadIdx.x) * V; }
   static __device__ __forceinline__ int whole(int K) { return K / V * V; }
   // vector i's address (a base that the workgroup shares and 32 bits of the
   // thread's own), and whether it exists
   template <typename P> static __device__ __forceinline__ P* at(P* s, int i) {
     typedef typename std::conditional<std::is_const<P>::value, const char, char>::type C;
-    return (P*)((C*)(s + i * RT * V) + (uint32_t)(threadIdx.x * (V * sizeof(P))));
+    return (P*)((C*)(s + i * T * V) + (uint32_t)(threadIdx.x * (V * sizeof(P))));
   }
-  static __device__ __forceinline__ bool has(int i, int n) { return (int)threadIdx.x * V < n - i * RT * V; }
+  static __device__ __forceinline__ bool has(int i, int n) { return (int)threadIdx.x * V < n - i * T * V; }
   // the thread's column behind the whole vectors (K or more: none)
   static __device__ __forceinline__ int tail_col(int K) { return V == 1 ? K : whole(K) + (int)threadIdx.x; }
   __device__ __forceinline__ float get(int i, int j) const {
@@ -110,21 +111,26 @@ template <typename TI, int V, int NV, int RT> struct Row {
 // Rows longer than registers hold: calls f(column, value) for the thread's
 // columns, read from memory (the caches) by every pass.
 // ONE: element by element, in fewer registers.
-template <typename TI, int RT, bool ONE = false, typename F>
+template <typename TI, int T, bool ONE = false, typename F>
 __device__ __forceinline__ void each(const TI* s, int K, F f) {
   if constexpr (ONE) {
 #pragma unroll 4
-    for (int c = (int)threadIdx.x; c < K; c += RT) f(c, to_f32(s[c]));
+    for (int c = (int)threadIdx.x; c < K; c += T) f(c, to_f32(s[c]));
     return;
   }
   constexpr int V = Wide<TI>::n;
   const int done = K / V * V;
-#pragma unroll 1
-  for (int c = (int)threadIdx.x * V; c < done; c += RT * V) {
-    TI v[V];
-    __builtin_memcpy(v, s + c, V * sizeof(TI));
+  for (int c = (int)threadIdx.x * V; c < done; c += 4 * T * V) {   // four loads in flight
+    TI v[4][V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) f(c + i, to_f32(v[i]));
+    for (int u = 0; u < 4; ++u)
+      if (c + u * T * V < done) __builtin_memcpy(v[u], s + c + u * T * V, V * sizeof(TI));
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (c + u * T * V >= done) break;
+#pragma unroll
+      for (int i = 0; i < V; ++i) f(c + u * T * V + i, to_f32(v[u][i]));
+    }
   }
   const int c = done + (int)threadIdx.x;
   if (c < K) f(c, to_f32(s[c]));
@@ -143,21 +149,22 @@ __device__ __forceinline__ float order_value(uint32_t w) {
 }
 
 // ---------------------------------------------------------------------------
-// The k largest of a row.  Each thread's maximum is one of RT; the k-th
+// The k largest of a row.  Each thread's maximum is one of T; the k-th
 // largest of those is no larger than the row's k-th, and few logits lie above
-// it (about RT ln(RT / (RT - k)) of them in no particular order), so the
+// it (about T ln(T / (T - k)) of them in no particular order), so the
 // logits from there on are collected and ranked by counting.  Rows whose
 // logits bunch (ties, or all large ones in one thread's columns) can have
 // more than CAND candidates: their k-th logit, and the last class that ties
 // with it, are then found bit by bit.
 // ---------------------------------------------------------------------------
-struct TopkLds {
-  uint32_t tmax[RT];
+template <int T> struct TopkLds {
+  uint32_t tmax[T];
   uint64_t cand[CAND];   // order word, complement of the class
-  uint32_t thr, count, cnt[2][RW], flag;
+  uint32_t thr, count, cnt[2][T / 64], flag;
   uint64_t kth;
-  float buf[RW];
+  float buf[T / 64];
 };
+static constexpr uint32_t LOWEST = 0x007fffffu;   // order word of -inf
 struct TopkP {
   int64_t ld;
   int K, k;
@@ -166,20 +173,24 @@ struct TopkP {
   int32_t* idx;
 };
 
+// A word of LDS that every lane reads alike, as a scalar: a branch on it is one
+// for the whole wave, and what lives on past the branch not taken takes no registers from it.
+__device__ __forceinline__ uint32_t same(uint32_t v) { return __builtin_amdgcn_readfirstlane(v); }
+
 // The k-th largest of the threads' maxima (order words), down to its bits from LOW on.
-template <int LOW>
-__device__ __forceinline__ uint32_t kth_max(TopkLds& l, int k) {
+template <int LOW, int T>
+__device__ __forceinline__ uint32_t kth_max(TopkLds<T>& l, int k) {
   const int lane = threadIdx.x & 63;
   __syncthreads();
   if (threadIdx.x < 64) {
-    uint32_t w[RW], t = 0;
+    uint32_t w[T / 64], t = 0;
 #pragma unroll
-    for (int i = 0; i < RW; ++i) w[i] = l.tmax[i * 64 + lane];
+    for (int i = 0; i < T / 64; ++i) w[i] = l.tmax[i * 64 + lane];
     for (int bit = 31; bit >= LOW; --bit) {
       const uint32_t c = t | (1u << bit);
       int n = 0;
 #pragma unroll
-      for (int i = 0; i < RW; ++i) n += __popcll(__ballot(w[i] >= c));
+      for (int i = 0; i < T / 64; ++i) n += __popcll(__ballot(w[i] >= c));
       if (n >= k) t = c;
     }
     if (lane == 0) l.thr = t;
@@ -187,17 +198,18 @@ __device__ __forceinline__ uint32_t kth_max(TopkLds& l, int k) {
   __syncthreads();
   return l.thr;
 }
-__device__ __forceinline__ void push(TopkLds& l, float v, int c) {
+template <int T>
+__device__ __forceinline__ void push(TopkLds<T>& l, float v, int c) {
   const uint32_t at = atomicAdd(&l.count, 1u);
   if (at < (uint32_t)CAND) l.cand[at] = ((uint64_t)order_word(v) << 32) | (uint32_t)~c;
 }
 // Writes the k largest of n candidates; f(candidate, rank) for every candidate.
-template <typename F>
-__device__ __forceinline__ void rank(TopkLds& l, int n, int64_t m, const TopkP& p, F f) {
-  for (int i = threadIdx.x; i < n; i += RT) {
+template <int T, typename F>
+__device__ __forceinline__ void rank(TopkLds<T>& l, int n, int64_t m, const TopkP& p, F f) {
+  for (int i = threadIdx.x; i < n; i += T) {
     const uint64_t w = l.cand[i];
     int r = 0;
-#pragma unroll 8
+#pragma unroll 4
     for (int j = 0; j < n; ++j) r += l.cand[j] > w;
     if (r < p.k) {
       p.top[m * p.k + r] = order_value((uint32_t)(w >> 32));
@@ -208,22 +220,43 @@ __device__ __forceinline__ void rank(TopkLds& l, int n, int64_t m, const TopkP& 
   }
 }
 
+// The log-sum-exp of what orders behind the k-th, from its own maximum, from memory.
+template <typename TI, int T, bool ONE>
+__device__ __forceinline__ void rest_of(TopkLds<T>& l, const TI* s, int64_t m, const TopkP& p) {
+  const int tid = threadIdx.x, K = p.K;
+  const uint64_t last = l.kth;
+  float rm = -INFINITY;
+  each<TI, T, ONE>(s, K, [&](int c, float v) {
+    if ((((uint64_t)order_word(v) << 32) | (uint32_t)~c) < last) rm = max_nan(rm, v);
+  });
+  rm = row_max<T>(rm, l.buf);
+  float sum = 0.f;
+  if (fabsf(rm) < INFINITY) {
+    each<TI, T, ONE>(s, K, [&](int c, float v) {
+      if ((((uint64_t)order_word(v) << 32) | (uint32_t)~c) < last) sum += exp2_((v - rm) * p.l2t);
+    });
+  }
+  sum = row_sum<T>(sum, l.buf);
+  // the others' largest logit alone where it is infinite or a NaN, or there is none
+  if (tid == 0) p.rest[m] = fabsf(rm) < INFINITY ? rm * (p.l2t * LN2_F) + log2f(sum) * LN2_F : rm;
+}
+
 // Any row, from memory.
-template <typename TI, bool ONE>
-__device__ __forceinline__ void topk_any(TopkLds& l, const TI* s, int64_t m, const TopkP& p) {
+template <typename TI, int T, bool ONE>
+__device__ __forceinline__ void topk_any(TopkLds<T>& l, const TI* s, int64_t m, const TopkP& p) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, K = p.K;
   uint32_t mx = 0;
-  each<TI, RT, ONE>(s, K, [&](int, float v) { mx = max(mx, order_word(v)); });
+  each<TI, T, ONE>(s, K, [&](int, float v) { mx = max(mx, order_word(v)); });
   __syncthreads();
   l.tmax[tid] = mx;
   if (tid == 0) l.count = 0;
-  const uint32_t th = kth_max<0>(l, p.k);
-  each<TI, RT, ONE>(s, K, [&](int c, float v) {
+  const uint32_t th = kth_max<0, T>(l, p.k);
+  each<TI, T, ONE>(s, K, [&](int c, float v) {
     if (order_word(v) >= th) push(l, v, c);
   });
   __syncthreads();
-  int n = (int)min(l.count, (uint32_t)CAND);
-  if (l.count > (uint32_t)CAND) {
+  int n = (int)min(same(l.count), (uint32_t)CAND);
+  if (same(l.count) > (uint32_t)CAND) {
     // the k-th: the largest word (and complement of the class) with k of them from it on
     uint64_t t = 0;
     int par = 0;
@@ -234,7 +267,7 @@ __device__ __forceinline__ void topk_any(TopkLds& l, const TI* s, int64_t m, con
         continue;
       }
       uint32_t mine = 0;
-      each<TI, RT, ONE>(s, K, [&](int col, float v) {
+      each<TI, T, ONE>(s, K, [&](int col, float v) {
         mine += ((((uint64_t)order_word(v)) << 32) | (uint32_t)~col) >= c;
       });
 #pragma unroll
@@ -243,13 +276,13 @@ __device__ __forceinline__ void topk_any(TopkLds& l, const TI* s, int64_t m, con
       __syncthreads();
       uint32_t all = 0;
 #pragma unroll
-      for (int i = 0; i < RW; ++i) all += l.cnt[par][i];
+      for (int i = 0; i < T / 64; ++i) all += l.cnt[par][i];
       if (all >= (uint32_t)p.k) t = c;
       par ^= 1;
     }
     if (tid == 0) l.count = 0;
     __syncthreads();
-    each<TI, RT, ONE>(s, K, [&](int c, float v) {
+    each<TI, T, ONE>(s, K, [&](int c, float v) {
       if ((((uint64_t)order_word(v) << 32) | (uint32_t)~c) >= t) push(l, v, c);   // exactly k
     });
     __syncthreads();
@@ -258,40 +291,70 @@ __device__ __forceinline__ void topk_any(TopkLds& l, const TI* s, int64_t m, con
   rank(l, n, m, p, [](uint64_t, int) {});
   if (!p.rest) return;
   __syncthreads();
-  const uint64_t last = l.kth;
-  float rm = -INFINITY;
-  each<TI, RT, ONE>(s, K, [&](int c, float v) {
-    if ((((uint64_t)order_word(v) << 32) | (uint32_t)~c) < last) rm = max_nan(rm, v);
-  });
-  rm = row_max(rm, l.buf);
-  float sum = 0.f;
-  if (fabsf(rm) < INFINITY) {
-    each<TI, RT, ONE>(s, K, [&](int c, float v) {
-      if ((((uint64_t)order_word(v) << 32) | (uint32_t)~c) < last) sum += exp2_((v - rm) * p.l2t);
-    });
-  }
-  sum = row_sum(sum, l.buf);
-  // the others' largest logit alone where it is infinite or a NaN, or there is none
-  if (tid == 0) p.rest[m] = fabsf(rm) < INFINITY ? rm * (p.l2t * LN2_F) + log2f(sum) * LN2_F : rm;
+  rest_of<TI, T, ONE>(l, s, m, p);
 }
 
-template <typename TI>
-__global__ __launch_bounds__(RT) void topk_any_kernel(const TI* __restrict__ logits, const TopkP p) {
-  __shared__ TopkLds l;
-  topk_any<TI, false>(l, logits + (int64_t)blockIdx.x * p.ld, blockIdx.x, p);
+// A longer row than registers hold: read for its threshold, and again for its
+// candidates and the sum of the others, which is taken from the threshold as below.
+template <typename TI, int T>
+__global__ __launch_bounds__(T) void topk_long_kernel(const TI* __restrict__ logits, const TopkP p) {
+  __shared__ TopkLds<T> l;
+  const int64_t m = blockIdx.x;
+  const TI* s = logits + m * p.ld;
+  const int tid = threadIdx.x;
+  if (tid == 0) {
+    l.count = 0;
+    l.flag = 0;
+  }
+  __syncthreads();
+  float mx = -INFINITY;
+  bool nan = false;
+  each<TI, T>(s, p.K, [&](int, float v) {
+    mx = fmaxf(mx, v);
+    nan |= v != v;
+  });
+  if (nan) l.flag = 1;
+  l.tmax[tid] = order_word(mx);
+  const float thr = order_value(max(kth_max<12, T>(l, p.k), LOWEST));
+  if (same(l.flag)) {
+    topk_any<TI, T, true>(l, s, m, p);
+    return;
+  }
+  const float ref = fabsf(thr) < INFINITY ? thr * p.l2t : 0.f;
+  float sum = 0.f;
+  each<TI, T>(s, p.K, [&](int c, float v) {
+    if (v >= thr) push(l, v, c);
+    else sum += exp2_(v * p.l2t - ref);
+  });
+  __syncthreads();
+  const int n = (int)same(l.count);
+  if (n > CAND) {
+    topk_any<TI, T, true>(l, s, m, p);
+    return;
+  }
+  rank(l, n, m, p, [&](uint64_t w, int r) {
+    if (r >= p.k) sum += exp2_(order_value((uint32_t)(w >> 32)) * p.l2t - ref);
+  });
+  if (!p.rest) return;
+  sum = row_sum<T>(sum, l.buf);   // its barriers: every rank is written, the k-th known
+  if (same(sum > 1e-20f && sum < 1e30f)) {
+    if (tid == 0) p.rest[m] = (ref + log2f(sum)) * LN2_F;
+    return;
+  }
+  rest_of<TI, T, false>(l, s, m, p);
 }
 
 // A row in registers, read once.  Candidates leave the registers (-inf in
 // their place), so that what stays is of the others; their sum is taken from the threshold,
 // which no other exceeds, and again from their own maximum where that leaves
 // nothing.  Rows with a NaN, and rows with too many candidates, go the way of any row.
-template <typename TI, int V, int NV>
-__global__ __launch_bounds__(RT, 4) void topk_rows_kernel(const TI* __restrict__ logits, const TopkP p) {
-  __shared__ TopkLds l;
+template <typename TI, int T, int V, int NV>
+__global__ __launch_bounds__(T, 4) void topk_rows_kernel(const TI* __restrict__ logits, const TopkP p) {
+  __shared__ TopkLds<T> l;
   const int64_t m = blockIdx.x;
   const TI* s = logits + m * p.ld;
   const int tid = threadIdx.x;
-  Row<TI, V, NV, RT> row;
+  Row<TI, V, NV, T> row;
   row.load(s, p.K);
   if (tid == 0) {
     l.count = 0;
@@ -318,12 +381,11 @@ __global__ __launch_bounds__(RT, 4) void topk_rows_kernel(const TI* __restrict__
   l.tmax[tid] = order_word(mx);
   // bf16: the lower 16 bits of all order words are alike; float32: a threshold
   // rounded down to 11 bits lets a few more pass and takes a third fewer steps
-  constexpr uint32_t LOWEST = 0x007fffffu;   // of -inf
-  const uint32_t tw = max(kth_max<std::is_same<TI, bf16>::value ? 16 : 12>(l, p.k), LOWEST);
+  const uint32_t tw = max(kth_max<std::is_same<TI, bf16>::value ? 16 : 12, T>(l, p.k), LOWEST);
   const float thr = order_value(tw);
   row.again();
-  if (l.flag) {
-    topk_any<TI, true>(l, s, m, p);
+  if (same(l.flag)) {
+    topk_any<TI, T, true>(l, s, m, p);
     return;
   }
   const int whole = row.whole(p.K);
@@ -350,9 +412,9 @@ __global__ __launch_bounds__(RT, 4) void topk_rows_kernel(const TI* __restrict__
     row.tail = -INFINITY;
   }
   __syncthreads();
-  const int n = (int)l.count;
+  const int n = (int)same(l.count);
   if (n > CAND) {
-    topk_any<TI, true>(l, s, m, p);
+    topk_any<TI, T, true>(l, s, m, p);
     return;
   }
   const float ref = fabsf(thr) < INFINITY ? thr * p.l2t : 0.f;
@@ -366,12 +428,14 @@ __global__ __launch_bounds__(RT, 4) void topk_rows_kernel(const TI* __restrict__
   if (!p.rest) return;
   row.again();
 #pragma unroll
-  for (int i = 0; i < NV; ++i)
+  for (int i = 0; i < NV; ++i) {
 #pragma unroll
     for (int j = 0; j < V; ++j) sum += exp2_(row.get(i, j) * p.l2t - ref);
+    if constexpr (V > 1) __builtin_amdgcn_sched_barrier(0);   // one vector at a time: fewer registers
+  }
   sum += exp2_(row.tail * p.l2t - ref);
-  sum = row_sum(sum, l.buf);
-  if (sum > 1e-20f && sum < 1e30f) {
+  sum = row_sum<T>(sum, l.buf);
+  if (same(sum > 1e-20f && sum < 1e30f)) {
     if (tid == 0) p.rest[m] = (ref + log2f(sum)) * LN2_F;
     return;
   }
@@ -381,7 +445,7 @@ __global__ __launch_bounds__(RT, 4) void topk_rows_kernel(const TI* __restrict__
   for (int i = 0; i < NV; ++i)
 #pragma unroll
     for (int j = 0; j < V; ++j) rm = fmaxf(rm, row.get(i, j));
-  rm = row_max(fmaxf(rm, row.tail), l.buf);
+  rm = row_max<T>(fmaxf(rm, row.tail), l.buf);
   sum = 0.f;
   if (fabsf(rm) < INFINITY) {
 #pragma unroll
@@ -389,10 +453,10 @@ __global__ __launch_bounds__(RT, 4) void topk_rows_kernel(const TI* __restrict__
 #pragma unroll
       for (int j = 0; j < V; ++j) sum += exp2_((row.get(i, j) - rm) * p.l2t);
     sum += exp2_((row.tail - rm) * p.l2t);
-    for (int i = tid; i < n; i += RT)
+    for (int i = tid; i < n; i += T)
       if (l.cand[i] < l.kth) sum += exp2_((order_value((uint32_t)(l.cand[i] >> 32)) - rm) * p.l2t);
   }
-  sum = row_sum(sum, l.buf);
+  sum = row_sum<T>(sum, l.buf);
   if (tid == 0) p.rest[m] = fabsf(rm) < INFINITY ? rm * (p.l2t * LN2_F) + log2f(sum) * LN2_F : rm;
 }
 
@@ -416,12 +480,10 @@ struct DistillP {
 // Threads of a row: 512 with 64 values each, two rows on a CU.  (2688 bf16 rows
 // of 32000, labels given / not: 100 / 70 us; 256 threads 99 / 74, but float32 279 against 79; 1024
 // threads 142 / 115.)
-static constexpr int DT = RT;
-static_assert(MAXK <= DT, "an entry a thread");
-struct DistillLds {
+template <int T> struct DistillLds {
   float pv[MAXK];
   int32_t iv[MAXK];
-  float buf[8][DT / 64];
+  float buf[8][T / 64];
   uint32_t dup;
 };
 
@@ -434,24 +496,26 @@ __device__ __forceinline__ float wave_max(float v) {
 __device__ __forceinline__ void put_wave(float* buf, float v) {
   if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = v;
 }
+template <int T>
 __device__ __forceinline__ float all_sum(const float* buf) {
   float t = buf[0];
 #pragma unroll
-  for (int w = 1; w < DT / 64; ++w) t += buf[w];
+  for (int w = 1; w < T / 64; ++w) t += buf[w];
   return t;
 }
+template <int T>
 __device__ __forceinline__ float all_max(const float* buf) {
   float t = buf[0];
 #pragma unroll
-  for (int w = 1; w < DT / 64; ++w) t = fmaxf(t, buf[w]);
+  for (int w = 1; w < T / 64; ++w) t = fmaxf(t, buf[w]);
   return t;
 }
 
 // A row's other classes (those that are not listed): in registers, or, NV = 0, read
 // from memory by each pass.  others(f) calls f(value) for each, the listed
 // ones and what lies behind K as -inf; write(f) stores f(value) in their place.
-template <typename TI, typename TO, int V, int NV> struct Others {
-  Row<TI, V, NV, DT> row;
+template <typename TI, typename TO, int T, int V, int NV> struct Others {
+  Row<TI, V, NV, T> row;
   __device__ __forceinline__ void load(const TI* s, int K) { row.load(s, K); }
   __device__ __forceinline__ void mask(const uint32_t* listed, int K) {
 #pragma unroll
@@ -492,20 +556,20 @@ template <typename TI, typename TO, int V, int NV> struct Others {
     if (row.tail_col(K) < K) d[row.tail_col(K)] = from_f32<TO>(f(row.tail));
   }
 };
-template <typename TI, typename TO, int V> struct Others<TI, TO, V, 0> {
+template <typename TI, typename TO, int T, int V> struct Others<TI, TO, T, V, 0> {
   __device__ __forceinline__ void load(const TI*, int) {}
   __device__ __forceinline__ void mask(const uint32_t*, int) {}
   static __device__ __forceinline__ float of(const uint32_t* listed, int c, float v) {
     return ((listed[c >> 5] >> (c & 31)) & 1u) ? -INFINITY : v;
   }
   template <typename F> __device__ __forceinline__ void others(const TI* s, int K, const uint32_t* listed, F f) const {
-    each<TI, DT>(s, K, [&](int c, float v) { f(of(listed, c, v)); });
+    each<TI, T>(s, K, [&](int c, float v) { f(of(listed, c, v)); });
   }
   template <typename F>
   __device__ __forceinline__ void write(const TI* s, TO* d, int K, const uint32_t* listed, F f) const {
     // a thread writes only where it has read (d may be s)
     const int done = K / V * V;
-    for (int c = (int)threadIdx.x * V; c < done; c += DT * V) {
+    for (int c = (int)threadIdx.x * V; c < done; c += T * V) {
       TI v[V];
       TO o[V];
       __builtin_memcpy(v, s + c, V * sizeof(TI));
@@ -519,25 +583,25 @@ template <typename TI, typename TO, int V> struct Others<TI, TO, V, 0> {
 };
 
 // HARD: with the labels' cross-entropy.
-template <typename TI, typename TO, int V, int NV, bool HARD>
-__global__ __launch_bounds__(DT, 4) void distill_rows_kernel(const TI* logits, TO* dlogits, const DistillP p) {
+template <typename TI, typename TO, int T, int V, int NV, bool HARD>
+__global__ __launch_bounds__(T, 4) void distill_rows_kernel(const TI* logits, TO* dlogits, const DistillP p) {
   extern __shared__ uint32_t listed[];   // a bit per class, to the end of the registers' columns
-  __shared__ DistillLds l;
+  __shared__ DistillLds<T> l;
   const int64_t m = blockIdx.x;
   const TI* s = logits + m * p.ld;
   TO* d = dlogits + m * p.ldd;
   const int tid = threadIdx.x, K = p.K;
   const float weight = p.weights ? p.weights[m] : 1.f;
-  for (int c = K + tid; c < K + p.pad; c += DT) d[c] = from_f32<TO>(0.f);
+  for (int c = K + tid; c < K + p.pad; c += T) d[c] = from_f32<TO>(0.f);
   if (weight == 0.f) {
-    for (int c = tid; c < K; c += DT) d[c] = from_f32<TO>(0.f);
+    for (int c = tid; c < K; c += T) d[c] = from_f32<TO>(0.f);
     if (tid == 0) p.row_loss[m] = 0.f;
     return;
   }
-  Others<TI, TO, V, NV> row;
+  Others<TI, TO, T, V, NV> row;
   row.load(s, K);   // in flight while the teacher's part runs
-  const int words = (NV ? NV * V * DT : K + 31) / 32;
-  for (int i = tid; i < words; i += DT) listed[i] = 0;
+  const int words = (NV ? NV * V * T : K + 31) / 32;
+  for (int i = tid; i < words; i += T) listed[i] = 0;
   if (tid == 0) l.dup = 0;
   int at = -1;
   float t2 = -INFINITY, sv = -INFINITY;   // the entry's teacher logit (times log2 e / tau), student logit
@@ -560,7 +624,7 @@ __global__ __launch_bounds__(DT, 4) void distill_rows_kernel(const TI* logits, T
   put_wave(l.buf[1], wave_max(sv));
   __syncthreads();
   // the teacher's probabilities (base-2 exponents throughout)
-  const float tm = fmaxf(all_max(l.buf[0]), r2), lm = all_max(l.buf[1]);
+  const float tm = fmaxf(all_max<T>(l.buf[0]), r2), lm = all_max<T>(l.buf[1]);
   const bool taught = !(tm == -INFINITY);
   const float e = taught ? exp2_(t2 - tm) : 0.f, er = taught ? exp2_(r2 - tm) : 0.f;
   if (tid < p.k) l.pv[tid] = e;
@@ -570,7 +634,7 @@ __global__ __launch_bounds__(DT, 4) void distill_rows_kernel(const TI* logits, T
   row.others(s, K, listed, [&](float v) { rm = fmaxf(rm, v); });
   put_wave(l.buf[3], wave_max(rm));
   __syncthreads();
-  const float tz = all_sum(l.buf[2]) + er, l2tz = taught ? tm + log2f(tz) : 0.f;
+  const float tz = all_sum<T>(l.buf[2]) + er, l2tz = taught ? tm + log2f(tz) : 0.f;
   const float prob = taught ? e / tz : 0.f, r = taught ? er / tz : 0.f;
   float lp = t2 - l2tz;     // log2 of the entry's probability
   float own = prob;         // of its class
@@ -586,7 +650,7 @@ __global__ __launch_bounds__(DT, 4) void distill_rows_kernel(const TI* logits, T
     lp = log2f(own);
   }
   // maxima: the others' (as an exponent), the row's
-  rm = all_max(l.buf[3]);
+  rm = all_max<T>(l.buf[3]);
   const float am = fmaxf(rm, lm), aref = am == -INFINITY ? 0.f : am;
   const float rref = rm == -INFINITY ? 0.f : rm * p.it2, um = aref * p.it2;
   const float eo = rm == -INFINITY ? 0.f : exp2_(rref - um);   // the others' sums, from the row's maximum
@@ -603,9 +667,9 @@ __global__ __launch_bounds__(DT, 4) void distill_rows_kernel(const TI* logits, T
   put_wave(l.buf[5], wave_sum(ez));
   if constexpr (HARD) put_wave(l.buf[6], wave_sum(z1));
   __syncthreads();   // every listed logit and the label's have been read, too
-  zr = all_sum(l.buf[4]);
-  const float z = all_sum(l.buf[5]) + zr * eo;
-  if constexpr (HARD) z1 = all_sum(l.buf[6]);
+  zr = all_sum<T>(l.buf[4]);
+  const float z = all_sum<T>(l.buf[5]) + zr * eo;
+  if constexpr (HARD) z1 = all_sum<T>(l.buf[6]);
   const float l2z = log2f(z);
   put_wave(l.buf[7], wave_sum(at >= 0 && prob > 0.f ? prob * (lp - (u - um - l2z)) : 0.f));
   const float ks = taught ? p.scale * weight * p.soft * p.tau : 0.f, kh = marked ? p.scale * weight * p.hard : 0.f;
@@ -630,7 +694,7 @@ __global__ __launch_bounds__(DT, 4) void distill_rows_kernel(const TI* logits, T
     d[lab] = from_f32<TO>(cr * exp2_(sl * p.it2 - rref) + ch * exp2_(sl * LOG2E_F + h2) - kh);
   float loss = 0.f;
   if (taught) {
-    float kl = all_sum(l.buf[7]);
+    float kl = all_sum<T>(l.buf[7]);
     if (r > 0.f) kl += r * (r2 - l2tz - (log2f(zr) + rref - um - l2z));
     loss = p.soft * p.tau * p.tau * kl * LN2_F;
   }
@@ -641,25 +705,38 @@ __global__ __launch_bounds__(DT, 4) void distill_rows_kernel(const TI* logits, T
 // ---------------------------------------------------------------------------
 // Host side.
 // ---------------------------------------------------------------------------
-// Columns that a row in registers may have, element by element and 16 bytes at
-// a time.  Short rows go element by element: their few 16-byte pieces would
-// leave most threads without a maximum of their own.
+// How a row is read.  Short rows go element by element: their few 16-byte
+// pieces would leave most threads without a maximum of their own.  Longer ones
+// go 16 bytes at a time, 64 values a thread, with 1024 threads where 512 do not
+// reach (few rows do not gain from them: 256 rows of 32000 logits 11.1 us with 512,
+// 11.6 with 1024), and, packed bf16 pairs, 128 values in rows of up to
+// PACKED.  What no registers hold is read by every pass.
 static constexpr int SHORT = 8 * RT;
-static constexpr int LONG = 64 * RT;
-template <typename TI, int T> struct Long { static constexpr int V = Wide<TI>::n, NV = LONG / T / V, K = LONG; };
+template <typename TI, int PACKED, typename F> static void by_length(int32_t K, F f) {
+  constexpr int V = Wide<TI>::n;
+  typedef std::integral_constant<int, 512> T5;
+  typedef std::integral_constant<int, 1024> T10;
+#define NVEC(n) std::integral_constant<int, n>{}
+  if (K <= SHORT) return f(T5{}, NVEC(1), NVEC(8));
+  if (K <= 64 * 512) return f(T5{}, NVEC(V), NVEC(64 / V));
+  if (K <= 64 * 1024) return f(T10{}, NVEC(V), NVEC(64 / V));
+  if constexpr (sizeof(TI) == 2 && PACKED > 64 * 1024)
+    if (K <= PACKED) return f(T10{}, NVEC(V), NVEC(128 / V));
+  f(T10{}, NVEC(V), NVEC(0));
+#undef NVEC
+}
 
 template <typename TI>
 int topk_rows(const TI* logits, int64_t ld, int64_t M, int32_t K, int32_t k, float temperature, float* top,
               int32_t* idx, float* rest, hipStream_t stream) {
-  using L = Long<TI, RT>;
   const TopkP p{ld, K, k, LOG2E_F / temperature, top, rest, idx};
-  const dim3 grid((unsigned)M), block(RT);
-  if (K <= SHORT)
-    BLSTM_LAUNCH("softmax_topk_rows", (topk_rows_kernel<TI, 1, 8>), grid, block, 0, stream, logits, p);
-  else if (K <= L::K)
-    BLSTM_LAUNCH("softmax_topk_rows", (topk_rows_kernel<TI, L::V, L::NV>), grid, block, 0, stream, logits, p);
-  else
-    BLSTM_LAUNCH("softmax_topk_rows", topk_any_kernel<TI>, grid, block, 0, stream, logits, p);
+  by_length<TI, 0>(K, [&](auto t, auto v, auto nv) {
+    constexpr int T = decltype(t)::value, V = decltype(v)::value, NV = decltype(nv)::value;
+    if constexpr (NV > 0)
+      BLSTM_LAUNCH("softmax_topk_rows", (topk_rows_kernel<TI, T, V, NV>), dim3((unsigned)M), dim3(T), 0, stream, logits, p);
+    else
+      BLSTM_LAUNCH("softmax_topk_rows", (topk_long_kernel<TI, T>), dim3((unsigned)M), dim3(T), 0, stream, logits, p);
+  });
   return blstm_check_launch("softmax_topk_rows");
 }
 template int topk_rows<float>(const float*, int64_t, int64_t, int32_t, int32_t, float, float*, int32_t*, float*, hipStream_t);
@@ -668,20 +745,21 @@ template int topk_rows<bf16>(const bf16*, int64_t, int64_t, int32_t, int32_t, fl
 template <typename TI, typename TO>
 int distill_rows(const TI* logits, int64_t ld, int64_t M, int32_t K, const softmax_teacher* t, float loss_scale,
                  float* row_loss, TO* dlogits, int64_t ldd, int32_t pad, hipStream_t stream) {
-  using L = Long<TI, DT>;
   DistillP p{};
   p.ld = ld; p.ldd = ldd; p.top = t->top; p.rest = t->rest; p.weights = t->weights; p.idx = t->idx;
   p.labels = t->hard != 0.f ? t->labels : nullptr;
   p.row_loss = row_loss; p.K = K; p.k = t->k; p.pad = pad;
   p.it2 = LOG2E_F / t->temperature; p.tau = t->temperature; p.soft = t->soft; p.hard = t->hard; p.scale = loss_scale;
-#define ROWS(V, NV, HARD, BYTES)                                                                                      \
-  BLSTM_LAUNCH("softmax_distill_rows", (distill_rows_kernel<TI, TO, V, NV, HARD>), dim3((unsigned)M), dim3(DT), BYTES, \
-               stream, logits, dlogits, p)
-#define ROWS_BY_K(HARD)                                           \
-  if (K <= SHORT) ROWS(1, SHORT / DT, HARD, SHORT / 8);                    \
-  else if (K <= L::K) ROWS(L::V, L::NV, HARD, L::K / 8);          \
-  else ROWS(L::V, 0, HARD, (size_t)cdiv(K, 32) * 4);
-  if (p.labels) { ROWS_BY_K(true) } else { ROWS_BY_K(false) }
+  by_length<TI, 128 * 1024>(K, [&](auto tt, auto v, auto nv) {
+    constexpr int T = decltype(tt)::value, V = decltype(v)::value, NV = decltype(nv)::value;
+    const size_t bits = (size_t)(NV ? NV * V * T : rup(K, 32)) / 8;
+    if (p.labels)
+      BLSTM_LAUNCH("softmax_distill_rows", (distill_rows_kernel<TI, TO, T, V, NV, true>), dim3((unsigned)M), dim3(T), bits,
+                   stream, logits, dlogits, p);
+    else
+      BLSTM_LAUNCH("softmax_distill_rows", (distill_rows_kernel<TI, TO, T, V, NV, false>), dim3((unsigned)M), dim3(T), bits,
+                   stream, logits, dlogits, p);
+  });
   return blstm_check_launch("softmax_distill_rows");
 }
 template int distill_rows<float, float>(const float*, int64_t, int64_t, int32_t, const softmax_teacher*, float, float*, float*, int64_t, int32_t, hipStream_t);
