@@ -216,7 +216,8 @@ enum {
   SSM_SILU = 2u        /* convolution: y = silu(pre), else y = pre */
 };
 
-/* Sizes in bytes of caller-allocated buffers:
+/* Sizes in bytes of caller-allocated buffers (16-byte aligned; a size of 0
+ * needs none):
  *   saved    -- states that ssm_scan_fwd keeps for ssm_scan_bwd
  *   fwd, bwd -- scratch of ssm_scan_fwd and ssm_scan_bwd
  *   conv_bwd -- scratch of ssm_conv_bwd
@@ -318,7 +319,8 @@ int softmax_topk_rows(const void* logits, int64_t ld, int64_t M, int32_t K, int3
  * both probabilities; a row without entries and rest has no soft loss.
  * labels (NULL: none) outside 0..K-1: the row has no hard loss.
  * weights [M] float32 (NULL: ones): a row of weight 0 has loss and gradient 0
- * whatever it holds. */
+ * whatever it holds (on the head, whose products sum over frames, its y_top
+ * has to be finite all the same). */
 typedef struct softmax_teacher {
   const float* top;       /* [M][k] */
   const int32_t* idx;     /* [M][k] */

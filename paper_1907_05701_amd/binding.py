@@ -296,7 +296,7 @@ def _bytes(name, t, n, dev):
     if n == 0:
         return None
     if t is None or not t.is_contiguous() or t.get_device() != dev or t.numel() * t.element_size() < n:
-        raise ValueError(f"{name} must be a contiguous buffer of at least {n} bytes on cuda:{dev} (ssm_workspace_bytes)")
+        raise ValueError(f"{name} must be a contiguous buffer of at least {n} bytes on cuda:{dev}")
     p = t.data_ptr()
     if p % 16:
         raise ValueError(f"{name} must be 16-byte aligned")
@@ -478,17 +478,33 @@ def softmax_head_ws_bytes(dims: Dims) -> int:
     return n.value
 
 
+def _head_args(dims, dev, theta, theta_lp, y_top, ws):
+    """Addresses of the head's inputs and workspace, whose sizes dims give."""
+    key = tuple(getattr(dims, n) for n, _ in Dims._fields_)
+    got = dims.__dict__.get("head")
+    if got is None or got[0] != key:
+        got = dims.__dict__["head"] = (key, blstm_param_count(dims), softmax_head_ws_bytes(dims))
+    n, e = got[1], _elem(dims)
+    return (_have("theta", theta, (n,), torch.float32, dev),
+            _have("theta_lp", theta_lp, (n,), torch.bfloat16, dev) if dims.precision == BLSTM_BF16 else None,
+            _have("y_top", y_top, (dims.T, dims.B, 2 * dims.H), e, dev), _bytes("ws", ws, got[2], dev))
+
+
 def softmax_topk(dims, theta, theta_lp, y_top, top, idx, ws, rest=None, temperature=1.0, stream=None):
     """top, idx [T*B][k], rest [T*B]; k is top's width."""
     dev, M, k = _on(y_top), dims.T * dims.B, top.shape[-1]
-    return _call("softmax_topk", dev, stream, ctypes.byref(dims), _ptr(theta), _ptr(theta_lp), _ptr(y_top), k,
-                 temperature, _have("top", top, (M, k), torch.float32, dev), _have("idx", idx, (M, k), torch.int32, dev),
-                 _have("rest", rest, (M,), torch.float32, dev, True), _ptr(ws))
+    pt, pl, py, pw = _head_args(dims, dev, theta, theta_lp, y_top, ws)
+    return _call("softmax_topk", dev, stream, ctypes.byref(dims), pt, pl, py, k, temperature,
+                 _have("top", top, (M, k), torch.float32, dev), _have("idx", idx, (M, k), torch.int32, dev),
+                 _have("rest", rest, (M,), torch.float32, dev, True), pw)
 
 
 def softmax_distill_fwd_bwd(dims, theta, theta_lp, y_top, top, idx, loss_scale, loss, dy_top, grad, ws, rest=None,
                             labels=None, weights=None, temperature=1.0, soft=1.0, hard=0.0, stream=None):
     dev, M = _on(y_top), dims.T * dims.B
+    pt, pl, py, pw = _head_args(dims, dev, theta, theta_lp, y_top, ws)
     t = _teacher(M, dev, top, idx, rest, labels, weights, temperature, soft, hard)
-    return _call("softmax_distill_fwd_bwd", dev, stream, ctypes.byref(dims), _ptr(theta), _ptr(theta_lp), _ptr(y_top),
-                 ctypes.byref(t), loss_scale, _ptr(loss), _ptr(dy_top), _ptr(grad), _ptr(ws))
+    return _call("softmax_distill_fwd_bwd", dev, stream, ctypes.byref(dims), pt, pl, py, ctypes.byref(t), loss_scale,
+                 _have("loss", loss, (1,), torch.float32, dev),
+                 _have("dy_top", dy_top, (dims.T, dims.B, 2 * dims.H), torch.float32, dev),
+                 _have("grad", grad, tuple(theta.shape), torch.float32, dev), pw)

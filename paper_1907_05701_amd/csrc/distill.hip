@@ -159,7 +159,8 @@ __device__ __forceinline__ float order_value(uint32_t w) {
 // ---------------------------------------------------------------------------
 template <int T> struct TopkLds {
   uint32_t tmax[T];
-  uint64_t cand[CAND];   // order word, complement of the class
+  uint64_t cand[CAND];   // order word, complement of the class; in the order of arrival
+  float left[CAND];      // logits of the candidates behind the k-th, in their order
   uint32_t thr, count, cnt[2][T / 64], flag;
   uint64_t kth;
   float buf[T / 64];
@@ -203,9 +204,10 @@ __device__ __forceinline__ void push(TopkLds<T>& l, float v, int c) {
   const uint32_t at = atomicAdd(&l.count, 1u);
   if (at < (uint32_t)CAND) l.cand[at] = ((uint64_t)order_word(v) << 32) | (uint32_t)~c;
 }
-// Writes the k largest of n candidates; f(candidate, rank) for every candidate.
-template <int T, typename F>
-__device__ __forceinline__ void rank(TopkLds<T>& l, int n, int64_t m, const TopkP& p, F f) {
+// Writes the k largest of n candidates, and what is left to l.left (so that sums
+// over it do not depend on who arrived first).
+template <int T>
+__device__ __forceinline__ void rank(TopkLds<T>& l, int n, int64_t m, const TopkP& p) {
   for (int i = threadIdx.x; i < n; i += T) {
     const uint64_t w = l.cand[i];
     int r = 0;
@@ -215,8 +217,9 @@ __device__ __forceinline__ void rank(TopkLds<T>& l, int n, int64_t m, const Topk
       p.top[m * p.k + r] = order_value((uint32_t)(w >> 32));
       p.idx[m * p.k + r] = (int32_t)~(uint32_t)w;
       if (r == p.k - 1) l.kth = w;
+    } else {
+      l.left[r - p.k] = order_value((uint32_t)(w >> 32));
     }
-    f(w, r);
   }
 }
 
@@ -288,7 +291,7 @@ __device__ __forceinline__ void topk_any(TopkLds<T>& l, const TI* s, int64_t m, 
     __syncthreads();
     n = p.k;
   }
-  rank(l, n, m, p, [](uint64_t, int) {});
+  rank(l, n, m, p);
   if (!p.rest) return;
   __syncthreads();
   rest_of<TI, T, ONE>(l, s, m, p);
@@ -332,11 +335,11 @@ __global__ __launch_bounds__(T) void topk_long_kernel(const TI* __restrict__ log
     topk_any<TI, T, true>(l, s, m, p);
     return;
   }
-  rank(l, n, m, p, [&](uint64_t w, int r) {
-    if (r >= p.k) sum += exp2_(order_value((uint32_t)(w >> 32)) * p.l2t - ref);
-  });
+  rank(l, n, m, p);
   if (!p.rest) return;
-  sum = row_sum<T>(sum, l.buf);   // its barriers: every rank is written, the k-th known
+  __syncthreads();
+  for (int i = tid; i < n - p.k; i += T) sum += exp2_(l.left[i] * p.l2t - ref);
+  sum = row_sum<T>(sum, l.buf);
   if (same(sum > 1e-20f && sum < 1e30f)) {
     if (tid == 0) p.rest[m] = (ref + log2f(sum)) * LN2_F;
     return;
@@ -419,13 +422,13 @@ __global__ __launch_bounds__(T, 4) void topk_rows_kernel(const TI* __restrict__ 
   }
   const float ref = fabsf(thr) < INFINITY ? thr * p.l2t : 0.f;
   float sum = 0.f, rm = -INFINITY;
-  rank(l, n, m, p, [&](uint64_t w, int r) {
-    if (r < p.k) return;
-    const float v = order_value((uint32_t)(w >> 32));
-    sum += exp2_(v * p.l2t - ref);
-    rm = fmaxf(rm, v);
-  });
+  rank(l, n, m, p);
   if (!p.rest) return;
+  __syncthreads();
+  for (int i = tid; i < n - p.k; i += T) {
+    sum += exp2_(l.left[i] * p.l2t - ref);
+    rm = fmaxf(rm, l.left[i]);
+  }
   row.again();
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
@@ -453,8 +456,7 @@ __global__ __launch_bounds__(T, 4) void topk_rows_kernel(const TI* __restrict__ 
 #pragma unroll
       for (int j = 0; j < V; ++j) sum += exp2_((row.get(i, j) - rm) * p.l2t);
     sum += exp2_((row.tail - rm) * p.l2t);
-    for (int i = tid; i < n; i += T)
-      if (l.cand[i] < l.kth) sum += exp2_((order_value((uint32_t)(l.cand[i] >> 32)) - rm) * p.l2t);
+    for (int i = tid; i < n - p.k; i += T) sum += exp2_((l.left[i] - rm) * p.l2t);
   }
   sum = row_sum<T>(sum, l.buf);
   if (tid == 0) p.rest[m] = fabsf(rm) < INFINITY ? rm * (p.l2t * LN2_F) + log2f(sum) * LN2_F : rm;
@@ -625,7 +627,7 @@ __global__ __launch_bounds__(T, 4) void distill_rows_kernel(const TI* logits, TO
   __syncthreads();
   // the teacher's probabilities (base-2 exponents throughout)
   const float tm = fmaxf(all_max<T>(l.buf[0]), r2), lm = all_max<T>(l.buf[1]);
-  const bool taught = !(tm == -INFINITY);
+  const bool taught = p.soft != 0.f && !(tm == -INFINITY);   // an unwanted loss may be infinite
   const float e = taught ? exp2_(t2 - tm) : 0.f, er = taught ? exp2_(r2 - tm) : 0.f;
   if (tid < p.k) l.pv[tid] = e;
   put_wave(l.buf[2], wave_sum(e));
@@ -639,14 +641,14 @@ __global__ __launch_bounds__(T, 4) void distill_rows_kernel(const TI* logits, TO
   float lp = t2 - l2tz;     // log2 of the entry's probability
   float own = prob;         // of its class
   bool lead = at >= 0;      // the class's first entry
-  if (l.dup && at >= 0) {
+  if (l.dup && at >= 0) {   // (the sums below are zeros where the row is not taught)
     own = 0.f;
     for (int j = 0; j < p.k; ++j)
       if (l.iv[j] == at) {
         own += l.pv[j];
         if (j < tid) lead = false;
       }
-    own /= tz;
+    own = taught ? own / tz : 0.f;
     lp = log2f(own);
   }
   // maxima: the others' (as an exponent), the row's

@@ -856,6 +856,7 @@ static int scan_plan(const ssm_dims* d, ScanPlan* o) {
   o->par = up256((size_t)o->nseg * d->B * 2 * d->D * 4);
   o->bwd = o->fwd + o->bc + o->dA + o->par;
   if (o->blocks * o->nseg > 0x7fffffff) return blstm_fail(BLSTM_EUNSUPPORTED, "ssm_scan: B*D too large");
+  if ((int64_t)d->T * d->B * d->G * d->N > ((int64_t)1 << 36)) return blstm_fail(BLSTM_EUNSUPPORTED, "ssm_scan: T*B*G*N too large");
   return BLSTM_OK;
 }
 
@@ -913,8 +914,7 @@ static bool near(const ssm_dims* d, std::initializer_list<int64_t> lds) {
   return most < (1 << 28) && (int64_t)TS * d->B * most * 4 < 0x7fffffff;
 }
 
-static void scan_stretches(const ssm_dims* d, const ScanPlan& pl, char* ws, ScanP* p) {
-  (void)d;
+static void scan_stretches(const ScanPlan& pl, char* ws, ScanP* p) {
   p->nseg = pl.nseg;
   p->segt = pl.segt;
   p->ends = (float*)ws;
@@ -937,9 +937,11 @@ extern "C" int ssm_scan_fwd(const ssm_dims* dims, const ssm_scan_in* in, void* y
   if (ldy < dims->D) return blstm_fail(BLSTM_EINVAL, "ssm_scan_fwd: a row pitch is below its row");
   p.y = y; p.ldy = ldy; p.hlast = h_last; p.saved = (float*)saved; p.tpg = pl.tpg;
   const int mode = !near(dims, {p.ldx, p.lddt, p.ldb, p.ldc, p.ldz, ldy}) ? FAR : p.z ? GATED : PLAIN;
+  if ((uintptr_t)saved % 16 || (uintptr_t)ws % 16)
+    return blstm_fail(BLSTM_EINVAL, "ssm_scan_fwd: saved and ws must be 16-byte aligned");
   if (pl.nseg > 1) {
     if (!ws) return blstm_fail(BLSTM_EINVAL, "ssm_scan_fwd: NULL pointer");
-    scan_stretches(dims, pl, (char*)ws, &p);
+    scan_stretches(pl, (char*)ws, &p);
     const unsigned nb = (unsigned)(pl.blocks * (pl.nseg - 1));
 #define ENDS(T, L, M) \
   BLSTM_LAUNCH("ssm_scan_ends", (ssm_scan_fwd_kernel<T, L, M, true>), dim3(nb), dim3(Tile<L>::NT), 0, stream, p)
@@ -969,6 +971,8 @@ extern "C" int ssm_scan_bwd(const ssm_dims* dims, const ssm_scan_in* in, const v
   if (lddy < dims->D || out->lddx < dims->D || out->ldddt < dims->D || out->lddb < bcw || out->lddc < bcw ||
       (in->z && out->lddz < dims->D))
     return blstm_fail(BLSTM_EINVAL, "ssm_scan_bwd: a row pitch is below its row");
+  if ((uintptr_t)saved % 16 || (uintptr_t)ws % 16)
+    return blstm_fail(BLSTM_EINVAL, "ssm_scan_bwd: saved and ws must be 16-byte aligned");
   const size_t es = dims->precision == BLSTM_BF16 ? 2 : 4;
   char* w = (char*)ws;
   p.dy = dy; p.lddy = lddy; p.dhl = dh_last; p.saved = (float*)saved;
@@ -976,7 +980,7 @@ extern "C" int ssm_scan_bwd(const ssm_dims* dims, const ssm_scan_in* in, const v
   p.lddx = out->lddx; p.ldddt = out->ldddt; p.lddB = out->lddb; p.lddC = out->lddc; p.lddz = out->lddz;
   p.dh0 = out->dh0;
   if (pl.nseg > 1) {
-    scan_stretches(dims, pl, w, &p);
+    scan_stretches(pl, w, &p);
     w += pl.fwd;
   }
   p.bc = pl.bc ? (float*)w : nullptr;
@@ -1006,7 +1010,6 @@ extern "C" int ssm_scan_bwd(const ssm_dims* dims, const ssm_scan_in* in, const v
   s.nbc = pl.bc ? s.M * dims->G * 2 * dims->N : 0;
   s.blocks_bc = cdiv(s.nbc, 256);
   const int64_t nb = s.blocks_bc + cdiv((int64_t)dims->D * (dims->N + 2), 16);
-  if (nb > 0x7fffffff) return blstm_fail(BLSTM_EUNSUPPORTED, "ssm_scan_bwd: T*B*G*N too large");
   if (es == 2) BLSTM_LAUNCH("ssm_scan_sum", ssm_scan_sum_kernel<bf16>, dim3((unsigned)nb), dim3(256), 0, stream, s);
   else BLSTM_LAUNCH("ssm_scan_sum", ssm_scan_sum_kernel<float>, dim3((unsigned)nb), dim3(256), 0, stream, s);
   return blstm_check_launch("ssm_scan_bwd");

@@ -77,7 +77,7 @@ def distill_row(s, top, idx, rest, label, tau, soft, hard):
     ok = [i for i, c in enumerate(idx) if 0 <= c < K]
     loss = s.new_zeros(())
     v = torch.cat((top[ok] / tau, rest.view(1)))
-    if not torch.isneginf(v.max()):
+    if soft and not torch.isneginf(v.max()):   # a loss that is not asked for may be infinite
         p = torch.softmax(v, 0)
         lq = torch.log_softmax(s / tau, 0)
         per = {}

@@ -85,6 +85,30 @@ def test_topk_where_logits_bunch(gpu_lib, precision):
         check_topk(s.to(t).cuda(), k)
 
 
+@pytest.mark.parametrize("K", [33000, 70001])
+def test_topk_of_long_rows_that_bunch(gpu_lib, K):
+    """The same for rows that 1024 threads hold, and for those that no registers hold."""
+    s = torch.zeros(4, K)
+    s[1] = torch.arange(K) / 64
+    s[2, 4000:5500] = 3.0
+    s[2, 9000] = math.nan
+    s[3] = -80.0
+    s[3, [5, K - 1]] = torch.tensor([90.0, 95.0])     # the others far below the threshold
+    for t in (torch.float32, torch.bfloat16):
+        check_topk(s.to(t).cuda(), 2)
+        check_topk(s.to(t).cuda(), 200, tau=0.5)
+
+
+def test_topk_is_the_same_every_time(gpu_lib):
+    """Candidates arrive in any order; sums over those that are left do not depend on it."""
+    g = torch.Generator(device="cuda").manual_seed(8)
+    for K in (900, 32000, 70000):
+        s = torch.randn(64, K, generator=g, device="cuda") * 3
+        first = run_topk(s, 100)
+        for _ in range(5):
+            assert all(torch.equal(a, b) for a, b in zip(first, run_topk(s, 100)))
+
+
 def test_topk_of_strided_rows(gpu_lib):
     g = torch.Generator().manual_seed(5)
     wide = (torch.randn(4, 1200, generator=g) * 3).cuda()
@@ -150,6 +174,30 @@ def test_distill(gpu_lib, M, K, k, precision):
     s, top, idx, rest, lab = make_rows(M, K, k, precision, K + k, rest=k < K)
     check_distill(s, top, idx, rest, lab, tau=2.0, soft=0.7, hard=0.3)
     check_distill(s, top, idx, None, None)
+
+
+@pytest.mark.parametrize("K", [33001, 65537, 100000, 131072])
+def test_distill_of_long_rows(gpu_lib, K):
+    for precision in ("fp32", "bf16"):
+        s, top, idx, rest, lab = make_rows(1, K, 12, precision, K)
+        lab[0] = K - 1
+        idx[0, 0] = K - 1
+        idx[0, 1:] = idx[0, 1:].clamp(max=K - 2)
+        check_distill(s, top, idx, rest, lab, tau=2.0, soft=0.5, hard=0.5, inplace=K == 33001)
+
+
+def test_a_loss_that_is_not_asked_for_may_be_infinite(gpu_lib):
+    """The teacher is sure of a class that the student excludes: the soft loss is
+    infinite and its gradient finite; with soft = 0 neither is there."""
+    s, top, idx, rest, lab = make_rows(2, 50, 3, "fp32", 31)
+    s[:, idx[0, 0]] = -math.inf
+    idx[1] = idx[0]
+    lab[:] = (idx[0, 0] + 1) % 50
+    check_distill(s, top, idx, rest, lab, soft=0.0, hard=1.0)
+    from paper_1907_05701_amd import binding as bd
+    loss, d = torch.empty(2, device="cuda"), torch.empty(2, 50, device="cuda")
+    bd.softmax_distill_rows(s.cuda(), top.cuda(), idx.cuda(), loss, d, rest=rest.cuda())
+    assert bool(torch.isinf(loss).all()) and bool(torch.isfinite(d).all())
 
 
 def test_distill_of_the_most_classes(gpu_lib):
@@ -266,10 +314,44 @@ def test_head_distillation(gpu_lib, M, H, P, K, k, precision, bound):
     rel = lambda a, b: float((a - b).norm() / b.norm())  # noqa: E731
     err = {k2: rel(c(st.grad[sl]).view(shape), v[k2].grad) for k2, (sl, shape) in par.items()}
     err["dy"] = rel(c(st.dy_top).view(M, -1), y.grad)
+    loss = loss.detach()
     err["loss"] = abs(float(st.loss) - float(loss)) / abs(float(loss))
     print("[head]", {a: f"{b:.1e}" for a, b in err.items()}, flush=True)
     assert max(err.values()) <= bound, err
     assert bool((st.grad[:par["W_l"][0].start] == 7).all())   # the stack's slots are not the head's
+
+
+def test_head_distillation_at_the_paper_batch(gpu_lib):
+    """2688 frames of 32000 states in bf16: three pieces of the logits, the last a short one."""
+    M, K, k = 2688, 32000, 32
+    st, par, g = head_case("bf16", M, 512, 256, K, k, seed=2)
+    top = torch.randn(M, k, generator=g, device="cuda") * 2 + 8
+    idx = ((torch.randint(0, K, (M, 1), generator=g, device="cuda") + 991 * torch.arange(k, device="cuda")) % K).int()
+    rest = torch.randn(M, generator=g, device="cuda") + 8
+    st.labels.copy_(torch.randint(0, K, (1, M), generator=g, device="cuda"))
+    st.distill(top, idx, rest, temperature=2.0, soft=0.6, hard=0.4)
+    p = {n: st.theta[sl].double().view(shape) for n, (sl, shape) in par.items()}
+    y = st.y_top.double().view(M, -1)
+    z = y @ p["W_l"].t() + p["b_l"]
+    s = z @ p["W_s"].t() + p["b_s"]
+    t = torch.softmax(torch.cat((top.double() / 2, rest.double()[:, None]), 1), 1)
+    q = torch.softmax(s / 2, 1)
+    at = torch.zeros_like(q).scatter_(1, idx.long(), 1.0)
+    qr = (q * (1 - at)).sum(1, keepdim=True)
+    lab = st.labels.view(-1, 1).long()
+    q1 = torch.softmax(s, 1)
+    kl = (t[:, :-1] * (t[:, :-1].log() - q.gather(1, idx.long()).log())).sum(1) + t[:, -1] * (t[:, -1:].log() - qr.log())[:, 0]
+    loss = float((0.6 * 4 * kl - 0.4 * q1.gather(1, lab).log()[:, 0]).mean())
+    ds = 0.6 * 2 * (q - (1 - at) * q * (t[:, -1:] / qr)).scatter_add(1, idx.long(), -t[:, :-1])
+    ds = (ds + 0.4 * q1.scatter_add(1, lab, torch.full_like(qr, -1.0))) / M
+    dz = ds @ p["W_s"]
+    want = {"W_l": dz.t() @ y, "b_l": dz.sum(0), "W_s": ds.t() @ z, "b_s": ds.sum(0)}
+    rel = lambda a, b: float((a - b).norm() / b.norm())  # noqa: E731
+    err = {n: rel(st.grad[sl].double().view(shape), want[n]) for n, (sl, shape) in par.items()}
+    err["dy"] = rel(st.dy_top.double().view(M, -1), dz @ p["W_l"])
+    err["loss"] = abs(float(st.loss) - loss) / loss
+    print("[head]", {a: f"{b:.1e}" for a, b in err.items()}, flush=True)
+    assert max(err.values()) <= 2e-2, err
 
 
 @pytest.mark.parametrize("precision", ["fp32", "bf16"])
@@ -335,6 +417,7 @@ def test_a_causal_student_learns_from_the_blstm_teacher(gpu_lib):
     loss.backward()
     got = dict(x=dx, dt=ddt, z=dz, Bm=dB, Cm=dC, w=dw, bias=dbias, A=dA, Ds=dD, dtb=ddtb)
     err = {a: float((c(t) - v[a].grad).norm() / v[a].grad.norm()) for a, t in got.items()}
+    loss = loss.detach()
     err["loss"] = abs(float(student.loss) - float(loss)) / float(loss)
     print("[student]", {a: f"{b:.1e}" for a, b in err.items()}, flush=True)
     assert max(err.values()) <= 1e-4, err

@@ -339,6 +339,31 @@ def test_rows_past_32_bits(gpu_lib):
     assert om.far(y, om.conv(xd, w.double().cpu(), None)[0], tol(4)) <= 1.0
 
 
+def test_backward_of_far_rows(gpu_lib):
+    """The same pitch on the backward's inputs and outputs."""
+    from paper_1907_05701_amd import binding as bd
+    T, D, N, ld = 20, 8, 4, 1 << 27
+    g = torch.Generator(device="cuda").manual_seed(4)
+    big = torch.empty(T * ld, dtype=torch.bfloat16, device="cuda")
+    v = [torch.as_strided(big, (T, 1, D), (ld, ld, 1), 32 * i) for i in range(8)]
+    x, dt, z, dy, y, dx, ddt, dz = v
+    for t in (x, dt, z, dy):
+        t.copy_(torch.randn(T, 1, D, generator=g, device="cuda"))
+    bc = torch.randn(T, 1, 2 * N, generator=g, device="cuda").bfloat16()
+    A = -torch.rand(D, N, generator=g, device="cuda")
+    d = bd.make_ssm_dims(T=T, B=1, D=D, N=N, precision="bf16")
+    ws = {k: torch.empty(max(1, n), dtype=torch.uint8, device="cuda") for k, n in bd.ssm_workspace_bytes(d).items()}
+    dA, dB = torch.empty_like(A), torch.empty(T, 1, N, dtype=torch.bfloat16, device="cuda")
+    dC = torch.empty_like(dB)
+    bd.ssm_scan_fwd(d, x, dt, A, bc[..., :N], bc[..., N:], y, ws["fwd"], z=z, saved=ws["saved"])
+    bd.ssm_scan_bwd(d, x, dt, A, bc[..., :N], bc[..., N:], dy, ws["saved"], ws["bwd"], dx, ddt, dA, dB, dC, z=z, dz=dz)
+    leaves = [t.double().cpu().requires_grad_() for t in (x, dt, A, bc[..., :N], bc[..., N:], z)]
+    wy, _ = om.scan(*leaves[:5], z=leaves[5])
+    want = torch.autograd.grad((wy * dy.double().cpu()).sum(), leaves)
+    for a, b in zip((dx, ddt, dA, dB, dC, dz), want):
+        assert om.far(a, b, tol(T)) <= 1.0
+
+
 def test_captured_passes_on_another_stream(gpu_lib):
     """A graph of the convolution, the scan and their backward, replayed between
     eager passes on other inputs, gives what eager calls give, bit for bit."""

@@ -89,7 +89,7 @@ def test_distill_from_itself_is_zero_with_zero_gradient():
     top, at, rest = om.topk(s.detach(), k, tau)
     loss = om.distill_row(s, top, at, rest, -1, tau, 1.0, 0.0)
     (g,) = torch.autograd.grad(loss, s)
-    assert abs(float(loss)) < 1e-14 and float(g.abs().max()) < 1e-14
+    assert abs(float(loss.detach())) < 1e-14 and float(g.abs().max()) < 1e-14
 
 
 @pytest.mark.parametrize("k", [1, 3, 6])

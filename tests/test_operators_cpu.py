@@ -82,6 +82,17 @@ def test_scan_refusals():
              bd.BLSTM_EINVAL)
 
 
+def test_scan_refuses_misaligned_buffers():
+    L, d = bd.lib(), _dims()
+    i = ctypes.byref(_scan_in(d))
+    odd = ctypes.c_void_p(264)
+    _refused(L.ssm_scan_fwd(ctypes.byref(d), i, PTR, 12, None, odd, PTR, None), bd.BLSTM_EINVAL)
+    _refused(L.ssm_scan_fwd(ctypes.byref(d), i, PTR, 12, None, None, odd, None), bd.BLSTM_EINVAL)
+    g = bd.SsmScanGrads(256, 256, 256, 256, 256, 12, 12, 8, 8, 12, 256, None, None, None)
+    _refused(L.ssm_scan_bwd(ctypes.byref(d), i, PTR, 12, None, odd, ctypes.byref(g), PTR, None), bd.BLSTM_EINVAL)
+    _refused(L.ssm_scan_bwd(ctypes.byref(d), i, PTR, 12, None, PTR, ctypes.byref(g), odd, None), bd.BLSTM_EINVAL)
+
+
 def test_conv_refusals():
     L, d, one = bd.lib(), _dims(), _dims(T=1)
     r = ctypes.byref(d)
