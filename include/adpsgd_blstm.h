@@ -257,7 +257,7 @@ int ssm_conv_step(const ssm_dims* dims, const void* x, int64_t ldx, const float*
  *   h_t[n] = exp(s_t A[d][n]) h_{t-1}[n] + s_t x_t B_t[g][n],   h_{-1} = h0 or 0
  *   o_t = sum_n C_t[g][n] h_t[n] + Dskip[d] x_t
  *   y_t = o_t silu(z_t)   (z given), else o_t
- * x, dt, z [T][B][D]; Bm, Cm [T][B][G*N]; A [D][N]; Dskip, dt_bias [D];
+ * x, dt, z [T][B][D]; Bm, Cm [T][B][G*N]; A [D][N], finite; Dskip, dt_bias [D];
  * h0 [B][D][N].  z, Dskip, dt_bias, h0 and lens may be NULL. */
 typedef struct ssm_scan_in {
   const void *x, *dt, *Bm, *Cm, *z;
@@ -305,7 +305,7 @@ int ssm_scan_step(const ssm_dims* dims, const ssm_scan_in* in, const int32_t* sl
  *   rest [M] float32 (or NULL), log of the sum over the other classes of
  *        exp(logit / temperature); -inf where there are none
  * logits [M][K] of the precision's type, row pitch ld; 1 <= k <= K and
- * k <= SOFTMAX_MAX_TOP, K <= SOFTMAX_MAX_CLASSES.  A NaN orders above +inf. */
+ * k <= SOFTMAX_MAX_TOP, K <= SOFTMAX_MAX_CLASSES, M < 2^22.  A NaN orders above +inf. */
 int softmax_topk_rows(const void* logits, int64_t ld, int64_t M, int32_t K, int32_t precision, int32_t k,
                       float temperature, float* top, int32_t* idx, float* rest, hipStream_t stream);
 

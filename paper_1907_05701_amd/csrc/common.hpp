@@ -143,5 +143,6 @@ struct TimedRun {
     if (_slot >= 0) timing_post(_slot, stream);                                        \
   } while (0)
 
+static constexpr int64_t LAUNCH_THREADS = 0xffffffff;   // most threads of a launch along x
 __host__ __device__ static inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 __host__ __device__ static inline int64_t rup(int64_t a, int64_t b) { return cdiv(a, b) * b; }

@@ -774,7 +774,7 @@ static int check_rows(const char* fn, const void* logits, int64_t ld, int64_t M,
   if (precision != BLSTM_FP32 && precision != BLSTM_BF16)
     return blstm_fail(BLSTM_EINVAL, "%s: precision must be BLSTM_FP32 or BLSTM_BF16", fn);
   if (ld < K) return blstm_fail(BLSTM_EINVAL, "%s: a row pitch is below its row", fn);
-  if (M > 0x7fffffff) return blstm_fail(BLSTM_EUNSUPPORTED, "%s: too many rows", fn);
+  if (M * 1024 > LAUNCH_THREADS) return blstm_fail(BLSTM_EUNSUPPORTED, "%s: too many rows", fn);
   return BLSTM_OK;
 }
 static int check_k(int32_t k, int32_t K, float temperature, const char* fn) {

@@ -294,7 +294,7 @@ extern "C" int ssm_conv_fwd(const ssm_dims* dims, const void* x, int64_t ldx, co
   while (p.tx < 256 && p.tx < p.C4) p.tx *= 2;
   p.ncb = (int)cdiv(p.C4, p.tx);
   const int64_t blocks = cdiv((int64_t)p.B * p.nseg, 256 / p.tx) * p.ncb;
-  if (blocks > 0x7fffffff) return blstm_fail(BLSTM_EUNSUPPORTED, "ssm_conv_fwd: T*B*D too large");
+  if (blocks * 256 > LAUNCH_THREADS) return blstm_fail(BLSTM_EUNSUPPORTED, "ssm_conv_fwd: T*B*D too large");
 #define FWD(T, W) \
   BLSTM_LAUNCH("ssm_conv_fwd", (ssm_conv_fwd_kernel<T, W>), dim3((unsigned)blocks), dim3(256), 0, stream, p)
   CONV_DISPATCH(FWD)
@@ -339,7 +339,7 @@ extern "C" int ssm_conv_step(const ssm_dims* dims, const void* x, int64_t ldx, c
   p.y = y; p.ldy = ldy;
   p.vy = four(y, ldy, dims->precision == BLSTM_BF16 ? 2 : 4);
   const int64_t blocks = (int64_t)dims->B * cdiv(p.C4, 256);
-  if (blocks > 0x7fffffff) return blstm_fail(BLSTM_EUNSUPPORTED, "ssm_conv_step: B*D too large");
+  if (blocks * 256 > LAUNCH_THREADS) return blstm_fail(BLSTM_EUNSUPPORTED, "ssm_conv_step: B*D too large");
 #define STEP(T, W)                                                                                            \
   BLSTM_LAUNCH("ssm_conv_step", (ssm_conv_step_kernel<T, W>), dim3((unsigned)blocks), dim3(256), 0, stream, p, \
                slots, n_slots, (T*)state)

@@ -167,9 +167,17 @@ def test_scan_of_unaligned_rows(gpu_lib, D, N, G, precision):
     check(Case(18, 2, D, N, G, precision, odd=True))
 
 
-@pytest.mark.parametrize("T,B,D,N", [(300, 1, 64, 16), (200, 3, 20, 4), (530, 2, 8, 24)])
+@pytest.mark.parametrize("precision", ["fp32", "bf16"])
+@pytest.mark.parametrize("T,B,D,N,G", [(9, 2050, 3, 7, 1), (11, 350, 6, 13, 3), (10, 520, 8, 16, 2)], ids=str)
+def test_scan_of_many_sequences(gpu_lib, T, B, D, N, G, precision):
+    """Enough of them that a lane holds eight states of a channel."""
+    check(Case(T, B, D, N, G, precision, lens=[(5 * b) % (T + 2) for b in range(B)]))
+
+
+@pytest.mark.parametrize("T,B,D,N", [(300, 1, 64, 16), (200, 3, 20, 4), (530, 2, 8, 24), (260, 2, 70, 8), (170, 80, 66, 10),
+                                     (150, 70, 130, 6)])
 def test_scan_of_long_sequences(gpu_lib, T, B, D, N):
-    check(Case(T, B, D, N, 1, "fp32", lens=[T, T // 2, 0][:B]))
+    check(Case(T, B, D, N, 1, "fp32", lens=([T, T // 2, 0] * B)[:B]))
 
 
 def test_a_scan_in_pieces_is_the_whole(gpu_lib):

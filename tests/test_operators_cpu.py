@@ -40,12 +40,24 @@ def test_bad_ssm_dims(over, code):
     _refused(L.ssm_conv_fwd(ctypes.byref(d), PTR, 1 << 30, PTR, None, None, None, PTR, 1 << 30, None, 0, None), code)
 
 
+def test_scans_of_more_threads_than_a_launch_has_are_refused():
+    for over in (dict(T=1, B=1 << 24, D=512, G=1), dict(T=1 << 10, B=1 << 10, D=64, N=64, G=64)):
+        with pytest.raises(bd.BlstmError) as e:
+            bd.ssm_workspace_bytes(_dims(**over))
+        assert e.value.code == bd.BLSTM_EUNSUPPORTED
+    L, d = bd.lib(), _dims(T=1, B=1 << 24, D=512, G=1)
+    i = ctypes.byref(_scan_in(d))
+    _refused(L.ssm_scan_step(ctypes.byref(d), i, None, 1 << 24, PTR, PTR, 512, None), bd.BLSTM_EUNSUPPORTED)
+    _refused(L.ssm_conv_step(ctypes.byref(d), PTR, 512, PTR, None, None, 1 << 24, PTR, PTR, 512, 0, None),
+             bd.BLSTM_EUNSUPPORTED)
+
+
 def test_workspaces_hold_a_state_for_every_eight_frames():
     a = bd.ssm_workspace_bytes(_dims(T=8, N=16))
     b = bd.ssm_workspace_bytes(_dims(T=9, N=16))
     assert a["saved"] == 3 * 12 * 16 * 4 and b["saved"] == 2 * a["saved"]
-    # states are held in whole lanes of eight
-    assert bd.ssm_workspace_bytes(_dims(T=8, N=9))["saved"] == a["saved"]
+    # states are held in whole lanes
+    assert bd.ssm_workspace_bytes(_dims(T=8, N=13))["saved"] == a["saved"]
 
 
 @pytest.mark.parametrize("field", ["x", "dt", "Bm", "Cm", "A"])
