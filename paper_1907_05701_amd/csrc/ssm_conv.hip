@@ -6,10 +6,12 @@
 // issues every load (the W - 1 frames on either side among them, which
 // neighbours read too and the caches serve) before it computes, so one trip to memory is all that
 // it waits for.  (Frame after frame, 128 chunks of 21 frames of 1024 channels: forward
-// 9.7 us, backward 17.)
+// 9.7 us, backward 17.)  The backward computes dpre of W - 1 frames again in
+// each stretch, and still shorter ones, which are more waves at a time, cost less there: 8
+// frames 72, 4 frames 62 us at 16 sequences of 1500; the forward 28.3, 31.1 at 1024 of 21.
 #include "ssm.hpp"
 
-static constexpr int SEG = 8;
+static constexpr int SEG = 8, BSEG = 4;   // frames of a thread, forward and backward
 
 struct ConvP {
   const void *x, *dy, *state, *dsto;
@@ -100,9 +102,11 @@ __global__ __launch_bounds__(256) void ssm_conv_fwd_kernel(const ConvP p) {
 }
 
 // 64 threads a row of 256 channels, 4 rows a workgroup; a row takes every
-// gridDim.y * 4-th stretch of SEG frames.
+// gridDim.y * 4-th stretch of BSEG frames.  There are as many workgroups as run at
+// a time, so that none waits behind the others and the partial sums are few.
+static constexpr int conv_resident(int W) { return W <= 4 ? 3 : 2; }   // workgroups of a CU: what the registers hold
 template <typename T, int W>
-__global__ __launch_bounds__(256) void ssm_conv_bwd_kernel(const ConvP p) {
+__global__ __launch_bounds__(256, conv_resident(W)) void ssm_conv_bwd_kernel(const ConvP p) {
   const int cl = threadIdx.x & 63, rl = threadIdx.x >> 6;
   const int c = ((int)blockIdx.x * 64 + cl) * 4, nv = min(4, p.D - c);
   f32x4 w[W], bias, dw[W], db{0.f, 0.f, 0.f, 0.f};
@@ -111,14 +115,14 @@ __global__ __launch_bounds__(256) void ssm_conv_bwd_kernel(const ConvP p) {
   for (int j = 0; j < W; ++j) dw[j] = db;
   const int items = p.nseg * p.B;   // at most T * B
   for (int it = (int)blockIdx.y * 4 + rl; it < items && nv > 0; it += (int)gridDim.y * 4) {
-    const int b = (int)((unsigned)it % (unsigned)p.B), t0 = (int)((unsigned)it / (unsigned)p.B) * SEG, t1 = min(p.T, t0 + SEG);
+    const int b = (int)((unsigned)it % (unsigned)p.B), t0 = (int)((unsigned)it / (unsigned)p.B) * BSEG, t1 = min(p.T, t0 + BSEG);
     const int len = conv_len(p, b);
-    // inputs t0 - W + 1 .. t0 + SEG + W - 2, gradients t0 .. t0 + SEG + W - 2
-    typename Vec4<T>::type in[SEG + 2 * W - 2], gy[SEG + W - 1];
+    // inputs t0 - W + 1 .. t0 + BSEG + W - 2, gradients t0 .. t0 + BSEG + W - 2
+    typename Vec4<T>::type in[BSEG + 2 * W - 2], gy[BSEG + W - 1];
 #pragma unroll
-    for (int j = 0; j < SEG + 2 * W - 2; ++j) in[j] = conv_input<T, W>(p, t0 - W + 1 + j, b, len, c, nv);
+    for (int j = 0; j < BSEG + 2 * W - 2; ++j) in[j] = conv_input<T, W>(p, t0 - W + 1 + j, b, len, c, nv);
 #pragma unroll
-    for (int j = 0; j < SEG + W - 1; ++j) {
+    for (int j = 0; j < BSEG + W - 1; ++j) {
       gy[j] = typename Vec4<T>::type{};
       if (t0 + j < len) gy[j] = ld4_raw((const T*)p.dy + ((int64_t)(t0 + j) * p.B + b) * p.lddy + c, nv, p.vdy);
     }
@@ -126,7 +130,7 @@ __global__ __launch_bounds__(256) void ssm_conv_bwd_kernel(const ConvP p) {
 #pragma unroll
     for (int j = 0; j < W; ++j) dp[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int t = 0; t < SEG + W - 1; ++t) {
+    for (int t = 0; t < BSEG + W - 1; ++t) {
 #pragma unroll
       for (int j = 0; j < W - 1; ++j) dp[j] = dp[j + 1];
       f32x4 g = widen(gy[t]);   // zero behind the end
@@ -138,7 +142,7 @@ __global__ __launch_bounds__(256) void ssm_conv_bwd_kernel(const ConvP p) {
         for (int i = 0; i < 4; ++i) g[i] *= dsiluf_(pre[i]);
       }
       if (t0 + t >= len) g = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (t < SEG) {
+      if (t < BSEG) {
         db += g;
 #pragma unroll
         for (int j = 0; j < W; ++j) dw[j] += g * widen(in[t + j]);
@@ -233,11 +237,11 @@ __global__ __launch_bounds__(256) void ssm_conv_step_kernel(const ConvP p, const
 // ---------------------------------------------------------------------------
 // Host side.
 // ---------------------------------------------------------------------------
-static constexpr int CONV_ROWS = 128;   // most row blocks of the backward
-
+// Row blocks of the backward, on 256 CUs.  (16 sequences of 1500 frames of 1024 channels, bf16,
+// 4 taps: 512 workgroups 62, 768 53, 1024 62 us; 8 taps, two a CU: 512 best.)
 static int conv_rows(const ssm_dims* d) {
-  const int64_t items = cdiv(d->T, SEG) * d->B;
-  return (int)std::min<int64_t>(CONV_ROWS, cdiv(items, 4));
+  const int64_t items = cdiv(d->T, BSEG) * d->B, most = 256 * conv_resident(d->W) / cdiv(d->D, 256);
+  return (int)std::min(std::max<int64_t>(1, most), cdiv(items, 4));
 }
 size_t ssm_conv_bwd_bytes(const ssm_dims* d) { return (size_t)conv_rows(d) * (d->W + 1) * d->D * 4; }
 
@@ -315,6 +319,7 @@ extern "C" int ssm_conv_bwd(const ssm_dims* dims, const void* x, int64_t ldx, co
   p.vdy = four(dy, lddy, es);
   p.vdx = four(dx, lddx, es);
   p.vs = p.vs && ((uintptr_t)dstate_out % (4 * es)) == 0 && ((uintptr_t)dstate % (4 * es)) == 0;
+  p.nseg = (int)cdiv(dims->T, BSEG);
   const int rows = conv_rows(dims);
 #define BWD(T, W)                                                                                          \
   BLSTM_LAUNCH("ssm_conv_bwd", (ssm_conv_bwd_kernel<T, W>), dim3((unsigned)cdiv(p.C4, 64), (unsigned)rows), \
