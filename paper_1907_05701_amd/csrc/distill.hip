@@ -108,6 +108,16 @@ template <typename TI, int V, int NV, int T> struct Row {
   }
 };
 
+// Waves of a SIMD that the registers are kept to.  Three rows on a CU instead
+// of two hide more of each other's barriers and waits: 2688 bf16 rows of 32000 (64
+// values a thread) 4 waves 59.6, 6 waves 53 us for the top, 92 and 85 for the loss.  float32 rows
+// of 64 values have no room for it.
+template <typename TI, int T, int V, int NV> constexpr int waves_of() {
+  if (NV == 0 || T > 512) return 4;
+  if (V * NV * sizeof(TI) <= 64) return 8;
+  return V * NV <= 32 || sizeof(TI) == 2 ? 6 : 4;
+}
+
 // Rows longer than registers hold: calls f(column, value) for the thread's
 // columns, read from memory (the caches) by every pass.
 // ONE: element by element, in fewer registers.
@@ -178,21 +188,39 @@ struct TopkP {
 // for the whole wave, and what lives on past the branch not taken takes no registers from it.
 __device__ __forceinline__ uint32_t same(uint32_t v) { return __builtin_amdgcn_readfirstlane(v); }
 
-// The k-th largest of the threads' maxima (order words), down to its bits from LOW on.
+// The k-th largest of the threads' maxima (order words), down to its bits from
+// LOW on; where k is small, of the maxima of groups of 4 or 8 threads, two words a
+// lane: a few more logits pass (37 instead of 33 of a row of 32 from 512 threads), and each step of
+// the search takes a quarter of the instructions.
+template <int LOW, int NW>
+__device__ __forceinline__ uint32_t kth_word(const uint32_t (&w)[NW], int k) {
+  uint32_t t = 0;
+  for (int bit = 31; bit >= LOW; --bit) {
+    const uint32_t c = t | (1u << bit);
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) n += __popcll(__ballot(w[i] >= c));
+    if (n >= k) t = c;
+  }
+  return t;
+}
+static constexpr int FOLD = 64;   // largest k for groups
 template <int LOW, int T>
 __device__ __forceinline__ uint32_t kth_max(TopkLds<T>& l, int k) {
   const int lane = threadIdx.x & 63;
   __syncthreads();
   if (threadIdx.x < 64) {
-    uint32_t w[T / 64], t = 0;
+    constexpr int NW = T / 64;
+    uint32_t w[NW], t;
 #pragma unroll
-    for (int i = 0; i < T / 64; ++i) w[i] = l.tmax[i * 64 + lane];
-    for (int bit = 31; bit >= LOW; --bit) {
-      const uint32_t c = t | (1u << bit);
-      int n = 0;
+    for (int i = 0; i < NW; ++i) w[i] = l.tmax[i * 64 + lane];
+    if (k <= FOLD) {
+      uint32_t g[2] = {w[0], w[1]};
 #pragma unroll
-      for (int i = 0; i < T / 64; ++i) n += __popcll(__ballot(w[i] >= c));
-      if (n >= k) t = c;
+      for (int i = 2; i < NW; ++i) g[i & 1] = max(g[i & 1], w[i]);
+      t = kth_word<LOW>(g, k);
+    } else {
+      t = kth_word<LOW>(w, k);
     }
     if (lane == 0) l.thr = t;
   }
@@ -352,7 +380,7 @@ __global__ __launch_bounds__(T) void topk_long_kernel(const TI* __restrict__ log
 // which no other exceeds, and again from their own maximum where that leaves
 // nothing.  Rows with a NaN, and rows with too many candidates, go the way of any row.
 template <typename TI, int T, int V, int NV>
-__global__ __launch_bounds__(T, 4) void topk_rows_kernel(const TI* __restrict__ logits, const TopkP p) {
+__global__ __launch_bounds__(T, (waves_of<TI, T, V, NV>())) void topk_rows_kernel(const TI* __restrict__ logits, const TopkP p) {
   __shared__ TopkLds<T> l;
   const int64_t m = blockIdx.x;
   const TI* s = logits + m * p.ld;
@@ -377,6 +405,10 @@ __global__ __launch_bounds__(T, 4) void topk_rows_kernel(const TI* __restrict__ 
       for (int j = 0; j < V; j += 2) nan |= __builtin_isunordered(row.get(i, j), row.get(i, j + 1));
     }
     mx = fmaxf(mx, vm[i]);
+    if constexpr (V > 1) {
+      asm volatile("" : "+v"(vm[i]));
+      __builtin_amdgcn_sched_barrier(0);   // one vector at a time: fewer registers
+    }
   }
   mx = fmaxf(mx, row.tail);
   nan |= row.tail != row.tail;
@@ -395,15 +427,20 @@ __global__ __launch_bounds__(T, 4) void topk_rows_kernel(const TI* __restrict__ 
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     if (vm[i] >= thr && row.has(i, whole)) {
-      // few vectors come here, and fewer of their values: those are read
-      // again, so that this is one loop and not a branch per value
+      // few vectors come here, most with one value; the others of a vector are
+      // read again, so that this is one loop and not a branch per value
       uint32_t bits = 0;
+      float v = 0.f;
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const bool in = row.get(i, j) >= thr;
+      for (int j = V - 1; j >= 0; --j) {
+        const float x = row.get(i, j);
+        const bool in = x >= thr;
         bits |= in ? 1u << j : 0u;
+        v = in ? x : v;   // ends with the first of them
         if (in) row.drop(i, j);
       }
+      push(l, v, row.col(i) + __builtin_ctz(bits));
+      bits &= bits - 1;
       for (; bits; bits &= bits - 1) {
         const int c = row.col(i) + __builtin_ctz(bits);
         push(l, to_f32(s[c]), c);
@@ -479,9 +516,8 @@ struct DistillP {
   int K, k, pad;
   float it2, tau, soft, hard, scale;   // it2: log2 e / tau
 };
-// Threads of a row: 512 with 64 values each, two rows on a CU.  (2688 bf16 rows
-// of 32000, labels given / not: 100 / 70 us; 256 threads 99 / 74, but float32 279 against 79; 1024
-// threads 142 / 115.)
+// Threads of a row: 512.  (2688 bf16 rows of 32000 without labels: 70 us, with 256 threads
+// 74, and float32 279 against 79; 1024 threads 115.)
 template <int T> struct DistillLds {
   float pv[MAXK];
   int32_t iv[MAXK];
@@ -584,9 +620,13 @@ template <typename TI, typename TO, int T, int V> struct Others<TI, TO, T, V, 0>
   }
 };
 
-// HARD: with the labels' cross-entropy.
-template <typename TI, typename TO, int T, int V, int NV, bool HARD>
-__global__ __launch_bounds__(T, 4) void distill_rows_kernel(const TI* logits, TO* dlogits, const DistillP p) {
+// HARD: how the labels' cross-entropy has e^s of the others, NO: no labels, OWN: an
+// exponential of its own, POW1, POW2: from e^u, its first or second power.
+// (Temperatures of 1 and 2.  2688 bf16 rows of 32000: NO 70, POW1 78, POW2 84, OWN 86 us: half the
+// exponentials of OWN, which the vector unit shares with the rounding and the moves.)
+enum { NO, OWN, POW1, POW2 };
+template <typename TI, typename TO, int T, int V, int NV, int HARD>
+__global__ __launch_bounds__(T, (waves_of<TI, T, V, NV>())) void distill_rows_kernel(const TI* logits, TO* dlogits, const DistillP p) {
   extern __shared__ uint32_t listed[];   // a bit per class, to the end of the registers' columns
   __shared__ DistillLds<T> l;
   const int64_t m = blockIdx.x;
@@ -659,9 +699,16 @@ __global__ __launch_bounds__(T, 4) void distill_rows_kernel(const TI* logits, TO
   const float h2 = -aref * LOG2E_F;
   float zr = 0.f, z1 = 0.f;
   row.others(s, K, listed, [&](float v) {
-    zr += exp2_(v * p.it2 - rref);
-    if constexpr (HARD) z1 += exp2_(v * LOG2E_F + h2);
+    const float x = exp2_(v * p.it2 - rref);
+    zr += x;
+    if constexpr (HARD == OWN) z1 += exp2_(v * LOG2E_F + h2);
+    if constexpr (HARD == POW2) z1 += x * x;
+    // or the compiler would sink this sum past the loop, and carry every exponential there
+    if constexpr (HARD == OWN || HARD == POW2) asm volatile("" : "+v"(z1));
   });
+  const float eh = HARD < POW1 || rm == -INFINITY ? 0.f : exp2_(rm * LOG2E_F + h2);   // as eo, of e^s
+  if constexpr (HARD == POW1) z1 = zr * eh;
+  if constexpr (HARD == POW2) z1 *= eh;
   const float u = sv * p.it2;
   const float ez = lead ? exp2_(u - um) : 0.f;
   if (HARD && lead) z1 += exp2_(sv * LOG2E_F + h2);
@@ -677,10 +724,13 @@ __global__ __launch_bounds__(T, 4) void distill_rows_kernel(const TI* logits, TO
   const float ks = taught ? p.scale * weight * p.soft * p.tau : 0.f, kh = marked ? p.scale * weight * p.hard : 0.f;
   const float cr = ks * (eo / z - (r > 0.f && zr > 0.f ? r / zr : 0.f));   // of e^(u - rref) in the others
   const float ch = marked ? kh / z1 : 0.f;
+  const float cp = HARD == POW1 ? cr + ch * eh : ch * eh;
   row.write(s, d, K, listed, [&](float v) {
-    float g = cr * exp2_(v * p.it2 - rref);
-    if constexpr (HARD) g += ch * exp2_(v * LOG2E_F + h2);
-    return g;
+    const float x = exp2_(v * p.it2 - rref);
+    if constexpr (HARD == OWN) return cr * x + ch * exp2_(v * LOG2E_F + h2);
+    else if constexpr (HARD == POW1) return cp * x;
+    else if constexpr (HARD == POW2) return (cr + cp * x) * x;
+    else return cr * x;
   });
   __syncthreads();   // the others lie before what replaces the listed ones' and the label's values
   if (lead) {
@@ -709,7 +759,9 @@ __global__ __launch_bounds__(T, 4) void distill_rows_kernel(const TI* logits, TO
 // ---------------------------------------------------------------------------
 // How a row is read.  Short rows go element by element: their few 16-byte
 // pieces would leave most threads without a maximum of their own.  Longer ones
-// go 16 bytes at a time, 64 values a thread, with 1024 threads where 512 do not
+// go 16 bytes at a time, 16, 32 or 64 values a thread, since what a thread holds room for it also
+// computes (top logits / loss of 12000 bf16 rows, us: of 9001, 32 values 115 / 124, 64 values 188 /
+// 163; of 6000, 16 values 85 / 102, 32 values 98 / 121), with 1024 threads where 512 do not
 // reach (few rows do not gain from them: 256 rows of 32000 logits 11.1 us with 512,
 // 11.6 with 1024), and, packed bf16 pairs, 128 values in rows of up to
 // PACKED.  What no registers hold is read by every pass.
@@ -720,6 +772,8 @@ template <typename TI, int PACKED, typename F> static void by_length(int32_t K, 
   typedef std::integral_constant<int, 1024> T10;
 #define NVEC(n) std::integral_constant<int, n>{}
   if (K <= SHORT) return f(T5{}, NVEC(1), NVEC(8));
+  if (K <= 16 * 512) return f(T5{}, NVEC(V), NVEC(16 / V));
+  if (K <= 32 * 512) return f(T5{}, NVEC(V), NVEC(32 / V));
   if (K <= 64 * 512) return f(T5{}, NVEC(V), NVEC(64 / V));
   if (K <= 64 * 1024) return f(T10{}, NVEC(V), NVEC(64 / V));
   if constexpr (sizeof(TI) == 2 && PACKED > 64 * 1024)
@@ -755,12 +809,13 @@ int distill_rows(const TI* logits, int64_t ld, int64_t M, int32_t K, const softm
   by_length<TI, 128 * 1024>(K, [&](auto tt, auto v, auto nv) {
     constexpr int T = decltype(tt)::value, V = decltype(v)::value, NV = decltype(nv)::value;
     const size_t bits = (size_t)(NV ? NV * V * T : rup(K, 32)) / 8;
-    if (p.labels)
-      BLSTM_LAUNCH("softmax_distill_rows", (distill_rows_kernel<TI, TO, T, V, NV, true>), dim3((unsigned)M), dim3(T), bits,
-                   stream, logits, dlogits, p);
-    else
-      BLSTM_LAUNCH("softmax_distill_rows", (distill_rows_kernel<TI, TO, T, V, NV, false>), dim3((unsigned)M), dim3(T), bits,
-                   stream, logits, dlogits, p);
+#define DISTILL(HARD)                                                                                                  \
+  BLSTM_LAUNCH("softmax_distill_rows", (distill_rows_kernel<TI, TO, T, V, NV, HARD>), dim3((unsigned)M), dim3(T), bits, \
+               stream, logits, dlogits, p)
+    if (!p.labels) DISTILL(NO);
+    else if (p.tau == 1.f) DISTILL(POW1);
+    else if (p.tau == 2.f) DISTILL(POW2);
+    else DISTILL(OWN);
   });
   return blstm_check_launch("softmax_distill_rows");
 }

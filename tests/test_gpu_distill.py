@@ -85,6 +85,18 @@ def test_topk_where_logits_bunch(gpu_lib, precision):
         check_topk(s.to(t).cuda(), k)
 
 
+@pytest.mark.parametrize("precision", ["fp32", "bf16"])
+@pytest.mark.parametrize("k", [64, 65, 128])
+@pytest.mark.parametrize("K", [130, 4097, 8195, 16391, 32768, 33001])
+def test_topk_of_adjacent_large_logits(gpu_lib, K, k, precision):
+    """Several of the k within the same 16 bytes; k on either side of where maxima are joined."""
+    g = torch.Generator().manual_seed(K)
+    s = torch.randn(3, K, generator=g)
+    s[1, 16:16 + 40] += 20
+    s[2, K - 60:] = torch.arange(60) / 4.0 + 5
+    check_topk(s.to(TYPES[precision]).cuda(), k, 2.0)
+
+
 @pytest.mark.parametrize("K", [33000, 70001])
 def test_topk_of_long_rows_that_bunch(gpu_lib, K):
     """The same for rows that 1024 threads hold, and for those that no registers hold."""
@@ -174,6 +186,22 @@ def test_distill(gpu_lib, M, K, k, precision):
     s, top, idx, rest, lab = make_rows(M, K, k, precision, K + k, rest=k < K)
     check_distill(s, top, idx, rest, lab, tau=2.0, soft=0.7, hard=0.3)
     check_distill(s, top, idx, None, None)
+
+
+@pytest.mark.parametrize("precision", ["fp32", "bf16"])
+@pytest.mark.parametrize("tau", [0.5, 1.0, 2.0, 3.0])
+@pytest.mark.parametrize("K", [100, 4097, 8195, 16391, 20003])
+def test_distill_at_every_temperature_and_length(gpu_lib, K, tau, precision):
+    """Labels among the listed classes, beside them and missing; a row whose
+    others lie 200 below its listed ones, one whose listed ones lie below, one of spread logits."""
+    s, top, idx, rest, lab = make_rows(5, K, 6, precision, K)
+    lab[0], lab[1] = idx[0, 2], -1
+    s[2] -= 200
+    s[2, idx[2].long()] += 200
+    s[3, idx[3].long()] -= 60
+    s[4] *= 20
+    check_distill(s, top, idx, rest, lab, tau=tau, soft=0.6, hard=0.4)
+    check_distill(s, top, idx, rest, lab, tau=tau, soft=0.0, hard=1.0)
 
 
 @pytest.mark.parametrize("K", [33001, 65537, 100000, 131072])
