@@ -2,7 +2,10 @@
 // and logit gradients against them.  One workgroup per row.
 //
 // Exponentials are base-2 hardware ones of differences from a row maximum;
-// sums are float32 in a fixed order.
+// sums are float32 in a fixed order.  Memory bounds both: 2688 bf16 rows of 32000
+// logits, the top 32 in 49 us (172 MB, 3.5 TB/s; the vector unit issues 36 us of it,
+// and a row's search, candidates and ranks are barriers that only other rows hide), loss and gradients
+// with labels in 76 us (344 MB, 4.5 TB/s).
 #include <math.h>
 
 #include <cmath>

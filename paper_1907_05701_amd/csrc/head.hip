@@ -1006,18 +1006,23 @@ static void head_z(const Layout& lo, const float* theta, const T* W, const T* yt
   }
 }
 
-// Rows of float32 logits that the bf16 head's distillation holds at a time:
-// at 32000 classes 131 MB, which the last-level cache keeps between the
-// product that writes them and the row pass that reads them.
-static constexpr int64_t HEAD_ROWS = 1024;
+// Rows of float32 logits that the bf16 head's distillation holds at a time, all
+// frames in equal parts: at 32000 classes at most 180 MB, which the last-level
+// cache keeps between the product that writes them and the row pass that reads
+// them.  (2688 frames, distillation / top logits, us: parts of 512 459 / 235,
+// 1024 443 / 202, 1344 448 / 183, all at once 446 / 221.)
+static int64_t head_rows(const Layout& lo) {
+  if (lo.es != 2) return lo.M;
+  return std::min(lo.M, rup(cdiv(lo.M, cdiv(lo.M, 1408)), 64));
+}
 // Behind head_ws, bf16: those logits, then column-sum partials of db_s.
 static size_t head_logits_bytes(const Layout& lo) {
-  return lo.es == 2 ? (size_t)std::min(lo.M, HEAD_ROWS) * lo.Kp * 4 : 0;
+  return lo.es == 2 ? (size_t)head_rows(lo) * lo.Kp * 4 : 0;
 }
 static size_t head_extra_bytes(const Layout& lo) {
   return lo.es == 2 ? head_logits_bytes(lo) + (size_t)COLSUM_MAX_CHUNKS * lo.Kp * 4 : 0;
 }
-// float32 logits of rows [r0, r0 + n) of z (n <= HEAD_ROWS in bf16), row pitch Kp.
+// float32 logits of rows [r0, r0 + n) of z (n <= head_rows in bf16), row pitch Kp.
 template <typename T>
 static float* head_logits(const Layout& lo, const float* theta, const T* W, char* hws, int64_t r0, int64_t n,
                           hipStream_t s) {
@@ -1049,8 +1054,8 @@ static int head_impl(const Layout& lo, const float* theta, const T* W, const T* 
   constexpr bool lp = std::is_same<T, bf16>::value;
   T* DS = (T*)(hws + lo.S);
   if (teacher) {
-    // float32: every row's logits at once, overwritten by ds in place; bf16: HEAD_ROWS at a time
-    const int64_t step = lp ? std::min(M, HEAD_ROWS) : M;
+    // float32: every row's logits at once, overwritten by ds in place
+    const int64_t step = head_rows(lo);
     for (int64_t r0 = 0; r0 < M; r0 += step) {
       const int64_t n = std::min(step, M - r0);
       const float* S = head_logits<T>(lo, theta, W, hws, r0, n, s);
@@ -1320,7 +1325,7 @@ template <typename T>
 static int topk_impl(const Layout& lo, const float* theta, const T* W, const T* ytop, int32_t k, float temperature,
                      float* top, int32_t* idx, float* rest, char* ws, hipStream_t s) {
   head_z<T>(lo, theta, W, ytop, ws, s);
-  const int64_t step = std::is_same<T, bf16>::value ? std::min(lo.M, HEAD_ROWS) : lo.M;
+  const int64_t step = head_rows(lo);
   for (int64_t r0 = 0; r0 < lo.M; r0 += step) {
     const int64_t n = std::min(step, lo.M - r0);
     const float* S = head_logits<T>(lo, theta, W, ws, r0, n, s);

@@ -115,7 +115,8 @@ class LearnerStep:
 
     def capture(self, lr, steps=1, flags=0, teacher=None):
         """Record `steps` learner steps into a HIP graph (replaying it runs
-        them again on the current buffers, i.e. continues training)."""
+        them again on the current buffers, i.e. continues training).  Each replay
+        reads `teacher`'s tensors where they lie, too: keep them."""
         if teacher is not None:
             self._distill_ws()   # allocated outside the graph's memory
         graph = torch.cuda.CUDAGraph()

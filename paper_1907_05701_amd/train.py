@@ -51,6 +51,9 @@ class Trainer:
         self.flags = flags
         self.teacher = [None] * len(self.x)
         if teacher is not None:
+            for n in ("T", "B", "D", "K"):   # a class behind the student's would count as absent
+                if teacher.shape[n] != step.shape[n]:
+                    raise ValueError(f"the teacher's {n} is {teacher.shape[n]}, the learner's {step.shape[n]}")
             for i, x in enumerate(self.x):
                 teacher.x.copy_(x)
                 teacher.forward()

@@ -163,3 +163,15 @@ def test_the_binding_refuses_host_tensors():
         bd.ssm_conv_fwd(d, x, x, None, x)
     with pytest.raises(ValueError):
         bd.softmax_topk_rows(torch.zeros(2, 4), torch.zeros(2, 1), torch.zeros(2, 1, dtype=torch.int32))
+
+
+@pytest.mark.parametrize("n", ["T", "B", "D", "K"])
+def test_a_teacher_of_another_shape_is_refused(n):
+    from types import SimpleNamespace
+
+    from paper_1907_05701_amd.train import Trainer
+    shape = dict(T=3, B=2, D=4, K=10)
+    step = SimpleNamespace(shape=shape, device="cpu")
+    teacher = SimpleNamespace(shape=dict(shape, **{n: 11}))
+    with pytest.raises(ValueError, match=f"teacher's {n} is 11"):
+        Trainer(step, [], 0.1, 4, teacher=teacher)
