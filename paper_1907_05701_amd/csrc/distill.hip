@@ -17,7 +17,7 @@
 #define LOG2E_F 1.4426950408889634f
 #define LN2_F 0.6931471805599453f
 static_assert(SOFTMAX_MAX_CLASSES == 1 << 18, "bits of a class");
-static constexpr int RT = 512;             // least threads of a row (T below: 512 or 1024)
+static constexpr int RT = 256;             // least threads of a row (T below: 256, 512 or 1024)
 static constexpr int CAND = 1024;          // most candidates kept in LDS
 static constexpr int MAXK = SOFTMAX_MAX_TOP;
 static_assert(MAXK <= RT && MAXK <= CAND, "an entry a thread; the k-th largest of the threads' maxima bounds the k-th logit");
@@ -519,7 +519,7 @@ struct DistillP {
   int K, k, pad;
   float it2, tau, soft, hard, scale;   // it2: log2 e / tau
 };
-// Threads of a row: 512.  (2688 bf16 rows of 32000 without labels: 70 us, with 256 threads
+// Threads of a row of 32000: 512.  (2688 bf16 rows without labels: 70 us, with 256 threads
 // 74, and float32 279 against 79; 1024 threads 115.)
 template <int T> struct DistillLds {
   float pv[MAXK];
@@ -762,40 +762,48 @@ __global__ __launch_bounds__(T, (waves_of<TI, T, V, NV>())) void distill_rows_ke
 // ---------------------------------------------------------------------------
 // How a row is read.  Short rows go element by element: their few 16-byte
 // pieces would leave most threads without a maximum of their own.  Longer ones
-// go 16 bytes at a time, 16, 32 or 64 values a thread, since what a thread holds room for it also
-// computes (top logits / loss of 12000 bf16 rows, us: of 9001, 32 values 115 / 124, 64 values 188 /
-// 163; of 6000, 16 values 85 / 102, 32 values 98 / 121), with 1024 threads where 512 do not
-// reach (few rows do not gain from them: 256 rows of 32000 logits 11.1 us with 512,
-// 11.6 with 1024), and, packed bf16 pairs, 128 values in rows of up to
-// PACKED.  What no registers hold is read by every pass.
-static constexpr int SHORT = 8 * RT;
-template <typename TI, int PACKED, typename F> static void by_length(int32_t K, F f) {
+// go 16 bytes at a time, 16, 32 or 64 values a thread, since what a thread holds room for
+// it also computes, with as few threads as that takes: a row's barriers and searches
+// then keep less of the CU waiting.  (12000 bf16 rows, top logits / loss with labels, us: of
+// 3500 classes 256 threads 43 / 59, 512 78 / 119; of 6000 59 / 72 and 85 / 101; of 9001 86 / 113 and
+// 94 / 157.  Few rows do not gain from more: 256 rows of 32000 logits 11.1 us with 512 threads, 11.6 with
+// 1024.)  Packed bf16 pairs go to 128 values in rows of up to PACKED; what no
+// registers hold is read by every pass.
+// FEW: 256 threads have maxima enough for the threshold, k <= 128 of them (of
+// more, the k-th largest would let too many logits pass).
+template <typename TI, int PACKED, bool FEW, typename F> static void by_length(int32_t K, F f) {
   constexpr int V = Wide<TI>::n;
-  typedef std::integral_constant<int, 512> T5;
-  typedef std::integral_constant<int, 1024> T10;
-#define NVEC(n) std::integral_constant<int, n>{}
-  if (K <= SHORT) return f(T5{}, NVEC(1), NVEC(8));
-  if (K <= 16 * 512) return f(T5{}, NVEC(V), NVEC(16 / V));
-  if (K <= 32 * 512) return f(T5{}, NVEC(V), NVEC(32 / V));
-  if (K <= 64 * 512) return f(T5{}, NVEC(V), NVEC(64 / V));
-  if (K <= 64 * 1024) return f(T10{}, NVEC(V), NVEC(64 / V));
+#define INT(n) std::integral_constant<int, n>{}
+  if constexpr (FEW) {
+    if (K <= 8 * 256) return f(INT(256), INT(1), INT(8));
+    if (K <= 16 * 256) return f(INT(256), INT(V), INT(16 / V));
+    if (K <= 32 * 256) return f(INT(256), INT(V), INT(32 / V));
+    if (K <= 64 * 256) return f(INT(256), INT(V), INT(64 / V));
+  } else {
+    if (K <= 8 * 512) return f(INT(512), INT(1), INT(8));
+    if (K <= 32 * 512) return f(INT(512), INT(V), INT(32 / V));
+  }
+  if (K <= 64 * 512) return f(INT(512), INT(V), INT(64 / V));
+  if (K <= 64 * 1024) return f(INT(1024), INT(V), INT(64 / V));
   if constexpr (sizeof(TI) == 2 && PACKED > 64 * 1024)
-    if (K <= PACKED) return f(T10{}, NVEC(V), NVEC(128 / V));
-  f(T10{}, NVEC(V), NVEC(0));
-#undef NVEC
+    if (K <= PACKED) return f(INT(1024), INT(V), INT(128 / V));
+  f(INT(1024), INT(V), INT(0));
+#undef INT
 }
 
 template <typename TI>
 int topk_rows(const TI* logits, int64_t ld, int64_t M, int32_t K, int32_t k, float temperature, float* top,
               int32_t* idx, float* rest, hipStream_t stream) {
   const TopkP p{ld, K, k, LOG2E_F / temperature, top, rest, idx};
-  by_length<TI, 0>(K, [&](auto t, auto v, auto nv) {
+  auto launch = [&](auto t, auto v, auto nv) {
     constexpr int T = decltype(t)::value, V = decltype(v)::value, NV = decltype(nv)::value;
     if constexpr (NV > 0)
       BLSTM_LAUNCH("softmax_topk_rows", (topk_rows_kernel<TI, T, V, NV>), dim3((unsigned)M), dim3(T), 0, stream, logits, p);
     else
       BLSTM_LAUNCH("softmax_topk_rows", (topk_long_kernel<TI, T>), dim3((unsigned)M), dim3(T), 0, stream, logits, p);
-  });
+  };
+  if (k <= 128) by_length<TI, 0, true>(K, launch);
+  else by_length<TI, 0, false>(K, launch);
   return blstm_check_launch("softmax_topk_rows");
 }
 template int topk_rows<float>(const float*, int64_t, int64_t, int32_t, int32_t, float, float*, int32_t*, float*, hipStream_t);
@@ -809,7 +817,7 @@ int distill_rows(const TI* logits, int64_t ld, int64_t M, int32_t K, const softm
   p.labels = t->hard != 0.f ? t->labels : nullptr;
   p.row_loss = row_loss; p.K = K; p.k = t->k; p.pad = pad;
   p.it2 = LOG2E_F / t->temperature; p.tau = t->temperature; p.soft = t->soft; p.hard = t->hard; p.scale = loss_scale;
-  by_length<TI, 128 * 1024>(K, [&](auto tt, auto v, auto nv) {
+  by_length<TI, 128 * 1024, true>(K, [&](auto tt, auto v, auto nv) {
     constexpr int T = decltype(tt)::value, V = decltype(v)::value, NV = decltype(nv)::value;
     const size_t bits = (size_t)(NV ? NV * V * T : rup(K, 32)) / 8;
 #define DISTILL(HARD)                                                                                                  \
