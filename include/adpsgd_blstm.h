@@ -200,7 +200,8 @@ int adpsgd_step(float* theta, float* theta_peer, const float* const* grads, int3
  * float32, the scan's state is float32, sums and states are float32 inside.
  *   D channels in G groups of D/G adjacent ones, N states per channel
  *   (1..64), W convolution taps (1..8), T frames, B sequences; T*B at most
- *   2^24.
+ *   2^24, D at most 2^20, and no more of them together than a launch has
+ *   threads for (about 2^32 / 64 sequences of 64 channels; EUNSUPPORTED).
  *   lens (NULL, or B int32 on the device): frames t >= lens[b] do not belong
  *   to sequence b (values outside 0..T count as the nearer end).  Their inputs
  *   are not read, outputs and gradients there are zero, and the state
