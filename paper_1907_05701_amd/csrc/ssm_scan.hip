@@ -232,7 +232,8 @@ static int lanes_of(int N, int ns) {
 static size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
 
 struct ScanPlan {
-  int ns, lpc, np, tpg, nseg, segt;   // ns: states of a lane
+  int ns, lpc, np, tpg, nseg, segt;   // ns: states of a lane (forward)
+  int bns, blpc;                      // of the backward, ns * lpc alike
   int64_t blocks;   // of one stretch
   // bytes; the stretches' ends, starts and sums lie first in either scratch,
   // then the backward's bc, dA, par
@@ -261,6 +262,11 @@ static int scan_plan(const ssm_dims* d, ScanPlan* o) {
     o->lpc = lanes_of(d->N, 4);
   }
   o->np = o->ns * o->lpc;
+  // The backward always: three waves a SIMD have room for half the states, two for all of
+  // them (us, backward of 128 rows of 21 frames, 1024 channels, 16 states: 8 states 58, 4
+  // states 55; 512 of 21, 512 channels 111, 102; 64 of 200, 640 channels, 12 states, fp32 151, 141).
+  o->bns = d->N <= 16 ? 4 : 8;
+  o->blpc = o->np / o->bns;
   o->segt = (int)(cdiv(tiles, want) * TS);
   o->nseg = (int)cdiv(d->T, o->segt);
   o->saved = (size_t)cdiv(d->T, TS) * d->B * d->D * o->np * 4;
@@ -271,7 +277,7 @@ static int scan_plan(const ssm_dims* d, ScanPlan* o) {
   o->dA = up256((size_t)o->nseg * d->B * d->D * d->N * 4);
   o->par = up256((size_t)o->nseg * d->B * 2 * d->D * 4);
   o->bwd = o->fwd + o->bc + o->dA + o->par;
-  if (o->blocks * o->nseg * SCAN_CT * o->lpc > LAUNCH_THREADS)
+  if (o->blocks * o->nseg * SCAN_CT * o->blpc > LAUNCH_THREADS)
     return blstm_fail(BLSTM_EUNSUPPORTED, "ssm_scan: B*D too large");
   // a thread of ssm_scan_sum for each element of dB and dC, and 16 for a column of dA
   if (2 * (int64_t)d->T * d->B * d->G * d->N + 16 * (int64_t)d->D * (d->N + 2) + 512 > LAUNCH_THREADS)
@@ -319,8 +325,9 @@ static bool near(const ssm_dims* d, std::initializer_list<int64_t> lds) {
 
 static void scan_launch(ScanPass pass, const ssm_dims* d, const ScanPlan& pl, const ScanP& p, int mode, hipStream_t s) {
   const int stretches = pass == SCAN_ENDS || pass == SCAN_ADJ ? pl.nseg - 1 : pl.nseg;
-  (pl.ns == 4 ? scan_launch_ns4 : scan_launch_ns8)(pass, p, pl.lpc, d->precision, mode,
-                                                  (unsigned)(pl.blocks * stretches), s);
+  const bool back = pass == SCAN_ADJ || pass == SCAN_BWD;
+  ((back ? pl.bns : pl.ns) == 4 ? scan_launch_ns4 : scan_launch_ns8)(pass, p, back ? pl.blpc : pl.lpc, d->precision, mode,
+                                                                    (unsigned)(pl.blocks * stretches), s);
 }
 static void scan_stretches(const ScanPlan& pl, char* ws, ScanP* p) {
   p->nseg = pl.nseg;

@@ -20,11 +20,11 @@
 // multiply-adds and a product a state and frame forward, three times that
 // backward), so what is beside the states is kept small.  Measured with 1024
 // channels, 16 states, gates, bf16 (us; in brackets the share of it that the vector unit issues):
-//   128 rows of 21 frames       forward 23 (0.54), backward 58 (0.67)
+//   128 rows of 21 frames       forward 23 (0.54), backward 55
 //   one row of 6000             ends 26 (0.75), forward 35 (0.71)
-//   four padded rows of 1500    ends 26, forward 39 (0.42), adjoint ends 25, backward 83 (0.56)
+//   four padded rows of 1500    ends 26, forward 39 (0.42), adjoint ends 23, backward 80
 // The rest is waiting for a tile's first loads and at its barriers, with four
-// (backward: two) waves a SIMD.
+// (backward: three) waves a SIMD.
 #include <math.h>
 
 #include <cmath>
@@ -390,8 +390,8 @@ __device__ __forceinline__ float join2(float a, float b) {
 // saved one into registers (TS + 1 of them) and then runs the adjoint from
 // its last frame to its first.  dB and dC are sums over channels: a wave adds
 // its channels by swaps between rows of lanes, the workgroup's waves meet in
-// LDS, the tiles of a group in a second launch.  Two waves a SIMD: the states of a tile are
-// 72 registers, and bounds of three and four waves spill them and run slower.
+// LDS, the tiles of a group in a second launch.  Three waves a SIMD with four
+// states a lane (36 registers for those of a tile), two with eight: tighter bounds spill and run slower.
 template <typename T, int LPC, int MODE>
 __global__ __launch_bounds__(Tile<LPC>::NT, LPC == 2 || LPC == 4 ? 2 : 1) void ssm_scan_bwd_kernel(const ScanP p) {
   __shared__ __attribute__((aligned(16))) float sB[2][TS][Tile<LPC>::NP], sC[2][TS][Tile<LPC>::NP];
@@ -551,12 +551,21 @@ __global__ __launch_bounds__(Tile<LPC>::NT, LPC == 2 || LPC == 4 ? 2 : 1) void s
   }
 }
 
-// LAUNCH(type, lanes, mode); four states a lane go with up to four lanes
-#define SCAN_BY_LANES(T, M, LAUNCH)                                  \
-  if (lpc == 1) { LAUNCH(T, 1, M); }                                 \
-  else if (lpc == 2) { LAUNCH(T, 2, M); }                            \
-  else if (NS == 4 || lpc == 4) { LAUNCH(T, 4, M); }                 \
-  else if constexpr (NS == 8) { LAUNCH(T, 8, M); }
+// LAUNCH(type, lanes, mode); four states a lane go with up to four lanes, eight
+// states a lane in the backward with four and more
+template <int NUM> struct Lanes { static constexpr int value = NUM; };
+template <bool BACK, typename F> static void by_lanes(int lpc, F f) {
+  if constexpr (NS == 4 || !BACK) {
+    if (lpc == 1) return f(Lanes<1>{});
+    if (lpc == 2) return f(Lanes<2>{});
+  }
+  if constexpr (NS == 8) {
+    if (lpc == 8) return f(Lanes<8>{});
+  }
+  f(Lanes<4>{});
+}
+#define SCAN_BY_LANES(T, M, LAUNCH) \
+  by_lanes<BACK>(lpc, [&](auto lanes) { LAUNCH(T, decltype(lanes)::value, M); });
 #define SCAN_BY_MODE(T, LAUNCH)                        \
   if (mode == FAR) { SCAN_BY_LANES(T, FAR, LAUNCH) }   \
   else if (mode == PLAIN) { SCAN_BY_LANES(T, PLAIN, LAUNCH) } \
@@ -572,9 +581,14 @@ static void launch(ScanPass pass, const ScanP& p, int lpc, int precision, int mo
   BLSTM_LAUNCH("ssm_scan_ends", (ssm_scan_fwd_kernel<T, L, M, true>), dim3(blocks), dim3(Tile<L>::NT), 0, s, p)
 #define ADJ(T, L, M) BLSTM_LAUNCH("ssm_scan_adj", (ssm_scan_adj_kernel<T, L, M>), dim3(blocks), dim3(Tile<L>::NT), 0, s, p)
 #define BWD(T, L, M) BLSTM_LAUNCH("ssm_scan_bwd", (ssm_scan_bwd_kernel<T, L, M>), dim3(blocks), dim3(Tile<L>::NT), 0, s, p)
-  if (pass == SCAN_FWD) { SCAN_DISPATCH(FWD) }
-  else if (pass == SCAN_ENDS) { SCAN_DISPATCH(ENDS) }
-  else if (pass == SCAN_ADJ) { SCAN_DISPATCH(ADJ) }
-  else { SCAN_DISPATCH(BWD) }
+  if (pass == SCAN_FWD || pass == SCAN_ENDS) {
+    constexpr bool BACK = false;
+    if (pass == SCAN_FWD) { SCAN_DISPATCH(FWD) }
+    else { SCAN_DISPATCH(ENDS) }
+  } else {
+    constexpr bool BACK = true;
+    if (pass == SCAN_ADJ) { SCAN_DISPATCH(ADJ) }
+    else { SCAN_DISPATCH(BWD) }
+  }
 }
 }  // namespace SCAN_NAMESPACE
