@@ -20,9 +20,9 @@
 // multiply-adds and a product a state and frame forward, three times that
 // backward), so what is beside the states is kept small.  Measured with 1024
 // channels, 16 states, gates, bf16 (us; in brackets the share of it that the vector unit issues):
-//   128 rows of 21 frames       forward 23 (0.54), backward 55
+//   128 rows of 21 frames       forward 23 (0.54), backward 55 (0.80)
 //   one row of 6000             ends 26 (0.75), forward 35 (0.71)
-//   four padded rows of 1500    ends 26, forward 39 (0.42), adjoint ends 23, backward 80
+//   four padded rows of 1500    ends 26, forward 39 (0.42), adjoint ends 22, backward 79 (0.68)
 // The rest is waiting for a tile's first loads and at its barriers, with four
 // (backward: three) waves a SIMD.
 #include <math.h>
