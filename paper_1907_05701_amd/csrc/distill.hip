@@ -5,7 +5,8 @@
 // sums are float32 in a fixed order.  Memory bounds both: 2688 bf16 rows of 32000
 // logits, the top 32 in 49 us (172 MB, 3.5 TB/s; the vector unit issues 36 us of it,
 // and a row's search, candidates and ranks are barriers that only other rows hide), loss and gradients
-// with labels in 76 us (344 MB, 4.5 TB/s).
+// with labels in 77 us (344 MB, 4.5 TB/s).
+#include <float.h>
 #include <math.h>
 
 #include <cmath>
@@ -510,7 +511,10 @@ __global__ __launch_bounds__(T, (waves_of<TI, T, V, NV>())) void topk_rows_kerne
 //   KL = sum p (log p - log q) + r (log r - log(Zr / Z)),  q = e^u / Z
 //   d(tau^2 KL)/ds = tau (q - p) where listed, tau e^u (1/Z - r/Zr) elsewhere
 // The others' sum has a maximum of its own, so that it does not vanish
-// beside listed logits however large they are.
+// beside listed logits however large they are.  Every exponent is a difference of logits,
+// scaled: a mask of -1e9 or of the type's lowest value times log2 e / tau would overflow, or
+// carry a rounding of its own size into the exponential.  What differences cost (KL = sum p
+// (log p + log z - (s - max) / tau)) stays unscaled up to the loss for the same reason.
 // ---------------------------------------------------------------------------
 struct DistillP {
   int64_t ld, ldd;
@@ -626,7 +630,7 @@ template <typename TI, typename TO, int T, int V> struct Others<TI, TO, T, V, 0>
 
 // HARD: how the labels' cross-entropy has e^s of the others, NO: no labels, OWN: an
 // exponential of its own, POW1, POW2: from e^u, its first or second power.
-// (Temperatures of 1 and 2.  2688 bf16 rows of 32000: NO 70, POW1 78, POW2 84, OWN 86 us: half the
+// (Temperatures of 1 and 2.  2688 bf16 rows of 32000: NO 72, POW1 77, POW2 78, OWN 90 us: half the
 // exponentials of OWN, which the vector unit shares with the rounding and the moves.)
 enum { NO, OWN, POW1, POW2 };
 template <typename TI, typename TO, int T, int V, int NV, int HARD>
@@ -650,29 +654,33 @@ __global__ __launch_bounds__(T, (waves_of<TI, T, V, NV>())) void distill_rows_ke
   for (int i = tid; i < words; i += T) listed[i] = 0;
   if (tid == 0) l.dup = 0;
   int at = -1;
-  float t2 = -INFINITY, sv = -INFINITY;   // the entry's teacher logit (times log2 e / tau), student logit
+  float tv = -INFINITY, sv = -INFINITY;   // the entry's teacher logit, student logit
   if (tid < p.k) {
     at = p.idx[m * p.k + tid];
     if (at < 0 || at >= K) at = -1;
     else {
-      t2 = p.top[m * p.k + tid] * p.it2;
+      tv = p.top[m * p.k + tid];
       sv = to_f32(s[at]);
     }
     l.iv[tid] = at;
   }
-  const float r2 = p.rest ? p.rest[m] * LOG2E_F : -INFINITY;
+  const float rest = p.rest ? p.rest[m] : -INFINITY;   // log of the rest: a logit over tau
   const int lab = HARD ? p.labels[m] : -1;
   const bool marked = HARD && lab >= 0 && lab < K;
   const float sl = marked ? to_f32(s[lab]) : 0.f;
   __syncthreads();
   if (at >= 0 && (atomicOr(&listed[at >> 5], 1u << (at & 31)) & (1u << (at & 31)))) l.dup = 1;
-  put_wave(l.buf[0], wave_max(t2));
+  put_wave(l.buf[0], wave_max(tv));
   put_wave(l.buf[1], wave_max(sv));
   __syncthreads();
-  // the teacher's probabilities (base-2 exponents throughout)
-  const float tm = fmaxf(all_max<T>(l.buf[0]), r2), lm = all_max<T>(l.buf[1]);
+  // the teacher's probabilities; lt: log2 of the entry's, lr: of the rest's, but for the sum
+  const float tmax = all_max<T>(l.buf[0]), lm = all_max<T>(l.buf[1]);
+  const float tbase = tmax == -INFINITY ? 0.f : tmax;   // of the listed ones; over tau, as far as float32 goes:
+  const float ta = fabsf(tmax) < INFINITY ? fminf(fmaxf(tmax / p.tau, -FLT_MAX), FLT_MAX) : tmax;
+  const float tm = fmaxf(ta, rest);
   const bool taught = p.soft != 0.f && !(tm == -INFINITY);   // an unwanted loss may be infinite
-  const float e = taught ? exp2_(t2 - tm) : 0.f, er = taught ? exp2_(r2 - tm) : 0.f;
+  const float lt = (tv - tbase) * p.it2 + (ta - tm) * LOG2E_F, lr = (rest - tm) * LOG2E_F;
+  const float e = taught ? exp2_(lt) : 0.f, er = taught ? exp2_(lr) : 0.f;
   if (tid < p.k) l.pv[tid] = e;
   put_wave(l.buf[2], wave_sum(e));
   row.mask(listed, K);
@@ -680,9 +688,9 @@ __global__ __launch_bounds__(T, (waves_of<TI, T, V, NV>())) void distill_rows_ke
   row.others(s, K, listed, [&](float v) { rm = fmaxf(rm, v); });
   put_wave(l.buf[3], wave_max(rm));
   __syncthreads();
-  const float tz = all_sum<T>(l.buf[2]) + er, l2tz = taught ? tm + log2f(tz) : 0.f;
+  const float tz = all_sum<T>(l.buf[2]) + er, l2tz = taught ? log2f(tz) : 0.f;
   const float prob = taught ? e / tz : 0.f, r = taught ? er / tz : 0.f;
-  float lp = t2 - l2tz;     // log2 of the entry's probability
+  float lp = lt - l2tz;     // log2 of the entry's probability
   float own = prob;         // of its class
   bool lead = at >= 0;      // the class's first entry
   if (l.dup && at >= 0) {   // (the sums below are zeros where the row is not taught)
@@ -695,27 +703,23 @@ __global__ __launch_bounds__(T, (waves_of<TI, T, V, NV>())) void distill_rows_ke
     own = taught ? own / tz : 0.f;
     lp = log2f(own);
   }
-  // maxima: the others' (as an exponent), the row's
+  // maxima: the others', the row's; from where their exponents count
   rm = all_max<T>(l.buf[3]);
-  const float am = fmaxf(rm, lm), aref = am == -INFINITY ? 0.f : am;
-  const float rref = rm == -INFINITY ? 0.f : rm * p.it2, um = aref * p.it2;
-  const float eo = rm == -INFINITY ? 0.f : exp2_(rref - um);   // the others' sums, from the row's maximum
-  const float h2 = -aref * LOG2E_F;
+  const float am = fmaxf(rm, lm), aref = am == -INFINITY ? 0.f : am, rref = rm == -INFINITY ? 0.f : rm;
+  const float eo = exp2_((rm - aref) * p.it2);   // the others' sums, from the row's maximum
   float zr = 0.f, z1 = 0.f;
   row.others(s, K, listed, [&](float v) {
-    const float x = exp2_(v * p.it2 - rref);
+    const float y = v - rref, x = exp2_(y * p.it2);
     zr += x;
-    if constexpr (HARD == OWN) z1 += exp2_(v * LOG2E_F + h2);
+    if constexpr (HARD == OWN) z1 += exp2_(y * LOG2E_F);
     if constexpr (HARD == POW2) z1 += x * x;
     // or the compiler would sink this sum past the loop, and carry every exponential there
     if constexpr (HARD == OWN || HARD == POW2) asm volatile("" : "+v"(z1));
   });
-  const float eh = HARD < POW1 || rm == -INFINITY ? 0.f : exp2_(rm * LOG2E_F + h2);   // as eo, of e^s
-  if constexpr (HARD == POW1) z1 = zr * eh;
-  if constexpr (HARD == POW2) z1 *= eh;
-  const float u = sv * p.it2;
-  const float ez = lead ? exp2_(u - um) : 0.f;
-  if (HARD && lead) z1 += exp2_(sv * LOG2E_F + h2);
+  const float eh = HARD ? exp2_((rm - aref) * LOG2E_F) : 0.f;   // as eo, of e^s
+  z1 = (HARD == POW1 ? zr : z1) * eh;
+  const float ez = lead ? exp2_((sv - aref) * p.it2) : 0.f;
+  if (HARD && lead) z1 += exp2_((sv - aref) * LOG2E_F);
   put_wave(l.buf[4], wave_sum(zr));
   put_wave(l.buf[5], wave_sum(ez));
   if constexpr (HARD) put_wave(l.buf[6], wave_sum(z1));
@@ -724,14 +728,15 @@ __global__ __launch_bounds__(T, (waves_of<TI, T, V, NV>())) void distill_rows_ke
   const float z = all_sum<T>(l.buf[5]) + zr * eo;
   if constexpr (HARD) z1 = all_sum<T>(l.buf[6]);
   const float l2z = log2f(z);
-  put_wave(l.buf[7], wave_sum(at >= 0 && prob > 0.f ? prob * (lp - (u - um - l2z)) : 0.f));
+  const float tln = p.tau * LN2_F;
+  put_wave(l.buf[7], wave_sum(at >= 0 && prob > 0.f ? prob * ((lp + l2z) * tln + (aref - sv)) : 0.f));   // tau KL
   const float ks = taught ? p.scale * weight * p.soft * p.tau : 0.f, kh = marked ? p.scale * weight * p.hard : 0.f;
-  const float cr = ks * (eo / z - (r > 0.f && zr > 0.f ? r / zr : 0.f));   // of e^(u - rref) in the others
+  const float cr = ks * (eo / z - (r > 0.f && zr > 0.f ? r / zr : 0.f));   // of x in the others
   const float ch = marked ? kh / z1 : 0.f;
-  const float cp = HARD == POW1 ? cr + ch * eh : ch * eh;
+  const float cp = HARD == POW1 ? cr + ch * eh : ch * eh;   // of x at POW1, of the exponential of its own or x^2
   row.write(s, d, K, listed, [&](float v) {
-    const float x = exp2_(v * p.it2 - rref);
-    if constexpr (HARD == OWN) return cr * x + ch * exp2_(v * LOG2E_F + h2);
+    const float y = v - rref, x = exp2_(y * p.it2);
+    if constexpr (HARD == OWN) return cr * x + cp * exp2_(y * LOG2E_F);
     else if constexpr (HARD == POW1) return cp * x;
     else if constexpr (HARD == POW2) return (cr + cp * x) * x;
     else return cr * x;
@@ -740,21 +745,21 @@ __global__ __launch_bounds__(T, (waves_of<TI, T, V, NV>())) void distill_rows_ke
   if (lead) {
     float g = ks * (ez / z - own);
     if constexpr (HARD) {
-      g += ch * exp2_(sv * LOG2E_F + h2);
+      g += ch * exp2_((sv - aref) * LOG2E_F);
       if (at == lab) g -= kh;
     }
     d[at] = from_f32<TO>(g);
   }
   if (tid != 0) return;
   if (marked && !((listed[lab >> 5] >> (lab & 31)) & 1u))
-    d[lab] = from_f32<TO>(cr * exp2_(sl * p.it2 - rref) + ch * exp2_(sl * LOG2E_F + h2) - kh);
+    d[lab] = from_f32<TO>(cr * exp2_((sl - rref) * p.it2) + ch * exp2_((sl - aref) * LOG2E_F) - kh);
   float loss = 0.f;
   if (taught) {
     float kl = all_sum<T>(l.buf[7]);
-    if (r > 0.f) kl += r * (r2 - l2tz - (log2f(zr) + rref - um - l2z));
-    loss = p.soft * p.tau * p.tau * kl * LN2_F;
+    if (r > 0.f) kl += r * ((lr - l2tz - log2f(zr) + l2z) * tln + (aref - rm));
+    loss = p.soft * p.tau * kl;
   }
-  if (marked) loss += p.hard * (aref + log2f(z1) * LN2_F - sl);
+  if (marked) loss += p.hard * ((aref - sl) + log2f(z1) * LN2_F);
   p.row_loss[m] = weight * loss;
 }
 

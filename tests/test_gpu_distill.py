@@ -291,6 +291,76 @@ def test_a_teacher_that_is_the_student(gpu_lib):
     assert bool((d.abs() <= 2 * TOL * torch.softmax(s / 2, 1)).all())
 
 
+def closed_row(s, top, idx, rest, label, tau, soft, hard):
+    """Loss and gradient of a row of distinct classes in float64, from differences
+    alone.  (Autograd of logsumexp forms exp(x - (max + log n)), and beside a max of 3.4e38 log n
+    is lost in 64 bits, too: n equal classes would weigh 1 each.)"""
+    u = (s - s.max()) / tau
+    lz = u.exp().sum().log()
+    other = torch.ones_like(s, dtype=torch.bool)
+    other[idx] = False
+    mo = u[other].max()
+    w = (u[other] - mo).exp()
+    p = torch.softmax(torch.cat((top / tau, rest.view(1))), 0)
+    kl = (p[:-1] * (p[:-1].log() - u[idx] + lz)).sum() + p[-1] * (p[-1].log() - mo - w.sum().log() + lz)
+    d = (u - lz).exp()
+    d[idx] -= p[:-1]
+    d[other] -= p[-1] * w / w.sum()
+    loss, d = soft * tau * tau * kl, soft * tau * d
+    if label >= 0 and hard:
+        v = s - s.max()
+        lse = v.exp().sum().log()
+        loss = loss + hard * (lse - v[label])
+        d += hard * (v - lse).exp()
+        d[label] -= hard
+    return loss, d
+
+
+MASKS = {"lowest": None, "-1e9": -1e9, "-1e4": -1e4, "1e9": 1e9}
+
+
+@pytest.mark.parametrize("precision,K", [("fp32", 300), ("bf16", 300), ("bf16", 33001), ("fp32", 65540), ("bf16", 131080)])
+@pytest.mark.parametrize("tau", [0.5, 1.0, 2.0, 3.0])
+@pytest.mark.parametrize("mask", MASKS)
+def test_distill_where_a_mask_leaves_nothing(gpu_lib, mask, tau, precision, K):
+    """Every class that is not listed at the mask's value, and the whole row at it,
+    with and without labels; rows that registers hold and rows that none do.
+    Equal logits are equal probabilities however large they are: the bounds are the others'.
+    A row a call: the loss of one (up to 1e38) is no measure for another."""
+    s, top, idx, rest, lab = make_rows(2, K, 4, precision, 41)
+    m = torch.finfo(s.dtype).min if MASKS[mask] is None else MASKS[mask]
+    keep = s[0, idx[0].long()].clone()
+    rest[0] = -1.0   # a small share, so that what it costs is below float32's largest
+    s[:] = m
+    s[0, idx[0].long()] = keep
+    lab[0] = idx[0, 1]
+    from paper_1907_05701_amd import binding as bd
+    for i in (0, 1):
+        gs, *t = (v[i:i + 1].cuda() for v in (s, top, idx, rest))
+        for labels, soft, hard in ((lab, 0.5, 0.5), (None, 1.0, 0.0)):
+            loss, d = torch.full((1,), 99.0, device="cuda"), torch.full_like(gs, 99.0)
+            bd.softmax_distill_rows(gs, t[0], t[1], loss, d, rest=t[2], temperature=tau, soft=soft, hard=hard,
+                                    labels=None if labels is None else labels[i:i + 1].cuda())
+            wl, wd = closed_row(s[i].double(), top[i].double(), idx[i].long(), rest[i].double(), int(lab[i]), tau, soft, hard)
+            far = {"loss": om.far(loss[0], wl, TOL * soft * tau * tau + TOL), "dlogits": om.far(d[0], wd, TOL)}
+            print("[mask]", i, {k: f"{v:.2f}" for k, v in far.items()}, flush=True)
+            assert max(far.values()) <= 1.0, (i, far)
+
+
+@pytest.mark.parametrize("tau", [0.5, 1.0, 2.0])
+def test_a_teacher_of_lowest_values(gpu_lib, tau):
+    """Listed logits at float32's lowest value: equal among themselves, nothing beside an ordinary one or a rest."""
+    s, top, idx, rest, lab = make_rows(5, 200, 4, "fp32", 43)
+    low = torch.finfo(torch.float32).min
+    top[0], rest[0] = low, -math.inf
+    top[1] = low
+    top[2, 1:], rest[2] = low, -math.inf
+    rest[3] = low
+    top[4], rest[4] = 1e9, -math.inf
+    check_distill(s, top, idx, rest, lab, tau=tau, soft=0.5, hard=0.5)
+    check_distill(s, top, idx, rest, None, tau=tau)
+
+
 # ------------------------------------------------------------------ the head ---
 def head_case(precision, M, H, P, K, k, seed=0):
     from paper_1907_05701_amd.step import LearnerStep
