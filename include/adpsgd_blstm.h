@@ -317,7 +317,9 @@ int softmax_topk_rows(const void* logits, int64_t ld, int64_t M, int32_t K, int3
  * bucket; the hard loss is the cross-entropy of softmax(logits) with labels:
  *   row_loss = weight (soft temperature^2 KL + hard CE)
  * An entry whose idx is outside 0..K-1 is absent; a class listed twice has
- * both probabilities; a row without entries and rest has no soft loss.
+ * both probabilities; a row without entries and rest has no soft loss; one whose
+ * entries or rest hold a NaN or +inf has no probabilities, and its loss and gradient
+ * are NaN (unless its weight or soft is 0).
  * labels (NULL: none) outside 0..K-1: the row has no hard loss.
  * weights [M] float32 (NULL: ones): a row of weight 0 has loss and gradient 0
  * whatever it holds (on the head, whose products sum over frames, its y_top

@@ -533,10 +533,13 @@ template <int T> struct DistillLds {
   uint32_t dup;
 };
 
-// Joins a wave's values (0: sum, 1: maximum) into buf; after a barrier all_of adds the waves up.
+// Joins a wave's values into buf; after a barrier all_sum and all_max join the waves'.
+// NAN_MAX: a NaN is the maximum (a teacher's is seen so; a student's is in the sums).
+template <bool NAN_MAX = false> __device__ __forceinline__ float max_of(float a, float b) { return NAN_MAX ? max_nan(a, b) : fmaxf(a, b); }
+template <bool NAN_MAX = false>
 __device__ __forceinline__ float wave_max(float v) {
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
+  for (int o = 32; o > 0; o >>= 1) v = max_of<NAN_MAX>(v, __shfl_xor(v, o));
   return v;
 }
 __device__ __forceinline__ void put_wave(float* buf, float v) {
@@ -549,11 +552,11 @@ __device__ __forceinline__ float all_sum(const float* buf) {
   for (int w = 1; w < T / 64; ++w) t += buf[w];
   return t;
 }
-template <int T>
+template <int T, bool NAN_MAX = false>
 __device__ __forceinline__ float all_max(const float* buf) {
   float t = buf[0];
 #pragma unroll
-  for (int w = 1; w < T / 64; ++w) t = fmaxf(t, buf[w]);
+  for (int w = 1; w < T / 64; ++w) t = max_of<NAN_MAX>(t, buf[w]);
   return t;
 }
 
@@ -670,15 +673,16 @@ __global__ __launch_bounds__(T, (waves_of<TI, T, V, NV>())) void distill_rows_ke
   const float sl = marked ? to_f32(s[lab]) : 0.f;
   __syncthreads();
   if (at >= 0 && (atomicOr(&listed[at >> 5], 1u << (at & 31)) & (1u << (at & 31)))) l.dup = 1;
-  put_wave(l.buf[0], wave_max(tv));
+  put_wave(l.buf[0], wave_max<true>(tv));
   put_wave(l.buf[1], wave_max(sv));
   __syncthreads();
   // the teacher's probabilities; lt: log2 of the entry's, lr: of the rest's, but for the sum
-  const float tmax = all_max<T>(l.buf[0]), lm = all_max<T>(l.buf[1]);
+  const float tmax = all_max<T, true>(l.buf[0]), lm = all_max<T>(l.buf[1]);
   const float tbase = tmax == -INFINITY ? 0.f : tmax;   // of the listed ones; over tau, as far as float32 goes:
   const float ta = fabsf(tmax) < INFINITY ? fminf(fmaxf(tmax / p.tau, -FLT_MAX), FLT_MAX) : tmax;
-  const float tm = fmaxf(ta, rest);
-  const bool taught = p.soft != 0.f && !(tm == -INFINITY);   // an unwanted loss may be infinite
+  const float tm = max_nan(ta, rest);
+  // an unwanted loss may be infinite; a teacher's NaN or +inf makes tz, every probability and r a NaN
+  const bool taught = p.soft != 0.f && !(tm == -INFINITY);
   const float lt = (tv - tbase) * p.it2 + (ta - tm) * LOG2E_F, lr = (rest - tm) * LOG2E_F;
   const float e = taught ? exp2_(lt) : 0.f, er = taught ? exp2_(lr) : 0.f;
   if (tid < p.k) l.pv[tid] = e;
@@ -729,9 +733,9 @@ __global__ __launch_bounds__(T, (waves_of<TI, T, V, NV>())) void distill_rows_ke
   if constexpr (HARD) z1 = all_sum<T>(l.buf[6]);
   const float l2z = log2f(z);
   const float tln = p.tau * LN2_F;
-  put_wave(l.buf[7], wave_sum(at >= 0 && prob > 0.f ? prob * ((lp + l2z) * tln + (aref - sv)) : 0.f));   // tau KL
+  put_wave(l.buf[7], wave_sum(at >= 0 && prob != 0.f ? prob * ((lp + l2z) * tln + (aref - sv)) : 0.f));   // tau KL
   const float ks = taught ? p.scale * weight * p.soft * p.tau : 0.f, kh = marked ? p.scale * weight * p.hard : 0.f;
-  const float cr = ks * (eo / z - (r > 0.f && zr > 0.f ? r / zr : 0.f));   // of x in the others
+  const float cr = ks * (eo / z - (r == 0.f || (r > 0.f && zr == 0.f) ? 0.f : r / zr));   // of x in the others
   const float ch = marked ? kh / z1 : 0.f;
   const float cp = HARD == POW1 ? cr + ch * eh : ch * eh;   // of x at POW1, of the exponential of its own or x^2
   row.write(s, d, K, listed, [&](float v) {
@@ -756,7 +760,7 @@ __global__ __launch_bounds__(T, (waves_of<TI, T, V, NV>())) void distill_rows_ke
   float loss = 0.f;
   if (taught) {
     float kl = all_sum<T>(l.buf[7]);
-    if (r > 0.f) kl += r * ((lr - l2tz - log2f(zr) + l2z) * tln + (aref - rm));
+    if (r != 0.f) kl += r * ((lr - l2tz - log2f(zr) + l2z) * tln + (aref - rm));
     loss = p.soft * p.tau * kl;
   }
   if (marked) loss += p.hard * ((aref - sl) + log2f(z1) * LN2_F);

@@ -361,6 +361,38 @@ def test_a_teacher_of_lowest_values(gpu_lib, tau):
     check_distill(s, top, idx, rest, None, tau=tau)
 
 
+@pytest.mark.parametrize("precision", ["fp32", "bf16"])
+@pytest.mark.parametrize("tau", [1.0, 2.0, 3.0])
+def test_a_teacher_that_has_diverged_is_seen(gpu_lib, tau, precision):
+    """A NaN or +inf among the listed logits or as the rest: no probabilities, so
+    the loss and every gradient of the row are NaN, with labels, too.  Not where the
+    entry is absent, the row weighs nothing or the soft loss is not wanted."""
+    from paper_1907_05701_amd import binding as bd
+    s, top, idx, rest, lab = make_rows(9, 500, 4, precision, 44)
+    top[0, 2] = math.nan
+    top[1] = math.nan
+    top[2], rest[2] = math.nan, -math.inf
+    top[3, 0] = math.inf
+    rest[4] = math.nan
+    rest[5] = math.inf
+    idx[5, 1] = idx[5, 0]
+    top[6, 3], idx[6, 3] = math.nan, -1
+    top[7] = math.nan
+    w = torch.ones(9)
+    w[7] = 0
+    bad = torch.tensor([True] * 6 + [False] * 3)
+    s, top, idx, rest, lab, w = (v.cuda() for v in (s, top, idx, rest, lab, w))
+    for labels, soft, hard in ((None, 1.0, 0.0), (lab, 0.5, 0.5)):
+        loss, d = torch.zeros(9, device="cuda"), torch.zeros_like(s)
+        bd.softmax_distill_rows(s, top, idx, loss, d, rest=rest, labels=labels, weights=w, temperature=tau, soft=soft,
+                                hard=hard)
+        assert torch.equal(torch.isnan(loss).cpu(), bad), loss
+        n = torch.isnan(d).sum(1).cpu()
+        assert bool((n[bad] == 500).all()) and bool((n[~bad] == 0).all()), n
+        assert float(loss[7]) == 0 and not bool(d[7].any())
+    check_distill(s.cpu(), top.cpu(), idx.cpu(), rest.cpu(), lab.cpu(), w.cpu(), tau=tau, soft=0.0, hard=1.0)
+
+
 # ------------------------------------------------------------------ the head ---
 def head_case(precision, M, H, P, K, k, seed=0):
     from paper_1907_05701_amd.step import LearnerStep
