@@ -258,7 +258,9 @@ int ssm_conv_step(const ssm_dims* dims, const void* x, int64_t ldx, const float*
  *   h_t[n] = exp(s_t A[d][n]) h_{t-1}[n] + s_t x_t B_t[g][n],   h_{-1} = h0 or 0
  *   o_t = sum_n C_t[g][n] h_t[n] + Dskip[d] x_t
  *   y_t = o_t silu(z_t)   (z given), else o_t
- * x, dt, z [T][B][D]; Bm, Cm [T][B][G*N]; A [D][N], finite; Dskip, dt_bias [D];
+ * x, dt, z [T][B][D]; Bm, Cm [T][B][G*N]; A [D][N], finite, and exp(s_t A) of any one
+ * frame within float32 (s_t A below 88: past it 0 * inf makes NaN of a zero state);
+ * Dskip, dt_bias [D];
  * h0 [B][D][N].  z, Dskip, dt_bias, h0 and lens may be NULL. */
 typedef struct ssm_scan_in {
   const void *x, *dt, *Bm, *Cm, *z;

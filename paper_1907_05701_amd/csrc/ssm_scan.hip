@@ -8,6 +8,12 @@
 
 #include "ssm_scan.hpp"
 
+// The square root of 2^(2 e), by which a state is multiplied twice: any finite A is allowed, and over
+// a whole stretch the power itself can pass float32's range where its product does not (a state of zero
+// stays zero).  2^254 takes every normal float32 past the largest one, 2^-254 below the least, so
+// exponents beyond are as good as these (a NaN among them is in the stretch's end, too).
+__device__ __forceinline__ float root_decay(float e) { return __builtin_amdgcn_exp2f(__builtin_amdgcn_fmed3f(e, -127.f, 127.f)); }
+
 // The states (REV: adjoints) that reach each stretch, from those that the
 // stretches add.  A thread has four states of a channel and one of 16 runs of
 // adjacent stretches: it joins its run, the runs meet in LDS, and it goes
@@ -31,7 +37,7 @@ __global__ __launch_bounds__(512) void ssm_scan_join_kernel(const float* __restr
   const int part = (int)(e % per);
   const bool on = row < BD;
   States<4> A2 = ld_states<4>(A, row % D, N, part * 4, on);
-  for (int j = 0; j < 4; ++j) A2.v[j] *= LOG2E_F;
+  for (int j = 0; j < 4; ++j) A2.v[j] *= LOG2E_F / 2;
   const int64_t n4 = BD * per;
   const f32x4* in = (const f32x4*)ends + e;
   const int len = (nseg - 1 + RUNS - 1) / RUNS, k0 = run * len, k1 = on ? min(nseg - 1, k0 + len) : 0;
@@ -52,7 +58,10 @@ __global__ __launch_bounds__(512) void ssm_scan_join_kernel(const float* __restr
       const int g = REV ? nseg - 1 - (k + i) : k + i;
       sum += s[i];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) h[j] = __builtin_amdgcn_exp2f(s[i] * A2.v[j]) * h[j] + v[i][j];
+      for (int j = 0; j < 4; ++j) {
+        const float w = root_decay(s[i] * A2.v[j]);
+        h[j] = h[j] * w * w + v[i][j];
+      }
       // a stretch's end, from its start, reaches the next one
       if (write) ((f32x4*)starts)[(REV ? g - 1 : g + 1) * n4 + e] = h;
     }
@@ -72,7 +81,10 @@ __global__ __launch_bounds__(512) void ssm_scan_join_kernel(const float* __restr
   if (run == 0) ((f32x4*)starts)[(REV ? nseg - 1 : 0) * n4 + e] = h;
   for (int r = 0; r < run; ++r) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) h[j] = __builtin_amdgcn_exp2f(ss[r][el] * A2.v[j]) * h[j] + sh[r][el][j];
+    for (int j = 0; j < 4; ++j) {
+      const float w = root_decay(ss[r][el] * A2.v[j]);
+      h[j] = h[j] * w * w + sh[r][el][j];
+    }
   }
   for (int k = k0; k < k1; k += 8) {
     if (len > 8) load(k);

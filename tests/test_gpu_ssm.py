@@ -180,6 +180,42 @@ def test_scan_of_long_sequences(gpu_lib, T, B, D, N):
     check(Case(T, B, D, N, 1, "fp32", lens=([T, T // 2, 0] * B)[:B]))
 
 
+@pytest.mark.parametrize("precision", ["fp32", "bf16"])
+def test_split_scan_of_growing_states_from_silence(gpu_lib, precision):
+    """Decays above one (any finite A is allowed): a state of zero stays zero however
+    much a stretch would multiply it by, and so does an adjoint."""
+    c = Case(300, 1, 64, 16, 1, precision, gate=False, state=False, softplus=False, extras=False)
+    assert c.bd.ssm_workspace_bytes(c.dims)["fwd"] > 0
+    c.act["x"][:298] = 0
+    c.act["dt"][:] = 1
+    c.par["A"] = c.par["A"].abs().clamp(max=1) + 7
+    c.dy[2:] = 0
+    c.dhl[:] = 0
+    c.gpu = {k: rows(v, c.t, False) for k, v in c.act.items()}
+    c.gpar["A"], c.gdy = c.par["A"].float().cuda(), rows(c.dy, c.t, False)
+    c.par["A"] = c.gpar["A"].double().cpu()
+    check(c)
+
+
+def test_split_scan_joins_what_a_stretch_multiplies_past_float32(gpu_lib):
+    """1e-36 times e^96 over one stretch is an ordinary number, e^96 alone is none.
+    The exponent, 139 in base 2, has three roundings (log2 e, its product with A, that with the sum):
+    3 * 139 ln 2 = 289 half-steps of the result, within the 40 + 16 T = 1960 of tol."""
+    c = Case(120, 1, 64, 16, 1, "fp32", gate=False, softplus=False, extras=False)
+    assert c.bd.ssm_workspace_bytes(c.dims)["fwd"] > 0
+    c.act["x"][:] = 0
+    c.act["dt"][:] = 0
+    c.act["dt"][16:24] = 1
+    c.par["A"][:] = 12
+    c.par["h0"][:] = 1e-36
+    c.gpu = {k: rows(v, c.t, False) for k, v in c.act.items()}
+    c.gpar = {k: v.float().cuda() for k, v in c.par.items()}
+    c.par = {k: v.double().cpu() for k, v in c.gpar.items()}
+    y, h = c.forward()
+    wy, wh, _ = c.model()
+    assert om.far(y, wy, tol(120)) <= 1.0 and om.far(h, wh, tol(120)) <= 1.0
+
+
 def test_a_scan_in_pieces_is_the_whole(gpu_lib):
     """h_last of one call as h0 of the next (in place, too); no saved states."""
     c = Case(48, 2, 64, 16, precision="fp32")
