@@ -201,7 +201,12 @@ int adpsgd_step(float* theta, float* theta_peer, const float* const* grads, int3
  *   D channels in G groups of D/G adjacent ones, N states per channel
  *   (1..64), W convolution taps (1..8), T frames, B sequences; T*B at most
  *   2^24, D at most 2^20, and no more of them together than a launch has
- *   threads for (about 2^32 / 64 sequences of 64 channels; EUNSUPPORTED).
+ *   threads for, 2^32 - 1 (EUNSUPPORTED).  The scan takes 64 a tile of 64
+ *   channels of a group, stretch of a sequence and lane of a channel, with up to
+ *   8 states a lane forward, 4 backward where N <= 16: 2^24 sequences of one tile of
+ *   16 states go forward and not back.  The backward also refuses
+ *   2 T B G N + 16 D (N + 2) above 2^32 - 513.  The convolution and the single
+ *   steps take a thread for 4 channels of 8 frames, 4 channels, and 2 channels' 4 states.
  *   lens (NULL, or B int32 on the device): frames t >= lens[b] do not belong
  *   to sequence b (values outside 0..T count as the nearer end).  Their inputs
  *   are not read, outputs and gradients there are zero, and the state
@@ -223,7 +228,8 @@ enum {
  *   fwd, bwd -- scratch of ssm_scan_fwd and ssm_scan_bwd
  *   conv_bwd -- scratch of ssm_conv_bwd
  * A buffer belongs to one call (or one captured graph) at a time.  Any output
- * pointer may be NULL.  Returns 0 or BLSTM_EINVAL/EUNSUPPORTED. */
+ * pointer may be NULL: a size that is not asked for is not held to its call's
+ * limits.  Returns 0 or BLSTM_EINVAL/EUNSUPPORTED. */
 int ssm_workspace_bytes(const ssm_dims* dims, size_t* saved, size_t* fwd, size_t* bwd, size_t* conv_bwd);
 
 /* pre[t] = bias + sum_j w[j] x[t - W + 1 + j] per channel, y = silu(pre) or pre.

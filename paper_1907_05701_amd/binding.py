@@ -313,19 +313,28 @@ def make_ssm_dims(T, B, D, N=1, G=1, W=1, precision="bf16"):
     return SsmDims(T, B, D, N, G, W, precision)
 
 
-def ssm_workspace_bytes(dims: SsmDims) -> dict:
-    vals = [ctypes.c_size_t() for _ in range(4)]
-    _check("ssm_workspace_bytes", lib().ssm_workspace_bytes(ctypes.byref(dims), *[ctypes.byref(v) for v in vals]))
-    return dict(zip(("saved", "fwd", "bwd", "conv_bwd"), (v.value for v in vals)))
+_SSM_SIZES = ("saved", "fwd", "bwd", "conv_bwd")
 
 
-def _ssm_bytes(dims):
-    """ssm_workspace_bytes, looked up once per dims object and values."""
+def ssm_workspace_bytes(dims: SsmDims, only=_SSM_SIZES) -> dict:
+    """Sizes in bytes by name; `only`: the buffers asked for (dims that one
+    pass is too large for are refused where its buffer is asked for)."""
+    vals = {n: ctypes.c_size_t() for n in only}
+    _check("ssm_workspace_bytes", lib().ssm_workspace_bytes(
+        ctypes.byref(dims), *[ctypes.byref(vals[n]) if n in vals else None for n in _SSM_SIZES]))
+    return {n: v.value for n, v in vals.items()}
+
+
+def _ssm_bytes(dims, name):
+    """One of ssm_workspace_bytes, looked up once per dims object and values."""
     key = (dims.T, dims.B, dims.D, dims.N, dims.G, dims.W, dims.precision)
     got = dims.__dict__.get("sizes")
     if got is None or got[0] != key:
-        got = dims.__dict__["sizes"] = (key, ssm_workspace_bytes(dims))
-    return got[1]
+        got = dims.__dict__["sizes"] = (key, {})
+    n = got[1].get(name)
+    if n is None:
+        n = got[1][name] = ssm_workspace_bytes(dims, (name,))[name]
+    return n
 
 
 def ssm_conv_fwd(dims, x, w, bias, y, lens=None, state=None, state_out=None, silu=True, stream=None):
@@ -352,7 +361,7 @@ def ssm_conv_bwd(dims, x, w, bias, dy, dx, dw, dbias, ws, lens=None, state=None,
                  _have("dstate_out", dstate_out, (B, W - 1, D), e, dev, True), pdx, lddx,
                  _have("dw", dw, (D, W), f, dev), _have("dbias", dbias, (D,), f, dev, True),
                  _have("dstate", dstate, (B, W - 1, D), e, dev, True),
-                 _bytes("ws", ws, _ssm_bytes(dims)["conv_bwd"], dev), SSM_SILU if silu else 0)
+                 _bytes("ws", ws, _ssm_bytes(dims, "conv_bwd"), dev), SSM_SILU if silu else 0)
 
 
 def _slots(state, slots, B, row, dtype, dev):
@@ -400,10 +409,10 @@ def ssm_scan_fwd(dims, x, dt, A, Bm, Cm, y, ws, Dskip=None, z=None, dt_bias=None
     T, B, D, N = dims.T, dims.B, dims.D, dims.N
     arg = _scan_in(dims, (T, B), dev, x, dt, A, Bm, Cm, Dskip, z, dt_bias, h0, lens, softplus)
     py, ldy = _rows("y", y, (T, B, D), _elem(dims), dev)
-    n = _ssm_bytes(dims)
     return _call("ssm_scan_fwd", dev, stream, ctypes.byref(dims), arg, py, ldy,
                  _have("h_last", h_last, (B, D, N), torch.float32, dev, True),
-                 None if saved is None else _bytes("saved", saved, n["saved"], dev), _bytes("ws", ws, n["fwd"], dev))
+                 None if saved is None else _bytes("saved", saved, _ssm_bytes(dims, "saved"), dev),
+                 _bytes("ws", ws, _ssm_bytes(dims, "fwd"), dev))
 
 
 def ssm_scan_bwd(dims, x, dt, A, Bm, Cm, dy, saved, ws, dx, ddt, dA, dBm, dCm, Dskip=None, dDskip=None, z=None,
@@ -420,10 +429,9 @@ def ssm_scan_bwd(dims, x, dt, A, Bm, Cm, dy, saved, ws, dx, ddt, dA, dBm, dCm, D
     out = SsmScanGrads(pdx, pdt, pdb, pdc, pdz, lddx, ldddt, lddb, lddc, lddz, _have("dA", dA, (D, N), f, dev),
                        _have("dDskip", dDskip, (D,), f, dev, True), _have("ddt_bias", ddt_bias, (D,), f, dev, True),
                        _have("dh0", dh0, (B, D, N), f, dev, True))
-    n = _ssm_bytes(dims)
     return _call("ssm_scan_bwd", dev, stream, ctypes.byref(dims), arg, pdy, lddy,
-                 _have("dh_last", dh_last, (B, D, N), f, dev, True), _bytes("saved", saved, n["saved"], dev),
-                 ctypes.byref(out), _bytes("ws", ws, n["bwd"], dev))
+                 _have("dh_last", dh_last, (B, D, N), f, dev, True), _bytes("saved", saved, _ssm_bytes(dims, "saved"), dev),
+                 ctypes.byref(out), _bytes("ws", ws, _ssm_bytes(dims, "bwd"), dev))
 
 
 def ssm_scan_step(dims, x, dt, A, Bm, Cm, state, y, Dskip=None, z=None, dt_bias=None, slots=None, softplus=True,

@@ -251,7 +251,7 @@ struct ScanPlan {
   // then the backward's bc, dA, par
   size_t saved, ends, sums, fwd, bc, dA, par, bwd;
 };
-static int scan_plan(const ssm_dims* d, ScanPlan* o) {
+static void scan_plan(const ssm_dims* d, ScanPlan* o) {
   o->tpg = (int)cdiv(d->D / d->G, SCAN_CT);
   o->blocks = (int64_t)d->B * d->G * o->tpg;
   // Stretches: a sequence is split where its waves are few, so that 6144 run
@@ -289,12 +289,18 @@ static int scan_plan(const ssm_dims* d, ScanPlan* o) {
   o->dA = up256((size_t)o->nseg * d->B * d->D * d->N * 4);
   o->par = up256((size_t)o->nseg * d->B * 2 * d->D * 4);
   o->bwd = o->fwd + o->bc + o->dA + o->par;
-  if (o->blocks * o->nseg * SCAN_CT * o->blpc > LAUNCH_THREADS)
-    return blstm_fail(BLSTM_EUNSUPPORTED, "ssm_scan: B*D too large");
+}
+// Whether a launch has threads enough, for the forward and for the backward.
+static int scan_fits(const ScanPlan& pl, int lanes, const char* fn) {
+  return pl.blocks * pl.nseg * SCAN_CT * lanes > LAUNCH_THREADS
+             ? blstm_fail(BLSTM_EUNSUPPORTED, "%s: B*D too large", fn) : BLSTM_OK;
+}
+static int scan_fits_fwd(const ScanPlan& pl, const char* fn) { return scan_fits(pl, pl.lpc, fn); }
+static int scan_fits_bwd(const ssm_dims* d, const ScanPlan& pl, const char* fn) {
   // a thread of ssm_scan_sum for each element of dB and dC, and 16 for a column of dA
   if (2 * (int64_t)d->T * d->B * d->G * d->N + 16 * (int64_t)d->D * (d->N + 2) + 512 > LAUNCH_THREADS)
-    return blstm_fail(BLSTM_EUNSUPPORTED, "ssm_scan: T*B*G*N too large");
-  return BLSTM_OK;
+    return blstm_fail(BLSTM_EUNSUPPORTED, "%s: T*B*G*N too large", fn);
+  return scan_fits(pl, pl.blpc, fn);
 }
 
 size_t ssm_conv_bwd_bytes(const ssm_dims* d);
@@ -302,7 +308,10 @@ size_t ssm_conv_bwd_bytes(const ssm_dims* d);
 extern "C" int ssm_workspace_bytes(const ssm_dims* dims, size_t* saved, size_t* fwd, size_t* bwd, size_t* conv_bwd) {
   ScanPlan pl;
   int rc = ssm_check_dims(dims, "ssm_workspace_bytes");
-  if (!rc) rc = scan_plan(dims, &pl);
+  if (rc) return rc;
+  scan_plan(dims, &pl);
+  if (saved || fwd || bwd) rc = scan_fits_fwd(pl, "ssm_workspace_bytes");
+  if (!rc && bwd) rc = scan_fits_bwd(dims, pl, "ssm_workspace_bytes");
   if (rc) return rc;
   if (saved) *saved = pl.saved;
   if (fwd) *fwd = pl.fwd;
@@ -357,7 +366,9 @@ extern "C" int ssm_scan_fwd(const ssm_dims* dims, const ssm_scan_in* in, void* y
   ScanPlan pl;
   ScanP p;
   int rc = ssm_check_dims(dims, "ssm_scan_fwd");
-  if (!rc) rc = scan_plan(dims, &pl);
+  if (rc) return rc;
+  scan_plan(dims, &pl);
+  rc = scan_fits_fwd(pl, "ssm_scan_fwd");
   if (!rc) rc = scan_in(dims, in, "ssm_scan_fwd", &p);
   if (rc) return rc;
   if (!y) return blstm_fail(BLSTM_EINVAL, "ssm_scan_fwd: NULL pointer");
@@ -383,7 +394,9 @@ extern "C" int ssm_scan_bwd(const ssm_dims* dims, const ssm_scan_in* in, const v
   ScanPlan pl;
   ScanP p;
   int rc = ssm_check_dims(dims, "ssm_scan_bwd");
-  if (!rc) rc = scan_plan(dims, &pl);
+  if (rc) return rc;
+  scan_plan(dims, &pl);
+  rc = scan_fits_bwd(dims, pl, "ssm_scan_bwd");
   if (!rc) rc = scan_in(dims, in, "ssm_scan_bwd", &p);
   if (rc) return rc;
   if (!dy || !saved || !ws || !out || !out->dx || !out->ddt || !out->dBm || !out->dCm || !out->dA || (in->z && !out->dz))

@@ -466,3 +466,31 @@ def test_the_binding_refuses_wrong_tensors(gpu_lib):
         c.forward(dt=c.gpu["dt"][:3])
     with pytest.raises(ValueError, match="h0"):
         c.forward(h0=c.gpar["h0"].cpu())
+
+
+def test_a_forward_past_the_backwards_limit(gpu_lib):
+    """2 T B G N past the threads of a launch: no backward, and a forward as any other."""
+    from paper_1907_05701_amd import binding as bd
+    T, B, D, N, G = 1024, 1024, 64, 64, 64
+    g = torch.Generator(device="cuda").manual_seed(7)
+    bc = torch.empty(T, B, G * N, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    x = torch.empty(T, B, D, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    A = -torch.rand(D, N, generator=g, device="cuda") - 0.1
+    y = torch.empty_like(x)
+    d = bd.make_ssm_dims(T=T, B=B, D=D, N=N, G=G, precision="bf16")
+    with pytest.raises(bd.BlstmError):
+        bd.ssm_workspace_bytes(d)
+    ws = torch.empty(max(1, bd.ssm_workspace_bytes(d, ("fwd",))["fwd"]), dtype=torch.uint8, device="cuda")
+    bd.ssm_scan_fwd(d, x, x, A, bc, bc, y, ws)
+    at = [0, 517, 1023]
+    xs, bs = x[:40, at].double().cpu(), bc[:40, at].double().cpu()
+    want, _ = om.scan(xs, xs, A.double().cpu(), bs, bs)
+    assert om.far(y[:40, at], want, tol(40)) <= 1.0
+    # every frame of those sequences against the same ones scanned alone, in stretches
+    short = bd.make_ssm_dims(T=T, B=1, D=D, N=N, G=G, precision="bf16")
+    w1 = torch.empty(max(1, bd.ssm_workspace_bytes(short, ("fwd",))["fwd"]), dtype=torch.uint8, device="cuda")
+    for b in at:
+        y1 = torch.empty(T, 1, D, dtype=torch.bfloat16, device="cuda")
+        v = [t[:, b:b + 1].contiguous() for t in (x, bc)]
+        bd.ssm_scan_fwd(short, v[0], v[0], A, v[1], v[1], y1, w1)
+        assert om.far(y[:, b:b + 1], y1.double().cpu(), tol(T)) <= 2.0   # both rounded to bf16

@@ -175,3 +175,45 @@ def test_a_teacher_of_another_shape_is_refused(n):
     teacher = SimpleNamespace(shape=dict(shape, **{n: 11}))
     with pytest.raises(ValueError, match=f"teacher's {n} is 11"):
         Trainer(step, [], 0.1, 4, teacher=teacher)
+
+
+# -------------------------------------------------------- limits by direction ---
+def _sizes(d, *names):
+    """ssm_workspace_bytes of some buffers alone: (code, their sizes)."""
+    v = {n: ctypes.c_size_t() for n in names}
+    args = [ctypes.byref(v[n]) if n in v else None for n in ("saved", "fwd", "bwd", "conv_bwd")]
+    return bd.lib().ssm_workspace_bytes(ctypes.byref(d), *args), {n: x.value for n, x in v.items()}
+
+
+def test_a_forward_is_not_held_to_the_backwards_limits():
+    """The launch that sums the backward's partials, and its lanes, are the backward's alone."""
+    L = bd.lib()
+    # 2 T B G N past a launch's threads; states on four lanes in the backward where the forward has two
+    for over in (dict(T=1 << 10, B=1 << 10, D=64, N=64, G=64), dict(T=1, B=1 << 24, D=64, N=16, G=1)):
+        d = _dims(**over)
+        assert _sizes(d, "saved", "fwd")[0] == 0
+        _refused(_sizes(d, "bwd")[0], bd.BLSTM_EUNSUPPORTED)
+        i = _scan_in(d)
+        # past the limits, to the next check (nothing is launched: y, then dy are missing)
+        _refused(L.ssm_scan_fwd(ctypes.byref(d), ctypes.byref(i), None, d.D, None, None, PTR, None), bd.BLSTM_EINVAL)
+        g = bd.SsmScanGrads(256, 256, 256, 256, 256, d.D, d.D, d.G * d.N, d.G * d.N, d.D, 256, None, None, None)
+        _refused(L.ssm_scan_bwd(ctypes.byref(d), ctypes.byref(i), None, d.D, None, PTR, ctypes.byref(g), PTR, None),
+                 bd.BLSTM_EUNSUPPORTED)
+
+
+def test_a_convolution_is_not_held_to_the_scans_limits():
+    d = _dims(T=1, B=1 << 24, D=512, G=1, N=1)
+    rc, n = _sizes(d, "conv_bwd")
+    assert rc == 0 and n["conv_bwd"] > 0
+    _refused(_sizes(d, "fwd")[0], bd.BLSTM_EUNSUPPORTED)
+
+
+def test_the_binding_asks_for_the_sizes_of_its_call():
+    big = dict(T=1 << 10, B=1 << 10, D=64, N=64, G=64)
+    assert bd._ssm_bytes(_dims(**big), "saved") > 0
+    with pytest.raises(bd.BlstmError):
+        bd._ssm_bytes(_dims(**big), "bwd")
+    d = _dims()
+    assert {n: bd._ssm_bytes(d, n) for n in ("saved", "fwd", "bwd", "conv_bwd")} == bd.ssm_workspace_bytes(d)
+    d.T = 50   # other values of the same object
+    assert bd._ssm_bytes(d, "saved") == bd.ssm_workspace_bytes(d)["saved"]
