@@ -284,7 +284,7 @@ int ssm_scan_fwd(const ssm_dims* dims, const ssm_scan_in* in, void* y, int64_t l
 
 /* Gradients of ssm_scan_fwd's inputs, all overwritten.  dx, ddt, dz [T][B][D]
  * and dBm, dCm [T][B][G*N] in the precision's type, the others float32.
- * dz is required with z; dDskip, ddt_bias and dh0 may be NULL.
+ * dz is required with z and refused without; dDskip, ddt_bias and dh0 may be NULL.
  * dh_last [B][D][N]: the loss gradient of h_last, NULL for zeros. */
 typedef struct ssm_scan_grads {
   void *dx, *ddt, *dBm, *dCm, *dz;

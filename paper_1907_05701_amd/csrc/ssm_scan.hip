@@ -401,6 +401,7 @@ extern "C" int ssm_scan_bwd(const ssm_dims* dims, const ssm_scan_in* in, const v
   if (rc) return rc;
   if (!dy || !saved || !ws || !out || !out->dx || !out->ddt || !out->dBm || !out->dCm || !out->dA || (in->z && !out->dz))
     return blstm_fail(BLSTM_EINVAL, "ssm_scan_bwd: NULL pointer");
+  if (!in->z && out->dz) return blstm_fail(BLSTM_EINVAL, "ssm_scan_bwd: dz without z");
   const int64_t bcw = (int64_t)dims->G * dims->N;
   if (lddy < dims->D || out->lddx < dims->D || out->ldddt < dims->D || out->lddb < bcw || out->lddc < bcw ||
       (in->z && out->lddz < dims->D))

@@ -217,3 +217,16 @@ def test_the_binding_asks_for_the_sizes_of_its_call():
     assert {n: bd._ssm_bytes(d, n) for n in ("saved", "fwd", "bwd", "conv_bwd")} == bd.ssm_workspace_bytes(d)
     d.T = 50   # other values of the same object
     assert bd._ssm_bytes(d, "saved") == bd.ssm_workspace_bytes(d)["saved"]
+
+
+# ------------------------------------------------------------------ refusals ---
+def test_a_gate_gradient_without_a_gate_is_refused():
+    """There is none to write: dz would stay as it was."""
+    L, d = bd.lib(), _dims()
+    i = _scan_in(d, z=None)
+    g = bd.SsmScanGrads(256, 256, 256, 256, 256, 12, 12, 8, 8, 12, 256, None, None, None)
+    # lddx is short, too: refused either way, but for the gate first
+    g.lddx = 3
+    _refused(L.ssm_scan_bwd(ctypes.byref(d), ctypes.byref(i), PTR, 12, None, PTR, ctypes.byref(g), PTR, None),
+             bd.BLSTM_EINVAL)
+    assert b"dz" in L.blstm_last_error()
