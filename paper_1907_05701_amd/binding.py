@@ -283,6 +283,9 @@ def _rows(name, t, shape, dtype, dev, optional=False):
 def _call(fn, dev, stream, *args):
     """Calls fn on device `dev` (made current for the launch if it is not) and
     `stream`, by default the device's current one."""
+    on = getattr(stream, "device", None)
+    if on is not None and on.index != dev:   # its kernels would reach for another device's memory
+        raise ValueError(f"the stream is on {on}, the tensors are on cuda:{dev}")
     if dev != torch.cuda.current_device():
         with torch.cuda.device(dev):
             return _call(fn, dev, stream, *args)

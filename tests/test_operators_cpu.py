@@ -230,3 +230,12 @@ def test_a_gate_gradient_without_a_gate_is_refused():
     _refused(L.ssm_scan_bwd(ctypes.byref(d), ctypes.byref(i), PTR, 12, None, PTR, ctypes.byref(g), PTR, None),
              bd.BLSTM_EINVAL)
     assert b"dz" in L.blstm_last_error()
+
+
+def test_a_stream_of_another_device_is_refused():
+    from types import SimpleNamespace
+
+    import torch
+    other = SimpleNamespace(device=torch.device("cuda", 1), cuda_stream=0)
+    with pytest.raises(ValueError, match="stream"):
+        bd._call("softmax_topk_rows", 0, other)
