@@ -14,6 +14,12 @@ import torch
 from . import binding as bd
 
 
+def _given(teacher):
+    """A teacher as an argument where there is one: a learner whose step() or
+    gradient() knows of none is called as it is."""
+    return () if teacher is None else (teacher,)
+
+
 class LearnerStep:
     def __init__(self, L, D, H, P, K, T, B, precision="bf16", device="cuda:0"):
         self.dims = bd.make_dims(L, D, H, P, K, T, B, precision)
@@ -110,7 +116,7 @@ class LearnerStep:
 
     def step(self, lr, flags=0, teacher=None):
         """The whole learner step: gradient, then the fused update."""
-        self.gradient(teacher)
+        self.gradient(*_given(teacher))
         self.update(lr, flags)
 
     def capture(self, lr, steps=1, flags=0, teacher=None):
@@ -122,5 +128,5 @@ class LearnerStep:
         graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(graph):
             for _ in range(steps):
-                self.step(lr, flags, teacher)
+                self.step(lr, flags, *_given(teacher))
         return graph

@@ -72,7 +72,10 @@ class Trainer:
             for x, y, teacher in zip(self.x, self.lab, self.teacher):
                 self.step.x.copy_(x)
                 self.step.labels.copy_(y)
-                self.step.step(lr, self.flags, teacher)
+                if teacher is None:
+                    self.step.step(lr, self.flags)
+                else:
+                    self.step.step(lr, self.flags, teacher)
                 acc += self.step.loss
             torch.cuda.synchronize()
             self.step.check_recurrence()

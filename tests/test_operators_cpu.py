@@ -239,3 +239,58 @@ def test_a_stream_of_another_device_is_refused():
     other = SimpleNamespace(device=torch.device("cuda", 1), cuda_stream=0)
     with pytest.raises(ValueError, match="stream"):
         bd._call("softmax_topk_rows", 0, other)
+
+
+# ------------------------------------------------- calls that have no teacher ---
+def test_a_trainer_calls_a_step_without_a_teacher_as_before(monkeypatch):
+    """A step object whose step() takes the rate and the flags alone."""
+    import numpy as np
+    import torch
+
+    from paper_1907_05701_amd.train import Trainer
+    monkeypatch.setattr(torch.cuda, "synchronize", lambda *a: None)
+
+    class Step:
+        shape, device = dict(T=3, B=2, D=4, K=10), torch.device("cpu")
+        x, labels, loss = torch.zeros(3, 2, 4), torch.zeros(3, 2, dtype=torch.int32), torch.ones(1)
+        calls = []
+
+        def step(self, lr, flags=0):
+            self.calls.append((lr, flags))
+
+        def check_recurrence(self):
+            pass
+
+    got = Trainer(Step(), [(np.zeros((3, 2, 4), np.float32), np.zeros((3, 2), np.int32))], 0.1, 2, warmup_epochs=1,
+                  flags=2).run(2)
+    assert len(Step.calls) == 2 and all(f == 2 for _, f in Step.calls) and [h[2] for h in got] == [1.0, 1.0]
+
+
+def test_a_learner_step_calls_its_own_methods_as_before(monkeypatch):
+    """A learner whose gradient() and step() take what they took before there were teachers."""
+    import contextlib
+
+    import torch
+
+    from paper_1907_05701_amd.step import LearnerStep
+    calls = []
+
+    class Own(LearnerStep):
+        def gradient(self):
+            calls.append("gradient")
+
+        def update(self, lr, flags=0, grads=None, scale=1.0):
+            calls.append("update")
+
+    shape = dict(L=1, D=4, H=16, P=8, K=10, T=2, B=2, precision="fp32", device="cpu")
+    Own(**shape).step(0.1)
+    assert calls == ["gradient", "update"]
+
+    class Stepping(LearnerStep):
+        def step(self, lr, flags=0):
+            calls.append((lr, flags))
+
+    monkeypatch.setattr(torch.cuda, "CUDAGraph", lambda: "graph")
+    monkeypatch.setattr(torch.cuda, "graph", lambda g: contextlib.nullcontext())
+    assert Stepping(**shape).capture(0.5, steps=2, flags=3) == "graph"
+    assert calls[2:] == [(0.5, 3), (0.5, 3)]
