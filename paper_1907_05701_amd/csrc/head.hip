@@ -1006,13 +1006,14 @@ static void head_z(const Layout& lo, const float* theta, const T* W, const T* yt
   }
 }
 
-// Rows of float32 logits that the bf16 head's distillation holds at a time, all
+// Rows of logits that a row pass takes at a time.  float32: as many as a launch has threads for (up to
+// 1024 a row).  bf16: rows of float32 logits that the head's distillation holds at a time, all
 // frames in equal parts: at 32000 classes at most 180 MB, which the last-level
 // cache keeps between the product that writes them and the row pass that reads
 // them.  (2688 frames, distillation / top logits, us: parts of 512 459 / 235,
 // 1024 443 / 202, 1344 448 / 183, all at once 446 / 221.)
 static int64_t head_rows(const Layout& lo) {
-  if (lo.es != 2) return lo.M;
+  if (lo.es != 2) return std::min<int64_t>(lo.M, 1 << 21);
   return std::min(lo.M, rup(cdiv(lo.M, cdiv(lo.M, 1408)), 64));
 }
 // Behind head_ws, bf16: those logits, then column-sum partials of db_s.
@@ -1022,7 +1023,7 @@ static size_t head_logits_bytes(const Layout& lo) {
 static size_t head_extra_bytes(const Layout& lo) {
   return lo.es == 2 ? head_logits_bytes(lo) + (size_t)COLSUM_MAX_CHUNKS * lo.Kp * 4 : 0;
 }
-// float32 logits of rows [r0, r0 + n) of z (n <= head_rows in bf16), row pitch Kp.
+// float32 logits of rows [r0, r0 + n) of z (n <= head_rows), row pitch Kp.
 template <typename T>
 static float* head_logits(const Layout& lo, const float* theta, const T* W, char* hws, int64_t r0, int64_t n,
                           hipStream_t s) {
@@ -1054,7 +1055,7 @@ static int head_impl(const Layout& lo, const float* theta, const T* W, const T* 
   constexpr bool lp = std::is_same<T, bf16>::value;
   T* DS = (T*)(hws + lo.S);
   if (teacher) {
-    // float32: every row's logits at once, overwritten by ds in place
+    // float32: every row's logits have their place, overwritten by ds
     const int64_t step = head_rows(lo);
     for (int64_t r0 = 0; r0 < M; r0 += step) {
       const int64_t n = std::min(step, M - r0);

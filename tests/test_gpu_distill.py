@@ -501,6 +501,31 @@ def test_head_top_logits(gpu_lib, precision):
     assert all(len(set(r)) == k for r in idx.tolist())
 
 
+def test_float32_head_of_more_rows_than_a_launch_holds(gpu_lib):
+    """2^23 frames and more at 512 threads a row: rows on either side of the parts, as in test_head_top_logits."""
+    from paper_1907_05701_amd import binding as bd
+    T, B, H, P, K, k = 8195, 1024, 16, 8, 136, 129
+    M = T * B
+    d = bd.make_dims(1, 8, H, P, K, T, B, "fp32")
+    g = torch.Generator(device="cuda").manual_seed(5)
+    theta = torch.rand(bd.blstm_param_count(d), generator=g, device="cuda") - 0.5
+    y = torch.rand(T, B, 2 * H, generator=g, device="cuda") * 2 - 1
+    ws = torch.empty(bd.softmax_head_ws_bytes(d), dtype=torch.uint8, device="cuda")
+    top, rest = torch.full((M, k), 99.0, device="cuda"), torch.full((M,), 99.0, device="cuda")
+    idx = torch.full((M, k), -7, dtype=torch.int32, device="cuda")
+    bd.softmax_topk(d, theta, None, y, top, idx, ws, rest, temperature=2.0)
+    at = torch.tensor([0, 1] + [n * (1 << 21) + e for n in (1, 2, 3, 4) for e in (-1, 0, 1)] + [M - 2, M - 1])
+    th = theta[-(P * 2 * H + P + K * P + K):].double().cpu()
+    Wl, bl, Ws, bs = torch.split(th, [P * 2 * H, P, K * P, K])
+    s = (y.view(M, -1)[at.cuda()].double().cpu() @ Wl.view(P, -1).t() + bl) @ Ws.view(K, P).t() + bs
+    t, i, r = top[at.cuda()].double().cpu(), idx[at.cuda()].long().cpu(), rest[at.cuda()].double().cpu()
+    want = torch.sort(s, 1, descending=True).values
+    assert float((s.gather(1, i) - t).abs().max()) <= 1e-5
+    assert float((want[:, :k] - t).abs().max()) <= 1e-5
+    assert float((torch.logsumexp(want[:, k:] / 2, 1) - r).abs().max()) <= 1e-5
+    assert int((idx < 0).sum()) == 0 and int((rest == 99.0).sum()) == 0
+
+
 # -------------------------------------------------- the operators as one run ---
 def test_a_causal_student_learns_from_the_blstm_teacher(gpu_lib):
     """Teacher's forward and top logits, then the student's convolution, scan and
