@@ -180,6 +180,69 @@ def test_scan_of_long_sequences(gpu_lib, T, B, D, N):
     check(Case(T, B, D, N, 1, "fp32", lens=([T, T // 2, 0] * B)[:B]))
 
 
+SPLIT = [  # T, B, D, N, G, lens: every count of lanes, groups, a short last stretch, one row that ends early
+    (300, 1, 64, 16, 1, None), (90, 3, 20, 4, 2, None), (260, 1, 66, 7, 3, None), (150, 2, 70, 24, 1, [150, 31]),
+    (200, 2, 96, 40, 2, [77, 200]), (133, 1, 72, 64, 1, None),
+]
+SPLIT_WIDE = [(100, 80, 66, 10, 1, None), (80, 72, 130, 6, 2, None), (90, 40, 64, 48, 1, None)]   # eight states a lane forward
+
+
+@pytest.mark.parametrize("softplus", [True, False])
+@pytest.mark.parametrize("gate", [True, False])
+@pytest.mark.parametrize("precision", ["fp32", "bf16"])
+@pytest.mark.parametrize("T,B,D,N,G,lens", SPLIT, ids=str)
+def test_split_scans(gpu_lib, T, B, D, N, G, lens, precision, gate, softplus):
+    """Sequences in stretches, which a scratch buffer of the forward tells: every
+    type, with and without a gate, groups, up to 64 states."""
+    c = Case(T, B, D, N, G, precision, gate=gate, softplus=softplus, lens=lens)
+    assert c.bd.ssm_workspace_bytes(c.dims)["fwd"] > 0
+    check(c)
+
+
+@pytest.mark.parametrize("precision,gate", [("fp32", True), ("bf16", False)])
+@pytest.mark.parametrize("T,B,D,N,G,lens", SPLIT_WIDE, ids=str)
+def test_split_scans_of_many_sequences(gpu_lib, T, B, D, N, G, lens, precision, gate):
+    c = Case(T, B, D, N, G, precision, gate=gate, lens=lens)
+    assert c.bd.ssm_workspace_bytes(c.dims)["fwd"] > 0
+    check(c)
+
+
+@pytest.mark.parametrize("precision,N", [("fp32", 16), ("bf16", 5)])
+def test_scan_of_more_stretches_than_the_join_holds(gpu_lib, precision, N):
+    """138 stretches: more than eight in a run of the join, which then reads them twice."""
+    c = Case(1100, 1, 8, N, 1, precision, lens=[1093])
+    assert c.bd.ssm_workspace_bytes(c.dims)["fwd"] > 130 * 8 * N * 4 * 2
+    check(c)
+
+
+@pytest.mark.parametrize("N", [4, 20])
+def test_split_scan_of_far_rows(gpu_lib, N):
+    """A row pitch past what 32-bit offsets reach, in stretches, forward and backward."""
+    from paper_1907_05701_amd import binding as bd
+    T, D, ld = 96, 8, 1 << 26
+    g = torch.Generator(device="cuda").manual_seed(6)
+    big = torch.empty(T * ld, dtype=torch.bfloat16, device="cuda")
+    x, dt, z, dy, y, dx, ddt, dz = [torch.as_strided(big, (T, 1, D), (ld, ld, 1), 32 * i) for i in range(8)]
+    for t in (x, dt, z, dy):
+        t.copy_(torch.randn(T, 1, D, generator=g, device="cuda"))
+    bc = torch.randn(T, 1, 2 * N, generator=g, device="cuda").bfloat16()
+    A = -torch.rand(D, N, generator=g, device="cuda")
+    d = bd.make_ssm_dims(T=T, B=1, D=D, N=N, precision="bf16")
+    n = bd.ssm_workspace_bytes(d)
+    assert n["fwd"] > 0
+    ws = {k: torch.empty(max(1, v), dtype=torch.uint8, device="cuda") for k, v in n.items()}
+    dA, dB = torch.empty_like(A), torch.empty(T, 1, N, dtype=torch.bfloat16, device="cuda")
+    dC = torch.empty_like(dB)
+    bd.ssm_scan_fwd(d, x, dt, A, bc[..., :N], bc[..., N:], y, ws["fwd"], z=z, saved=ws["saved"])
+    bd.ssm_scan_bwd(d, x, dt, A, bc[..., :N], bc[..., N:], dy, ws["saved"], ws["bwd"], dx, ddt, dA, dB, dC, z=z, dz=dz)
+    leaves = [t.double().cpu().requires_grad_() for t in (x, dt, A, bc[..., :N], bc[..., N:], z)]
+    wy, _ = om.scan(*leaves[:5], z=leaves[5])
+    want = torch.autograd.grad((wy * dy.double().cpu()).sum(), leaves)
+    assert om.far(y, wy, tol(T)) <= 1.0
+    for a, b in zip((dx, ddt, dA, dB, dC, dz), want):
+        assert om.far(a, b, tol(T)) <= 1.0
+
+
 @pytest.mark.parametrize("precision", ["fp32", "bf16"])
 def test_split_scan_of_growing_states_from_silence(gpu_lib, precision):
     """Decays above one (any finite A is allowed): a state of zero stays zero however
