@@ -329,8 +329,8 @@ int softmax_topk_rows(const void* logits, int64_t ld, int64_t M, int32_t K, int3
  * entries or rest hold a NaN or +inf has no probabilities, and its loss and gradient
  * are NaN (unless its weight or soft is 0).
  * labels (NULL: none) outside 0..K-1: the row has no hard loss.
- * weights [M] float32 (NULL: ones): a row of weight 0 has loss and gradient 0
- * whatever it holds (on the head, whose products sum over frames, its y_top
+ * weights [M] float32 (NULL: ones): a row of weight 0, or with neither loss, has loss
+ * and gradient 0 whatever it holds (on the head, whose products sum over frames, its y_top
  * has to be finite all the same). */
 typedef struct softmax_teacher {
   const float* top;       /* [M][k] */

@@ -646,11 +646,11 @@ __global__ __launch_bounds__(T, (waves_of<TI, T, V, NV>())) void distill_rows_ke
   const int tid = threadIdx.x, K = p.K;
   const float weight = p.weights ? p.weights[m] : 1.f;
   for (int c = K + tid; c < K + p.pad; c += T) d[c] = from_f32<TO>(0.f);
-  if (weight == 0.f) {
+  auto nothing = [&]() {   // a row that has no loss
     for (int c = tid; c < K; c += T) d[c] = from_f32<TO>(0.f);
     if (tid == 0) p.row_loss[m] = 0.f;
-    return;
-  }
+  };
+  if (weight == 0.f) return nothing();
   Others<TI, TO, T, V, NV> row;
   row.load(s, K);   // in flight while the teacher's part runs
   const int words = (NV ? NV * V * T : K + 31) / 32;
@@ -683,6 +683,7 @@ __global__ __launch_bounds__(T, (waves_of<TI, T, V, NV>())) void distill_rows_ke
   const float tm = max_nan(ta, rest);
   // an unwanted loss may be infinite; a teacher's NaN or +inf makes tz, every probability and r a NaN
   const bool taught = p.soft != 0.f && !(tm == -INFINITY);
+  if (same(!taught && !marked)) return nothing();   // whatever it holds: below, 0 times its z would count
   const float lt = (tv - tbase) * p.it2 + (ta - tm) * LOG2E_F, lr = (rest - tm) * LOG2E_F;
   const float e = taught ? exp2_(lt) : 0.f, er = taught ? exp2_(lr) : 0.f;
   if (tid < p.k) l.pv[tid] = e;

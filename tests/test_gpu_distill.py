@@ -393,6 +393,24 @@ def test_a_teacher_that_has_diverged_is_seen(gpu_lib, tau, precision):
     check_distill(s.cpu(), top.cpu(), idx.cpu(), rest.cpu(), lab.cpu(), w.cpu(), tau=tau, soft=0.0, hard=1.0)
 
 
+@pytest.mark.parametrize("precision,K", [("fp32", 130), ("bf16", 9001), ("fp32", 70001)])
+def test_a_row_with_neither_loss_has_no_gradient(gpu_lib, precision, K):
+    """No entry, no rest and no label, over logits that a mask has left nothing of, NaN or ordinary: zeros,
+    in place, too."""
+    from paper_1907_05701_amd import binding as bd
+    s, top, idx, rest, lab = make_rows(5, K, 6, precision, 51)
+    idx[:4], rest[:4], lab[:4] = -1, -math.inf, -1
+    s[0], s[1], s[3, 7] = -math.inf, math.nan, math.inf
+    for labels, soft, hard in ((None, 1.0, 0.0), (lab, 0.5, 0.5), (lab, 0.0, 1.0)):
+        for inplace in (False, True):
+            g = s.cuda()
+            loss, d = torch.full((5,), 99.0, device="cuda"), g if inplace else torch.full_like(g, 99.0)
+            bd.softmax_distill_rows(g, top.cuda(), idx.cuda(), loss, d, rest=rest.cuda(), soft=soft, hard=hard,
+                                    labels=None if labels is None else labels.cuda(), temperature=2.0)
+            assert not bool(loss[:4].any()) and not bool(d[:4].any())
+            assert float(loss[4]) > 0 and bool(torch.isfinite(d[4]).all()) and bool(d[4].any())
+
+
 # ------------------------------------------------------------------ the head ---
 def head_case(precision, M, H, P, K, k, seed=0):
     from paper_1907_05701_amd.step import LearnerStep
