@@ -1008,13 +1008,16 @@ static void head_z(const Layout& lo, const float* theta, const T* W, const T* yt
 
 // Rows of logits that a row pass takes at a time.  float32: as many as a launch has threads for (up to
 // 1024 a row).  bf16: rows of float32 logits that the head's distillation holds at a time, all
-// frames in equal parts: at 32000 classes at most 180 MB, which the last-level
-// cache keeps between the product that writes them and the row pass that reads
-// them.  (2688 frames, distillation / top logits, us: parts of 512 459 / 235,
-// 1024 443 / 202, 1344 448 / 183, all at once 446 / 221.)
+// frames in equal parts of up to about 180 MB, which the last-level cache keeps between the
+// product that writes them and the row pass that reads them.  (Distillation / top logits, us.
+// 2688 frames of 32000 classes: parts of 512 frames 459 / 235, 1024 443 / 202, 1344 (two) 448 / 183, all at once
+// 446 / 221; of 200000, in 12 parts 3071 / 1592, in two 3127 / 1752; 90112 frames of 500 classes: at once
+// 1213 / 336, in 64 parts 1869 / 889; 12000 of 4000: at once 330 / 132, in 9 parts 424 / 228.)
+static constexpr int64_t HEAD_PART = 180 << 20;   // bytes
 static int64_t head_rows(const Layout& lo) {
-  if (lo.es != 2) return std::min<int64_t>(lo.M, 1 << 21);
-  return std::min(lo.M, rup(cdiv(lo.M, cdiv(lo.M, 1408)), 64));
+  const int64_t most = std::min<int64_t>(lo.M, 1 << 21);
+  if (lo.es != 2) return most;
+  return std::min(most, rup(cdiv(lo.M, cdiv(lo.M * lo.Kp * 4, HEAD_PART)), 64));
 }
 // Behind head_ws, bf16: those logits, then column-sum partials of db_s.
 static size_t head_logits_bytes(const Layout& lo) {
