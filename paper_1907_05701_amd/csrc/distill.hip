@@ -114,8 +114,9 @@ template <typename TI, int V, int NV, int T> struct Row {
 
 // Waves of a SIMD that the registers are kept to.  Three rows on a CU instead
 // of two hide more of each other's barriers and waits: 2688 bf16 rows of 32000 (64
-// values a thread) 4 waves 59.6, 6 waves 53 us for the top, 92 and 85 for the loss.  float32 rows
-// of 64 values have no room for it.  (8 waves: the top of 12000 bf16 rows of 9001, 32
+// values a thread) 4 waves 56.5, 6 waves 49.3 us for the top, 82 and 77 for the loss with labels at
+// temperature 1, 95 and 88 at 3, although six waves spill one register at temperature 2 and two at other ones
+// than 1.  float32 rows of 64 values have no room for it.  (8 waves: the top of 12000 bf16 rows of 9001, 32
 // values a thread, 95 us, with 6 114.)
 template <typename TI, int T, int V, int NV> constexpr int waves_of() {
   if (NV == 0 || T > 512) return 4;
@@ -524,8 +525,8 @@ struct DistillP {
   int K, k, pad;
   float it2, tau, soft, hard, scale;   // it2: log2 e / tau
 };
-// Threads of a row of 32000: 512.  (2688 bf16 rows without labels: 70 us, with 256 threads
-// 74, and float32 279 against 79; 1024 threads 115.)
+// Threads of a row of 32000: 512.  (2688 rows without labels, us: bf16 73, with 256 threads 108, with 1024
+// 125; float32 136, 426 and 155.  256 threads spill their 128 values; 1024 leave a CU one row, or two of 32 values.)
 template <int T> struct DistillLds {
   float pv[MAXK];
   int32_t iv[MAXK];
@@ -775,9 +776,9 @@ __global__ __launch_bounds__(T, (waves_of<TI, T, V, NV>())) void distill_rows_ke
 // pieces would leave most threads without a maximum of their own.  Longer ones
 // go 16 bytes at a time, 16, 32 or 64 values a thread, since what a thread holds room for
 // it also computes, with as few threads as that takes: a row's barriers and searches
-// then keep less of the CU waiting.  (12000 bf16 rows, top logits / loss with labels, us: of
-// 3500 classes 256 threads 43 / 59, 512 78 / 119; of 6000 59 / 72 and 85 / 101; of 9001 86 / 113 and
-// 94 / 157.  Few rows do not gain from more: 256 rows of 32000 logits 11.1 us with 512 threads, 11.6 with
+// then keep less of the CU waiting.  (12000 bf16 rows, top logits / loss with labels at temperature 1, us: of
+// 3500 classes 256 threads 37 / 57, 512 75 / 119; of 6000 51 / 70 and 84 / 116; of 9001 84 / 114 and
+// 93 / 137.  Few rows do not gain from more: 256 rows of 32000 logits 11.1 us with 512 threads, 11.6 with
 // 1024.)  Packed bf16 pairs go to 128 values in rows of up to PACKED; what no
 // registers hold is read by every pass.
 // FEW: 256 threads have maxima enough for the threshold, k <= 128 of them (of

@@ -1190,8 +1190,9 @@ static int head_impl(const Layout& lo, const float* theta, const T* W, const T* 
     gemm_f32<T, true, false, V, V>("gemm_dz", s, Az, Bz2, M, P, K, 1, lo.sp_dz, DZ, P, 0, part, lp ? DZT : nullptr, P,
                                    lo.big_dz);
   }
-  // db_s and db_l, the sums over frames of ds and dz (bf16: already done,
-  // but not against a teacher: there of the ds that the products read)
+  // db_s and db_l, the sums over frames of ds and dz (bf16: already done, but not
+  // against a teacher: there in float32 of the rounded ds that the products read, each term off by at
+  // most 2^-8 of itself, as in dW_s; the float32 ones are not kept)
   if constexpr (lp) {
     if (teacher) {
       colsum<T>("colsum_dbs", s, DS, M, K, Kp, (float*)(hws + lo.head_bytes + head_logits_bytes(lo)), K, 0,

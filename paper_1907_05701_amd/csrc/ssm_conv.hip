@@ -107,7 +107,8 @@ __global__ __launch_bounds__(256) void ssm_conv_fwd_kernel(const ConvP p) {
 // 64 threads a row of 256 channels, 4 rows a workgroup; a row takes every
 // gridDim.y * 4-th stretch of BSEG frames.  There are as many workgroups as run at
 // a time, so that none waits behind the others and the partial sums are few.
-static constexpr int conv_resident(int W) { return W <= 4 ? 3 : 2; }   // workgroups of a CU: what the registers hold
+// workgroups of a CU: what the registers hold (but for 6 that float32 with 8 taps spills)
+static constexpr int conv_resident(int W) { return W <= 4 ? 3 : 2; }
 template <typename T, int W>
 __global__ __launch_bounds__(256, conv_resident(W)) void ssm_conv_bwd_kernel(const ConvP p) {
   const int cl = threadIdx.x & 63, rl = threadIdx.x >> 6;

@@ -18,10 +18,11 @@ __device__ __forceinline__ float root_decay(float e) { return __builtin_amdgcn_e
 // stretches add.  A thread has four states of a channel and one of 16 runs of
 // adjacent stretches: it joins its run, the runs meet in LDS, and it goes
 // through its run again from what reaches it.  The loads of eight stretches
-// are in flight at a time, and up to 128 stretches they are read once.  (One
+// are in flight at a time, and up to 129 stretches they are read once.  (One
 // thread over all of 64 stretches waited for memory 26 us, eight runs that
-// read twice took 15 us at 128.)  94 stretches of 1024 channels of 16 states: 9 us for 20 MB of
-// traffic, most of it the latency of two dependent trips to memory.
+// read twice took 15 us at 128.)  188 stretches of 1024 channels of 16 states, whose runs of 12 are read
+// twice: 10 us for 26 MB of ends, sums and starts (20 MB of it HBM's), most of it the latency of dependent
+// trips to memory.
 template <bool REV>
 __global__ __launch_bounds__(512) void ssm_scan_join_kernel(const float* __restrict__ ends, const float* __restrict__ sums,
                                                             float* __restrict__ starts, const float* __restrict__ A,
