@@ -344,7 +344,7 @@ typedef struct softmax_teacher {
 
 /* row_loss [M] float32 as above (without loss_scale) and dlogits [M][K] =
  * loss_scale * d(sum of row losses)/dlogits in the precision's type, row pitch
- * ldd.  dlogits may equal logits where ldd = ld. */
+ * ldd.  dlogits may equal logits where ldd = ld, and overlaps no input otherwise. */
 int softmax_distill_rows(const void* logits, int64_t ld, int64_t M, int32_t K, int32_t precision,
                          const softmax_teacher* teacher, float loss_scale, float* row_loss, void* dlogits,
                          int64_t ldd, hipStream_t stream);

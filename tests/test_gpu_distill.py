@@ -85,6 +85,25 @@ def test_topk_where_logits_bunch(gpu_lib, precision):
         check_topk(s.to(t).cuda(), k)
 
 
+@pytest.mark.parametrize("precision,K", [("fp32", 300), ("bf16", 9001), ("fp32", 40007), ("bf16", 70001)])
+@pytest.mark.parametrize("mask", [None, -1e9, -1e4, 1e9])
+def test_topk_of_masked_rows(gpu_lib, mask, precision, K):
+    """A few ordinary logits beside a mask's value (None: the type's lowest), fewer of them than k, and a row of nothing
+    else.  The rest of the lowest value over a temperature below one is past float32, so it starts at one."""
+    t = TYPES[precision]
+    m = torch.finfo(t).min if mask is None else mask
+    s = torch.full((3, K), m)
+    s[0, 5:45] = torch.linspace(-3, 3, 40)
+    s[1, [7, K - 1]] = torch.tensor([1.0, 2.0])
+    for tau in (1.0, 2.0, 3.0) if mask is None else (0.5, 1.0, 3.0):
+        for k in (4, 40, 130):
+            top, idx, rest = run_topk(s.to(t).cuda(), k, tau)
+            w, at = torch.sort(s.to(t).double(), 1, descending=True, stable=True)   # the lower class first
+            assert torch.equal(idx.cpu().long(), at[:, :k]) and torch.equal(top.double().cpu(), w[:, :k])
+            wr = torch.logsumexp(w[:, k:] / tau, 1)
+            assert bool(((rest.double().cpu() - wr).abs() <= TOL * (1 + wr.abs())).all())
+
+
 @pytest.mark.parametrize("precision", ["fp32", "bf16"])
 @pytest.mark.parametrize("k", [64, 65, 128])
 @pytest.mark.parametrize("K", [130, 4097, 8195, 16391, 32768, 33001])
