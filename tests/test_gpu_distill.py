@@ -98,7 +98,7 @@ def test_topk_of_masked_rows(gpu_lib, mask, precision, K):
     for tau in (1.0, 2.0, 3.0) if mask is None else (0.5, 1.0, 3.0):
         for k in (4, 40, 130):
             top, idx, rest = run_topk(s.to(t).cuda(), k, tau)
-            w, at = torch.sort(s.to(t).double(), 1, descending=True, stable=True)   # the lower class first
+            w, at = torch.sort(s.to(t).double(), dim=1, descending=True, stable=True)   # the lower class first
             assert torch.equal(idx.cpu().long(), at[:, :k]) and torch.equal(top.double().cpu(), w[:, :k])
             wr = torch.logsumexp(w[:, k:] / tau, 1)
             assert bool(((rest.double().cpu() - wr).abs() <= TOL * (1 + wr.abs())).all())
