@@ -115,8 +115,8 @@ template <typename TI, int V, int NV, int T> struct Row {
 // Waves of a SIMD that the registers are kept to.  Three rows on a CU instead
 // of two hide more of each other's barriers and waits: 2688 bf16 rows of 32000 (64
 // values a thread) 4 waves 56.5, 6 waves 49.3 us for the top, 82 and 77 for the loss with labels at
-// temperature 1, 95 and 88 at 3, although six waves spill one register at temperature 2 and two at other ones
-// than 1.  float32 rows of 64 values have no room for it.  (8 waves: the top of 12000 bf16 rows of 9001, 32
+// temperature 1, 95 and 88 at 3, although six waves spill one register at temperature 2 and two at others than
+// 1 and 2.  float32 rows of 64 values have no room for it.  (8 waves: the top of 12000 bf16 rows of 9001, 32
 // values a thread, 95 us, with 6 114.)
 template <typename TI, int T, int V, int NV> constexpr int waves_of() {
   if (NV == 0 || T > 512) return 4;
@@ -526,7 +526,7 @@ struct DistillP {
   float it2, tau, soft, hard, scale;   // it2: log2 e / tau
 };
 // Threads of a row of 32000: 512.  (2688 rows without labels, us: bf16 73, with 256 threads 108, with 1024
-// 125; float32 136, 426 and 155.  256 threads spill their 128 values; 1024 leave a CU one row, or two of 32 values.)
+// 125; float32 136, 426 and 155.  256 threads spill their 128 values; 1024 leave a CU one row or two.)
 template <int T> struct DistillLds {
   float pv[MAXK];
   int32_t iv[MAXK];
