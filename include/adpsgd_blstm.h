@@ -365,6 +365,100 @@ int softmax_distill_fwd_bwd(const blstm_dims* dims, const float* theta, const vo
                             const softmax_teacher* teacher, float loss_scale, float* loss, float* dy_top,
                             float* grad, void* ws, hipStream_t stream);
 
+/* ---------------------------------------------------------------------------
+ * Scoring: what a model says of given classes, for alignment, rescoring and
+ * confidences, and the gradient for training on sequences.
+ * ------------------------------------------------------------------------- */
+
+/* What is asked of every row.  With p = softmax(logits / temperature):
+ *   logprob [M][n] float32, log p of the classes ids [M][n] int32 (n = 0: none; up to
+ *           SOFTMAX_MAX_TOP); 0 where an id is outside 0..K-1 (a list that ends early)
+ *   entropy [M] float32 (or NULL), -sum p log p in nats; classes of logit -inf count 0
+ *   top     [M][k] float32, the log probabilities of the k most likely classes in descending order,
+ *   idx     [M][k] int32, those classes; among equal logits the lower class first
+ *           (k = 0: none; up to SOFTMAX_MAX_TOP)
+ * A row whose logits are all -inf has log probabilities of -inf and an entropy of 0; one that
+ * holds a NaN or +inf has NaN for both (idx orders a NaN above +inf).  At least one of the three is asked for. */
+typedef struct softmax_scores {
+  const int32_t* ids;
+  float* logprob;
+  float* entropy;
+  float* top;
+  int32_t* idx;
+  int32_t n, k;
+  float temperature;
+} softmax_scores;
+
+/* logits [M][K] of the precision's type, row pitch ld; K <= SOFTMAX_MAX_CLASSES, M < 2^22. */
+int softmax_logprob_rows(const void* logits, int64_t ld, int64_t M, int32_t K, int32_t precision,
+                         const softmax_scores* scores, hipStream_t stream);
+
+/* The loss gradients of logprob (dlogprob [M][n] float32, with its ids; n = 0: none) and of entropy
+ * (dentropy [M] float32, or NULL).  Those of top are given as dlogprob, with idx for ids.  A class listed twice
+ * has both; an id outside 0..K-1 has none. */
+typedef struct softmax_score_grads {
+  const int32_t* ids;
+  const float* dlogprob;
+  const float* dentropy;
+  int32_t n;
+  float temperature;
+} softmax_score_grads;
+
+/* dlogits [M][K] = the loss gradient of the logits, in the precision's type, row pitch ldd.  A row whose
+ * gradients are all 0, or whose logits are all -inf, has a gradient of 0 whatever it holds; one with a NaN or +inf
+ * has NaN.  dlogits may equal logits where ldd = ld, and overlaps no input otherwise. */
+int softmax_logprob_bwd_rows(const void* logits, int64_t ld, int64_t M, int32_t K, int32_t precision,
+                             const softmax_score_grads* grads, void* dlogits, int64_t ldd, hipStream_t stream);
+
+/* The two on the acoustic model's head, from y_top, for dims as in softmax_topk (ws: softmax_head_ws_bytes).
+ * softmax_logprob_bwd writes dy_top and the head slots of grad as softmax_ce_fwd_bwd does; y_top has to be
+ * finite. */
+int softmax_logprob(const blstm_dims* dims, const float* theta, const void* theta_lp, const void* y_top,
+                    const softmax_scores* scores, void* ws, hipStream_t stream);
+int softmax_logprob_bwd(const blstm_dims* dims, const float* theta, const void* theta_lp, const void* y_top,
+                        const softmax_score_grads* grads, float* dy_top, float* grad, void* ws, hipStream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * Products in 8-bit integers with a scale for each token (a row of x) and each
+ * channel (a row of the weights), for serving.
+ * Integers lie in rows of K columns, K a multiple of 16 and at most 131056, at a row pitch
+ * that 16 divides (at most 2^22), 16-byte aligned.  A matrix of fewer columns is padded with zeros,
+ * as int8_quantize_rows does.
+ * ------------------------------------------------------------------------- */
+
+/* Rows of x [M][K] (the precision's type, row pitch ldx) in integers:
+ *   scale [M] float32 = max |x| / 127 of the row
+ *   q     [M][Kq] = x / scale to the nearest integer (of x 127 / max |x| as it is, without a rounding
+ *         before that), ties to the even one; columns K..Kq-1 zero
+ * A row of zeros has a scale of 0; one with a NaN or an infinite value a scale of NaN, and integers of 0.
+ * For weights [N][K] as for tokens.  M < 2^22. */
+int int8_quantize_rows(const void* x, int64_t ldx, int64_t M, int32_t K, int32_t precision, int8_t* q, int64_t ldq,
+                       int32_t Kq, float* scale, hipStream_t stream);
+
+/* y[m][n] = float(sum_k q[m][k] w[n][k]) (x_scale[m] w_scale[n]) + bias[n]:
+ * the sum is exact, each step behind it a single float32 rounding, then one to the precision's type.
+ *   q [M][K], w [N][K] integers, x_scale [M], w_scale [N], bias [N] float32 (or NULL); y [M][N], row pitch ldy.
+ * M < 2^22, N < 2^24, and (M / 128) (N / 128) < 2^22, each rounded up. */
+int int8_linear(const int8_t* q, int64_t ldq, const float* x_scale, int64_t M, const int8_t* w, int64_t ldw,
+                const float* w_scale, int32_t N, int32_t K, const float* bias, void* y, int64_t ldy, int32_t precision,
+                hipStream_t stream);
+
+/* The same from tokens x [M][K] of the precision's type (also y's), quantised on the way; the weights have
+ * Kw >= K columns, those from K on zero.
+ *   ws  int8_linear_ws_bytes(M, Kw) bytes, 16-byte aligned; it belongs to one call (or one captured graph) at a time. */
+int int8_linear_ws_bytes(int64_t M, int32_t Kw, size_t* bytes);
+int int8_linear_rows(const void* x, int64_t ldx, int64_t M, int32_t K, int32_t precision, const int8_t* w, int64_t ldw,
+                     const float* w_scale, int32_t N, int32_t Kw, const float* bias, void* y, int64_t ldy, void* ws,
+                     hipStream_t stream);
+
+/* A head of 8-bit weights: softmax_logprob_rows of the logits int8_linear_rows gives in float32, from tokens
+ * x [M][P] and weights w [K][Kw] of K classes.  The logits are the same bits as there.
+ *   ws  int8_logprob_ws_bytes(M, K, Kw) bytes, as above. */
+int int8_logprob_ws_bytes(int64_t M, int32_t K, int32_t Kw, size_t* bytes);
+int int8_logprob_rows(const void* x, int64_t ldx, int64_t M, int32_t P, int32_t precision, const int8_t* w, int64_t ldw,
+                      const float* w_scale, int32_t K, int32_t Kw, const float* bias, const softmax_scores* scores,
+                      void* ws, hipStream_t stream);
+
 /* Message describing the last failure on the calling thread ("" if none). */
 const char* blstm_last_error(void);
 

@@ -29,7 +29,9 @@ EXPORTED = ("blstm_param_count", "blstm_workspace_bytes", "blstm_pack_params", "
             "blstm_recurrence_ok", "blstm_last_error", "blstm_timing_begin", "blstm_timing_end",
             "ssm_workspace_bytes", "ssm_conv_fwd", "ssm_conv_bwd", "ssm_conv_step", "ssm_scan_fwd", "ssm_scan_bwd",
             "ssm_scan_step", "softmax_topk_rows", "softmax_distill_rows", "softmax_head_ws_bytes", "softmax_topk",
-            "softmax_distill_fwd_bwd")
+            "softmax_distill_fwd_bwd", "softmax_logprob_rows", "softmax_logprob_bwd_rows", "softmax_logprob",
+            "softmax_logprob_bwd", "int8_quantize_rows", "int8_linear", "int8_linear_ws_bytes", "int8_linear_rows",
+            "int8_logprob_ws_bytes", "int8_logprob_rows")
 SSM_SOFTPLUS = 1
 SSM_SILU = 2
 SOFTMAX_MAX_TOP = 256                  # most listed classes a row (adpsgd_blstm.h)
@@ -59,6 +61,16 @@ class SsmScanGrads(ctypes.Structure):
 class SoftmaxTeacher(ctypes.Structure):
     _fields_ = ([(n, ctypes.c_void_p) for n in ("top", "idx", "rest", "labels", "weights")] +
                 [("k", ctypes.c_int32)] + [(n, ctypes.c_float) for n in ("temperature", "soft", "hard")])
+
+
+class SoftmaxScores(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("ids", "logprob", "entropy", "top", "idx")] +
+                [("n", ctypes.c_int32), ("k", ctypes.c_int32), ("temperature", ctypes.c_float)])
+
+
+class SoftmaxScoreGrads(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("ids", "dlogprob", "dentropy")] +
+                [("n", ctypes.c_int32), ("temperature", ctypes.c_float)])
 
 
 class KernelTime(ctypes.Structure):
@@ -117,7 +129,18 @@ def lib():
         L.softmax_head_ws_bytes.argtypes = [DP, ctypes.POINTER(S)]
         L.softmax_topk.argtypes = [DP, P, P, P, I, F, P, P, P, P, P]
         L.softmax_distill_fwd_bwd.argtypes = [DP, P, P, P, ST, F, P, P, P, P, P]
-        for name in EXPORTED[-12:]:
+        SS, SP = ctypes.POINTER(SoftmaxScores), ctypes.POINTER(SoftmaxScoreGrads)
+        L.softmax_logprob_rows.argtypes = [P, I64, I64, I, I, SS, P]
+        L.softmax_logprob_bwd_rows.argtypes = [P, I64, I64, I, I, SP, P, I64, P]
+        L.softmax_logprob.argtypes = [DP, P, P, P, SS, P, P]
+        L.softmax_logprob_bwd.argtypes = [DP, P, P, P, SP, P, P, P, P]
+        L.int8_quantize_rows.argtypes = [P, I64, I64, I, I, P, I64, I, P, P]
+        L.int8_linear.argtypes = [P, I64, P, I64, P, I64, P, I, I, P, P, I64, I, P]
+        L.int8_linear_ws_bytes.argtypes = [I64, I, ctypes.POINTER(S)]
+        L.int8_linear_rows.argtypes = [P, I64, I64, I, I, P, I64, P, I, I, P, P, I64, P, P]
+        L.int8_logprob_ws_bytes.argtypes = [I64, I, I, ctypes.POINTER(S)]
+        L.int8_logprob_rows.argtypes = [P, I64, I64, I, I, P, I64, P, I, I, P, SS, P, P]
+        for name in EXPORTED[-22:]:
             getattr(L, name).restype = ctypes.c_int
         for name in ("blstm_workspace_bytes", "blstm_pack_params", "blstm_fwd", "softmax_ce_fwd_bwd",
                      "softmax_ce_fwd_bwd_static",
@@ -519,3 +542,145 @@ def softmax_distill_fwd_bwd(dims, theta, theta_lp, y_top, top, idx, loss_scale, 
                  _have("loss", loss, (1,), torch.float32, dev),
                  _have("dy_top", dy_top, (dims.T, dims.B, 2 * dims.H), torch.float32, dev),
                  _have("grad", grad, tuple(theta.shape), torch.float32, dev), pw)
+
+
+# --------------------------------------------------------------------- scoring ---
+def _scores(M, dev, ids, logprob, entropy, top, idx, temperature):
+    n = 0 if ids is None else ids.shape[-1]
+    k = 0 if top is None else top.shape[-1]
+    f, i = torch.float32, torch.int32
+    if (ids is None) != (logprob is None) or (top is None) != (idx is None):
+        raise ValueError("ids and logprob belong together, and top and idx")
+    return SoftmaxScores(_have("ids", ids, (M, n), i, dev, True), _have("logprob", logprob, (M, n), f, dev, True),
+                         _have("entropy", entropy, (M,), f, dev, True), _have("top", top, (M, k), f, dev, True),
+                         _have("idx", idx, (M, k), i, dev, True), n, k, temperature)
+
+
+def _score_grads(M, dev, ids, dlogprob, dentropy, temperature):
+    n = 0 if ids is None else ids.shape[-1]
+    if (ids is None) != (dlogprob is None):
+        raise ValueError("ids and dlogprob belong together")
+    return SoftmaxScoreGrads(_have("ids", ids, (M, n), torch.int32, dev, True),
+                             _have("dlogprob", dlogprob, (M, n), torch.float32, dev, True),
+                             _have("dentropy", dentropy, (M,), torch.float32, dev, True), n, temperature)
+
+
+def softmax_logprob_rows(logits, ids=None, logprob=None, entropy=None, top=None, idx=None, temperature=1.0,
+                         stream=None):
+    """n is ids' width, k top's."""
+    p, ld, M, K, prec = _logits(logits)
+    dev = logits.get_device()
+    q = _scores(M, dev, ids, logprob, entropy, top, idx, temperature)
+    return _call("softmax_logprob_rows", dev, stream, p, ld, M, K, prec, ctypes.byref(q))
+
+
+def softmax_logprob_bwd_rows(logits, dlogits, ids=None, dlogprob=None, dentropy=None, temperature=1.0, stream=None):
+    p, ld, M, K, prec = _logits(logits)
+    dev = logits.get_device()
+    g = _score_grads(M, dev, ids, dlogprob, dentropy, temperature)
+    pd, ldd = _rows("dlogits", dlogits, (M, K), logits.dtype, dev)
+    return _call("softmax_logprob_bwd_rows", dev, stream, p, ld, M, K, prec, ctypes.byref(g), pd, ldd)
+
+
+def softmax_logprob(dims, theta, theta_lp, y_top, ws, ids=None, logprob=None, entropy=None, top=None, idx=None,
+                    temperature=1.0, stream=None):
+    """softmax_logprob_rows of the head's logits; ids, logprob [T*B][n], entropy [T*B], top, idx [T*B][k]."""
+    dev = _on(y_top)
+    pt, pl, py, pw = _head_args(dims, dev, theta, theta_lp, y_top, ws)
+    q = _scores(dims.T * dims.B, dev, ids, logprob, entropy, top, idx, temperature)
+    return _call("softmax_logprob", dev, stream, ctypes.byref(dims), pt, pl, py, ctypes.byref(q), pw)
+
+
+def softmax_logprob_bwd(dims, theta, theta_lp, y_top, dy_top, grad, ws, ids=None, dlogprob=None, dentropy=None,
+                        temperature=1.0, stream=None):
+    dev = _on(y_top)
+    pt, pl, py, pw = _head_args(dims, dev, theta, theta_lp, y_top, ws)
+    g = _score_grads(dims.T * dims.B, dev, ids, dlogprob, dentropy, temperature)
+    return _call("softmax_logprob_bwd", dev, stream, ctypes.byref(dims), pt, pl, py, ctypes.byref(g),
+                 _have("dy_top", dy_top, (dims.T, dims.B, 2 * dims.H), torch.float32, dev),
+                 _have("grad", grad, tuple(theta.shape), torch.float32, dev), pw)
+
+
+# ----------------------------------------------------------------- 8-bit products ---
+def _ints(name, q, rows, dev):
+    """(address, row pitch, columns) of rows of 8-bit integers."""
+    if q is None or q.dim() != 2 or q.shape[0] != rows or q.dtype != torch.int8:
+        raise ValueError(f"{name} must be {rows} rows of int8" + ("" if q is None else f": got {q.dtype} {tuple(q.shape)}"))
+    p, ld = _rows(name, q, tuple(q.shape), torch.int8, dev)
+    return p, ld, q.shape[1]
+
+
+def _floats(name, x, dev):
+    """(address, row pitch, rows, columns, precision) of rows of bfloat16 or float32."""
+    if x.dim() != 2 or x.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError(f"{name} must be bfloat16 or float32 rows: got {x.dtype} {tuple(x.shape)}")
+    p, ld = _rows(name, x, tuple(x.shape), x.dtype, dev)
+    return p, ld, x.shape[0], x.shape[1], BLSTM_BF16 if x.dtype == torch.bfloat16 else BLSTM_FP32
+
+
+def int8_quantize_rows(x, q, scale, stream=None):
+    """q [M][Kq], Kq at least x's columns and a multiple of 16; scale [M]."""
+    dev = _on(x)
+    p, ld, M, K, prec = _floats("x", x, dev)
+    pq, ldq, Kq = _ints("q", q, M, dev)
+    return _call("int8_quantize_rows", dev, stream, p, ld, M, K, prec, pq, ldq, Kq,
+                 _have("scale", scale, (M,), torch.float32, dev))
+
+
+def int8_linear(q, q_scale, w, w_scale, y, bias=None, stream=None):
+    """q [M][K], w [N][K] integers; y [M][N] bfloat16 or float32."""
+    dev, f = _on(q), torch.float32
+    py, ldy, M, N, prec = _floats("y", y, dev)
+    pq, ldq, K = _ints("q", q, M, dev)
+    pw, ldw, Kw = _ints("w", w, N, dev)
+    if K != Kw:
+        raise ValueError(f"q has {K} columns, w {Kw}")
+    return _call("int8_linear", dev, stream, pq, ldq, _have("q_scale", q_scale, (M,), f, dev), M, pw, ldw,
+                 _have("w_scale", w_scale, (N,), f, dev), N, K, _have("bias", bias, (N,), f, dev, True), py, ldy, prec)
+
+
+_INT8_SIZES = {}   # workspace sizes by arguments: asking for them costs a tenth of a small call
+
+
+def _int8_bytes(fn, *args):
+    n = _INT8_SIZES.get((fn, args))
+    if n is None:
+        v = ctypes.c_size_t()
+        _check(fn, getattr(lib(), fn)(*args, ctypes.byref(v)))
+        if len(_INT8_SIZES) > 4096:
+            _INT8_SIZES.clear()
+        n = _INT8_SIZES[fn, args] = v.value
+    return n
+
+
+def int8_linear_ws_bytes(M: int, Kw: int) -> int:
+    return _int8_bytes("int8_linear_ws_bytes", M, Kw)
+
+
+def int8_linear_rows(x, w, w_scale, y, ws, bias=None, stream=None):
+    """x [M][K], w [N][Kw] integers with Kw >= K; y [M][N] of x's type."""
+    dev, f = _on(x), torch.float32
+    p, ld, M, K, prec = _floats("x", x, dev)
+    N = y.shape[-1]
+    pw, ldw, Kw = _ints("w", w, N, dev)
+    py, ldy = _rows("y", y, (M, N), x.dtype, dev)
+    return _call("int8_linear_rows", dev, stream, p, ld, M, K, prec, pw, ldw, _have("w_scale", w_scale, (N,), f, dev),
+                 N, Kw, _have("bias", bias, (N,), f, dev, True), py, ldy,
+                 _bytes("ws", ws, int8_linear_ws_bytes(M, Kw), dev))
+
+
+def int8_logprob_ws_bytes(M: int, K: int, Kw: int) -> int:
+    return _int8_bytes("int8_logprob_ws_bytes", M, K, Kw)
+
+
+def int8_logprob_rows(x, w, w_scale, ws, bias=None, ids=None, logprob=None, entropy=None, top=None, idx=None,
+                      temperature=1.0, stream=None):
+    """x [M][P], w [K][Kw] integers with Kw >= P, of K classes."""
+    dev, f = _on(x), torch.float32
+    p, ld, M, P, prec = _floats("x", x, dev)
+    K = w.shape[0]
+    pw, ldw, Kw = _ints("w", w, K, dev)
+    q = _scores(M, dev, ids, logprob, entropy, top, idx, temperature)
+    return _call("int8_logprob_rows", dev, stream, p, ld, M, P, prec, pw, ldw,
+                 _have("w_scale", w_scale, (K,), f, dev), K, Kw, _have("bias", bias, (K,), f, dev, True),
+                 ctypes.byref(q), _bytes("ws", ws, int8_logprob_ws_bytes(M, K, Kw), dev))

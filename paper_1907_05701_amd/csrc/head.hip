@@ -17,6 +17,7 @@
 
 #include "common.hpp"
 #include "distill.hpp"
+#include "score.hpp"
 #include "gemm_kc.hpp"
 #include "reduce.hpp"
 
@@ -1038,12 +1039,14 @@ static float* head_logits(const Layout& lo, const float* theta, const T* W, char
   return S;
 }
 
-// The head forward and backward: against labels, or with `teacher` given
-// against a teacher's top logits.
+// The head forward and backward: against labels, with `teacher` given
+// against a teacher's top logits, or with `given` from the gradients of
+// its log probabilities (no loss then).
 template <typename T>
 static int head_impl(const Layout& lo, const float* theta, const T* W, const T* ytop,
                      const int32_t* labels, float scale, float* loss, float* dytop, float* grad,
-                     char* hws, hipStream_t s, const softmax_teacher* teacher = nullptr) {
+                     char* hws, hipStream_t s, const softmax_teacher* teacher = nullptr,
+                     const softmax_score_grads* given = nullptr) {
   constexpr int V = VecH<T>::v;
   const int64_t M = lo.M;
   const int P = lo.P, K = lo.K, Kp = lo.Kp, H2 = 2 * lo.H;
@@ -1057,12 +1060,17 @@ static int head_impl(const Layout& lo, const float* theta, const T* W, const T* 
   head_z<T>(lo, theta, W, ytop, hws, s);
   constexpr bool lp = std::is_same<T, bf16>::value;
   T* DS = (T*)(hws + lo.S);
-  if (teacher) {
+  if (teacher || given) {
     // float32: every row's logits have their place, overwritten by ds
     const int64_t step = head_rows(lo);
     for (int64_t r0 = 0; r0 < M; r0 += step) {
       const int64_t n = std::min(step, M - r0);
       const float* S = head_logits<T>(lo, theta, W, hws, r0, n, s);
+      if (given) {
+        const int rc = score_grad_rows<float, T>(S, Kp, n, K, score_grads_from(*given, r0), DS + r0 * Kp, Kp, Kp - K, s);
+        if (rc) return rc;
+        continue;
+      }
       softmax_teacher t = *teacher;
       t.top += r0 * t.k;
       t.idx += r0 * t.k;
@@ -1072,7 +1080,7 @@ static int head_impl(const Layout& lo, const float* theta, const T* W, const T* 
       const int rc = distill_rows<float, T>(S, Kp, n, K, &t, scale, RL + r0, DS + r0 * Kp, Kp, Kp - K, s);
       if (rc) return rc;
     }
-    BLSTM_LAUNCH("loss_sum", loss_sum_kernel, dim3(1), dim3(256), 0, s, RL, M, scale, loss);
+    if (teacher) BLSTM_LAUNCH("loss_sum", loss_sum_kernel, dim3(1), dim3(256), 0, s, RL, M, scale, loss);
   } else if constexpr (lp) {
     // logits transposed (classes x frames) twice: strip statistics, then ds,
     // the frame losses and the db_s partials
@@ -1191,10 +1199,10 @@ static int head_impl(const Layout& lo, const float* theta, const T* W, const T* 
                                    lo.big_dz);
   }
   // db_s and db_l, the sums over frames of ds and dz (bf16: already done, but not
-  // against a teacher: there in float32 of the rounded ds that the products read, each term off by at
+  // against a teacher or from given gradients: there in float32 of the rounded ds that the products read, each term off by at
   // most 2^-8 of itself, as in dW_s; the float32 ones are not kept)
   if constexpr (lp) {
-    if (teacher) {
+    if (teacher || given) {
       colsum<T>("colsum_dbs", s, DS, M, K, Kp, (float*)(hws + lo.head_bytes + head_logits_bytes(lo)), K, 0,
                 grad + lo.bs, nullptr);
       colsum<float>("colsum_dbl", s, DZ, M, P, P, part, P, 0, grad + lo.bl, nullptr);
@@ -1373,4 +1381,52 @@ extern "C" int softmax_distill_fwd_bwd(const blstm_dims* dims, const float* thet
   }
   return head_impl<float>(lo, theta, theta, (const float*)y_top, nullptr, loss_scale, loss, dy_top, grad, (char*)ws,
                           stream, teacher);
+}
+
+// ---------------------------------------------------------------------------
+// Scoring on the head.
+// ---------------------------------------------------------------------------
+template <typename T>
+static int scores_impl(const Layout& lo, const float* theta, const T* W, const T* ytop, const softmax_scores& q, char* ws,
+                       hipStream_t s) {
+  head_z<T>(lo, theta, W, ytop, ws, s);
+  const int64_t step = head_rows(lo);
+  for (int64_t r0 = 0; r0 < lo.M; r0 += step) {
+    const int64_t n = std::min(step, lo.M - r0);
+    const float* S = head_logits<T>(lo, theta, W, ws, r0, n, s);
+    const int rc = score_rows<float>(S, lo.Kp, n, lo.K, scores_from(q, r0), s);
+    if (rc) return rc;
+  }
+  return BLSTM_OK;
+}
+
+extern "C" int softmax_logprob(const blstm_dims* dims, const float* theta, const void* theta_lp, const void* y_top,
+                               const softmax_scores* scores, void* ws, hipStream_t stream) {
+  Layout lo;
+  int rc = make_layout(dims, &lo);
+  if (!rc) rc = check_scores(scores, lo.K, "softmax_logprob");
+  if (rc) return rc;
+  if (!theta || !y_top || !ws) return blstm_fail(BLSTM_EINVAL, "softmax_logprob: NULL pointer");
+  if (lo.prec == BLSTM_BF16) {
+    if (!theta_lp) return blstm_fail(BLSTM_EINVAL, "softmax_logprob: theta_lp is NULL (bf16)");
+    return scores_impl<bf16>(lo, theta, (const bf16*)theta_lp, (const bf16*)y_top, *scores, (char*)ws, stream);
+  }
+  return scores_impl<float>(lo, theta, theta, (const float*)y_top, *scores, (char*)ws, stream);
+}
+
+extern "C" int softmax_logprob_bwd(const blstm_dims* dims, const float* theta, const void* theta_lp, const void* y_top,
+                                   const softmax_score_grads* grads, float* dy_top, float* grad, void* ws,
+                                   hipStream_t stream) {
+  Layout lo;
+  int rc = make_layout(dims, &lo);
+  if (!rc) rc = check_score_grads(grads, lo.K, "softmax_logprob_bwd");
+  if (rc) return rc;
+  if (!theta || !y_top || !dy_top || !grad || !ws) return blstm_fail(BLSTM_EINVAL, "softmax_logprob_bwd: NULL pointer");
+  if (lo.prec == BLSTM_BF16) {
+    if (!theta_lp) return blstm_fail(BLSTM_EINVAL, "softmax_logprob_bwd: theta_lp is NULL (bf16)");
+    return head_impl<bf16>(lo, theta, (const bf16*)theta_lp, (const bf16*)y_top, nullptr, 1.f, nullptr, dy_top, grad,
+                           (char*)ws, stream, nullptr, grads);
+  }
+  return head_impl<float>(lo, theta, theta, (const float*)y_top, nullptr, 1.f, nullptr, dy_top, grad, (char*)ws, stream,
+                          nullptr, grads);
 }

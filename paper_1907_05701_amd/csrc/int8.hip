@@ -1,0 +1,406 @@
+// Products in 8-bit integers with a scale for each token and each channel:
+//   y[m][n] = float(sum_k q[m][k] w[n][k]) (x_scale[m] w_scale[n]) + bias[n]
+// The sum is exact, and each step behind it one float32 rounding, so that every kernel here gives the same bits.
+#include <math.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "gemm_kc.hpp"
+#include "int8.hpp"
+#include "score.hpp"
+
+// ---------------------------------------------------------------------------
+// Tokens to integers.  T threads a row (a wave, or a workgroup of 256); a row
+// of up to NV vectors a thread is read once, longer ones (NV = 0) twice.
+// ---------------------------------------------------------------------------
+template <typename TI> struct Vec8;
+template <> struct Vec8<bf16> { static constexpr int n = 8; };
+template <> struct Vec8<float> { static constexpr int n = 4; };
+
+template <typename TI, int T, int NV>
+__global__ __launch_bounds__(256) void quantize_rows_kernel(const TI* __restrict__ x, int64_t ldx, int64_t M, int K,
+                                                            int8_t* __restrict__ q, int64_t ldq, int Kq,
+                                                            float* __restrict__ scale) {
+  constexpr int V = Vec8<TI>::n, NR = NV ? NV : 1;
+  __shared__ float buf[4];
+  const int tid = T == 64 ? threadIdx.x & 63 : threadIdx.x;
+  const int64_t m = T == 64 ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
+  if (T == 64 && m >= M) return;   // no barrier there
+  const TI* s = x + m * ldx;
+  int8_t* d = q + m * ldq;
+  TI v[NR][V];
+  float mx = 0.f;
+  auto load = [&](int c, TI (&o)[V]) {
+    if (c + V <= K) {
+      __builtin_memcpy(o, s + c, V * sizeof(TI));
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j) o[j] = c + j < K ? s[c + j] : from_f32<TI>(0.f);
+    }
+  };
+  auto see = [&](const TI (&o)[V]) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const float a = fabsf(to_f32(o[j]));
+      mx = mx > a || mx != mx ? mx : a;   // a NaN stays
+    }
+  };
+  if constexpr (NV > 0) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) load((i * T + tid) * V, v[i]);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) see(v[i]);
+  } else {
+    for (int c = tid * V; c < K; c += T * V) {
+      load(c, v[0]);
+      see(v[0]);
+    }
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    const float a = __shfl_xor(mx, o);
+    mx = mx > a || mx != mx ? mx : a;
+  }
+  if constexpr (T == 256) {
+    if ((tid & 63) == 0) buf[tid >> 6] = mx;
+    __syncthreads();
+    mx = buf[0];
+#pragma unroll
+    for (int i = 1; i < 4; ++i) mx = mx > buf[i] || mx != mx ? mx : buf[i];
+  }
+  const Quant to(mx);
+  if (tid == 0) scale[m] = to.scale;
+  auto store = [&](int c, const TI (&o)[V]) {
+    if (c >= Kq) return;   // Kq is a multiple of V
+    uint32_t w[V / 4];
+#pragma unroll
+    for (int j = 0; j < V / 4; ++j)
+      w[j] = pack4(to(to_f32(o[4 * j])), to(to_f32(o[4 * j + 1])), to(to_f32(o[4 * j + 2])), to(to_f32(o[4 * j + 3])));
+    __builtin_memcpy(d + c, w, V);
+  };
+  if constexpr (NV > 0) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) store((i * T + tid) * V, v[i]);
+  } else {
+    for (int c = tid * V; c < Kq; c += T * V) {
+      load(c, v[0]);
+      store(c, v[0]);
+    }
+  }
+}
+
+template <typename TI>
+void int8_quantize(const TI* x, int64_t ldx, int64_t M, int32_t K, int8_t* q, int64_t ldq, int32_t Kq, float* scale,
+                   hipStream_t stream) {
+  constexpr int V = Vec8<TI>::n;
+  auto launch = [&](auto t, auto nv) {
+    constexpr int T = decltype(t)::value, NV = decltype(nv)::value;
+    BLSTM_LAUNCH("int8_quantize_rows", (quantize_rows_kernel<TI, T, NV>), dim3((unsigned)(T == 64 ? cdiv(M, 4) : M)),
+                 dim3(256), 0, stream, x, ldx, M, (int)K, q, ldq, (int)Kq, scale);
+  };
+#define INT(n) std::integral_constant<int, n>{}
+  if (Kq <= 64 * V) launch(INT(64), INT(1));
+  else if (Kq <= 2 * 64 * V) launch(INT(64), INT(2));
+  else if (Kq <= 4 * 64 * V) launch(INT(64), INT(4));
+  else if (Kq <= 4 * 256 * V) launch(INT(256), INT(4));
+  else launch(INT(256), INT(0));
+#undef INT
+}
+template void int8_quantize<float>(const float*, int64_t, int64_t, int32_t, int8_t*, int64_t, int32_t, float*, hipStream_t);
+template void int8_quantize<bf16>(const bf16*, int64_t, int64_t, int32_t, int8_t*, int64_t, int32_t, float*, hipStream_t);
+
+// ---------------------------------------------------------------------------
+// The product.
+// ---------------------------------------------------------------------------
+struct Int8P {
+  const int8_t *x, *w;
+  int64_t ldx, ldw, ldy, M, N;   // M tokens, N channels
+  int K;
+  const float *xs, *ws, *bias;
+  void* y;
+  // tiles
+  int ntm, ntn, gm, total;
+};
+
+// Four channels of a token, from n on.
+template <typename TO>
+__device__ __forceinline__ void put4(const Int8P& p, int64_t m, int64_t n, i32x4 a) {
+  if (m >= p.M || n >= p.N) return;
+  TO* y = (TO*)p.y + m * p.ldy + n;
+  const float xs = p.xs[m];
+  TO o[4];
+  if (n + 4 <= p.N) {
+    float w[4], b[4] = {0.f, 0.f, 0.f, 0.f};
+    __builtin_memcpy(w, p.ws + n, 16);
+    if (p.bias) __builtin_memcpy(b, p.bias + n, 16);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[j] = from_f32<TO>(int8_value(a[j], scale_of(xs, w[j]), b[j]));
+    __builtin_memcpy(y, o, sizeof o);
+  } else {
+    for (int j = 0; j < 4 && n + j < p.N; ++j)
+      y[j] = from_f32<TO>(int8_value(a[j], scale_of(xs, p.ws[n + j]), p.bias ? p.bias[n + j] : 0.f));
+  }
+}
+
+// 128-byte rows of 8 chunks in LDS, chunk c of row r in slot kc_slot<64>(c, r).
+template <int ROWS, int NW>
+__device__ __forceinline__ void stage(const int8_t* base, int64_t ld, int64_t rows, int k0, int K, char* tile, int wid,
+                                      int lane) {
+  const __amdgpu_buffer_rsrc_t r = dma_rsrc(base);
+  constexpr int LOADS = ROWS / 8 / NW;
+#pragma unroll
+  for (int i = 0; i < LOADS; ++i) {
+    const int row = (i * NW + wid) * 8 + lane / 8;
+    const int k = k0 + kc_slot<64>(lane % 8, row) * 16;
+    dma16(r, row < rows && k < K ? (uint32_t)(row * ld + k) : DMA_OFF_NONE, tile + (i * NW + wid) * 1024);
+  }
+}
+
+// BM channels x BN tokens a workgroup of WM x WN waves, 128 k at a time, two stages.
+template <typename TO, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(WM * WN * 64) void int8_tile_kernel(const Int8P p) {
+  constexpr int NW = WM * WN, FM = BM / WM / 16, FN = BN / WN / 16, STAGE = (BM + BN) * 128;
+  constexpr int LOADS = (BM + BN) / 8 / NW;
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, wm = wid % WM, wn = wid / WM;
+  int z, tm, tn;
+  kc_tile_of(p, blockIdx.x, p.gm, z, tm, tn);
+  const int64_t n0 = (int64_t)tm * BM, m0 = (int64_t)tn * BN;
+  const int steps = (p.K + 127) / 128;
+  const int8_t *wb = p.w + n0 * p.ldw, *xb = p.x + m0 * p.ldx;
+  auto issue = [&](int j) {
+    char* st = lds + (j & 1) * STAGE;
+    stage<BM, NW>(wb, p.ldw, p.N - n0, j * 128, p.K, st, wid, lane);
+    stage<BN, NW>(xb, p.ldx, p.M - m0, j * 128, p.K, st + BM * 128, wid, lane);
+  };
+  i32x4 acc[FM][FN];
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+  const int fr = lane & 15, fc = lane >> 4;
+  issue(0);
+  for (int it = 0; it < steps; ++it) {
+    kc_wait_vm<0>();
+    kc_barrier();
+    if (it + 1 < steps) issue(it + 1);
+    const char* st = lds + (it & 1) * STAGE;
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      i32x4 a[FM], b[FN];
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+        a[i] = *(const i32x4*)(st + (wm * (BM / WM) + i * 16 + fr) * 128 + kc_slot<64>(ks * 4 + fc, fr) * 16);
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+        b[j] = *(const i32x4*)(st + BM * 128 + (wn * (BN / WN) + j * 16 + fr) * 128 + kc_slot<64>(ks * 4 + fc, fr) * 16);
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = mma_i8(a[i], b[j], acc[i][j]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+      put4<TO>(p, m0 + wn * (BN / WN) + j * 16 + fr, n0 + wm * (BM / WM) + i * 16 + 4 * fc, acc[i][j]);
+  (void)LOADS;
+}
+
+// Few tokens: 16 channels and up to 16 FN tokens a workgroup, whose four waves
+// each take every fourth 64 of K, both operands straight from memory.
+template <typename TO, int FN>
+__global__ __launch_bounds__(256) void int8_few_kernel(const Int8P p) {
+  __shared__ i32x4 part[3][FN][64];
+  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, fr = lane & 15, fc = lane >> 4;
+  const int64_t n0 = (int64_t)blockIdx.x * 16, m0 = (int64_t)blockIdx.y * 16 * FN;
+  const int8_t* wr = p.w + min(n0 + fr, p.N - 1) * p.ldw;   // rows past the last: any, dropped at the end
+  const int8_t* xr[FN];
+#pragma unroll
+  for (int j = 0; j < FN; ++j) xr[j] = p.x + min(m0 + j * 16 + fr, p.M - 1) * p.ldx;
+  i32x4 acc[FN];
+#pragma unroll
+  for (int j = 0; j < FN; ++j) acc[j] = i32x4{0, 0, 0, 0};
+#pragma unroll 4
+  for (int k = wid * 64 + fc * 16; k < p.K + fc * 16; k += 256) {
+    const bool in = k < p.K;   // both operands zero behind K
+    const i32x4 a = in ? *(const i32x4*)(wr + k) : i32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+      const i32x4 b = in ? *(const i32x4*)(xr[j] + k) : i32x4{0, 0, 0, 0};
+      acc[j] = mma_i8(a, b, acc[j]);
+    }
+  }
+  if (wid > 0) {
+#pragma unroll
+    for (int j = 0; j < FN; ++j) part[wid - 1][j][lane] = acc[j];
+  }
+  __syncthreads();
+  if (wid > 0) return;
+#pragma unroll
+  for (int j = 0; j < FN; ++j)
+    put4<TO>(p, m0 + j * 16 + fr, n0 + 4 * fc, acc[j] + part[0][j][lane] + part[1][j][lane] + part[2][j][lane]);
+}
+
+template <typename TO>
+static void product(Int8P p, hipStream_t s) {
+  if (p.M <= 64) {
+    const int fn = (int)cdiv(p.M, 16);
+    const dim3 grid((unsigned)cdiv(p.N, 16), 1);
+    if (fn == 1) BLSTM_LAUNCH("int8_linear_few", (int8_few_kernel<TO, 1>), grid, dim3(256), 0, s, p);
+    else if (fn == 2) BLSTM_LAUNCH("int8_linear_few", (int8_few_kernel<TO, 2>), grid, dim3(256), 0, s, p);
+    else BLSTM_LAUNCH("int8_linear_few", (int8_few_kernel<TO, 4>), grid, dim3(256), 0, s, p);
+    return;
+  }
+  auto tile = [&](auto bm, auto bn, auto wm, auto wn) {
+    constexpr int BM = decltype(bm)::value, BN = decltype(bn)::value, WM = decltype(wm)::value, WN = decltype(wn)::value;
+    constexpr size_t bytes = 2 * (BM + BN) * 128;
+    auto fn = int8_tile_kernel<TO, BM, BN, WM, WN>;
+    static std::atomic<uint64_t> raised{0};
+    kc_raise_lds_limit((const void*)fn, bytes, raised);
+    p.ntm = (int)cdiv(p.N, BM);
+    p.ntn = (int)cdiv(p.M, BN);
+    p.gm = kc_group_rows;
+    p.total = p.ntm * p.ntn;
+    BLSTM_LAUNCH("int8_linear", fn, dim3((unsigned)p.total), dim3(WM * WN * 64), bytes, s, p);
+  };
+#define INT(n) std::integral_constant<int, n>{}
+  if (cdiv(p.M, 256) * cdiv(p.N, 256) >= 256) tile(INT(256), INT(256), INT(2), INT(4));
+  else tile(INT(128), INT(128), INT(2), INT(4));
+#undef INT
+}
+
+// ---------------------------------------------------------------------------
+// Host side.
+// ---------------------------------------------------------------------------
+static bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+static int check_precision(const char* fn, int32_t precision) {
+  return precision == BLSTM_FP32 || precision == BLSTM_BF16
+             ? BLSTM_OK
+             : blstm_fail(BLSTM_EINVAL, "%s: precision must be BLSTM_FP32 or BLSTM_BF16", fn);
+}
+// Rows of integers: K columns, a multiple of 16, at a pitch of 16-byte pieces.
+static int check_ints(const char* fn, const char* what, const int8_t* q, int64_t ld, int32_t K) {
+  if (!q) return blstm_fail(BLSTM_EINVAL, "%s: NULL pointer", fn);
+  if (K % 16 || ld % 16 || !aligned16(q))
+    return blstm_fail(BLSTM_EINVAL, "%s: %s's columns and row pitch must be multiples of 16, its address 16-byte aligned", fn, what);
+  if (ld < K) return blstm_fail(BLSTM_EINVAL, "%s: a row pitch is below its row", fn);
+  if (K > INT8_MAX_K || ld > INT8_MAX_LD)
+    return blstm_fail(BLSTM_EUNSUPPORTED, "%s: %s's rows are too long", fn, what);
+  return BLSTM_OK;
+}
+static int check_sizes(const char* fn, int64_t M, int64_t N, int64_t K) {
+  if (M < 1 || N < 1 || K < 1)
+    return blstm_fail(BLSTM_EINVAL, "%s: sizes must be positive (%lld, %lld, %lld)", fn, (long long)M, (long long)N, (long long)K);
+  if (M > LAUNCH_THREADS / 1024 || N >= 1 << 24 || cdiv(M, 128) * cdiv(N, 128) > LAUNCH_THREADS / 1024)
+    return blstm_fail(BLSTM_EUNSUPPORTED, "%s: too many rows", fn);
+  return BLSTM_OK;
+}
+
+extern "C" int int8_quantize_rows(const void* x, int64_t ldx, int64_t M, int32_t K, int32_t precision, int8_t* q,
+                                  int64_t ldq, int32_t Kq, float* scale, hipStream_t stream) {
+  const char* fn = "int8_quantize_rows";
+  int rc = check_sizes(fn, M, 1, K);
+  if (!rc) rc = check_precision(fn, precision);
+  if (!rc) rc = check_ints(fn, "q", q, ldq, Kq);
+  if (rc) return rc;
+  if (!x || !scale) return blstm_fail(BLSTM_EINVAL, "%s: NULL pointer", fn);
+  if (ldx < K || Kq < K) return blstm_fail(BLSTM_EINVAL, "%s: a row is longer than its pitch or q's columns", fn);
+  if (precision == BLSTM_BF16) int8_quantize((const bf16*)x, ldx, M, K, q, ldq, Kq, scale, stream);
+  else int8_quantize((const float*)x, ldx, M, K, q, ldq, Kq, scale, stream);
+  return blstm_check_launch(fn);
+}
+
+extern "C" int int8_linear(const int8_t* q, int64_t ldq, const float* x_scale, int64_t M, const int8_t* w, int64_t ldw,
+                           const float* w_scale, int32_t N, int32_t K, const float* bias, void* y, int64_t ldy,
+                           int32_t precision, hipStream_t stream) {
+  const char* fn = "int8_linear";
+  int rc = check_sizes(fn, M, N, K);
+  if (!rc) rc = check_precision(fn, precision);
+  if (!rc) rc = check_ints(fn, "q", q, ldq, K);
+  if (!rc) rc = check_ints(fn, "w", w, ldw, K);
+  if (rc) return rc;
+  if (!x_scale || !w_scale || !y) return blstm_fail(BLSTM_EINVAL, "%s: NULL pointer", fn);
+  if (ldy < N) return blstm_fail(BLSTM_EINVAL, "%s: a row pitch is below its row", fn);
+  Int8P p{};
+  p.x = q; p.w = w; p.ldx = ldq; p.ldw = ldw; p.ldy = ldy; p.M = M; p.N = N; p.K = K;
+  p.xs = x_scale; p.ws = w_scale; p.bias = bias; p.y = y;
+  if (precision == BLSTM_BF16) product<bf16>(p, stream);
+  else product<float>(p, stream);
+  return blstm_check_launch(fn);
+}
+
+// ws: the tokens' integers [M][Kw], then their scales
+static size_t tokens_bytes(int64_t M, int64_t Kw) { return (size_t)(rup(M * Kw, 256) + rup(M * 4, 256)); }
+
+extern "C" int int8_linear_ws_bytes(int64_t M, int32_t K, size_t* bytes) {
+  const int rc = check_sizes("int8_linear_ws_bytes", M, 1, K);
+  if (rc) return rc;
+  if (K > INT8_MAX_K) return blstm_fail(BLSTM_EUNSUPPORTED, "int8_linear_ws_bytes: K > %d", INT8_MAX_K);
+  if (bytes) *bytes = tokens_bytes(M, rup(K, 16));
+  return BLSTM_OK;
+}
+
+// Everything that the two calls behind it check, before either launches.
+static int check_tokens(const char* fn, const void* x, int64_t ldx, int64_t M, int32_t K, int32_t precision,
+                        const int8_t* w, int64_t ldw, const float* w_scale, int32_t N, int32_t Kw, const void* ws) {
+  int rc = check_sizes(fn, M, N, K);
+  if (!rc) rc = check_precision(fn, precision);
+  if (!rc) rc = check_ints(fn, "w", w, ldw, Kw);
+  if (rc) return rc;
+  if (!x || !w_scale || !ws) return blstm_fail(BLSTM_EINVAL, "%s: NULL pointer", fn);
+  if (ldx < K || Kw < K) return blstm_fail(BLSTM_EINVAL, "%s: a row is longer than its pitch or w's columns", fn);
+  if (!aligned16(ws)) return blstm_fail(BLSTM_EINVAL, "%s: ws must be 16-byte aligned", fn);
+  return BLSTM_OK;
+}
+
+extern "C" int int8_linear_rows(const void* x, int64_t ldx, int64_t M, int32_t K, int32_t precision, const int8_t* w,
+                                int64_t ldw, const float* w_scale, int32_t N, int32_t Kw, const float* bias, void* y,
+                                int64_t ldy, void* ws, hipStream_t stream) {
+  const char* fn = "int8_linear_rows";
+  int rc = check_tokens(fn, x, ldx, M, K, precision, w, ldw, w_scale, N, Kw, ws);
+  if (rc) return rc;
+  if (!y) return blstm_fail(BLSTM_EINVAL, "%s: NULL pointer", fn);
+  if (ldy < N) return blstm_fail(BLSTM_EINVAL, "%s: a row pitch is below its row", fn);
+  int8_t* q = (int8_t*)ws;
+  float* scale = (float*)((char*)ws + rup(M * Kw, 256));
+  rc = int8_quantize_rows(x, ldx, M, K, precision, q, Kw, Kw, scale, stream);
+  if (rc) return rc;
+  return int8_linear(q, Kw, scale, M, w, ldw, w_scale, N, Kw, bias, y, ldy, precision, stream);
+}
+
+// ---------------------------------------------------------------------------
+// The head: logits of rows at a time, scored.
+// ---------------------------------------------------------------------------
+static int64_t logit_rows(int64_t M, int64_t K) { return std::min(M, std::max<int64_t>(64, (180 << 20) / (4 * rup(K, 4)))); }
+
+extern "C" int int8_logprob_ws_bytes(int64_t M, int32_t K, int32_t Kw, size_t* bytes) {
+  const int rc = check_sizes("int8_logprob_ws_bytes", M, K, Kw);
+  if (rc) return rc;
+  if (K > SOFTMAX_MAX_CLASSES || Kw > INT8_MAX_K) return blstm_fail(BLSTM_EUNSUPPORTED, "int8_logprob_ws_bytes: too many classes or columns");
+  if (bytes) *bytes = tokens_bytes(M, rup(Kw, 16)) + (size_t)logit_rows(M, K) * rup(K, 4) * 4;
+  return BLSTM_OK;
+}
+
+extern "C" int int8_logprob_rows(const void* x, int64_t ldx, int64_t M, int32_t P, int32_t precision, const int8_t* w,
+                                 int64_t ldw, const float* w_scale, int32_t K, int32_t Kw, const float* bias,
+                                 const softmax_scores* scores, void* ws, hipStream_t stream) {
+  const char* fn = "int8_logprob_rows";
+  int rc = check_tokens(fn, x, ldx, M, P, precision, w, ldw, w_scale, K, Kw, ws);
+  if (!rc) rc = check_scores(scores, K, fn);
+  if (rc) return rc;
+  int8_t* q = (int8_t*)ws;
+  float* scale = (float*)((char*)ws + rup(M * Kw, 256));
+  float* logits = (float*)((char*)ws + tokens_bytes(M, Kw));
+  rc = int8_quantize_rows(x, ldx, M, P, precision, q, Kw, Kw, scale, stream);
+  const int64_t ld = rup(K, 4), step = logit_rows(M, K);
+  for (int64_t r0 = 0; !rc && r0 < M; r0 += step) {
+    const int64_t n = std::min(step, M - r0);
+    rc = int8_linear(q + r0 * Kw, Kw, scale + r0, n, w, ldw, w_scale, K, Kw, bias, logits, ld, BLSTM_FP32, stream);
+    if (!rc) rc = score_rows<float>(logits, ld, n, K, scores_from(*scores, r0), stream);
+  }
+  return rc;
+}

@@ -1,0 +1,411 @@
+// Row operators of scoring: log probabilities of given classes, the entropy and
+// the most likely classes of rows of logits, and the gradient of the logits.
+//
+// With y_j = (s_j - max s) log2 e / tau, Z = sum 2^y and T = sum 2^y y:
+//   log p_j = (s_j - max s) / tau - ln Z,   H = ln Z - ln 2 T / Z
+// Exponents are scaled differences of logits, so that a mask of -1e9 or of the
+// type's lowest value is a value like any other.  Sums are float32 in a fixed order.
+#include <cmath>
+
+#include "rows.hpp"
+#include "score.hpp"
+
+struct ScoreP {
+  int64_t ld;
+  int K, n, k;
+  float it2, itau;   // log2 e / tau, 1 / tau
+  const int32_t* ids;
+  float *logprob, *entropy, *top;
+  int32_t* idx;
+};
+
+// Below this exponent 2^y is 0 in float32: y stops here, so that 0 times it is 0 for a class at -inf.
+static constexpr float Y_MIN = -200.f;
+
+// A row's statistics: what a class's log probability and the gradient are made of.
+struct RowStats {
+  float ref, z, t;   // the largest logit (0 where there is none above -inf), the sums
+  bool some, good;   // a class above -inf; no NaN and no +inf
+};
+// A logit's log probability; every class of a row with none above -inf has log probability -inf,
+// every one of a row with a NaN or +inf NaN.
+struct LogProb {
+  float ref, itau, lz;
+  bool some;
+  __device__ __forceinline__ LogProb(const RowStats& r, float itau_)
+      : ref(r.ref), itau(itau_), lz(r.good ? log2f(r.z) * LN2_F : NAN), some(r.some) {}
+  __device__ __forceinline__ float operator()(float v) const { return some ? (v - ref) * itau - lz : -INFINITY; }
+};
+
+template <int T> struct ScoreLds {
+  float buf[3][T / 64];
+  uint32_t flag;
+};
+
+template <typename TI, int T, int V, int NV, bool TOP>
+__global__ __launch_bounds__(T, (waves_of<TI, T, V, NV>())) void score_rows_kernel(const TI* __restrict__ logits, const ScoreP p) {
+  __shared__ TopkLds<TOP ? T : 64> l;
+  __shared__ ScoreLds<T> w;
+  const int64_t m = blockIdx.x;
+  const TI* s = logits + m * p.ld;
+  const int tid = threadIdx.x, K = p.K;
+  Row<TI, V, NV ? NV : 1, T> row;
+  if constexpr (NV > 0) row.load(s, K);   // in flight while the lists are read
+  if (tid == 0) {
+    w.flag = 0;
+    if constexpr (TOP) l.count = 0;
+  }
+  int at = -1;
+  float sv = 0.f;
+  if (tid < p.n) {
+    at = p.ids[m * p.n + tid];
+    if (at < 0 || at >= K) at = -1;
+    else sv = to_f32(s[at]);
+  }
+  __syncthreads();
+  // the thread's largest, of each vector of it
+  float vm[NV ? NV : 1], mx = -INFINITY;
+  bool nan = false;
+  if constexpr (NV > 0) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      vm[i] = row.get(i, 0);
+#pragma unroll
+      for (int j = 1; j < V; ++j) vm[i] = fmaxf(vm[i], row.get(i, j));
+      if constexpr (V == 1) nan |= vm[i] != vm[i];
+      else {
+#pragma unroll
+        for (int j = 0; j < V; j += 2) nan |= __builtin_isunordered(row.get(i, j), row.get(i, j + 1));
+      }
+      mx = fmaxf(mx, vm[i]);
+      if constexpr (V > 1) {
+        asm volatile("" : "+v"(vm[i]));
+        __builtin_amdgcn_sched_barrier(0);   // one vector at a time: fewer registers
+      }
+    }
+    mx = fmaxf(mx, row.tail);
+    nan |= row.tail != row.tail;
+  } else {
+    each<TI, T>(s, K, [&](int, float v) {
+      mx = fmaxf(mx, v);
+      nan |= v != v;
+    });
+  }
+  if (nan) w.flag = 1;
+  put_wave(w.buf[0], wave_max(mx));
+  if constexpr (TOP) l.tmax[tid] = order_word(mx);
+  // bf16: the lower 16 bits of all order words are alike; float32: a threshold
+  // rounded down to 11 bits lets a few more pass and takes a third fewer steps
+  float thr = INFINITY;
+  if constexpr (TOP) thr = order_value(max(kth_max<std::is_same<TI, bf16>::value ? 16 : 12, T>(l, p.k), LOWEST));
+  else __syncthreads();
+  RowStats r;
+  r.ref = all_max<T>(w.buf[0]);
+  r.some = !(r.ref == -INFINITY) || w.flag;
+  r.good = !w.flag && r.ref < INFINITY;
+  if (!r.some) r.ref = 0.f;
+  float z = 0.f, t = 0.f;
+  auto add = [&](float v) {
+    const float y = fmaxf((v - r.ref) * p.it2, Y_MIN), e = exp2_(y);
+    z += e;
+    t += e * y;
+  };
+  if constexpr (NV > 0) {
+    row.again();
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) add(row.get(i, j));
+      if constexpr (V > 1) __builtin_amdgcn_sched_barrier(0);
+    }
+    if constexpr (V > 1) add(row.tail);
+    if constexpr (TOP) {
+      const int whole = row.whole(K);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        if (vm[i] >= thr && row.has(i, whole)) {
+#pragma unroll
+          for (int j = 0; j < V; ++j)
+            if (row.get(i, j) >= thr) push(l, row.get(i, j), row.col(i) + j);
+        }
+      }
+      if (row.tail >= thr && row.tail_col(K) < K) push(l, row.tail, row.tail_col(K));
+    }
+  } else {
+    each<TI, T>(s, K, [&](int c, float v) {
+      add(v);
+      if constexpr (TOP)
+        if (v >= thr) push(l, v, c);
+    });
+  }
+  put_wave(w.buf[1], wave_sum(z));
+  put_wave(w.buf[2], wave_sum(t));
+  __syncthreads();
+  r.z = all_sum<T>(w.buf[1]);
+  r.t = all_sum<T>(w.buf[2]);
+  const LogProb lp(r, p.itau);
+  if (tid < p.n) p.logprob[m * p.n + tid] = at < 0 ? 0.f : lp(sv);
+  if (p.entropy && tid == 0) p.entropy[m] = !r.some ? 0.f : lp.lz - r.t / r.z * LN2_F;
+  if constexpr (TOP) {
+    TopkP tp{p.ld, K, p.k, p.it2, p.top, nullptr, p.idx};
+    const int n = (int)same(l.count);
+    if (same(w.flag) || n > CAND) topk_any<TI, T, true>(l, s, m, tp, lp);
+    else rank(l, n, m, tp, lp);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// The gradient.  With g_i of the log probability of class id_i and h of the
+// entropy, G = sum g:
+//   dL/ds_j = (sum_{id_i = j} g_i - p_j (G + h (log p_j + H))) / tau
+//           = 2^y_j (A + B y_j) + (sum_{id_i = j} g_i) / tau
+// Rows of zeros g and h have a gradient of zeros whatever they hold, and so has
+// a row with no class above -inf; one with a NaN or +inf has NaN.
+// ---------------------------------------------------------------------------
+struct ScoreGradP {
+  int64_t ld, ldd;
+  int K, n, pad;
+  float it2, itau;   // log2 e / tau, 1 / tau
+  const int32_t* ids;
+  const float *dlogprob, *dentropy;
+};
+
+template <typename TI, typename TO, int T, int V, int NV>
+__global__ __launch_bounds__(T, (waves_of<TI, T, V, NV>())) void score_grad_kernel(const TI* logits, TO* dlogits, const ScoreGradP p) {
+  __shared__ float gv[MAXK];
+  __shared__ int32_t iv[MAXK];
+  __shared__ float buf[4][T / 64];
+  __shared__ uint32_t flag, wanted;
+  const int64_t m = blockIdx.x;
+  const TI* s = logits + m * p.ld;
+  TO* d = dlogits + m * p.ldd;
+  const int tid = threadIdx.x, K = p.K;
+  Row<TI, V, NV ? NV : 1, T> row;
+  if constexpr (NV > 0) row.load(s, K);
+  if (tid == 0) flag = wanted = 0;
+  int at = -1;
+  float sv = 0.f, g = 0.f;
+  if (tid < p.n) {
+    at = p.ids[m * p.n + tid];
+    if (at < 0 || at >= K) at = -1;
+    else {
+      sv = to_f32(s[at]);
+      g = p.dlogprob[m * p.n + tid];
+    }
+    iv[tid] = at;
+    gv[tid] = g;
+  }
+  const float h = p.dentropy ? p.dentropy[m] : 0.f;
+  for (int c = K + tid; c < K + p.pad; c += T) d[c] = from_f32<TO>(0.f);
+  __syncthreads();
+  float mx = -INFINITY;
+  bool nan = false;
+  auto see = [&](float v) {
+    mx = fmaxf(mx, v);
+    nan |= v != v;
+  };
+  if constexpr (NV > 0) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) see(row.get(i, j));
+      if constexpr (V > 1) __builtin_amdgcn_sched_barrier(0);
+    }
+    if constexpr (V > 1) see(row.tail);
+  } else {
+    each<TI, T>(s, K, [&](int, float v) { see(v); });
+  }
+  if (nan) flag = 1;
+  if (!(g == 0.f)) wanted = 1;
+  put_wave(buf[0], wave_max(mx));
+  put_wave(buf[1], wave_sum(g));
+  __syncthreads();
+  RowStats r;
+  r.ref = all_max<T>(buf[0]);
+  r.some = !(r.ref == -INFINITY) || flag;
+  r.good = !flag && r.ref < INFINITY;
+  if (same((!wanted && h == 0.f) || !r.some)) {
+    for (int c = tid; c < K; c += T) d[c] = from_f32<TO>(0.f);
+    return;
+  }
+  const float sum_g = all_sum<T>(buf[1]);
+  float z = 0.f, t = 0.f;
+  auto y_of = [&](float v) { return fmaxf((v - r.ref) * p.it2, Y_MIN); };
+  auto add = [&](float v) {
+    const float y = y_of(v), e = exp2_(y);
+    z += e;
+    t += e * y;
+  };
+  if constexpr (NV > 0) {
+    row.again();
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) add(row.get(i, j));
+      if constexpr (V > 1) __builtin_amdgcn_sched_barrier(0);
+    }
+    if constexpr (V > 1) add(row.tail);
+  } else {
+    each<TI, T>(s, K, [&](int, float v) { add(v); });
+  }
+  put_wave(buf[2], wave_sum(z));
+  put_wave(buf[3], wave_sum(t));
+  __syncthreads();   // every listed logit has been read, too
+  z = all_sum<T>(buf[2]);
+  t = all_sum<T>(buf[3]);
+  // log p_j + H = ln 2 (y_j - T / Z)
+  const float per = r.good ? p.itau / z : NAN;
+  const float A = -per * (sum_g - h * LN2_F * (t / z)), B = -per * h * LN2_F;
+  auto grad = [&](float v) {
+    const float y = y_of(v);
+    return exp2_(y) * fmaf(B, y, A);
+  };
+  if constexpr (NV > 0) {
+    row.again();
+    const int whole = row.whole(K);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      TO o[V];
+#pragma unroll
+      for (int j = 0; j < V; ++j) o[j] = from_f32<TO>(grad(row.get(i, j)));
+      if (row.has(i, whole)) __builtin_memcpy(row.at(d, i), o, V * sizeof(TO));
+      if constexpr (V > 1) __builtin_amdgcn_sched_barrier(0);
+    }
+    if (row.tail_col(K) < K) d[row.tail_col(K)] = from_f32<TO>(grad(row.tail));
+  } else {
+    // a thread writes only where it has read (d may be s)
+    const int done = K / V * V;
+    for (int c = tid * V; c < done; c += T * V) {
+      TI v[V];
+      TO o[V];
+      __builtin_memcpy(v, s + c, V * sizeof(TI));
+#pragma unroll
+      for (int j = 0; j < V; ++j) o[j] = from_f32<TO>(grad(to_f32(v[j])));
+      __builtin_memcpy(d + c, o, V * sizeof(TO));
+    }
+    const int c = done + tid;
+    if (c < K) d[c] = from_f32<TO>(grad(to_f32(s[c])));
+  }
+  __syncthreads();   // the dense part lies before what replaces the listed classes' values
+  if (at < 0) return;
+  float own = 0.f;   // all that is listed of the class, written by its first entry
+  for (int j = 0; j < p.n; ++j) {
+    if (iv[j] != at) continue;
+    if (j < tid) return;
+    own += gv[j];
+  }
+  d[at] = from_f32<TO>(grad(sv) + own * p.itau);
+}
+
+// ---------------------------------------------------------------------------
+// Host side.
+// ---------------------------------------------------------------------------
+template <typename TI>
+int score_rows(const TI* logits, int64_t ld, int64_t M, int32_t K, const softmax_scores& q, hipStream_t stream) {
+  const ScoreP p{ld, K, q.n, q.k, LOG2E_F / q.temperature, 1.f / q.temperature, q.ids, q.logprob, q.entropy, q.top, q.idx};
+  auto launch = [&](auto t, auto v, auto nv, auto top) {
+    constexpr int T = decltype(t)::value, V = decltype(v)::value, NV = decltype(nv)::value;
+    BLSTM_LAUNCH("softmax_logprob_rows", (score_rows_kernel<TI, T, V, NV, decltype(top)::value>), dim3((unsigned)M),
+                 dim3(T), 0, stream, logits, p);
+  };
+  auto with = [&](auto t, auto v, auto nv) {
+    if (q.k) launch(t, v, nv, std::true_type{});
+    else launch(t, v, nv, std::false_type{});
+  };
+  if (q.k <= 128) by_length<TI, 0, true>(K, with);
+  else by_length<TI, 0, false>(K, with);
+  return blstm_check_launch("softmax_logprob_rows");
+}
+template int score_rows<float>(const float*, int64_t, int64_t, int32_t, const softmax_scores&, hipStream_t);
+template int score_rows<bf16>(const bf16*, int64_t, int64_t, int32_t, const softmax_scores&, hipStream_t);
+
+template <typename TI, typename TO>
+int score_grad_rows(const TI* logits, int64_t ld, int64_t M, int32_t K, const softmax_score_grads& q, TO* dlogits,
+                    int64_t ldd, int32_t pad, hipStream_t stream) {
+  const ScoreGradP p{ld, ldd, K, q.n, pad, LOG2E_F / q.temperature, 1.f / q.temperature, q.ids, q.dlogprob, q.dentropy};
+  by_length<TI, 128 * 1024, true>(K, [&](auto t, auto v, auto nv) {
+    constexpr int T = decltype(t)::value, V = decltype(v)::value, NV = decltype(nv)::value;
+    BLSTM_LAUNCH("softmax_logprob_bwd_rows", (score_grad_kernel<TI, TO, T, V, NV>), dim3((unsigned)M), dim3(T), 0,
+                 stream, logits, dlogits, p);
+  });
+  return blstm_check_launch("softmax_logprob_bwd_rows");
+}
+template int score_grad_rows<float, float>(const float*, int64_t, int64_t, int32_t, const softmax_score_grads&, float*, int64_t, int32_t, hipStream_t);
+template int score_grad_rows<float, bf16>(const float*, int64_t, int64_t, int32_t, const softmax_score_grads&, bf16*, int64_t, int32_t, hipStream_t);
+template int score_grad_rows<bf16, bf16>(const bf16*, int64_t, int64_t, int32_t, const softmax_score_grads&, bf16*, int64_t, int32_t, hipStream_t);
+
+softmax_scores scores_from(const softmax_scores& q, int64_t r0) {
+  softmax_scores o = q;
+  if (q.n) { o.ids += r0 * q.n; o.logprob += r0 * q.n; }
+  if (q.entropy) o.entropy += r0;
+  if (q.k) { o.top += r0 * q.k; o.idx += r0 * q.k; }
+  return o;
+}
+softmax_score_grads score_grads_from(const softmax_score_grads& g, int64_t r0) {
+  softmax_score_grads o = g;
+  if (g.n) { o.ids += r0 * g.n; o.dlogprob += r0 * g.n; }
+  if (g.dentropy) o.dentropy += r0;
+  return o;
+}
+
+static int check_list(int32_t n, int32_t K, float temperature, const char* what, const char* fn) {
+  if (K > SOFTMAX_MAX_CLASSES) return blstm_fail(BLSTM_EUNSUPPORTED, "%s: K > %d", fn, SOFTMAX_MAX_CLASSES);
+  if (n < 0) return blstm_fail(BLSTM_EINVAL, "%s: %s is negative", fn, what);
+  if (n > MAXK) return blstm_fail(BLSTM_EUNSUPPORTED, "%s: %s > %d", fn, what, MAXK);
+  if (!(temperature > 0.f) || !std::isnormal(temperature))
+    return blstm_fail(BLSTM_EINVAL, "%s: the temperature must be positive and finite", fn);
+  return BLSTM_OK;
+}
+int check_scores(const softmax_scores* q, int32_t K, const char* fn) {
+  if (!q) return blstm_fail(BLSTM_EINVAL, "%s: NULL pointer", fn);
+  int rc = check_list(q->n, K, q->temperature, "n", fn);
+  if (!rc) rc = check_list(q->k, K, q->temperature, "k", fn);
+  if (rc) return rc;
+  if (q->k > K) return blstm_fail(BLSTM_EINVAL, "%s: k=%d above K=%d", fn, q->k, K);
+  if ((q->n && (!q->ids || !q->logprob)) || (q->k && (!q->top || !q->idx)))
+    return blstm_fail(BLSTM_EINVAL, "%s: NULL pointer", fn);
+  if (!q->n && !q->k && !q->entropy) return blstm_fail(BLSTM_EINVAL, "%s: nothing is asked for", fn);
+  return BLSTM_OK;
+}
+int check_score_grads(const softmax_score_grads* g, int32_t K, const char* fn) {
+  if (!g) return blstm_fail(BLSTM_EINVAL, "%s: NULL pointer", fn);
+  const int rc = check_list(g->n, K, g->temperature, "n", fn);
+  if (rc) return rc;
+  if (g->n && (!g->ids || !g->dlogprob)) return blstm_fail(BLSTM_EINVAL, "%s: NULL pointer", fn);
+  if (!g->n && !g->dentropy) return blstm_fail(BLSTM_EINVAL, "%s: no gradient is given", fn);
+  return BLSTM_OK;
+}
+
+static int check_rows(const char* fn, const void* logits, int64_t ld, int64_t M, int32_t K, int32_t precision) {
+  if (M < 1 || K < 1) return blstm_fail(BLSTM_EINVAL, "%s: M and K must be positive (M=%lld K=%d)", fn, (long long)M, K);
+  if (!logits) return blstm_fail(BLSTM_EINVAL, "%s: NULL pointer", fn);
+  if (precision != BLSTM_FP32 && precision != BLSTM_BF16)
+    return blstm_fail(BLSTM_EINVAL, "%s: precision must be BLSTM_FP32 or BLSTM_BF16", fn);
+  if (ld < K) return blstm_fail(BLSTM_EINVAL, "%s: a row pitch is below its row", fn);
+  if (M > LAUNCH_THREADS / 1024) return blstm_fail(BLSTM_EUNSUPPORTED, "%s: too many rows", fn);
+  return BLSTM_OK;
+}
+
+extern "C" int softmax_logprob_rows(const void* logits, int64_t ld, int64_t M, int32_t K, int32_t precision,
+                                    const softmax_scores* scores, hipStream_t stream) {
+  int rc = check_rows("softmax_logprob_rows", logits, ld, M, K, precision);
+  if (!rc) rc = check_scores(scores, K, "softmax_logprob_rows");
+  if (rc) return rc;
+  return precision == BLSTM_BF16 ? score_rows((const bf16*)logits, ld, M, K, *scores, stream)
+                                 : score_rows((const float*)logits, ld, M, K, *scores, stream);
+}
+
+extern "C" int softmax_logprob_bwd_rows(const void* logits, int64_t ld, int64_t M, int32_t K, int32_t precision,
+                                        const softmax_score_grads* grads, void* dlogits, int64_t ldd,
+                                        hipStream_t stream) {
+  int rc = check_rows("softmax_logprob_bwd_rows", logits, ld, M, K, precision);
+  if (!rc) rc = check_score_grads(grads, K, "softmax_logprob_bwd_rows");
+  if (rc) return rc;
+  if (!dlogits) return blstm_fail(BLSTM_EINVAL, "softmax_logprob_bwd_rows: NULL pointer");
+  if (ldd < K) return blstm_fail(BLSTM_EINVAL, "softmax_logprob_bwd_rows: a row pitch is below its row");
+  if (dlogits == logits && ldd != ld)
+    return blstm_fail(BLSTM_EINVAL, "softmax_logprob_bwd_rows: dlogits over logits with another row pitch");
+  if (precision == BLSTM_BF16)
+    return score_grad_rows((const bf16*)logits, ld, M, K, *grads, (bf16*)dlogits, ldd, 0, stream);
+  return score_grad_rows((const float*)logits, ld, M, K, *grads, (float*)dlogits, ldd, 0, stream);
+}
