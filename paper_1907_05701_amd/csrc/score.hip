@@ -19,13 +19,25 @@ struct ScoreP {
   int32_t* idx;
 };
 
-// Below this exponent 2^y is 0 in float32: y stops here, so that 0 times it is 0 for a class at -inf.
+// Below this exponent 2^y is 0 in float32: y stops here in products with it, so that a class at -inf adds 0 to T.
 static constexpr float Y_MIN = -200.f;
 
-// A row's statistics: what a class's log probability and the gradient are made of.
+// A row's statistics, its sums from `ref`, the largest logit (0 where there is none above -inf).
+// A NaN in the row, or a difference of infinities, makes z a NaN.
 struct RowStats {
-  float ref, z, t;   // the largest logit (0 where there is none above -inf), the sums
-  bool some, good;   // a class above -inf; no NaN and no +inf
+  float ref, it2, z = 0.f, t = 0.f;
+  bool some;   // a class above -inf, or a NaN
+  __device__ __forceinline__ RowStats(float largest, float it2_)
+      : ref(largest == -INFINITY ? 0.f : largest), it2(it2_), some(!(largest == -INFINITY)) {}
+  __device__ __forceinline__ float y_of(float v) const { return (v - ref) * it2; }
+  __device__ __forceinline__ void add(float v) {
+    const float y = y_of(v), e = exp2_(y);
+    z += e;
+    t += e * fmaxf(y, Y_MIN);
+  }
+  // or the compiler would sink the sums past the loop over vectors, and carry every exponential there
+  __device__ __forceinline__ void keep() { asm volatile("" : "+v"(z), "+v"(t)); }
+  __device__ __forceinline__ bool good() const { return z == z; }
 };
 // A logit's log probability; every class of a row with none above -inf has log probability -inf,
 // every one of a row with a NaN or +inf NaN.
@@ -33,28 +45,50 @@ struct LogProb {
   float ref, itau, lz;
   bool some;
   __device__ __forceinline__ LogProb(const RowStats& r, float itau_)
-      : ref(r.ref), itau(itau_), lz(r.good ? log2f(r.z) * LN2_F : NAN), some(r.some) {}
+      : ref(r.ref), itau(itau_), lz(log2f(r.z) * LN2_F), some(r.some || !r.good()) {}
   __device__ __forceinline__ float operator()(float v) const { return some ? (v - ref) * itau - lz : -INFINITY; }
 };
 
-template <int T> struct ScoreLds {
-  float buf[3][T / 64];
-  uint32_t flag;
-};
+// The largest of a thread's logits, and (vm) of each vector of them; a NaN counts as none.
+template <typename TI, int V, int NV, int T>
+__device__ __forceinline__ float largest(const Row<TI, V, NV, T>& row, float (&vm)[NV]) {
+  float mx = row.tail;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    vm[i] = row.get(i, 0);
+#pragma unroll
+    for (int j = 1; j < V; ++j) vm[i] = fmaxf(vm[i], row.get(i, j));
+    mx = fmaxf(mx, vm[i]);
+    if constexpr (V > 1) {
+      asm volatile("" : "+v"(vm[i]));
+      __builtin_amdgcn_sched_barrier(0);   // one vector at a time: fewer registers
+    }
+  }
+  return mx;
+}
+template <typename TI, int V, int NV, int T>
+__device__ __forceinline__ void add_row(RowStats& r, Row<TI, V, NV, T>& row) {
+  row.again();
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) r.add(row.get(i, j));
+    r.keep();
+    if constexpr (V > 1) __builtin_amdgcn_sched_barrier(0);
+  }
+  if constexpr (V > 1) r.add(row.tail);
+}
 
 template <typename TI, int T, int V, int NV, bool TOP>
 __global__ __launch_bounds__(T, (waves_of<TI, T, V, NV>())) void score_rows_kernel(const TI* __restrict__ logits, const ScoreP p) {
   __shared__ TopkLds<TOP ? T : 64> l;
-  __shared__ ScoreLds<T> w;
+  __shared__ float buf[3][T / 64];
   const int64_t m = blockIdx.x;
   const TI* s = logits + m * p.ld;
   const int tid = threadIdx.x, K = p.K;
   Row<TI, V, NV ? NV : 1, T> row;
-  if constexpr (NV > 0) row.load(s, K);   // in flight while the lists are read
-  if (tid == 0) {
-    w.flag = 0;
-    if constexpr (TOP) l.count = 0;
-  }
+  if constexpr (NV > 0) row.load(s, K);   // in flight while the list is read
+  if (TOP && tid == 0) l.count = 0;
   int at = -1;
   float sv = 0.f;
   if (tid < p.n) {
@@ -62,94 +96,68 @@ __global__ __launch_bounds__(T, (waves_of<TI, T, V, NV>())) void score_rows_kern
     if (at < 0 || at >= K) at = -1;
     else sv = to_f32(s[at]);
   }
-  __syncthreads();
-  // the thread's largest, of each vector of it
   float vm[NV ? NV : 1], mx = -INFINITY;
-  bool nan = false;
-  if constexpr (NV > 0) {
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      vm[i] = row.get(i, 0);
-#pragma unroll
-      for (int j = 1; j < V; ++j) vm[i] = fmaxf(vm[i], row.get(i, j));
-      if constexpr (V == 1) nan |= vm[i] != vm[i];
-      else {
-#pragma unroll
-        for (int j = 0; j < V; j += 2) nan |= __builtin_isunordered(row.get(i, j), row.get(i, j + 1));
-      }
-      mx = fmaxf(mx, vm[i]);
-      if constexpr (V > 1) {
-        asm volatile("" : "+v"(vm[i]));
-        __builtin_amdgcn_sched_barrier(0);   // one vector at a time: fewer registers
-      }
-    }
-    mx = fmaxf(mx, row.tail);
-    nan |= row.tail != row.tail;
-  } else {
-    each<TI, T>(s, K, [&](int, float v) {
-      mx = fmaxf(mx, v);
-      nan |= v != v;
-    });
-  }
-  if (nan) w.flag = 1;
-  put_wave(w.buf[0], wave_max(mx));
-  if constexpr (TOP) l.tmax[tid] = order_word(mx);
-  // bf16: the lower 16 bits of all order words are alike; float32: a threshold
-  // rounded down to 11 bits lets a few more pass and takes a third fewer steps
+  if constexpr (NV > 0) mx = largest(row, vm);
+  else each<TI, T>(s, K, [&](int, float v) { mx = fmaxf(mx, v); });
+  mx = fmaxf(mx, -INFINITY);   // of NaN alone: none
+  put_wave(buf[0], wave_max(mx));
   float thr = INFINITY;
-  if constexpr (TOP) thr = order_value(max(kth_max<std::is_same<TI, bf16>::value ? 16 : 12, T>(l, p.k), LOWEST));
-  else __syncthreads();
-  RowStats r;
-  r.ref = all_max<T>(w.buf[0]);
-  r.some = !(r.ref == -INFINITY) || w.flag;
-  r.good = !w.flag && r.ref < INFINITY;
-  if (!r.some) r.ref = 0.f;
-  float z = 0.f, t = 0.f;
-  auto add = [&](float v) {
-    const float y = fmaxf((v - r.ref) * p.it2, Y_MIN), e = exp2_(y);
-    z += e;
-    t += e * y;
-  };
+  if constexpr (TOP) {
+    l.tmax[tid] = order_word(mx);
+    // bf16: the lower 16 bits of all order words are alike; float32: a threshold
+    // rounded down to 11 bits lets a few more pass and takes a third fewer steps
+    thr = order_value(max(kth_max<std::is_same<TI, bf16>::value ? 16 : 12, T>(l, p.k), LOWEST));
+  } else {
+    __syncthreads();
+  }
+  RowStats r(all_max<T>(buf[0]), p.it2);
   if constexpr (NV > 0) {
-    row.again();
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-#pragma unroll
-      for (int j = 0; j < V; ++j) add(row.get(i, j));
-      if constexpr (V > 1) __builtin_amdgcn_sched_barrier(0);
-    }
-    if constexpr (V > 1) add(row.tail);
+    add_row(r, row);
     if constexpr (TOP) {
+      row.again();
       const int whole = row.whole(K);
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         if (vm[i] >= thr && row.has(i, whole)) {
+          // few vectors come here, most with one value; the others of a vector are
+          // read again, so that this is one loop and not a branch per value
+          uint32_t bits = 0;
+          float v = 0.f;
 #pragma unroll
-          for (int j = 0; j < V; ++j)
-            if (row.get(i, j) >= thr) push(l, row.get(i, j), row.col(i) + j);
+          for (int j = V - 1; j >= 0; --j) {
+            const float x = row.get(i, j);
+            bits |= x >= thr ? 1u << j : 0u;
+            v = x >= thr ? x : v;   // ends with the first of them
+          }
+          push(l, v, row.col(i) + __builtin_ctz(bits));
+          bits &= bits - 1;
+          for (; bits; bits &= bits - 1) {
+            const int c = row.col(i) + __builtin_ctz(bits);
+            push(l, to_f32(s[c]), c);
+          }
         }
       }
       if (row.tail >= thr && row.tail_col(K) < K) push(l, row.tail, row.tail_col(K));
     }
   } else {
     each<TI, T>(s, K, [&](int c, float v) {
-      add(v);
+      r.add(v);
       if constexpr (TOP)
         if (v >= thr) push(l, v, c);
     });
   }
-  put_wave(w.buf[1], wave_sum(z));
-  put_wave(w.buf[2], wave_sum(t));
+  put_wave(buf[1], wave_sum(r.z));
+  put_wave(buf[2], wave_sum(r.t));
   __syncthreads();
-  r.z = all_sum<T>(w.buf[1]);
-  r.t = all_sum<T>(w.buf[2]);
+  r.z = all_sum<T>(buf[1]);
+  r.t = all_sum<T>(buf[2]);
   const LogProb lp(r, p.itau);
   if (tid < p.n) p.logprob[m * p.n + tid] = at < 0 ? 0.f : lp(sv);
-  if (p.entropy && tid == 0) p.entropy[m] = !r.some ? 0.f : lp.lz - r.t / r.z * LN2_F;
+  if (p.entropy && tid == 0) p.entropy[m] = lp.some ? lp.lz - r.t / r.z * LN2_F : 0.f;
   if constexpr (TOP) {
     TopkP tp{p.ld, K, p.k, p.it2, p.top, nullptr, p.idx};
     const int n = (int)same(l.count);
-    if (same(w.flag) || n > CAND) topk_any<TI, T, true>(l, s, m, tp, lp);
+    if (same(!r.good()) || n > CAND) topk_any<TI, T, true>(l, s, m, tp, lp);
     else rank(l, n, m, tp, lp);
   }
 }
@@ -175,14 +183,14 @@ __global__ __launch_bounds__(T, (waves_of<TI, T, V, NV>())) void score_grad_kern
   __shared__ float gv[MAXK];
   __shared__ int32_t iv[MAXK];
   __shared__ float buf[4][T / 64];
-  __shared__ uint32_t flag, wanted;
+  __shared__ uint32_t wanted;
   const int64_t m = blockIdx.x;
   const TI* s = logits + m * p.ld;
   TO* d = dlogits + m * p.ldd;
   const int tid = threadIdx.x, K = p.K;
   Row<TI, V, NV ? NV : 1, T> row;
   if constexpr (NV > 0) row.load(s, K);
-  if (tid == 0) flag = wanted = 0;
+  if (tid == 0) wanted = 0;
   int at = -1;
   float sv = 0.f, g = 0.f;
   if (tid < p.n) {
@@ -198,67 +206,32 @@ __global__ __launch_bounds__(T, (waves_of<TI, T, V, NV>())) void score_grad_kern
   const float h = p.dentropy ? p.dentropy[m] : 0.f;
   for (int c = K + tid; c < K + p.pad; c += T) d[c] = from_f32<TO>(0.f);
   __syncthreads();
-  float mx = -INFINITY;
-  bool nan = false;
-  auto see = [&](float v) {
-    mx = fmaxf(mx, v);
-    nan |= v != v;
-  };
-  if constexpr (NV > 0) {
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-#pragma unroll
-      for (int j = 0; j < V; ++j) see(row.get(i, j));
-      if constexpr (V > 1) __builtin_amdgcn_sched_barrier(0);
-    }
-    if constexpr (V > 1) see(row.tail);
-  } else {
-    each<TI, T>(s, K, [&](int, float v) { see(v); });
-  }
-  if (nan) flag = 1;
+  float vm[NV ? NV : 1], mx = -INFINITY;
+  if constexpr (NV > 0) mx = largest(row, vm);
+  else each<TI, T>(s, K, [&](int, float v) { mx = fmaxf(mx, v); });
   if (!(g == 0.f)) wanted = 1;
-  put_wave(buf[0], wave_max(mx));
+  put_wave(buf[0], wave_max(fmaxf(mx, -INFINITY)));
   put_wave(buf[1], wave_sum(g));
   __syncthreads();
-  RowStats r;
-  r.ref = all_max<T>(buf[0]);
-  r.some = !(r.ref == -INFINITY) || flag;
-  r.good = !flag && r.ref < INFINITY;
-  if (same((!wanted && h == 0.f) || !r.some)) {
+  RowStats r(all_max<T>(buf[0]), p.it2);
+  auto nothing = [&]() {
     for (int c = tid; c < K; c += T) d[c] = from_f32<TO>(0.f);
-    return;
-  }
-  const float sum_g = all_sum<T>(buf[1]);
-  float z = 0.f, t = 0.f;
-  auto y_of = [&](float v) { return fmaxf((v - r.ref) * p.it2, Y_MIN); };
-  auto add = [&](float v) {
-    const float y = y_of(v), e = exp2_(y);
-    z += e;
-    t += e * y;
   };
-  if constexpr (NV > 0) {
-    row.again();
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-#pragma unroll
-      for (int j = 0; j < V; ++j) add(row.get(i, j));
-      if constexpr (V > 1) __builtin_amdgcn_sched_barrier(0);
-    }
-    if constexpr (V > 1) add(row.tail);
-  } else {
-    each<TI, T>(s, K, [&](int, float v) { add(v); });
-  }
-  put_wave(buf[2], wave_sum(z));
-  put_wave(buf[3], wave_sum(t));
+  if (same(!wanted && h == 0.f)) return nothing();
+  const float sum_g = all_sum<T>(buf[1]);
+  if constexpr (NV > 0) add_row(r, row);
+  else each<TI, T>(s, K, [&](int, float v) { r.add(v); });
+  put_wave(buf[2], wave_sum(r.z));
+  put_wave(buf[3], wave_sum(r.t));
   __syncthreads();   // every listed logit has been read, too
-  z = all_sum<T>(buf[2]);
-  t = all_sum<T>(buf[3]);
+  r.z = all_sum<T>(buf[2]);
+  if (same(!r.some && r.good())) return nothing();
   // log p_j + H = ln 2 (y_j - T / Z)
-  const float per = r.good ? p.itau / z : NAN;
-  const float A = -per * (sum_g - h * LN2_F * (t / z)), B = -per * h * LN2_F;
+  const float mean = all_sum<T>(buf[3]) / r.z, per = p.itau / r.z;
+  const float A = -per * (sum_g - h * LN2_F * mean), B = -per * h * LN2_F;
   auto grad = [&](float v) {
-    const float y = y_of(v);
-    return exp2_(y) * fmaf(B, y, A);
+    const float y = r.y_of(v);
+    return exp2_(y) * fmaf(B, fmaxf(y, Y_MIN), A);
   };
   if constexpr (NV > 0) {
     row.again();
