@@ -21,7 +21,8 @@ ROOT = os.path.dirname(PKG)
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libadpsgd_blstm.so")
 SOURCES = ["abi.hip", "update.hip", "lstm.hip", "lstm_persist.hip", "lstm_persist32.hip", "head.hip",
-           "ssm_scan.hip", "ssm_scan_ns4.hip", "ssm_scan_ns8.hip", "ssm_conv.hip", "distill.hip", "score.hip", "int8.hip"]
+           "ssm_scan.hip", "ssm_scan_ns4.hip", "ssm_scan_ns8.hip", "ssm_conv.hip", "distill.hip", "score.hip", "int8.hip",
+           "int8_head.hip"]
 ARCH = "gfx950"
 
 HIPCC_FLAGS = [

@@ -182,7 +182,7 @@ __global__ __launch_bounds__(WM * WN * 64) void int8_tile_kernel(const Int8P p) 
   const int fr = lane & 15, fc = lane >> 4;
   issue(0);
   for (int it = 0; it < steps; ++it) {
-    kc_wait_vm<0>();
+    int8_stage_wait();
     kc_barrier();
     if (it + 1 < steps) issue(it + 1);
     const char* st = lds + (it & 1) * STAGE;
@@ -373,7 +373,7 @@ extern "C" int int8_linear_rows(const void* x, int64_t ldx, int64_t M, int32_t K
 }
 
 // ---------------------------------------------------------------------------
-// The head: logits of rows at a time, scored.
+// The head (int8_head.hip); tokens of more columns than that holds: logits of rows at a time, scored.
 // ---------------------------------------------------------------------------
 static int64_t logit_rows(int64_t M, int64_t K) { return std::min(M, std::max<int64_t>(64, (180 << 20) / (4 * rup(K, 4)))); }
 
@@ -381,7 +381,8 @@ extern "C" int int8_logprob_ws_bytes(int64_t M, int32_t K, int32_t Kw, size_t* b
   const int rc = check_sizes("int8_logprob_ws_bytes", M, K, Kw);
   if (rc) return rc;
   if (K > SOFTMAX_MAX_CLASSES || Kw > INT8_MAX_K) return blstm_fail(BLSTM_EUNSUPPORTED, "int8_logprob_ws_bytes: too many classes or columns");
-  if (bytes) *bytes = tokens_bytes(M, rup(Kw, 16)) + (size_t)logit_rows(M, K) * rup(K, 4) * 4;
+  if (bytes)
+    *bytes = tokens_bytes(M, rup(Kw, 16)) + (int8_head_fits(Kw) ? int8_head_bytes(M, K, Kw) : (size_t)logit_rows(M, K) * rup(K, 4) * 4);
   return BLSTM_OK;
 }
 
@@ -394,8 +395,11 @@ extern "C" int int8_logprob_rows(const void* x, int64_t ldx, int64_t M, int32_t 
   if (rc) return rc;
   int8_t* q = (int8_t*)ws;
   float* scale = (float*)((char*)ws + rup(M * Kw, 256));
-  float* logits = (float*)((char*)ws + tokens_bytes(M, Kw));
+  char* rest = (char*)ws + tokens_bytes(M, Kw);
   rc = int8_quantize_rows(x, ldx, M, P, precision, q, Kw, Kw, scale, stream);
+  if (rc) return rc;
+  if (int8_head_fits(Kw)) return int8_head(q, scale, M, w, ldw, w_scale, K, Kw, bias, *scores, rest, stream);
+  float* logits = (float*)rest;
   const int64_t ld = rup(K, 4), step = logit_rows(M, K);
   for (int64_t r0 = 0; !rc && r0 < M; r0 += step) {
     const int64_t n = std::min(step, M - r0);

@@ -57,6 +57,10 @@ __device__ __forceinline__ float scale_of(float x_scale, float w_scale) {
   return x_scale * w_scale;
 }
 
+// Before the barrier of a two-stage ring: this wave's loads into the next stage have landed, and its reads of the one that
+// is filled next are done.
+__device__ __forceinline__ void int8_stage_wait() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
+
 // Most columns of a row: 2^14 times them stays within int32.
 static constexpr int INT8_MAX_K = (1 << 17) - 16;
 // Longest row pitch: 256 rows within a buffer resource's 31 bits.
@@ -66,3 +70,10 @@ static constexpr int64_t INT8_MAX_LD = 1 << 22;
 template <typename TI>
 void int8_quantize(const TI* x, int64_t ldx, int64_t M, int32_t K, int8_t* q, int64_t ldq, int32_t Kq, float* scale,
                    hipStream_t stream);
+
+// Log probabilities of a head of K classes from tokens as integers [M][Kw] and their scales (int8_head.hip);
+// buf: int8_head_bytes.  For up to so many columns:
+bool int8_head_fits(int32_t Kw);
+size_t int8_head_bytes(int64_t M, int32_t K, int32_t Kw);
+int int8_head(const int8_t* q, const float* xs, int64_t M, const int8_t* w, int64_t ldw, const float* ws, int32_t K,
+              int32_t Kw, const float* bias, const softmax_scores& scores, char* buf, hipStream_t stream);
