@@ -17,20 +17,27 @@
 #include "score.hpp"
 
 static constexpr int CT = 64;             // classes of a tile: one stage in LDS
-static constexpr int PAIR = 2 * CT;       // classes over which group maxima are taken
-static constexpr float FLOOR = -1e30f;    // sums start from here; logits below count as nothing (second pass)
-static constexpr float SLACK = 30.f;      // how far above its reference a lane's largest exponent may get
+// Tiles over which a lane's group maxima are taken: 16 classes a group, 8 where four waves share a tile.  (Larger groups
+// mean fewer maxima, and more classes to compute again: with 32, the second pass of 2688 frames reads 172 MB of weights.)
+__host__ __device__ constexpr int group_tiles(int fw) { return fw == 4 ? 1 : 2; }
+// Biases below FLOOR count as FLOOR in the first pass, and sums start from a reference above it, so that such a class
+// adds 0; rows that have no other, or not k others, are for the second pass alone.
+static constexpr float FLOOR = -1e30f, START = 0.5f * FLOOR;
+// How far above its reference a lane's largest exponent may get: a reference that follows every new maximum takes
+// its branch in most tiles, one that follows far behind makes T large and its rounding with it (30: the entropy's
+// error 1.8e-6).
+static constexpr float SLACK = 4.f;
 
 struct HeadP {
   const int8_t *q, *w;
   int64_t ldw;
   const float *xs, *ws, *bias;
   int64_t M;
-  int K, Kw, ksteps;       // classes, columns, 64-column steps
-  int nf, ranges, ppr;     // frame tiles, class ranges, pairs of tiles a range
-  int nstat, ngroup;       // a frame's sums and group maxima
+  int K, Kw;               // classes, columns
+  int nf, ranges, per;     // frame tiles, class ranges, tiles a range
+  int ngroup;              // a frame's group maxima
   float it2, itau;         // log2 e / tau, 1 / tau
-  float4* stats;           // [M][nstat]: reference (an exponent of 2), Z, T
+  float4* stats;           // [M][ranges]: reference (an exponent of 2), Z, T
   float* gmax;             // [M][ngroup], or null
 };
 
@@ -52,6 +59,8 @@ struct Sums {
   }
 };
 
+__device__ __forceinline__ float fmax_nan(float v, float least) { return v < least ? least : v; }   // a NaN stays
+
 // 16-byte chunk c of row r of a tile of NCH chunks a row: the slot it lies in (16 rows' chunk c in 16 different
 // bank groups).
 template <int NCH>
@@ -61,9 +70,10 @@ __device__ __forceinline__ int head_slot(int c, int r) {
 
 // KS: most 64-column steps; 16 FN frames a wave; FW waves side by side along the
 // frames, the other 4 / FW along the classes of a tile.
+template <int KS> constexpr int head_per_cu() { return KS > 8 ? 1 : KS > 4 ? 2 : 3; }   // workgroups
 template <int KS, int FN, int FW>
-__global__ __launch_bounds__(256, KS > 8 ? 1 : 2) void int8_head_kernel(const HeadP p) {
-  constexpr int WC = 4 / FW, NI = 4 / WC, NCH = KS * 4, TILE = CT * KS * 64, STAGE = TILE + 512;
+__global__ __launch_bounds__(256, head_per_cu<KS>()) void int8_head_kernel(const HeadP p) {
+  constexpr int WC = 4 / FW, NI = 4 / WC, TG = group_tiles(FW), NCH = KS * 4, TILE = CT * KS * 64, STAGE = TILE + 512;
   constexpr int LOADS = TILE / 1024 / 4;   // of a wave
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), fr = lane & 15, fc = lane >> 4;
@@ -72,13 +82,21 @@ __global__ __launch_bounds__(256, KS > 8 ? 1 : 2) void int8_head_kernel(const He
   const int total = p.nf * p.ranges, share = total / 8;
   const int at = (int)blockIdx.x < 8 * share ? blockIdx.x % 8 * share + blockIdx.x / 8 : blockIdx.x, range = at / p.nf;
   const int64_t f0 = (int64_t)(at % p.nf) * (16 * FN * FW) + wf * 16 * FN;
-  const int tile0 = range * p.ppr * 2, tiles = min((int)((p.K + CT - 1) / CT) - tile0, p.ppr * 2);
+  const int tile0 = range * p.per, tiles = min((int)((p.K + CT - 1) / CT) - tile0, p.per);
   const int8_t* wb = p.w + (int64_t)tile0 * CT * p.ldw;
   const int rows = p.K - tile0 * CT;   // classes from the range's first on
 
-  const __amdgpu_buffer_rsrc_t rws = __builtin_amdgcn_make_buffer_rsrc((void*)(p.ws + tile0 * CT), (short)0, rows * 4, 0x00020000);
-  const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc((void*)(p.bias + (p.bias ? tile0 * CT : 0)), (short)0,
-                                                                     p.bias ? rows * 4 : 0, 0x00020000);
+  // a tile's scales and biases, one a lane of the first two waves, go through registers: a bias of -inf would make 0 times
+  // -inf of a class that adds nothing
+  float next = 0.f;
+  auto fetch = [&](int j) {
+    const int c = j * CT + lane;
+    if (wid == 0) next = c < rows ? p.ws[tile0 * CT + c] : 0.f;
+    if (wid == 1) next = c < rows ? (p.bias ? fmax_nan(p.bias[tile0 * CT + c], FLOOR) : 0.f) : FLOOR;
+  };
+  auto put = [&](int j) {
+    if (wid < 2) *(float*)(lds + (j & 1) * STAGE + TILE + wid * 256 + lane * 4) = next;
+  };
   auto issue = [&](int j) {
     char* st = lds + (j & 1) * STAGE;
     const __amdgpu_buffer_rsrc_t r = dma_rsrc(wb + (int64_t)j * CT * p.ldw);
@@ -88,11 +106,9 @@ __global__ __launch_bounds__(256, KS > 8 ? 1 : 2) void int8_head_kernel(const He
       const bool in = j * CT + row < rows && c * 16 < p.Kw;
       dma16(r, in ? (uint32_t)(row * p.ldw + c * 16) : DMA_OFF_NONE, st + (i * 4 + wid) * 1024);
     }
-    // scales and biases, 64 of each (0 behind the last class)
-    if (wid < 2)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(wid ? rb : rws, (lds_ptr_t)(st + TILE + wid * 256), 4, (j * CT + lane) * 4, 0, 0, 0);
   };
   issue(0);
+  fetch(0);
 
   i32x4 b[FN][KS];
   float xs[FN];
@@ -110,16 +126,20 @@ __global__ __launch_bounds__(256, KS > 8 ? 1 : 2) void int8_head_kernel(const He
   float lim[FN], gm[FN];
 #pragma unroll
   for (int j = 0; j < FN; ++j) {
-    s[j] = Sums{FLOOR * p.it2, 0.f, 0.f};
-    lim[j] = FLOOR;
+    s[j] = Sums{START * p.it2, 0.f, 0.f};
+    lim[j] = START;
     gm[j] = -INFINITY;
   }
   const float slack = SLACK / p.it2;
+  put(0);
 
   for (int it = 0; it < tiles; ++it) {
     int8_stage_wait();
     kc_barrier();
-    if (it + 1 < tiles) issue(it + 1);
+    if (it + 1 < tiles) {
+      issue(it + 1);
+      fetch(it + 1);
+    }
     const char* st = lds + (it & 1) * STAGE;
     float l[NI][FN][4];
 #pragma unroll
@@ -130,7 +150,6 @@ __global__ __launch_bounds__(256, KS > 8 ? 1 : 2) void int8_head_kernel(const He
       for (int j = 0; j < FN; ++j) acc[j] = i32x4{0, 0, 0, 0};
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        if (ks >= p.ksteps) continue;
         const i32x4 a = *(const i32x4*)(st + (row + fr) * (NCH * 16) + head_slot<NCH>(ks * 4 + fc, row + fr) * 16);
 #pragma unroll
         for (int j = 0; j < FN; ++j) acc[j] = mma_i8(a, b[j][ks], acc[j]);
@@ -140,16 +159,6 @@ __global__ __launch_bounds__(256, KS > 8 ? 1 : 2) void int8_head_kernel(const He
       for (int j = 0; j < FN; ++j)
 #pragma unroll
         for (int r = 0; r < 4; ++r) l[i][j][r] = int8_value(acc[j][r], scale_of(xs[j], w4[r]), b4[r]);
-    }
-    if ((it + 1) * CT > rows) {   // the last tile's classes past the last
-#pragma unroll
-      for (int i = 0; i < NI; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (it * CT + (wc * NI + i) * 16 + 4 * fc + r >= rows) {
-#pragma unroll
-            for (int j = 0; j < FN; ++j) l[i][j][r] = -INFINITY;
-          }
     }
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
@@ -163,29 +172,52 @@ __global__ __launch_bounds__(256, KS > 8 ? 1 : 2) void int8_head_kernel(const He
         s[j].rise(to);
         lim[j] = fmaxf(lim[j], mb + slack);
       }
+      float z = 0.f, t = 0.f;   // of the tile: shorter chains of additions
 #pragma unroll
       for (int i = 0; i < NI; ++i)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const float y = fmaf(l[i][j][r], p.it2, -s[j].rc), e = exp2_(y);
-          s[j].z += e;
-          s[j].t += e * fmaxf(y, -200.f);
+          z += e;
+          t += e * y;
         }
+      s[j].z += z;
+      s[j].t += t;
       gm[j] = fmaxf(gm[j], mb);
-      if (p.gmax && ((it & 1) || it + 1 == tiles)) {
+      if (p.gmax && (it % TG == TG - 1 || it + 1 == tiles)) {
         const int64_t f = f0 + j * 16 + fr;
-        if (f < p.M) p.gmax[f * p.ngroup + ((tile0 + it) / 2 * WC + wc) * 4 + fc] = gm[j];
+        if (f < p.M) p.gmax[f * p.ngroup + ((tile0 + it) / TG * WC + wc) * 4 + fc] = gm[j];
         gm[j] = -INFINITY;
       }
     }
+    if (it + 1 < tiles) put(it + 1);
   }
+  // a frame's lanes, then its waves
 #pragma unroll
   for (int j = 0; j < FN; ++j) {
 #pragma unroll
     for (int o = 16; o < 64; o <<= 1)
       s[j].join(Sums{__shfl_xor(s[j].rc, o), __shfl_xor(s[j].z, o), __shfl_xor(s[j].t, o)});
+  }
+  if constexpr (WC > 1) {
+    static_assert(4 * FN * 16 * sizeof(Sums) <= STAGE, "the first stage is done with");
+    __syncthreads();
+    Sums* part = (Sums*)lds;
+    if (fc == 0) {
+#pragma unroll
+      for (int j = 0; j < FN; ++j) part[(wid * FN + j) * 16 + fr] = s[j];
+    }
+    __syncthreads();
+    if (wc > 0) return;
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+#pragma unroll
+      for (int w = 1; w < WC; ++w) s[j].join(part[((w * FW + wf) * FN + j) * 16 + fr]);
+  }
+#pragma unroll
+  for (int j = 0; j < FN; ++j) {
     const int64_t f = f0 + j * 16 + fr;
-    if (fc == 0 && f < p.M) p.stats[f * p.nstat + range * WC + wc] = float4{s[j].rc, s[j].z, s[j].t, 0.f};
+    if (fc == 0 && f < p.M) p.stats[f * p.ranges + range] = float4{s[j].rc, s[j].z, s[j].t, 0.f};
   }
 }
 
@@ -196,11 +228,10 @@ struct HeadOut {
   const int32_t* ids;
   float *logprob, *entropy, *top;
   int32_t* idx;
-  int n, k, wc;   // wc: waves along the classes in the first pass
+  int n, k, fw;   // fw: waves along the frames in the first pass
 };
 static constexpr int FT_ = 256;          // threads
 static constexpr int GROUPS = 512;       // most groups computed again
-static constexpr int WIDE = 64;          // largest k for threads' maxima
 
 // A class's logit, the bits of the first pass.
 struct Logit {
@@ -210,22 +241,44 @@ struct Logit {
   const i32x4* x;   // the frame's integers, in LDS
   int chunks;
   float xs;
-  __device__ __forceinline__ float operator()(int c) const {
+  __device__ __forceinline__ float value(int sum, int c) const { return int8_value(sum, scale_of(xs, ws[c]), bias ? bias[c] : 0.f); }
+  __device__ __forceinline__ int dot(const i32x4* r, int i) const {
+    const i32x4 u = r[i], v = x[i];
+    int a = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) a = __builtin_amdgcn_sdot4(u[j], v[j], a, false);
+    return a;
+  }
+  __device__ __forceinline__ float operator()(int c) const {   // by one lane
     const i32x4* r = (const i32x4*)(w + c * ldw);
     int a = 0;
 #pragma unroll 4
-    for (int i = 0; i < chunks; ++i) {
-      const i32x4 u = r[i], v = x[i];
+    for (int i = 0; i < chunks; ++i) a += dot(r, i);
+    return value(a, c);
+  }
+  // by four adjacent lanes, U classes at once; each lane has the results
+  template <int U>
+  __device__ __forceinline__ void four(const int (&c)[U], float (&v)[U]) const {
+    int a[U];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) a = __builtin_amdgcn_sdot4(u[j], v[j], a, false);
+    for (int u = 0; u < U; ++u) a[u] = 0;
+#pragma unroll 4
+    for (int i = threadIdx.x & 3; i < chunks; i += 4)
+#pragma unroll
+      for (int u = 0; u < U; ++u) a[u] += dot((const i32x4*)(w + c[u] * ldw), i);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      a[u] += __shfl_xor(a[u], 1);
+      a[u] += __shfl_xor(a[u], 2);
+      v[u] = value(a[u], c[u]);
     }
-    return int8_value(a, scale_of(xs, ws[c]), bias ? bias[c] : 0.f);
   }
 };
 
 struct HeadLds {
   TopkLds<FT_> l;
   float buf[3][FT_ / 64];
+  float listed[SOFTMAX_MAX_TOP];   // the listed classes' logits
   int32_t groups[GROUPS];
   uint32_t ngroups, hist[256], want;
 };
@@ -239,8 +292,8 @@ struct HeadLogProb {
   }
 };
 
-// Any row, its logits computed again in every pass: one with a NaN or infinities, with nothing
-// above FLOOR, or with too many classes that reach the threshold.
+// Any row, its logits computed again in every pass: one with a NaN or infinities, with fewer than k classes
+// above FLOOR, or with too many that reach the threshold.
 __device__ __attribute__((noinline)) void head_any(HeadLds& h, const Logit& logit, const HeadP& p, const HeadOut& o, int64_t m) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, K = p.K;
   float mx = -INFINITY;
@@ -323,60 +376,78 @@ __global__ __launch_bounds__(FT_) void int8_head_finish_kernel(const HeadP p, co
   const int64_t m = blockIdx.x;
   for (int i = tid; i < p.Kw / 16; i += FT_) ((i32x4*)xl)[i] = ((const i32x4*)(p.q + m * p.Kw))[i];
   const Logit logit{p.w, p.ldw, p.ws, p.bias, (const i32x4*)xl, p.Kw / 16, p.xs[m]};
-  // the sums, in a fixed order
-  Sums s{FLOOR * p.it2, 0.f, 0.f};
-  for (int i = tid; i < p.nstat; i += FT_) {
-    const float4 v = p.stats[m * p.nstat + i];
-    s.join(Sums{v.x, v.y, v.z});
-  }
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) s.join(Sums{__shfl_xor(s.rc, off), __shfl_xor(s.z, off), __shfl_xor(s.t, off)});
-  if (lane == 0) {
-    h.buf[0][wave] = s.rc;
-    h.buf[1][wave] = s.z;
-    h.buf[2][wave] = s.t;
-  }
   if (tid == 0) h.ngroups = h.l.count = 0;
+  // the sums are for the second and third wave, the list for the last: their first loads go out with the others
+  constexpr int NS = 4;
+  const float4* st = p.stats + m * p.ranges;
+  float4 sv[NS];
+  if (wave == 1 || wave == 2) {
+#pragma unroll
+    for (int i = 0; i < NS; ++i) sv[i] = st[min(tid - 64 + i * 128, p.ranges - 1)];
+  }
+  int at = -1;
+  if (wave == 3 && lane / 4 < o.n) at = o.ids[m * o.n + lane / 4];
   const float* gmax = p.gmax + m * p.ngroup;
   uint32_t mx = 0;
   if (o.k) {
+#pragma unroll 4
     for (int g = tid; g < p.ngroup; g += FT_) mx = max(mx, order_word(gmax[g]));
     h.l.tmax[tid] = mx;
   }
   __syncthreads();
-  s = Sums{h.buf[0][0], h.buf[1][0], h.buf[2][0]};
+  if (wave == 0) {
+    if (o.k) {
+      const uint32_t t = kth_search<12>(h.l, o.k);
+      if (lane == 0) h.l.thr = t;
+    }
+  } else if (wave < 3) {
+    float rc = START * p.it2;
 #pragma unroll
-  for (int i = 1; i < FT_ / 64; ++i) s.join(Sums{h.buf[0][i], h.buf[1][i], h.buf[2][i]});
-  // (a NaN fails both)
-  if (same(!(s.z > 0.f && s.z < INFINITY))) {
+    for (int i = 0; i < NS; ++i) rc = fmaxf(rc, sv[i].x);
+    for (int i = tid - 64 + NS * 128; i < p.ranges; i += 128) rc = fmaxf(rc, st[i].x);
+    rc = wave_max(rc);
+    float z = 0.f, t = 0.f;
+    auto add = [&](float4 v) {
+      Sums s{v.x, v.y, v.z};
+      s.rise(rc);
+      z += s.z;
+      t += s.t;
+    };
+#pragma unroll
+    for (int i = 0; i < NS; ++i)
+      if (tid - 64 + i * 128 < p.ranges) add(sv[i]);
+    for (int i = tid - 64 + NS * 128; i < p.ranges; i += 128) add(st[i]);
+    z = wave_sum(z);
+    t = wave_sum(t);
+    if (lane == 0) {
+      h.buf[wave][0] = rc;
+      h.buf[wave][1] = z;
+      h.buf[wave][2] = t;
+    }
+  } else {
+    for (int e = lane / 4; e < o.n; e += 16) {   // the four lanes of an entry stay together
+      if (e >= 16) at = o.ids[m * o.n + e];
+      const int c[1] = {at < 0 || at >= K ? 0 : at};
+      float v[1];
+      logit.four(c, v);
+      h.listed[e] = v[0];
+    }
+  }
+  __syncthreads();
+  Sums sums{h.buf[1][0], h.buf[1][1], h.buf[1][2]};
+  sums.join(Sums{h.buf[2][0], h.buf[2][1], h.buf[2][2]});
+  const float rc = sums.rc, z = sums.z, t = sums.t;
+  // (a NaN fails both; a temperature beyond that would bring FLOOR's classes back in)
+  if (same(!(z > 0.f && z < INFINITY && p.it2 > 1e-15f))) {
     head_any(h, logit, p, o, m);
     return;
   }
-  const HeadLogProb lp{s.rc, log2f(s.z), p.it2, p.itau};
+  const HeadLogProb lp{rc, log2f(z), p.it2, p.itau};
   if (o.k) {
-    uint32_t tw;
-    if (o.k <= WIDE) {
-      tw = kth_max<12, FT_>(h.l, o.k);
-    } else {
-      // over all groups, bit by bit
-      tw = 0;
-      for (int bit = 31; bit >= 12; --bit) {
-        const uint32_t c = tw | (1u << bit);
-        int n = 0;
-        for (int g = tid; g < p.ngroup; g += FT_) n += order_word(gmax[g]) >= c;
-#pragma unroll
-        for (int off = 32; off > 0; off >>= 1) n += __shfl_xor(n, off);
-        __syncthreads();
-        if (lane == 0) h.hist[wave] = n;
-        __syncthreads();
-        n = 0;
-        for (int i = 0; i < FT_ / 64; ++i) n += (int)h.hist[i];
-        if (n >= o.k) tw = c;
-      }
-    }
-    tw = max(tw, LOWEST);
+    const uint32_t tw = max(same(h.l.thr), order_word(START));
     const float thr = order_value(tw);
     if (mx >= tw) {
+#pragma unroll 4
       for (int g = tid; g < p.ngroup; g += FT_)
         if (gmax[g] >= thr) {
           const uint32_t at = atomicAdd(&h.ngroups, 1u);
@@ -384,23 +455,34 @@ __global__ __launch_bounds__(FT_) void int8_head_finish_kernel(const HeadP p, co
         }
     }
     __syncthreads();
-    const int ng = (int)same(h.ngroups), size = 32 / o.wc, ni = 4 / o.wc;
-    if (ng > GROUPS) {
-      head_any(h, logit, p, o, m);
-      return;
-    }
-    for (int e = tid; e < ng * size; e += FT_) {
-      const int g = h.groups[e / size], q = g % 4, w = g / 4 % o.wc, pair = g / 4 / o.wc;
-      const int u = e % size / (4 * ni), i = e % (4 * ni) / 4, r = e % 4;
-      const int c = pair * PAIR + u * CT + (w * ni + i) * 16 + 4 * q + r;
-      if (c < K) {
-        const float v = logit(c);
-        if (v >= thr) push(h.l, v, c);
+    // a group's classes: 4 adjacent ones of every 16 that its wave has in a tile
+    const int ng = (int)same(h.ngroups), tg = group_tiles(o.fw), wc = 4 / o.fw, ni = o.fw, size = 4 * ni * tg;
+    constexpr int U = 2;
+    if (ng <= GROUPS) {
+      for (int e0 = 0; e0 < ng * size; e0 += U * FT_ / 4) {
+        int c[U];
+        float v[U];
+        bool in[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int e = e0 + u * (FT_ / 4) + tid / 4;
+          in[u] = e < ng * size;
+          const int g = in[u] ? h.groups[e / size] : 0, q = g % 4, w = g / 4 % wc, tile = g / 4 / wc * tg;
+          const int b = e % size / (4 * ni), i = e % (4 * ni) / 4, r = e % 4;
+          c[u] = (tile + b) * CT + (w * ni + i) * 16 + 4 * q + r;
+          in[u] = in[u] && c[u] < K;
+          c[u] = in[u] ? c[u] : 0;
+        }
+        logit.four(c, v);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (in[u] && (tid & 3) == 0 && v[u] >= thr) push(h.l, v[u], c[u]);
       }
+      __syncthreads();
     }
-    __syncthreads();
     const int n = (int)same(h.l.count);
-    if (n > CAND) {
+    // too many reach the threshold, or, where fewer than k classes lie above FLOOR, too few
+    if (ng > GROUPS || n > CAND || n < o.k) {
       head_any(h, logit, p, o, m);
       return;
     }
@@ -408,10 +490,10 @@ __global__ __launch_bounds__(FT_) void int8_head_finish_kernel(const HeadP p, co
     rank(h.l, n, m, tp, lp);
   }
   if (tid < o.n) {
-    const int at = o.ids[m * o.n + tid];
-    o.logprob[m * o.n + tid] = at < 0 || at >= K ? 0.f : lp(logit(at));
+    const int id = o.ids[m * o.n + tid];
+    o.logprob[m * o.n + tid] = id < 0 || id >= K ? 0.f : lp(h.listed[tid]);
   }
-  if (o.entropy && tid == 0) o.entropy[m] = (lp.l2z - s.t / s.z) * LN2_F;
+  if (o.entropy && tid == 0) o.entropy[m] = (lp.l2z - t / z) * LN2_F;
 }
 
 // ---------------------------------------------------------------------------
@@ -419,7 +501,7 @@ __global__ __launch_bounds__(FT_) void int8_head_finish_kernel(const HeadP p, co
 // ---------------------------------------------------------------------------
 struct HeadPlan {
   int fn, fw, ks;                 // frames / 16 of a wave, waves along the frames, column steps
-  int nf, ranges, ppr, nstat, ngroup;
+  int nf, ranges, per, ngroup;
   size_t stats, gmax, bytes;      // behind the tokens
 };
 static constexpr int HEAD_MAX_STEPS = 16;
@@ -428,25 +510,25 @@ static HeadPlan head_plan(int64_t M, int32_t K, int32_t Kw) {
   HeadPlan h{};
   h.ks = (int)cdiv(Kw, 64);
   h.fn = h.ks > 8 ? 1 : 2;
-  const int per = 16 * h.fn;
-  h.fw = M <= per ? 1 : M <= 2 * per ? 2 : 4;
-  h.nf = (int)cdiv(M, per * h.fw);
-  const int64_t pairs = cdiv(K, PAIR), slots = h.ks > 8 ? 256 : 512;
+  const int frames = 16 * h.fn;
+  h.fw = M <= frames ? 1 : M <= 2 * frames ? 2 : 4;
+  h.nf = (int)cdiv(M, frames * h.fw);
+  const int tg = group_tiles(h.fw);
+  const int64_t units = cdiv(K, CT * tg), slots = 256 * (h.ks > 8 ? 1 : h.ks > 4 ? 2 : 3);
   // as many ranges as take least: whole rounds of the chip, each as long as a range and its start
-  int64_t best = -1;
-  for (int64_t r = 1; r <= pairs && r <= std::max<int64_t>(1, 2 * slots / h.nf); ++r) {
-    const int64_t ppr = cdiv(pairs, r), t = cdiv(cdiv(pairs, ppr) * h.nf, slots) * (2 * ppr + 1);
+  int64_t best = -1, per = 1;
+  for (int64_t r = 1; r <= units && r <= std::max<int64_t>(1, 2 * slots / h.nf); ++r) {
+    const int64_t u = cdiv(units, r), t = cdiv(cdiv(units, u) * h.nf, slots) * (u * tg + 1);
     if (best < 0 || t < best) {
       best = t;
-      h.ppr = (int)ppr;
+      per = u;
     }
   }
-  h.ranges = (int)cdiv(pairs, h.ppr);
-  const int wc = 4 / h.fw;
-  h.nstat = h.ranges * wc;
-  h.ngroup = (int)pairs * wc * 4;
+  h.per = (int)per * tg;
+  h.ranges = (int)cdiv(units, per);
+  h.ngroup = (int)units * (4 / h.fw) * 4;
   h.stats = 0;
-  h.gmax = (size_t)rup(M * h.nstat * 16, 256);
+  h.gmax = (size_t)rup(M * h.ranges * 16, 256);
   h.bytes = h.gmax + (size_t)rup(M * h.ngroup * 4, 256);
   return h;
 }
@@ -458,8 +540,8 @@ int int8_head(const int8_t* q, const float* xs, int64_t M, const int8_t* w, int6
               int32_t Kw, const float* bias, const softmax_scores& sc, char* buf, hipStream_t s) {
   const HeadPlan h = head_plan(M, K, Kw);
   HeadP p{};
-  p.q = q; p.w = w; p.ldw = ldw; p.xs = xs; p.ws = ws; p.bias = bias; p.M = M; p.K = K; p.Kw = Kw; p.ksteps = h.ks;
-  p.nf = h.nf; p.ranges = h.ranges; p.ppr = h.ppr; p.nstat = h.nstat; p.ngroup = h.ngroup;
+  p.q = q; p.w = w; p.ldw = ldw; p.xs = xs; p.ws = ws; p.bias = bias; p.M = M; p.K = K; p.Kw = Kw;
+  p.nf = h.nf; p.ranges = h.ranges; p.per = h.per; p.ngroup = h.ngroup;
   p.it2 = LOG2E_F / sc.temperature; p.itau = 1.f / sc.temperature;
   p.stats = (float4*)(buf + h.stats);
   p.gmax = sc.k ? (float*)(buf + h.gmax) : nullptr;
@@ -485,7 +567,7 @@ int int8_head(const int8_t* q, const float* xs, int64_t M, const int8_t* w, int6
 #undef INT
   int rc = blstm_check_launch("int8_head");
   if (rc) return rc;
-  const HeadOut o{sc.ids, sc.logprob, sc.entropy, sc.top, sc.idx, sc.n, sc.k, 4 / h.fw};
+  const HeadOut o{sc.ids, sc.logprob, sc.entropy, sc.top, sc.idx, sc.n, sc.k, h.fw};
   BLSTM_LAUNCH("int8_head_finish", int8_head_finish_kernel, dim3((unsigned)M), dim3(FT_), (size_t)Kw, s, p, o);
   return blstm_check_launch("int8_head_finish");
 }

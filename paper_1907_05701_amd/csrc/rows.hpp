@@ -205,24 +205,28 @@ __device__ __forceinline__ uint32_t kth_word(const uint32_t (&w)[NW], int k) {
   return t;
 }
 static constexpr int FOLD = 64;   // largest k for groups
+// (of one wave, behind a barrier)
+template <int LOW, int T>
+__device__ __forceinline__ uint32_t kth_search(const TopkLds<T>& l, int k) {
+  const int lane = threadIdx.x & 63;
+  constexpr int NW = T / 64;
+  uint32_t w[NW];
+#pragma unroll
+  for (int i = 0; i < NW; ++i) w[i] = l.tmax[i * 64 + lane];
+  if (k <= FOLD) {
+    uint32_t g[2] = {w[0], w[1]};
+#pragma unroll
+    for (int i = 2; i < NW; ++i) g[i & 1] = max(g[i & 1], w[i]);
+    return kth_word<LOW>(g, k);
+  }
+  return kth_word<LOW>(w, k);
+}
 template <int LOW, int T>
 __device__ __forceinline__ uint32_t kth_max(TopkLds<T>& l, int k) {
-  const int lane = threadIdx.x & 63;
   __syncthreads();
   if (threadIdx.x < 64) {
-    constexpr int NW = T / 64;
-    uint32_t w[NW], t;
-#pragma unroll
-    for (int i = 0; i < NW; ++i) w[i] = l.tmax[i * 64 + lane];
-    if (k <= FOLD) {
-      uint32_t g[2] = {w[0], w[1]};
-#pragma unroll
-      for (int i = 2; i < NW; ++i) g[i & 1] = max(g[i & 1], w[i]);
-      t = kth_word<LOW>(g, k);
-    } else {
-      t = kth_word<LOW>(w, k);
-    }
-    if (lane == 0) l.thr = t;
+    const uint32_t t = kth_search<LOW>(l, k);
+    if ((threadIdx.x & 63) == 0) l.thr = t;
   }
   __syncthreads();
   return l.thr;

@@ -317,6 +317,15 @@ def test_head_of_large_logits(gpu_lib):
     check_head(x, w, ws, bias, ids, 9)
 
 
+def test_head_at_extreme_temperatures(gpu_lib):
+    """At 2^100 every class that is not at -inf is alike; at 2^-20 the largest has it all."""
+    x, w, ws, bias, ids = head_case(5, 64, 900, 2, "fp32")
+    bias[::7] = -math.inf
+    check_head(x, w, ws, bias, ids, 9, 2.0 ** 100)
+    check_head(x, w, ws, bias, ids, 9, 2.0 ** 40)
+    check_head(x, w, ws, bias, ids, 9, 2.0 ** -20)
+
+
 def test_head_asks_for_parts_and_leaves_the_rest(gpu_lib):
     x, w, ws, bias, ids = head_case(50, 256, 2000, 4, "bf16")
     full = head(x, w, ws, bias, ids, 6)
