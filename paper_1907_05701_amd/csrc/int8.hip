@@ -125,10 +125,9 @@ struct Int8P {
 
 // Four channels of a token, from n on.
 template <typename TO>
-__device__ __forceinline__ void put4(const Int8P& p, int64_t m, int64_t n, i32x4 a) {
+__device__ __forceinline__ void put4(const Int8P& p, int64_t m, int64_t n, i32x4 a, float xs) {
   if (m >= p.M || n >= p.N) return;
   TO* y = (TO*)p.y + m * p.ldy + n;
-  const float xs = p.xs[m];
   TO o[4];
   if (n + 4 <= p.N) {
     float w[4], b[4] = {0.f, 0.f, 0.f, 0.f};
@@ -161,7 +160,6 @@ __device__ __forceinline__ void stage(const int8_t* base, int64_t ld, int64_t ro
 template <typename TO, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(WM * WN * 64) void int8_tile_kernel(const Int8P p) {
   constexpr int NW = WM * WN, FM = BM / WM / 16, FN = BN / WN / 16, STAGE = (BM + BN) * 128;
-  constexpr int LOADS = (BM + BN) / 8 / NW;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, wm = wid % WM, wn = wid / WM;
   int z, tm, tn;
@@ -201,12 +199,14 @@ __global__ __launch_bounds__(WM * WN * 64) void int8_tile_kernel(const Int8P p) 
         for (int j = 0; j < FN; ++j) acc[i][j] = mma_i8(a[i], b[j], acc[i][j]);
     }
   }
+  float xs[FN];
+#pragma unroll
+  for (int j = 0; j < FN; ++j) xs[j] = p.xs[min(m0 + wn * (BN / WN) + j * 16 + fr, p.M - 1)];
 #pragma unroll
   for (int i = 0; i < FM; ++i)
 #pragma unroll
     for (int j = 0; j < FN; ++j)
-      put4<TO>(p, m0 + wn * (BN / WN) + j * 16 + fr, n0 + wm * (BM / WM) + i * 16 + 4 * fc, acc[i][j]);
-  (void)LOADS;
+      put4<TO>(p, m0 + wn * (BN / WN) + j * 16 + fr, n0 + wm * (BM / WM) + i * 16 + 4 * fc, acc[i][j], xs[j]);
 }
 
 // Few tokens: 16 channels and up to 16 FN tokens a workgroup, whose four waves
@@ -241,7 +241,67 @@ __global__ __launch_bounds__(256) void int8_few_kernel(const Int8P p) {
   if (wid > 0) return;
 #pragma unroll
   for (int j = 0; j < FN; ++j)
-    put4<TO>(p, m0 + j * 16 + fr, n0 + 4 * fc, acc[j] + part[0][j][lane] + part[1][j][lane] + part[2][j][lane]);
+    put4<TO>(p, m0 + j * 16 + fr, n0 + 4 * fc, acc[j] + part[0][j][lane] + part[1][j][lane] + part[2][j][lane],
+             p.xs[min(m0 + j * 16 + fr, p.M - 1)]);
+}
+
+// The same for up to 16 tokens of 16-bit or 32-bit floats (TO, also y's), quantised on the way by every workgroup: a wave
+// takes the maximum of its part of the tokens while its weights are in flight, the four join them in LDS.  The
+// first 1024 columns stay in registers between the two uses, others are read again.
+struct Int8FewP {
+  Int8P p;
+  const void* x;
+  int64_t ldx;
+  int K;   // columns of x; p.K those of the weights
+};
+template <typename TO>
+__global__ __launch_bounds__(256) void int8_few_tokens_kernel(const Int8FewP a) {
+  const Int8P& p = a.p;
+  constexpr int U = 4;
+  __shared__ i32x4 part[3][64];
+  __shared__ float amax[4][16], xs[16];
+  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, fr = lane & 15, fc = lane >> 4;
+  const int64_t n0 = (int64_t)blockIdx.x * 16;
+  const int8_t* wr = p.w + min(n0 + fr, p.N - 1) * p.ldw;   // rows past the last: any, dropped at the end
+  const TO* xr = (const TO*)a.x + min((int64_t)fr, p.M - 1) * a.ldx;
+  const int k0 = wid * 64 + fc * 16;
+  auto weights = [&](int k) { return k < p.K ? *(const i32x4*)(wr + k) : i32x4{0, 0, 0, 0}; };
+  i32x4 w[U];
+  Lane16<TO> x[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) lane16_load(x[u], xr, k0 + u * 256, a.K);
+#pragma unroll
+  for (int u = 0; u < U; ++u) w[u] = weights(k0 + u * 256);
+  float mx = 0.f;
+#pragma unroll
+  for (int u = 0; u < U; ++u) mx = lane16_max(x[u], mx);
+#pragma unroll 2
+  for (int k = k0 + U * 256; k < a.K; k += 256) {
+    Lane16<TO> more;
+    lane16_load(more, xr, k, a.K);
+    mx = lane16_max(more, mx);
+  }
+  mx = max_abs(mx, __shfl_xor(mx, 16));
+  mx = max_abs(mx, __shfl_xor(mx, 32));
+  if (fc == 0) amax[wid][fr] = mx;
+  __syncthreads();
+  mx = max_abs(max_abs(max_abs(amax[0][fr], amax[1][fr]), amax[2][fr]), amax[3][fr]);
+  const Quant to(mx);
+  i32x4 acc{0, 0, 0, 0};
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+    if (wid * 64 + u * 256 < p.K) acc = mma_i8(w[u], lane16_ints(x[u], to), acc);
+#pragma unroll 2
+  for (int k = k0 + U * 256; k < p.K + fc * 16; k += 256) {   // alike in every lane of the wave
+    Lane16<TO> more;
+    lane16_load(more, xr, k, a.K);
+    acc = mma_i8(weights(k), lane16_ints(more, to), acc);
+  }
+  if (wid > 0) part[wid - 1][lane] = acc;
+  if (wid == 0 && fc == 0) xs[fr] = to.scale;
+  __syncthreads();
+  if (wid > 0) return;
+  put4<TO>(p, fr, n0 + 4 * fc, acc + part[0][lane] + part[1][lane] + part[2][lane], xs[fr]);
 }
 
 template <typename TO>
@@ -365,6 +425,15 @@ extern "C" int int8_linear_rows(const void* x, int64_t ldx, int64_t M, int32_t K
   if (rc) return rc;
   if (!y) return blstm_fail(BLSTM_EINVAL, "%s: NULL pointer", fn);
   if (ldy < N) return blstm_fail(BLSTM_EINVAL, "%s: a row pitch is below its row", fn);
+  if (M <= 16) {
+    Int8FewP a{};
+    a.p.w = w; a.p.ldw = ldw; a.p.ldy = ldy; a.p.M = M; a.p.N = N; a.p.K = Kw; a.p.ws = w_scale; a.p.bias = bias; a.p.y = y;
+    a.x = x; a.ldx = ldx; a.K = K;
+    const dim3 grid((unsigned)cdiv(N, 16));
+    if (precision == BLSTM_BF16) BLSTM_LAUNCH("int8_linear_few", int8_few_tokens_kernel<bf16>, grid, dim3(256), 0, stream, a);
+    else BLSTM_LAUNCH("int8_linear_few", int8_few_tokens_kernel<float>, grid, dim3(256), 0, stream, a);
+    return blstm_check_launch(fn);
+  }
   int8_t* q = (int8_t*)ws;
   float* scale = (float*)((char*)ws + rup(M * Kw, 256));
   rc = int8_quantize_rows(x, ldx, M, K, precision, q, Kw, Kw, scale, stream);
@@ -382,7 +451,8 @@ extern "C" int int8_logprob_ws_bytes(int64_t M, int32_t K, int32_t Kw, size_t* b
   if (rc) return rc;
   if (K > SOFTMAX_MAX_CLASSES || Kw > INT8_MAX_K) return blstm_fail(BLSTM_EUNSUPPORTED, "int8_logprob_ws_bytes: too many classes or columns");
   if (bytes)
-    *bytes = tokens_bytes(M, rup(Kw, 16)) + (int8_head_fits(Kw) ? int8_head_bytes(M, K, Kw) : (size_t)logit_rows(M, K) * rup(K, 4) * 4);
+    *bytes = int8_head_fits(Kw) ? int8_head_bytes(M, K, (int32_t)rup(Kw, 16))
+                                : tokens_bytes(M, rup(Kw, 16)) + (size_t)logit_rows(M, K) * rup(K, 4) * 4;
   return BLSTM_OK;
 }
 
@@ -396,9 +466,11 @@ extern "C" int int8_logprob_rows(const void* x, int64_t ldx, int64_t M, int32_t 
   int8_t* q = (int8_t*)ws;
   float* scale = (float*)((char*)ws + rup(M * Kw, 256));
   char* rest = (char*)ws + tokens_bytes(M, Kw);
+  if (int8_head_fits(Kw))
+    return precision == BLSTM_BF16
+               ? int8_head((const bf16*)x, ldx, M, P, w, ldw, w_scale, K, Kw, bias, *scores, (char*)ws, stream)
+               : int8_head((const float*)x, ldx, M, P, w, ldw, w_scale, K, Kw, bias, *scores, (char*)ws, stream);
   rc = int8_quantize_rows(x, ldx, M, P, precision, q, Kw, Kw, scale, stream);
-  if (rc) return rc;
-  if (int8_head_fits(Kw)) return int8_head(q, scale, M, w, ldw, w_scale, K, Kw, bias, *scores, rest, stream);
   float* logits = (float*)rest;
   const int64_t ld = rup(K, 4), step = logit_rows(M, K);
   for (int64_t r0 = 0; !rc && r0 < M; r0 += step) {

@@ -47,6 +47,40 @@ __device__ __forceinline__ uint32_t pack4(int a, int b, int c, int d) {
   return (uint32_t)(a & 255) | (uint32_t)(b & 255) << 8 | (uint32_t)(c & 255) << 16 | (uint32_t)d << 24;
 }
 
+// 16 values of a row from column k on, as an MFMA lane takes them (0 behind column K).
+template <typename TI> struct Lane16 { TI v[16]; };
+template <typename TI>
+__device__ __forceinline__ void lane16_load(Lane16<TI>& o, const TI* row, int k, int K) {
+  constexpr int V = 16 / sizeof(TI);
+#pragma unroll
+  for (int i = 0; i < 16; i += V) {
+    if (k + i + V <= K) {
+      __builtin_memcpy(o.v + i, row + k + i, 16);
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j) o.v[i + j] = k + i + j < K ? row[k + i + j] : from_f32<TI>(0.f);
+    }
+  }
+}
+__device__ __forceinline__ float max_abs(float m, float v) {   // a NaN stays
+  const float a = fabsf(v);
+  return m > a || m != m ? m : a;
+}
+template <typename TI>
+__device__ __forceinline__ float lane16_max(const Lane16<TI>& x, float m) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) m = max_abs(m, to_f32(x.v[i]));
+  return m;
+}
+template <typename TI>
+__device__ __forceinline__ i32x4 lane16_ints(const Lane16<TI>& x, const Quant& to) {
+  i32x4 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    r[i] = (int)pack4(to(to_f32(x.v[4 * i])), to(to_f32(x.v[4 * i + 1])), to(to_f32(x.v[4 * i + 2])), to(to_f32(x.v[4 * i + 3])));
+  return r;
+}
+
 // A sum of products as a number: each step a single float32 rounding.
 __device__ __forceinline__ float int8_value(int sum, float scale, float bias) {
 #pragma clang fp contract(off)
@@ -71,9 +105,10 @@ template <typename TI>
 void int8_quantize(const TI* x, int64_t ldx, int64_t M, int32_t K, int8_t* q, int64_t ldq, int32_t Kq, float* scale,
                    hipStream_t stream);
 
-// Log probabilities of a head of K classes from tokens as integers [M][Kw] and their scales (int8_head.hip);
-// buf: int8_head_bytes.  For up to so many columns:
+// Log probabilities of a head of K classes from tokens x [M][P] (int8_head.hip); buf: int8_head_bytes.  For up to
+// so many columns:
 bool int8_head_fits(int32_t Kw);
 size_t int8_head_bytes(int64_t M, int32_t K, int32_t Kw);
-int int8_head(const int8_t* q, const float* xs, int64_t M, const int8_t* w, int64_t ldw, const float* ws, int32_t K,
+template <typename TI>
+int int8_head(const TI* x, int64_t ldx, int64_t M, int32_t P, const int8_t* w, int64_t ldw, const float* ws, int32_t K,
               int32_t Kw, const float* bias, const softmax_scores& scores, char* buf, hipStream_t stream);

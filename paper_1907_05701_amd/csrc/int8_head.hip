@@ -29,9 +29,14 @@ static constexpr float FLOOR = -1e30f, START = 0.5f * FLOOR;
 static constexpr float SLACK = 4.f;
 
 struct HeadP {
-  const int8_t *q, *w;
+  const void* x;           // tokens, where the first pass quantises them itself
+  int64_t ldx;
+  int P;
+  int8_t* q;               // their integers [M][Kw] and scales
+  float* xs;
+  const int8_t* w;
   int64_t ldw;
-  const float *xs, *ws, *bias;
+  const float *ws, *bias;
   int64_t M;
   int K, Kw;               // classes, columns
   int nf, ranges, per;     // frame tiles, class ranges, tiles a range
@@ -69,9 +74,10 @@ __device__ __forceinline__ int head_slot(int c, int r) {
 }
 
 // KS: most 64-column steps; 16 FN frames a wave; FW waves side by side along the
-// frames, the other 4 / FW along the classes of a tile.
+// frames, the other 4 / FW along the classes of a tile.  TI: tokens of this type are quantised here, by every workgroup
+// for itself (a launch less), and left for the second pass by the first range's; void: their integers lie in memory.
 template <int KS> constexpr int head_per_cu() { return KS > 8 ? 1 : KS > 4 ? 2 : 3; }   // workgroups
-template <int KS, int FN, int FW>
+template <int KS, int FN, int FW, typename TI>
 __global__ __launch_bounds__(256, head_per_cu<KS>()) void int8_head_kernel(const HeadP p) {
   constexpr int WC = 4 / FW, NI = 4 / WC, TG = group_tiles(FW), NCH = KS * 4, TILE = CT * KS * 64, STAGE = TILE + 512;
   constexpr int LOADS = TILE / 1024 / 4;   // of a wave
@@ -97,15 +103,19 @@ __global__ __launch_bounds__(256, head_per_cu<KS>()) void int8_head_kernel(const
   auto put = [&](int j) {
     if (wid < 2) *(float*)(lds + (j & 1) * STAGE + TILE + wid * 256 + lane * 4) = next;
   };
+  // a tile's rows end with the last class: what lies behind it, and behind a row's columns, reads as zeros
+  uint32_t off[LOADS];
+#pragma unroll
+  for (int i = 0; i < LOADS; ++i) {
+    const int pos = (i * 4 + wid) * 64 + lane, row = pos / NCH, c = head_slot<NCH>(pos % NCH, row);
+    off[i] = c * 16 < p.Kw ? (uint32_t)(row * p.ldw + c * 16) : DMA_OFF_NONE;
+  }
   auto issue = [&](int j) {
     char* st = lds + (j & 1) * STAGE;
-    const __amdgpu_buffer_rsrc_t r = dma_rsrc(wb + (int64_t)j * CT * p.ldw);
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
+        (void*)(wb + (int64_t)j * CT * p.ldw), (short)0, (int)(min(CT, rows - j * CT) * p.ldw), 0x00020000);
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      const int pos = (i * 4 + wid) * 64 + lane, row = pos / NCH, c = head_slot<NCH>(pos % NCH, row);
-      const bool in = j * CT + row < rows && c * 16 < p.Kw;
-      dma16(r, in ? (uint32_t)(row * p.ldw + c * 16) : DMA_OFF_NONE, st + (i * 4 + wid) * 1024);
-    }
+    for (int i = 0; i < LOADS; ++i) dma16(r, off[i], st + (i * 4 + wid) * 1024);
   };
   issue(0);
   fetch(0);
@@ -115,11 +125,40 @@ __global__ __launch_bounds__(256, head_per_cu<KS>()) void int8_head_kernel(const
 #pragma unroll
   for (int j = 0; j < FN; ++j) {
     const int64_t f = min(f0 + j * 16 + fr, p.M - 1);   // frames past the last: any, not stored
-    xs[j] = p.xs[f];
+    if constexpr (std::is_void<TI>::value) {
+      xs[j] = p.xs[f];
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      const int k = ks * 64 + fc * 16;
-      b[j][ks] = k < p.Kw ? *(const i32x4*)(p.q + f * p.Kw + k) : i32x4{0, 0, 0, 0};
+      for (int ks = 0; ks < KS; ++ks) {
+        const int k = ks * 64 + fc * 16;
+        b[j][ks] = k < p.Kw ? *(const i32x4*)(p.q + f * p.Kw + k) : i32x4{0, 0, 0, 0};
+      }
+    } else {
+      if (j > 0 && f0 + j * 16 >= p.M) {   // none of these frames exists
+        xs[j] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) b[j][ks] = i32x4{0, 0, 0, 0};
+        continue;
+      }
+      Lane16<TI> x[KS];
+      float mx = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) lane16_load(x[ks], (const TI*)p.x + f * p.ldx, ks * 64 + fc * 16, p.P);
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) mx = lane16_max(x[ks], mx);
+      mx = max_abs(mx, __shfl_xor(mx, 16));
+      mx = max_abs(mx, __shfl_xor(mx, 32));
+      const Quant to(mx);
+      xs[j] = to.scale;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) b[j][ks] = lane16_ints(x[ks], to);
+      if (range == 0 && wc == 0 && f0 + j * 16 + fr < p.M) {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          const int k = ks * 64 + fc * 16;
+          if (k < p.Kw) *(i32x4*)(p.q + f * p.Kw + k) = b[j][ks];
+        }
+        if (fc == 0) p.xs[f] = to.scale;
+      }
     }
   }
   Sums s[FN];
@@ -294,7 +333,7 @@ struct HeadLogProb {
 
 // Any row, its logits computed again in every pass: one with a NaN or infinities, with fewer than k classes
 // above FLOOR, or with too many that reach the threshold.
-__device__ __attribute__((noinline)) void head_any(HeadLds& h, const Logit& logit, const HeadP& p, const HeadOut& o, int64_t m) {
+__device__ __forceinline__ void head_any(HeadLds& h, const Logit& logit, const HeadP& p, const HeadOut& o, int64_t m) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, K = p.K;
   float mx = -INFINITY;
   bool nan = false;
@@ -369,7 +408,7 @@ __device__ __attribute__((noinline)) void head_any(HeadLds& h, const Logit& logi
   rank(h.l, o.k, m, tp, value);
 }
 
-__global__ __launch_bounds__(FT_) void int8_head_finish_kernel(const HeadP p, const HeadOut o) {
+__global__ __launch_bounds__(FT_, 8) void int8_head_finish_kernel(const HeadP p, const HeadOut o) {
   extern __shared__ __attribute__((aligned(16))) char xl[];
   __shared__ HeadLds h;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, K = p.K;
@@ -534,21 +573,26 @@ static HeadPlan head_plan(int64_t M, int32_t K, int32_t Kw) {
 }
 
 bool int8_head_fits(int32_t Kw) { return cdiv(Kw, 64) <= HEAD_MAX_STEPS; }
-size_t int8_head_bytes(int64_t M, int32_t K, int32_t Kw) { return head_plan(M, K, Kw).bytes; }
+static size_t ints_bytes(int64_t M, int32_t Kw) { return (size_t)(rup(M * Kw, 256) + rup(M * 4, 256)); }
+size_t int8_head_bytes(int64_t M, int32_t K, int32_t Kw) { return ints_bytes(M, Kw) + head_plan(M, K, Kw).bytes; }
 
-int int8_head(const int8_t* q, const float* xs, int64_t M, const int8_t* w, int64_t ldw, const float* ws, int32_t K,
+template <typename TI>
+int int8_head(const TI* x, int64_t ldx, int64_t M, int32_t P, const int8_t* w, int64_t ldw, const float* ws, int32_t K,
               int32_t Kw, const float* bias, const softmax_scores& sc, char* buf, hipStream_t s) {
   const HeadPlan h = head_plan(M, K, Kw);
   HeadP p{};
-  p.q = q; p.w = w; p.ldw = ldw; p.xs = xs; p.ws = ws; p.bias = bias; p.M = M; p.K = K; p.Kw = Kw;
+  p.x = x; p.ldx = ldx; p.P = P; p.q = (int8_t*)buf; p.xs = (float*)(buf + rup(M * Kw, 256));
+  p.w = w; p.ldw = ldw; p.ws = ws; p.bias = bias; p.M = M; p.K = K; p.Kw = Kw;
   p.nf = h.nf; p.ranges = h.ranges; p.per = h.per; p.ngroup = h.ngroup;
   p.it2 = LOG2E_F / sc.temperature; p.itau = 1.f / sc.temperature;
+  buf += ints_bytes(M, Kw);
   p.stats = (float4*)(buf + h.stats);
   p.gmax = sc.k ? (float*)(buf + h.gmax) : nullptr;
+  if (h.fw == 4) int8_quantize(x, ldx, M, P, p.q, Kw, Kw, p.xs, s);
   auto launch = [&](auto ks, auto fn, auto fw) {
     constexpr int KS = decltype(ks)::value, FN = decltype(fn)::value, FW = decltype(fw)::value;
     constexpr size_t bytes = 2 * (CT * KS * 64 + 512);
-    auto kernel = int8_head_kernel<KS, FN, FW>;
+    auto kernel = int8_head_kernel<KS, FN, FW, typename std::conditional<FW == 4, void, TI>::type>;
     static std::atomic<uint64_t> raised{0};
     kc_raise_lds_limit((const void*)kernel, bytes, raised);
     BLSTM_LAUNCH("int8_head", kernel, dim3((unsigned)(h.ranges * h.nf)), dim3(256), bytes, s, p);
@@ -565,9 +609,11 @@ int int8_head(const int8_t* q, const float* xs, int64_t M, const int8_t* w, int6
   else if (h.ks <= 8) waves(INT(8), INT(2));
   else waves(INT(16), INT(1));
 #undef INT
-  int rc = blstm_check_launch("int8_head");
+  const int rc = blstm_check_launch("int8_head");
   if (rc) return rc;
   const HeadOut o{sc.ids, sc.logprob, sc.entropy, sc.top, sc.idx, sc.n, sc.k, h.fw};
   BLSTM_LAUNCH("int8_head_finish", int8_head_finish_kernel, dim3((unsigned)M), dim3(FT_), (size_t)Kw, s, p, o);
   return blstm_check_launch("int8_head_finish");
 }
+template int int8_head<float>(const float*, int64_t, int64_t, int32_t, const int8_t*, int64_t, const float*, int32_t, int32_t, const float*, const softmax_scores&, char*, hipStream_t);
+template int int8_head<bf16>(const bf16*, int64_t, int64_t, int32_t, const int8_t*, int64_t, const float*, int32_t, int32_t, const float*, const softmax_scores&, char*, hipStream_t);
