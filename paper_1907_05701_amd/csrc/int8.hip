@@ -14,69 +14,42 @@
 // Tokens to integers.  T threads a row (a wave, or a workgroup of 256); a row
 // of up to NV vectors a thread is read once, longer ones (NV = 0) twice.
 // ---------------------------------------------------------------------------
-template <typename TI> struct Vec8;
-template <> struct Vec8<bf16> { static constexpr int n = 8; };
-template <> struct Vec8<float> { static constexpr int n = 4; };
-
 template <typename TI, int T, int NV>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(const TI* __restrict__ x, int64_t ldx, int64_t M, int K,
                                                             int8_t* __restrict__ q, int64_t ldq, int Kq,
                                                             float* __restrict__ scale) {
-  constexpr int V = Vec8<TI>::n, NR = NV ? NV : 1;
+  constexpr int V = Vec16<TI>::n, NR = NV ? NV : 1;
   __shared__ float buf[4];
   const int tid = T == 64 ? threadIdx.x & 63 : threadIdx.x;
   const int64_t m = T == 64 ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
   if (T == 64 && m >= M) return;   // no barrier there
   const TI* s = x + m * ldx;
   int8_t* d = q + m * ldq;
-  TI v[NR][V];
+  Vec16<TI> v[NR];
   float mx = 0.f;
-  auto load = [&](int c, TI (&o)[V]) {
-    if (c + V <= K) {
-      __builtin_memcpy(o, s + c, V * sizeof(TI));
-    } else {
-#pragma unroll
-      for (int j = 0; j < V; ++j) o[j] = c + j < K ? s[c + j] : from_f32<TI>(0.f);
-    }
-  };
-  auto see = [&](const TI (&o)[V]) {
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const float a = fabsf(to_f32(o[j]));
-      mx = mx > a || mx != mx ? mx : a;   // a NaN stays
-    }
-  };
   if constexpr (NV > 0) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) load((i * T + tid) * V, v[i]);
+    for (int i = 0; i < NV; ++i) v[i].load(s, (i * T + tid) * V, K);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) see(v[i]);
+    for (int i = 0; i < NV; ++i) mx = v[i].max(mx);
   } else {
     for (int c = tid * V; c < K; c += T * V) {
-      load(c, v[0]);
-      see(v[0]);
+      v[0].load(s, c, K);
+      mx = v[0].max(mx);
     }
   }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    const float a = __shfl_xor(mx, o);
-    mx = mx > a || mx != mx ? mx : a;
-  }
+  mx = wave_max_abs(mx);
   if constexpr (T == 256) {
     if ((tid & 63) == 0) buf[tid >> 6] = mx;
     __syncthreads();
-    mx = buf[0];
-#pragma unroll
-    for (int i = 1; i < 4; ++i) mx = mx > buf[i] || mx != mx ? mx : buf[i];
+    mx = max_abs(max_abs(max_abs(buf[0], buf[1]), buf[2]), buf[3]);
   }
   const Quant to(mx);
   if (tid == 0) scale[m] = to.scale;
-  auto store = [&](int c, const TI (&o)[V]) {
+  auto store = [&](int c, const Vec16<TI>& o) {
     if (c >= Kq) return;   // Kq is a multiple of V
     uint32_t w[V / 4];
-#pragma unroll
-    for (int j = 0; j < V / 4; ++j)
-      w[j] = pack4(to(to_f32(o[4 * j])), to(to_f32(o[4 * j + 1])), to(to_f32(o[4 * j + 2])), to(to_f32(o[4 * j + 3])));
+    quantize(to, o.v, w);
     __builtin_memcpy(d + c, w, V);
   };
   if constexpr (NV > 0) {
@@ -84,7 +57,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const TI* __restrict
     for (int i = 0; i < NV; ++i) store((i * T + tid) * V, v[i]);
   } else {
     for (int c = tid * V; c < Kq; c += T * V) {
-      load(c, v[0]);
+      v[0].load(s, c, K);
       store(c, v[0]);
     }
   }
@@ -93,7 +66,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const TI* __restrict
 template <typename TI>
 void int8_quantize(const TI* x, int64_t ldx, int64_t M, int32_t K, int8_t* q, int64_t ldq, int32_t Kq, float* scale,
                    hipStream_t stream) {
-  constexpr int V = Vec8<TI>::n;
+  constexpr int V = Vec16<TI>::n;
   auto launch = [&](auto t, auto nv) {
     constexpr int T = decltype(t)::value, NV = decltype(nv)::value;
     BLSTM_LAUNCH("int8_quantize_rows", (quantize_rows_kernel<TI, T, NV>), dim3((unsigned)(T == 64 ? cdiv(M, 4) : M)),
@@ -245,63 +218,62 @@ __global__ __launch_bounds__(256) void int8_few_kernel(const Int8P p) {
              p.xs[min(m0 + j * 16 + fr, p.M - 1)]);
 }
 
-// The same for up to 16 tokens of 16-bit or 32-bit floats (TO, also y's), quantised on the way by every workgroup: a wave
-// takes the maximum of its part of the tokens while its weights are in flight, the four join them in LDS.  The
-// first 1024 columns stay in registers between the two uses, others are read again.
+// The same for up to 16 tokens of floats (TO, also y's), quantised on the way by every workgroup for itself while its
+// weights are in flight.
 struct Int8FewP {
   Int8P p;
   const void* x;
   int64_t ldx;
-  int K;   // columns of x; p.K those of the weights
+  int K, cols;   // columns of x, p.K those of the weights; in LDS
 };
-template <typename TO>
+static constexpr int FEW_COLS = 4096;   // of 16 tokens in LDS
+template <typename TO, int NV>
 __global__ __launch_bounds__(256) void int8_few_tokens_kernel(const Int8FewP a) {
   const Int8P& p = a.p;
   constexpr int U = 4;
+  extern __shared__ __attribute__((aligned(16))) char tokens[];
   __shared__ i32x4 part[3][64];
-  __shared__ float amax[4][16], xs[16];
+  __shared__ float xs[16];
   const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, fr = lane & 15, fc = lane >> 4;
   const int64_t n0 = (int64_t)blockIdx.x * 16;
   const int8_t* wr = p.w + min(n0 + fr, p.N - 1) * p.ldw;   // rows past the last: any, dropped at the end
-  const TO* xr = (const TO*)a.x + min((int64_t)fr, p.M - 1) * a.ldx;
   const int k0 = wid * 64 + fc * 16;
   auto weights = [&](int k) { return k < p.K ? *(const i32x4*)(wr + k) : i32x4{0, 0, 0, 0}; };
   i32x4 w[U];
-  Lane16<TO> x[U];
-#pragma unroll
-  for (int u = 0; u < U; ++u) lane16_load(x[u], xr, k0 + u * 256, a.K);
 #pragma unroll
   for (int u = 0; u < U; ++u) w[u] = weights(k0 + u * 256);
-  float mx = 0.f;
-#pragma unroll
-  for (int u = 0; u < U; ++u) mx = lane16_max(x[u], mx);
-#pragma unroll 2
-  for (int k = k0 + U * 256; k < a.K; k += 256) {
-    Lane16<TO> more;
-    lane16_load(more, xr, k, a.K);
-    mx = lane16_max(more, mx);
-  }
-  mx = max_abs(mx, __shfl_xor(mx, 16));
-  mx = max_abs(mx, __shfl_xor(mx, 32));
-  if (fc == 0) amax[wid][fr] = mx;
+  tokens_to_lds<TO, NV < 8 ? 8 / NV : 1, NV>((const TO*)a.x, a.ldx, (int)p.M, a.K, a.cols, tokens, xs);
   __syncthreads();
-  mx = max_abs(max_abs(max_abs(amax[0][fr], amax[1][fr]), amax[2][fr]), amax[3][fr]);
-  const Quant to(mx);
+  const char* xr = tokens + (fr < p.M ? fr : 0) * (a.cols + 16);   // columns past the last token: any
   i32x4 acc{0, 0, 0, 0};
 #pragma unroll
   for (int u = 0; u < U; ++u)
-    if (wid * 64 + u * 256 < p.K) acc = mma_i8(w[u], lane16_ints(x[u], to), acc);
-#pragma unroll 2
-  for (int k = k0 + U * 256; k < p.K + fc * 16; k += 256) {   // alike in every lane of the wave
-    Lane16<TO> more;
-    lane16_load(more, xr, k, a.K);
-    acc = mma_i8(weights(k), lane16_ints(more, to), acc);
-  }
+    if (wid * 64 + u * 256 < a.cols) acc = mma_i8(w[u], *(const i32x4*)(xr + k0 + u * 256), acc);
+#pragma unroll 4
+  for (int k = wid * 64 + U * 256; k < a.cols; k += 256) acc = mma_i8(weights(k + fc * 16), *(const i32x4*)(xr + k + fc * 16), acc);
   if (wid > 0) part[wid - 1][lane] = acc;
-  if (wid == 0 && fc == 0) xs[fr] = to.scale;
   __syncthreads();
   if (wid > 0) return;
   put4<TO>(p, fr, n0 + 4 * fc, acc + part[0][lane] + part[1][lane] + part[2][lane], xs[fr]);
+}
+template <typename TO>
+static void few_tokens(Int8FewP a, hipStream_t s) {
+  constexpr int V = Vec16<TO>::n;
+  a.cols = (int)rup(a.p.K, 64);
+  const size_t bytes = 16 * (size_t)(a.cols + 16);
+  auto launch = [&](auto nv) {
+    auto fn = int8_few_tokens_kernel<TO, decltype(nv)::value>;
+    static std::atomic<uint64_t> raised{0};
+    kc_raise_lds_limit((const void*)fn, 16 * (FEW_COLS + 16), raised);
+    BLSTM_LAUNCH("int8_linear_few", fn, dim3((unsigned)cdiv(a.p.N, 16)), dim3(256), bytes, s, a);
+  };
+#define INT(n) std::integral_constant<int, n>{}
+  if (a.cols <= 64 * V) launch(INT(1));
+  else if (a.cols <= 2 * 64 * V) launch(INT(2));
+  else if (a.cols <= 4 * 64 * V) launch(INT(4));
+  else if (a.cols <= 8 * 64 * V) launch(INT(8));
+  else launch(INT(FEW_COLS / (64 * V)));
+#undef INT
 }
 
 template <typename TO>
@@ -425,13 +397,12 @@ extern "C" int int8_linear_rows(const void* x, int64_t ldx, int64_t M, int32_t K
   if (rc) return rc;
   if (!y) return blstm_fail(BLSTM_EINVAL, "%s: NULL pointer", fn);
   if (ldy < N) return blstm_fail(BLSTM_EINVAL, "%s: a row pitch is below its row", fn);
-  if (M <= 16) {
+  if (M <= 16 && Kw <= FEW_COLS) {
     Int8FewP a{};
     a.p.w = w; a.p.ldw = ldw; a.p.ldy = ldy; a.p.M = M; a.p.N = N; a.p.K = Kw; a.p.ws = w_scale; a.p.bias = bias; a.p.y = y;
     a.x = x; a.ldx = ldx; a.K = K;
-    const dim3 grid((unsigned)cdiv(N, 16));
-    if (precision == BLSTM_BF16) BLSTM_LAUNCH("int8_linear_few", int8_few_tokens_kernel<bf16>, grid, dim3(256), 0, stream, a);
-    else BLSTM_LAUNCH("int8_linear_few", int8_few_tokens_kernel<float>, grid, dim3(256), 0, stream, a);
+    if (precision == BLSTM_BF16) few_tokens<bf16>(a, stream);
+    else few_tokens<float>(a, stream);
     return blstm_check_launch(fn);
   }
   int8_t* q = (int8_t*)ws;

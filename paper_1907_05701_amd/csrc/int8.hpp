@@ -20,6 +20,7 @@ __device__ __forceinline__ i32x4 mma_i8(i32x4 a, i32x4 b, i32x4 c) {
 // A token with a NaN or an infinite value has a NaN for its scale and integers of 0.
 // ---------------------------------------------------------------------------
 struct Quant {
+  static constexpr float NEAR = 0.4999f;
   float amax, pre, inv, scale;
   __device__ __forceinline__ explicit Quant(float max_abs) {
     scale = max_abs / 127.0f;
@@ -32,53 +33,105 @@ struct Quant {
       inv = 0.f;
     }
   }
-  __device__ __forceinline__ int operator()(float x) const {
+  __device__ __forceinline__ int nearest(float x) const {
     const float v = x * pre, t = v * inv;
+    const double lo = floor((double)t), a = (double)v * 127.0, b = (double)amax * (lo + 0.5);
     float n = rintf(t);
-    if (fabsf(t - n) > 0.4999f) {
-      const double lo = floor((double)t), a = (double)v * 127.0, b = (double)amax * (lo + 0.5);
-      const bool odd = (int)lo & 1;
-      n = (float)(a > b || (a == b && odd) ? lo + 1.0 : lo);
+    if (fabsf(t - n) > NEAR) n = (float)(a > b || (a == b && ((int)lo & 1)) ? lo + 1.0 : lo);
+    return (int)n;
+  }
+  // N values, most often without a doubtful one: one branch for all
+  template <int N, typename F>
+  __device__ __forceinline__ void ints(F x, int (&q)[N]) const {
+    float far = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float t = x(i) * pre * inv, n = rintf(t);
+      far = fmaxf(far, fabsf(t - n));
+      q[i] = (int)n;
     }
-    return inv == 0.f ? 0 : (int)n;
+    if (far > NEAR) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) q[i] = nearest(x(i));
+    }
+    if (inv == 0.f) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) q[i] = 0;
+    }
   }
 };
 __device__ __forceinline__ uint32_t pack4(int a, int b, int c, int d) {
   return (uint32_t)(a & 255) | (uint32_t)(b & 255) << 8 | (uint32_t)(c & 255) << 16 | (uint32_t)d << 24;
 }
-
-// 16 values of a row from column k on, as an MFMA lane takes them (0 behind column K).
-template <typename TI> struct Lane16 { TI v[16]; };
-template <typename TI>
-__device__ __forceinline__ void lane16_load(Lane16<TI>& o, const TI* row, int k, int K) {
-  constexpr int V = 16 / sizeof(TI);
+// N adjacent values of a row, 4 a word.
+template <typename TI, int N>
+__device__ __forceinline__ void quantize(const Quant& to, const TI (&v)[N], uint32_t (&w)[N / 4]) {
+  int q[N];
+  to.ints([&](int i) { return to_f32(v[i]); }, q);
 #pragma unroll
-  for (int i = 0; i < 16; i += V) {
-    if (k + i + V <= K) {
-      __builtin_memcpy(o.v + i, row + k + i, 16);
-    } else {
-#pragma unroll
-      for (int j = 0; j < V; ++j) o.v[i + j] = k + i + j < K ? row[k + i + j] : from_f32<TI>(0.f);
-    }
-  }
+  for (int i = 0; i < N / 4; ++i) w[i] = pack4(q[4 * i], q[4 * i + 1], q[4 * i + 2], q[4 * i + 3]);
 }
+
 __device__ __forceinline__ float max_abs(float m, float v) {   // a NaN stays
   const float a = fabsf(v);
   return m > a || m != m ? m : a;
 }
-template <typename TI>
-__device__ __forceinline__ float lane16_max(const Lane16<TI>& x, float m) {
+__device__ __forceinline__ float wave_max_abs(float m) {
 #pragma unroll
-  for (int i = 0; i < 16; ++i) m = max_abs(m, to_f32(x.v[i]));
+  for (int o = 32; o > 0; o >>= 1) m = max_abs(m, __shfl_xor(m, o));
   return m;
 }
-template <typename TI>
-__device__ __forceinline__ i32x4 lane16_ints(const Lane16<TI>& x, const Quant& to) {
-  i32x4 r;
+// V adjacent values of a row: 16 bytes, 0 behind column K.
+template <typename TI> struct Vec16 {
+  static constexpr int n = 16 / sizeof(TI);
+  TI v[n];
+  __device__ __forceinline__ void load(const TI* row, int c, int K) {
+    if (c + n <= K) {
+      __builtin_memcpy(v, row + c, 16);
+    } else {
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    r[i] = (int)pack4(to(to_f32(x.v[4 * i])), to(to_f32(x.v[4 * i + 1])), to(to_f32(x.v[4 * i + 2])), to(to_f32(x.v[4 * i + 3])));
-  return r;
+      for (int j = 0; j < n; ++j) v[j] = c + j < K ? row[c + j] : from_f32<TI>(0.f);
+    }
+  }
+  __device__ __forceinline__ float max(float m) const {
+#pragma unroll
+    for (int j = 0; j < n; ++j) m = max_abs(m, to_f32(v[j]));
+    return m;
+  }
+};
+
+// A few tokens to integers in LDS, by a workgroup of four waves: each takes every fourth row, R of them at a time,
+// of up to NV vectors a lane.  Rows of `cols` bytes at a pitch of cols + 16, columns from K on zero; then their scales.
+// (A pitch of an odd number of 16-byte pieces: 16 rows' pieces at one column lie in 16 different bank groups.)
+template <typename TI, int R, int NV>
+__device__ __forceinline__ void tokens_to_lds(const TI* x, int64_t ldx, int rows, int K, int cols, char* dst, float* scales) {
+  constexpr int V = Vec16<TI>::n;
+  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  for (int r0 = wid; r0 < rows; r0 += 4 * R) {
+    Vec16<TI> v[R][NV];
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+      if (r0 + 4 * i < rows) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) v[i][j].load(x + (r0 + 4 * i) * ldx, (j * 64 + lane) * V, K);
+      }
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+      if (r0 + 4 * i < rows) {
+        float mx = 0.f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) mx = v[i][j].max(mx);
+        const Quant to(wave_max_abs(mx));
+        if (lane == 0) scales[r0 + 4 * i] = to.scale;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+          const int c = (j * 64 + lane) * V;
+          uint32_t w[V / 4];
+          quantize(to, v[i][j].v, w);
+          if (c < cols) __builtin_memcpy(dst + (r0 + 4 * i) * (cols + 16) + c, w, V);
+        }
+      }
+  }
 }
 
 // A sum of products as a number: each step a single float32 rounding.

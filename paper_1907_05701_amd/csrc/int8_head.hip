@@ -120,6 +120,13 @@ __global__ __launch_bounds__(256, head_per_cu<KS>()) void int8_head_kernel(const
   issue(0);
   fetch(0);
 
+  const int own = (int)min((int64_t)16 * FN * FW, p.M - (f0 - wf * 16 * FN));   // frames of the workgroup
+  float* scales = (float*)(lds + 2 * STAGE + 16 * FN * FW * (KS * 64 + 16));
+  if constexpr (!std::is_void<TI>::value) {
+    constexpr int V = 16 / sizeof(TI), NV = KS > V ? KS / V : 1;
+    tokens_to_lds<TI, NV < 4 ? 4 : 2, NV>((const TI*)p.x + (f0 - wf * 16 * FN) * p.ldx, p.ldx, own, p.P, KS * 64, lds + 2 * STAGE, scales);
+    __syncthreads();
+  }
   i32x4 b[FN][KS];
   float xs[FN];
 #pragma unroll
@@ -133,32 +140,16 @@ __global__ __launch_bounds__(256, head_per_cu<KS>()) void int8_head_kernel(const
         b[j][ks] = k < p.Kw ? *(const i32x4*)(p.q + f * p.Kw + k) : i32x4{0, 0, 0, 0};
       }
     } else {
-      if (j > 0 && f0 + j * 16 >= p.M) {   // none of these frames exists
-        xs[j] = 0.f;
+      const int row = (wf * FN + j) * 16 + fr;
+      const char* t = lds + 2 * STAGE + (row < own ? row : 0) * (KS * 64 + 16);   // frames past the last: any
+      xs[j] = scales[row < own ? row : 0];
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) b[j][ks] = i32x4{0, 0, 0, 0};
-        continue;
+      for (int ks = 0; ks < KS; ++ks) {
+        const int k = ks * 64 + fc * 16;
+        b[j][ks] = *(const i32x4*)(t + k);
+        if (range == 0 && wc == 0 && row < own && k < p.Kw) *(i32x4*)(p.q + f * p.Kw + k) = b[j][ks];
       }
-      Lane16<TI> x[KS];
-      float mx = 0.f;
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) lane16_load(x[ks], (const TI*)p.x + f * p.ldx, ks * 64 + fc * 16, p.P);
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) mx = lane16_max(x[ks], mx);
-      mx = max_abs(mx, __shfl_xor(mx, 16));
-      mx = max_abs(mx, __shfl_xor(mx, 32));
-      const Quant to(mx);
-      xs[j] = to.scale;
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) b[j][ks] = lane16_ints(x[ks], to);
-      if (range == 0 && wc == 0 && f0 + j * 16 + fr < p.M) {
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          const int k = ks * 64 + fc * 16;
-          if (k < p.Kw) *(i32x4*)(p.q + f * p.Kw + k) = b[j][ks];
-        }
-        if (fc == 0) p.xs[f] = to.scale;
-      }
+      if (range == 0 && wc == 0 && row < own && fc == 0) p.xs[f] = xs[j];
     }
   }
   Sums s[FN];
@@ -171,6 +162,9 @@ __global__ __launch_bounds__(256, head_per_cu<KS>()) void int8_head_kernel(const
   }
   const float slack = SLACK / p.it2;
   put(0);
+  uint32_t at_k[KS];   // of a lane's piece in the first 16 rows of its wave (the slot depends on the row in 16 alone)
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) at_k[ks] = (wc * NI * 16 + fr) * (NCH * 16) + head_slot<NCH>(ks * 4 + fc, fr) * 16;
 
   for (int it = 0; it < tiles; ++it) {
     int8_stage_wait();
@@ -189,7 +183,7 @@ __global__ __launch_bounds__(256, head_per_cu<KS>()) void int8_head_kernel(const
       for (int j = 0; j < FN; ++j) acc[j] = i32x4{0, 0, 0, 0};
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        const i32x4 a = *(const i32x4*)(st + (row + fr) * (NCH * 16) + head_slot<NCH>(ks * 4 + fc, row + fr) * 16);
+        const i32x4 a = *(const i32x4*)(st + at_k[ks] + i * 16 * NCH * 16);
 #pragma unroll
         for (int j = 0; j < FN; ++j) acc[j] = mma_i8(a, b[j][ks], acc[j]);
       }
@@ -269,7 +263,8 @@ struct HeadOut {
   int32_t* idx;
   int n, k, fw;   // fw: waves along the frames in the first pass
 };
-static constexpr int FT_ = 256;          // threads
+static constexpr int FT = 128;           // threads: the workgroups of 2688 frames then run all at once
+static constexpr int FCAND = 512;        // most candidates
 static constexpr int GROUPS = 512;       // most groups computed again
 
 // A class's logit, the bits of the first pass.
@@ -299,8 +294,13 @@ struct Logit {
   template <int U>
   __device__ __forceinline__ void four(const int (&c)[U], float (&v)[U]) const {
     int a[U];
+    float s[U], b[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) a[u] = 0;
+    for (int u = 0; u < U; ++u) {
+      a[u] = 0;
+      s[u] = ws[c[u]];
+      b[u] = bias ? bias[c[u]] : 0.f;
+    }
 #pragma unroll 4
     for (int i = threadIdx.x & 3; i < chunks; i += 4)
 #pragma unroll
@@ -309,14 +309,14 @@ struct Logit {
     for (int u = 0; u < U; ++u) {
       a[u] += __shfl_xor(a[u], 1);
       a[u] += __shfl_xor(a[u], 2);
-      v[u] = value(a[u], c[u]);
+      v[u] = int8_value(a[u], scale_of(xs, s[u]), b[u]);
     }
   }
 };
 
 struct HeadLds {
-  TopkLds<FT_> l;
-  float buf[3][FT_ / 64];
+  TopkLds<FT, FCAND, 4 * FT> l;   // four maxima a thread
+  float buf[4][4];
   float listed[SOFTMAX_MAX_TOP];   // the listed classes' logits
   int32_t groups[GROUPS];
   uint32_t ngroups, hist[256], want;
@@ -337,28 +337,28 @@ __device__ __forceinline__ void head_any(HeadLds& h, const Logit& logit, const H
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, K = p.K;
   float mx = -INFINITY;
   bool nan = false;
-  for (int c = tid; c < K; c += FT_) {
+  for (int c = tid; c < K; c += FT) {
     const float v = logit(c);
     mx = fmaxf(mx, v);
     nan |= v != v;
   }
   nan = __syncthreads_or(nan);
-  mx = row_max<FT_>(fmaxf(mx, -INFINITY), h.buf[0]);
+  mx = row_max<FT>(fmaxf(mx, -INFINITY), h.buf[0]);
   const bool some = nan || !(mx == -INFINITY);
   const float ref = some ? mx : 0.f;
   float z = 0.f, t = 0.f;
-  for (int c = tid; c < K; c += FT_) {
+  for (int c = tid; c < K; c += FT) {
     const float y = (logit(c) - ref) * p.it2, e = exp2_(y);
     z += e;
     t += e * fmaxf(y, -200.f);
   }
-  z = row_sum<FT_>(z, h.buf[1]);
-  t = row_sum<FT_>(t, h.buf[2]);
+  z = row_sum<FT>(z, h.buf[1]);
+  t = row_sum<FT>(t, h.buf[2]);
   const float lz = log2f(z) * LN2_F;   // a NaN where there is one, or +inf
   auto value = [&](float v) { return some ? (v - ref) * p.itau - lz : -INFINITY; };
-  if (tid < o.n) {
-    const int at = o.ids[m * o.n + tid];
-    o.logprob[m * o.n + tid] = at < 0 || at >= K ? 0.f : value(logit(at));
+  for (int i = tid; i < o.n; i += FT) {
+    const int at = o.ids[m * o.n + i];
+    o.logprob[m * o.n + i] = at < 0 || at >= K ? 0.f : value(logit(at));
   }
   if (o.entropy && tid == 0) o.entropy[m] = some ? lz - t / z * LN2_F : 0.f;
   if (!o.k) return;
@@ -367,9 +367,9 @@ __device__ __forceinline__ void head_any(HeadLds& h, const Logit& logit, const H
   int want = o.k;   // among the words that agree with `word` so far
   for (int shift = 24; shift >= 0; shift -= 8) {
     __syncthreads();
-    h.hist[tid] = 0;
+    for (int i = tid; i < 256; i += FT) h.hist[i] = 0;
     __syncthreads();
-    for (int c = tid; c < K; c += FT_) {
+    for (int c = tid; c < K; c += FT) {
       const uint32_t u = order_word(logit(c));
       if (shift == 24 || (u >> (shift + 8)) == (word >> (shift + 8))) atomicAdd(&h.hist[(u >> shift) & 255], 1u);
     }
@@ -387,7 +387,7 @@ __device__ __forceinline__ void head_any(HeadLds& h, const Logit& logit, const H
   __syncthreads();
   if (tid == 0) h.l.count = 0;
   int taken = 0;
-  for (int c0 = 0; c0 < K; c0 += FT_) {
+  for (int c0 = 0; c0 < K; c0 += FT) {
     const int c = c0 + tid;
     const float v = c < K ? logit(c) : 0.f;
     const uint32_t u = c < K ? order_word(v) : 0;
@@ -396,7 +396,7 @@ __device__ __forceinline__ void head_any(HeadLds& h, const Logit& logit, const H
     if (lane == 0) h.hist[wave] = __popcll(same_);
     __syncthreads();
     int before = taken;
-    for (int i = 0; i < FT_ / 64; ++i) {
+    for (int i = 0; i < FT / 64; ++i) {
       if (i < wave) before += (int)h.hist[i];
       taken += (int)h.hist[i];
     }
@@ -408,30 +408,36 @@ __device__ __forceinline__ void head_any(HeadLds& h, const Logit& logit, const H
   rank(h.l, o.k, m, tp, value);
 }
 
-__global__ __launch_bounds__(FT_, 8) void int8_head_finish_kernel(const HeadP p, const HeadOut o) {
+__global__ __launch_bounds__(FT, 6) void int8_head_finish_kernel(const HeadP p, const HeadOut o) {
   extern __shared__ __attribute__((aligned(16))) char xl[];
   __shared__ HeadLds h;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, K = p.K;
   const int64_t m = blockIdx.x;
-  for (int i = tid; i < p.Kw / 16; i += FT_) ((i32x4*)xl)[i] = ((const i32x4*)(p.q + m * p.Kw))[i];
+  // every first load goes out before any is waited for
+  for (int i = tid; i < p.Kw / 16; i += FT) ((i32x4*)xl)[i] = ((const i32x4*)(p.q + m * p.Kw))[i];
   const Logit logit{p.w, p.ldw, p.ws, p.bias, (const i32x4*)xl, p.Kw / 16, p.xs[m]};
   if (tid == 0) h.ngroups = h.l.count = 0;
-  // the sums are for the second and third wave, the list for the last: their first loads go out with the others
   constexpr int NS = 4;
   const float4* st = p.stats + m * p.ranges;
   float4 sv[NS];
-  if (wave == 1 || wave == 2) {
+  if (wave == 1) {
 #pragma unroll
-    for (int i = 0; i < NS; ++i) sv[i] = st[min(tid - 64 + i * 128, p.ranges - 1)];
+    for (int i = 0; i < NS; ++i) sv[i] = st[min(lane + i * 64, p.ranges - 1)];
   }
-  int at = -1;
-  if (wave == 3 && lane / 4 < o.n) at = o.ids[m * o.n + lane / 4];
-  const float* gmax = p.gmax + m * p.ngroup;
-  uint32_t mx = 0;
+  const int first = (1 - wave) * 16 + lane / 4;   // of the list: the first wave has the threshold to find
+  int at = first < o.n ? o.ids[m * o.n + first] : -1;
+  const f32x4* gmax = (const f32x4*)(p.gmax + m * p.ngroup);
+  const int quads = p.ngroup / 4;
+  f32x4 mx{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
   if (o.k) {
-#pragma unroll 4
-    for (int g = tid; g < p.ngroup; g += FT_) mx = max(mx, order_word(gmax[g]));
-    h.l.tmax[tid] = mx;
+#pragma unroll 8
+    for (int g = tid; g < quads; g += FT) {
+      const f32x4 v = gmax[g];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) mx[j] = fmaxf(mx[j], v[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) h.l.tmax[j * FT + tid] = order_word(mx[j]);
   }
   __syncthreads();
   if (wave == 0) {
@@ -439,11 +445,11 @@ __global__ __launch_bounds__(FT_, 8) void int8_head_finish_kernel(const HeadP p,
       const uint32_t t = kth_search<12>(h.l, o.k);
       if (lane == 0) h.l.thr = t;
     }
-  } else if (wave < 3) {
+  } else {
     float rc = START * p.it2;
 #pragma unroll
     for (int i = 0; i < NS; ++i) rc = fmaxf(rc, sv[i].x);
-    for (int i = tid - 64 + NS * 128; i < p.ranges; i += 128) rc = fmaxf(rc, st[i].x);
+    for (int i = lane + NS * 64; i < p.ranges; i += 64) rc = fmaxf(rc, st[i].x);
     rc = wave_max(rc);
     float z = 0.f, t = 0.f;
     auto add = [&](float4 v) {
@@ -454,28 +460,25 @@ __global__ __launch_bounds__(FT_, 8) void int8_head_finish_kernel(const HeadP p,
     };
 #pragma unroll
     for (int i = 0; i < NS; ++i)
-      if (tid - 64 + i * 128 < p.ranges) add(sv[i]);
-    for (int i = tid - 64 + NS * 128; i < p.ranges; i += 128) add(st[i]);
+      if (lane + i * 64 < p.ranges) add(sv[i]);
+    for (int i = lane + NS * 64; i < p.ranges; i += 64) add(st[i]);
     z = wave_sum(z);
     t = wave_sum(t);
     if (lane == 0) {
-      h.buf[wave][0] = rc;
-      h.buf[wave][1] = z;
-      h.buf[wave][2] = t;
-    }
-  } else {
-    for (int e = lane / 4; e < o.n; e += 16) {   // the four lanes of an entry stay together
-      if (e >= 16) at = o.ids[m * o.n + e];
-      const int c[1] = {at < 0 || at >= K ? 0 : at};
-      float v[1];
-      logit.four(c, v);
-      h.listed[e] = v[0];
+      h.buf[0][0] = rc;
+      h.buf[0][1] = z;
+      h.buf[0][2] = t;
     }
   }
+  for (int e = first; e < o.n; e += FT / 4) {   // the four lanes of an entry stay together
+    if (e > first) at = o.ids[m * o.n + e];
+    const int c[1] = {at < 0 || at >= K ? 0 : at};
+    float v[1];
+    logit.four(c, v);
+    h.listed[e] = v[0];
+  }
   __syncthreads();
-  Sums sums{h.buf[1][0], h.buf[1][1], h.buf[1][2]};
-  sums.join(Sums{h.buf[2][0], h.buf[2][1], h.buf[2][2]});
-  const float rc = sums.rc, z = sums.z, t = sums.t;
+  const float rc = h.buf[0][0], z = h.buf[0][1], t = h.buf[0][2];
   // (a NaN fails both; a temperature beyond that would bring FLOOR's classes back in)
   if (same(!(z > 0.f && z < INFINITY && p.it2 > 1e-15f))) {
     head_any(h, logit, p, o, m);
@@ -485,26 +488,30 @@ __global__ __launch_bounds__(FT_, 8) void int8_head_finish_kernel(const HeadP p,
   if (o.k) {
     const uint32_t tw = max(same(h.l.thr), order_word(START));
     const float thr = order_value(tw);
-    if (mx >= tw) {
+    if (fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) >= thr) {
 #pragma unroll 4
-      for (int g = tid; g < p.ngroup; g += FT_)
-        if (gmax[g] >= thr) {
-          const uint32_t at = atomicAdd(&h.ngroups, 1u);
-          if (at < GROUPS) h.groups[at] = g;
-        }
+      for (int g = tid; g < quads; g += FT) {
+        const f32x4 v = gmax[g];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (v[j] >= thr) {
+            const uint32_t at = atomicAdd(&h.ngroups, 1u);
+            if (at < GROUPS) h.groups[at] = 4 * g + j;
+          }
+      }
     }
     __syncthreads();
     // a group's classes: 4 adjacent ones of every 16 that its wave has in a tile
     const int ng = (int)same(h.ngroups), tg = group_tiles(o.fw), wc = 4 / o.fw, ni = o.fw, size = 4 * ni * tg;
     constexpr int U = 2;
     if (ng <= GROUPS) {
-      for (int e0 = 0; e0 < ng * size; e0 += U * FT_ / 4) {
+      for (int e0 = 0; e0 < ng * size; e0 += U * FT / 4) {
         int c[U];
         float v[U];
         bool in[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          const int e = e0 + u * (FT_ / 4) + tid / 4;
+          const int e = e0 + u * (FT / 4) + tid / 4;
           in[u] = e < ng * size;
           const int g = in[u] ? h.groups[e / size] : 0, q = g % 4, w = g / 4 % wc, tile = g / 4 / wc * tg;
           const int b = e % size / (4 * ni), i = e % (4 * ni) / 4, r = e % 4;
@@ -521,16 +528,16 @@ __global__ __launch_bounds__(FT_, 8) void int8_head_finish_kernel(const HeadP p,
     }
     const int n = (int)same(h.l.count);
     // too many reach the threshold, or, where fewer than k classes lie above FLOOR, too few
-    if (ng > GROUPS || n > CAND || n < o.k) {
+    if (ng > GROUPS || n > FCAND || n < o.k) {
       head_any(h, logit, p, o, m);
       return;
     }
     TopkP tp{0, K, o.k, p.it2, o.top, nullptr, o.idx};
     rank(h.l, n, m, tp, lp);
   }
-  if (tid < o.n) {
-    const int id = o.ids[m * o.n + tid];
-    o.logprob[m * o.n + tid] = id < 0 || id >= K ? 0.f : lp(h.listed[tid]);
+  for (int i = tid; i < o.n; i += FT) {
+    const int id = o.ids[m * o.n + i];
+    o.logprob[m * o.n + i] = id < 0 || id >= K ? 0.f : lp(h.listed[i]);
   }
   if (o.entropy && tid == 0) o.entropy[m] = (lp.l2z - t / z) * LN2_F;
 }
@@ -572,6 +579,8 @@ static HeadPlan head_plan(int64_t M, int32_t K, int32_t Kw) {
   return h;
 }
 
+// Whether the first pass quantises its tokens itself: where they are few, and beside two stages of long rows there is room.
+static constexpr bool quantised_here(int fw, int ks) { return fw == 1 || (fw == 2 && ks <= 8); }
 bool int8_head_fits(int32_t Kw) { return cdiv(Kw, 64) <= HEAD_MAX_STEPS; }
 static size_t ints_bytes(int64_t M, int32_t Kw) { return (size_t)(rup(M * Kw, 256) + rup(M * 4, 256)); }
 size_t int8_head_bytes(int64_t M, int32_t K, int32_t Kw) { return ints_bytes(M, Kw) + head_plan(M, K, Kw).bytes; }
@@ -588,11 +597,13 @@ int int8_head(const TI* x, int64_t ldx, int64_t M, int32_t P, const int8_t* w, i
   buf += ints_bytes(M, Kw);
   p.stats = (float4*)(buf + h.stats);
   p.gmax = sc.k ? (float*)(buf + h.gmax) : nullptr;
-  if (h.fw == 4) int8_quantize(x, ldx, M, P, p.q, Kw, Kw, p.xs, s);
   auto launch = [&](auto ks, auto fn, auto fw) {
     constexpr int KS = decltype(ks)::value, FN = decltype(fn)::value, FW = decltype(fw)::value;
-    constexpr size_t bytes = 2 * (CT * KS * 64 + 512);
-    auto kernel = int8_head_kernel<KS, FN, FW, typename std::conditional<FW == 4, void, TI>::type>;
+    constexpr bool here = quantised_here(FW, KS);
+    constexpr size_t bytes = 2 * (CT * KS * 64 + 512) + (here ? 16 * FN * FW * (KS * 64 + 16 + 4) : 0);
+    auto kernel = int8_head_kernel<KS, FN, FW, typename std::conditional<here, TI, void>::type>;
+    static_assert(bytes <= 160 * 1024, "LDS");
+    if (!here) int8_quantize(x, ldx, M, P, p.q, Kw, Kw, p.xs, s);
     static std::atomic<uint64_t> raised{0};
     kc_raise_lds_limit((const void*)kernel, bytes, raised);
     BLSTM_LAUNCH("int8_head", kernel, dim3((unsigned)(h.ranges * h.nf)), dim3(256), bytes, s, p);
@@ -612,7 +623,7 @@ int int8_head(const TI* x, int64_t ldx, int64_t M, int32_t P, const int8_t* w, i
   const int rc = blstm_check_launch("int8_head");
   if (rc) return rc;
   const HeadOut o{sc.ids, sc.logprob, sc.entropy, sc.top, sc.idx, sc.n, sc.k, h.fw};
-  BLSTM_LAUNCH("int8_head_finish", int8_head_finish_kernel, dim3((unsigned)M), dim3(FT_), (size_t)Kw, s, p, o);
+  BLSTM_LAUNCH("int8_head_finish", int8_head_finish_kernel, dim3((unsigned)M), dim3(FT), (size_t)Kw, s, p, o);
   return blstm_check_launch("int8_head_finish");
 }
 template int int8_head<float>(const float*, int64_t, int64_t, int32_t, const int8_t*, int64_t, const float*, int32_t, int32_t, const float*, const softmax_scores&, char*, hipStream_t);

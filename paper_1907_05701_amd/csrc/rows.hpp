@@ -167,10 +167,11 @@ __device__ __forceinline__ float order_value(uint32_t w) {
 // more than CAND candidates: their k-th logit, and the last class that ties
 // with it, are then found bit by bit.
 // ---------------------------------------------------------------------------
-template <int T> struct TopkLds {
-  uint32_t tmax[T];
-  uint64_t cand[CAND];   // order word, complement of the class; in the order of arrival
-  float left[CAND];      // logits of the candidates behind the k-th, in their order
+// (T threads; room for C candidates, and for N maxima)
+template <int T, int C = CAND, int N = T> struct TopkLds {
+  uint32_t tmax[N];
+  uint64_t cand[C];   // order word, complement of the class; in the order of arrival
+  float left[C];      // logits of the candidates behind the k-th, in their order
   uint32_t thr, count, cnt[2][T / 64], flag;
   uint64_t kth;
   float buf[T / 64];
@@ -206,10 +207,10 @@ __device__ __forceinline__ uint32_t kth_word(const uint32_t (&w)[NW], int k) {
 }
 static constexpr int FOLD = 64;   // largest k for groups
 // (of one wave, behind a barrier)
-template <int LOW, int T>
-__device__ __forceinline__ uint32_t kth_search(const TopkLds<T>& l, int k) {
+template <int LOW, int T, int C, int N>
+__device__ __forceinline__ uint32_t kth_search(const TopkLds<T, C, N>& l, int k) {
   const int lane = threadIdx.x & 63;
-  constexpr int NW = T / 64;
+  constexpr int NW = N / 64;
   uint32_t w[NW];
 #pragma unroll
   for (int i = 0; i < NW; ++i) w[i] = l.tmax[i * 64 + lane];
@@ -231,18 +232,18 @@ __device__ __forceinline__ uint32_t kth_max(TopkLds<T>& l, int k) {
   __syncthreads();
   return l.thr;
 }
-template <int T>
-__device__ __forceinline__ void push(TopkLds<T>& l, float v, int c) {
+template <int T, int C, int N>
+__device__ __forceinline__ void push(TopkLds<T, C, N>& l, float v, int c) {
   const uint32_t at = atomicAdd(&l.count, 1u);
-  if (at < (uint32_t)CAND) l.cand[at] = ((uint64_t)order_word(v) << 32) | (uint32_t)~c;
+  if (at < (uint32_t)C) l.cand[at] = ((uint64_t)order_word(v) << 32) | (uint32_t)~c;
 }
 // Writes the k largest of n candidates as value(logit), and what is left to l.left (so that
 // sums over it do not depend on who arrived first).
 struct Itself {
   __device__ __forceinline__ float operator()(float v) const { return v; }
 };
-template <int T, typename F = Itself>
-__device__ __forceinline__ void rank(TopkLds<T>& l, int n, int64_t m, const TopkP& p, F value = F()) {
+template <int T, int C, int N, typename F = Itself>
+__device__ __forceinline__ void rank(TopkLds<T, C, N>& l, int n, int64_t m, const TopkP& p, F value = F()) {
   for (int i = threadIdx.x; i < n; i += T) {
     const uint64_t w = l.cand[i];
     int r = 0;
