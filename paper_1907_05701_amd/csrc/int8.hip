@@ -6,8 +6,7 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "gemm_kc.hpp"
-#include "int8.hpp"
+#include "int8_tile.hpp"
 #include "score.hpp"
 
 // ---------------------------------------------------------------------------
@@ -19,14 +18,14 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const TI* __restrict
                                                             int8_t* __restrict__ q, int64_t ldq, int Kq,
                                                             float* __restrict__ scale) {
   constexpr int V = Vec16<TI>::n, NR = NV ? NV : 1;
-  __shared__ float buf[4];
+  __shared__ uint32_t buf[4];
   const int tid = T == 64 ? threadIdx.x & 63 : threadIdx.x;
   const int64_t m = T == 64 ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
   if (T == 64 && m >= M) return;   // no barrier there
   const TI* s = x + m * ldx;
   int8_t* d = q + m * ldq;
   Vec16<TI> v[NR];
-  float mx = 0.f;
+  uint32_t mx = 0;
   if constexpr (NV > 0) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) v[i].load(s, (i * T + tid) * V, K);
@@ -38,18 +37,18 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const TI* __restrict
       mx = v[0].max(mx);
     }
   }
-  mx = wave_max_abs(mx);
+  mx = wave_max_bits(Vec16<TI>::word(mx));
   if constexpr (T == 256) {
     if ((tid & 63) == 0) buf[tid >> 6] = mx;
     __syncthreads();
-    mx = max_abs(max_abs(max_abs(buf[0], buf[1]), buf[2]), buf[3]);
+    mx = max(max(buf[0], buf[1]), max(buf[2], buf[3]));
   }
   const Quant to(mx);
   if (tid == 0) scale[m] = to.scale;
   auto store = [&](int c, const Vec16<TI>& o) {
     if (c >= Kq) return;   // Kq is a multiple of V
     uint32_t w[V / 4];
-    quantize(to, o.v, w);
+    to(o.v, w);
     __builtin_memcpy(d + c, w, V);
   };
   if constexpr (NV > 0) {
@@ -86,138 +85,6 @@ template void int8_quantize<bf16>(const bf16*, int64_t, int64_t, int32_t, int8_t
 // ---------------------------------------------------------------------------
 // The product.
 // ---------------------------------------------------------------------------
-struct Int8P {
-  const int8_t *x, *w;
-  int64_t ldx, ldw, ldy, M, N;   // M tokens, N channels
-  int K;
-  const float *xs, *ws, *bias;
-  void* y;
-  // tiles
-  int ntm, ntn, gm, total;
-};
-
-// Four channels of a token, from n on.
-template <typename TO>
-__device__ __forceinline__ void put4(const Int8P& p, int64_t m, int64_t n, i32x4 a, float xs) {
-  if (m >= p.M || n >= p.N) return;
-  TO* y = (TO*)p.y + m * p.ldy + n;
-  TO o[4];
-  if (n + 4 <= p.N) {
-    float w[4], b[4] = {0.f, 0.f, 0.f, 0.f};
-    __builtin_memcpy(w, p.ws + n, 16);
-    if (p.bias) __builtin_memcpy(b, p.bias + n, 16);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) o[j] = from_f32<TO>(int8_value(a[j], scale_of(xs, w[j]), b[j]));
-    __builtin_memcpy(y, o, sizeof o);
-  } else {
-    for (int j = 0; j < 4 && n + j < p.N; ++j)
-      y[j] = from_f32<TO>(int8_value(a[j], scale_of(xs, p.ws[n + j]), p.bias ? p.bias[n + j] : 0.f));
-  }
-}
-
-// 128-byte rows of 8 chunks in LDS, chunk c of row r in slot kc_slot<64>(c, r).
-template <int ROWS, int NW>
-__device__ __forceinline__ void stage(const int8_t* base, int64_t ld, int64_t rows, int k0, int K, char* tile, int wid,
-                                      int lane) {
-  const __amdgpu_buffer_rsrc_t r = dma_rsrc(base);
-  constexpr int LOADS = ROWS / 8 / NW;
-#pragma unroll
-  for (int i = 0; i < LOADS; ++i) {
-    const int row = (i * NW + wid) * 8 + lane / 8;
-    const int k = k0 + kc_slot<64>(lane % 8, row) * 16;
-    dma16(r, row < rows && k < K ? (uint32_t)(row * ld + k) : DMA_OFF_NONE, tile + (i * NW + wid) * 1024);
-  }
-}
-
-// BM channels x BN tokens a workgroup of WM x WN waves, 128 k at a time, two stages.
-template <typename TO, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(WM * WN * 64) void int8_tile_kernel(const Int8P p) {
-  constexpr int NW = WM * WN, FM = BM / WM / 16, FN = BN / WN / 16, STAGE = (BM + BN) * 128;
-  extern __shared__ __attribute__((aligned(1024))) char lds[];
-  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, wm = wid % WM, wn = wid / WM;
-  int z, tm, tn;
-  kc_tile_of(p, blockIdx.x, p.gm, z, tm, tn);
-  const int64_t n0 = (int64_t)tm * BM, m0 = (int64_t)tn * BN;
-  const int steps = (p.K + 127) / 128;
-  const int8_t *wb = p.w + n0 * p.ldw, *xb = p.x + m0 * p.ldx;
-  auto issue = [&](int j) {
-    char* st = lds + (j & 1) * STAGE;
-    stage<BM, NW>(wb, p.ldw, p.N - n0, j * 128, p.K, st, wid, lane);
-    stage<BN, NW>(xb, p.ldx, p.M - m0, j * 128, p.K, st + BM * 128, wid, lane);
-  };
-  i32x4 acc[FM][FN];
-#pragma unroll
-  for (int i = 0; i < FM; ++i)
-#pragma unroll
-    for (int j = 0; j < FN; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
-  const int fr = lane & 15, fc = lane >> 4;
-  issue(0);
-  for (int it = 0; it < steps; ++it) {
-    int8_stage_wait();
-    kc_barrier();
-    if (it + 1 < steps) issue(it + 1);
-    const char* st = lds + (it & 1) * STAGE;
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      i32x4 a[FM], b[FN];
-#pragma unroll
-      for (int i = 0; i < FM; ++i)
-        a[i] = *(const i32x4*)(st + (wm * (BM / WM) + i * 16 + fr) * 128 + kc_slot<64>(ks * 4 + fc, fr) * 16);
-#pragma unroll
-      for (int j = 0; j < FN; ++j)
-        b[j] = *(const i32x4*)(st + BM * 128 + (wn * (BN / WN) + j * 16 + fr) * 128 + kc_slot<64>(ks * 4 + fc, fr) * 16);
-#pragma unroll
-      for (int i = 0; i < FM; ++i)
-#pragma unroll
-        for (int j = 0; j < FN; ++j) acc[i][j] = mma_i8(a[i], b[j], acc[i][j]);
-    }
-  }
-  float xs[FN];
-#pragma unroll
-  for (int j = 0; j < FN; ++j) xs[j] = p.xs[min(m0 + wn * (BN / WN) + j * 16 + fr, p.M - 1)];
-#pragma unroll
-  for (int i = 0; i < FM; ++i)
-#pragma unroll
-    for (int j = 0; j < FN; ++j)
-      put4<TO>(p, m0 + wn * (BN / WN) + j * 16 + fr, n0 + wm * (BM / WM) + i * 16 + 4 * fc, acc[i][j], xs[j]);
-}
-
-// Few tokens: 16 channels and up to 16 FN tokens a workgroup, whose four waves
-// each take every fourth 64 of K, both operands straight from memory.
-template <typename TO, int FN>
-__global__ __launch_bounds__(256) void int8_few_kernel(const Int8P p) {
-  __shared__ i32x4 part[3][FN][64];
-  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, fr = lane & 15, fc = lane >> 4;
-  const int64_t n0 = (int64_t)blockIdx.x * 16, m0 = (int64_t)blockIdx.y * 16 * FN;
-  const int8_t* wr = p.w + min(n0 + fr, p.N - 1) * p.ldw;   // rows past the last: any, dropped at the end
-  const int8_t* xr[FN];
-#pragma unroll
-  for (int j = 0; j < FN; ++j) xr[j] = p.x + min(m0 + j * 16 + fr, p.M - 1) * p.ldx;
-  i32x4 acc[FN];
-#pragma unroll
-  for (int j = 0; j < FN; ++j) acc[j] = i32x4{0, 0, 0, 0};
-#pragma unroll 4
-  for (int k = wid * 64 + fc * 16; k < p.K + fc * 16; k += 256) {
-    const bool in = k < p.K;   // both operands zero behind K
-    const i32x4 a = in ? *(const i32x4*)(wr + k) : i32x4{0, 0, 0, 0};
-#pragma unroll
-    for (int j = 0; j < FN; ++j) {
-      const i32x4 b = in ? *(const i32x4*)(xr[j] + k) : i32x4{0, 0, 0, 0};
-      acc[j] = mma_i8(a, b, acc[j]);
-    }
-  }
-  if (wid > 0) {
-#pragma unroll
-    for (int j = 0; j < FN; ++j) part[wid - 1][j][lane] = acc[j];
-  }
-  __syncthreads();
-  if (wid > 0) return;
-#pragma unroll
-  for (int j = 0; j < FN; ++j)
-    put4<TO>(p, m0 + j * 16 + fr, n0 + 4 * fc, acc[j] + part[0][j][lane] + part[1][j][lane] + part[2][j][lane],
-             p.xs[min(m0 + j * 16 + fr, p.M - 1)]);
-}
-
 // The same for up to 16 tokens of floats (TO, also y's), quantised on the way by every workgroup for itself while its
 // weights are in flight.
 struct Int8FewP {
@@ -286,22 +153,18 @@ static void product(Int8P p, hipStream_t s) {
     else BLSTM_LAUNCH("int8_linear_few", (int8_few_kernel<TO, 4>), grid, dim3(256), 0, s, p);
     return;
   }
-  auto tile = [&](auto bm, auto bn, auto wm, auto wn) {
-    constexpr int BM = decltype(bm)::value, BN = decltype(bn)::value, WM = decltype(wm)::value, WN = decltype(wn)::value;
-    constexpr size_t bytes = 2 * (BM + BN) * 128;
-    auto fn = int8_tile_kernel<TO, BM, BN, WM, WN>;
-    static std::atomic<uint64_t> raised{0};
-    kc_raise_lds_limit((const void*)fn, bytes, raised);
-    p.ntm = (int)cdiv(p.N, BM);
-    p.ntn = (int)cdiv(p.M, BN);
-    p.gm = kc_group_rows;
-    p.total = p.ntm * p.ntn;
-    BLSTM_LAUNCH("int8_linear", fn, dim3((unsigned)p.total), dim3(WM * WN * 64), bytes, s, p);
-  };
-#define INT(n) std::integral_constant<int, n>{}
-  if (cdiv(p.M, 256) * cdiv(p.N, 256) >= 256) tile(INT(256), INT(256), INT(2), INT(4));
-  else tile(INT(128), INT(128), INT(2), INT(4));
-#undef INT
+  // 256x256 blocks stage and read the fewest bytes a product, one a CU: where they fill whole rounds of the chip and
+  // their start and end count little.  128x192 ones, two a CU, where they leave few CUs idle; else 64x64 ones, with a
+  // deeper ring where two a CU hold them all.  (us, 256x256 / 128x192 / 64x64 with two stages / with four.
+  // 16384 x 4096 x 4096 217 / 238 / 346 / -, 8192 x 4096 x 1024 39 / 42 / 59 / -, 5000 x 4096 x 1024 34 / 28.6 / 38 / -,
+  // 2688 x 32000 x 256 56 / 53 / 63 / -, 2688 x 4096 x 1024 19.7 / 16.6 / 20.8 / 26, 2688 x 2048 x 1024 - / 10.6 / 12.2 /
+  // 14.5, 2688 x 1024 x 4096 49 / 26.5 / 19.7 / 22.9, 1000 x 1000 x 8192 83 / 49 / 31.7 / 20.5, 1000 x 2048 x 1024
+  // - / 9.8 / 5.7 / 5.9.)
+  const int64_t big = cdiv(p.M, 256) * cdiv(p.N, 256), rounds = cdiv(big, 256) * 256;
+  if (p.K >= 1024 && 5 * big >= 4 * rounds) int8_tile_launch<TO, 256, 256, 4, 4, 128, 2>(p, s);
+  else if (cdiv(p.M, 192) * cdiv(p.N, 128) >= 192) int8_tile_launch<TO, 128, 192, 2, 4, 128, 2>(p, s);
+  else if (cdiv(p.M, 64) * cdiv(p.N, 64) > 512) int8_tile_launch<TO, 64, 64, 2, 2, 128, 2>(p, s);
+  else int8_tile_launch<TO, 64, 64, 2, 2, 128, 4>(p, s);
 }
 
 // ---------------------------------------------------------------------------

@@ -14,73 +14,58 @@ __device__ __forceinline__ i32x4 mma_i8(i32x4 a, i32x4 b, i32x4 c) {
 
 // ---------------------------------------------------------------------------
 // A token's integers: q = 127 x / max |x| to the nearest, ties to the even one,
-// scale = max |x| / 127.  The product x (127 / max) is off by less than
-// 127 * 3 * 2^-24 < 2.5e-5, so that only within that of a half the nearest one is in doubt; there
+// scale = max |x| / 127.  x (127 / max) with a rounded quotient is off by less than
+// 127 * 2^-24 < 8e-6, so that only within that of a half the nearest one is in doubt; there
 // 127 x is compared with the half times max |x| in 64 bits, where both are exact (31 and 32 bits).
 // A token with a NaN or an infinite value has a NaN for its scale and integers of 0.
 // ---------------------------------------------------------------------------
 struct Quant {
-  static constexpr float NEAR = 0.4999f;
-  float amax, pre, inv, scale;
-  __device__ __forceinline__ explicit Quant(float max_abs) {
-    scale = max_abs / 127.0f;
-    // far below 1 the inverse would overflow: both sides times 2^64, exactly
-    pre = max_abs < 1e-30f ? 0x1p64f : 1.0f;
-    amax = max_abs * pre;
-    inv = amax > 0.f ? 127.0f / amax : 0.f;
-    if (!(max_abs < INFINITY)) {
-      scale = NAN;
-      inv = 0.f;
-    }
+  static constexpr float NEAR = 0.4999f;         // of a half
+  static constexpr float MAGIC = 12582912.0f;    // 1.5 * 2^23: a sum with it is rounded to a whole number, its low byte the integer's
+  float amax, inv, scale;
+  bool none, tiny;
+  // bits: the largest |x| as a word (as words, magnitudes order as floats do, NaN above infinity)
+  __device__ __forceinline__ explicit Quant(uint32_t bits) : amax(__uint_as_float(bits)) {
+    none = !(amax > 0.f && amax < INFINITY);
+    tiny = amax < 1e-30f;   // the quotient would overflow
+    scale = amax < INFINITY ? amax / 127.0f : NAN;
+    inv = none || tiny ? 0.f : 127.0f / amax;
   }
-  __device__ __forceinline__ int nearest(float x) const {
-    const float v = x * pre, t = v * inv;
-    const double lo = floor((double)t), a = (double)v * 127.0, b = (double)amax * (lo + 0.5);
-    float n = rintf(t);
-    if (fabsf(t - n) > NEAR) n = (float)(a > b || (a == b && ((int)lo & 1)) ? lo + 1.0 : lo);
-    return (int)n;
+  __device__ __forceinline__ uint32_t nearest(float x) const {
+    const double a = (double)x * 127.0, q = a / (double)amax, lo = floor(q), b = (double)amax * (lo + 0.5);
+    const double n = a > b || (a == b && ((int)lo & 1)) ? lo + 1.0 : lo;
+    return (uint32_t)(int)n;
   }
-  // N values, most often without a doubtful one: one branch for all
-  template <int N, typename F>
-  __device__ __forceinline__ void ints(F x, int (&q)[N]) const {
-    float far = 0.f;
+  // N adjacent values, 4 a word.  Most often none of them is in doubt: one branch for all.
+  template <typename TI, int N>
+  __device__ __forceinline__ void operator()(const TI (&x)[N], uint32_t (&w)[N / 4]) const {
+    uint32_t q[N];
+    float far = tiny ? 1.f : 0.f;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const float t = x(i) * pre * inv, n = rintf(t);
-      far = fmaxf(far, fabsf(t - n));
-      q[i] = (int)n;
+      const float v = to_f32(x[i]), f = fmaf(v, inv, MAGIC);
+      far = fmaxf(far, fabsf(fmaf(v, inv, MAGIC - f)));
+      q[i] = __float_as_uint(f);
     }
-    if (far > NEAR) {
+    if (far > NEAR && !none) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) q[i] = nearest(x(i));
+      for (int i = 0; i < N; ++i) q[i] = nearest(to_f32(x[i]));
     }
-    if (inv == 0.f) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) q[i] = 0;
+    for (int i = 0; i < N / 4; ++i) {
+      // low bytes: v_perm_b32's selectors 0-3 name its second operand's bytes, 4-7 its first's
+      const uint32_t lo = __builtin_amdgcn_perm(q[4 * i + 1], q[4 * i], 0x0c0c0400), hi = __builtin_amdgcn_perm(q[4 * i + 3], q[4 * i + 2], 0x04000c0c);
+      w[i] = none ? 0u : lo | hi;
     }
   }
 };
-__device__ __forceinline__ uint32_t pack4(int a, int b, int c, int d) {
-  return (uint32_t)(a & 255) | (uint32_t)(b & 255) << 8 | (uint32_t)(c & 255) << 16 | (uint32_t)d << 24;
-}
-// N adjacent values of a row, 4 a word.
-template <typename TI, int N>
-__device__ __forceinline__ void quantize(const Quant& to, const TI (&v)[N], uint32_t (&w)[N / 4]) {
-  int q[N];
-  to.ints([&](int i) { return to_f32(v[i]); }, q);
-#pragma unroll
-  for (int i = 0; i < N / 4; ++i) w[i] = pack4(q[4 * i], q[4 * i + 1], q[4 * i + 2], q[4 * i + 3]);
-}
 
-__device__ __forceinline__ float max_abs(float m, float v) {   // a NaN stays
-  const float a = fabsf(v);
-  return m > a || m != m ? m : a;
-}
-__device__ __forceinline__ float wave_max_abs(float m) {
+__device__ __forceinline__ uint32_t wave_max_bits(uint32_t m) {
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) m = max_abs(m, __shfl_xor(m, o));
+  for (int o = 32; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o));
   return m;
 }
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 // V adjacent values of a row: 16 bytes, 0 behind column K.
 template <typename TI> struct Vec16 {
   static constexpr int n = 16 / sizeof(TI);
@@ -93,10 +78,23 @@ template <typename TI> struct Vec16 {
       for (int j = 0; j < n; ++j) v[j] = c + j < K ? row[c + j] : from_f32<TI>(0.f);
     }
   }
-  __device__ __forceinline__ float max(float m) const {
+  // the largest magnitude so far: m in the type's own words (two of 16 bits side by side), word() as a float's
+  __device__ __forceinline__ uint32_t max(uint32_t m) const {
+    uint32_t w[4];
+    __builtin_memcpy(w, v, 16);
 #pragma unroll
-    for (int j = 0; j < n; ++j) m = max_abs(m, to_f32(v[j]));
+    for (int j = 0; j < 4; ++j) {
+      if constexpr (sizeof(TI) == 2) {
+        const uint32_t a = w[j] & 0x7fff7fffu;
+        m = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, m), __builtin_bit_cast(u16x2, a)));
+      } else {
+        m = ::max(m, w[j] & 0x7fffffffu);
+      }
+    }
     return m;
+  }
+  static __device__ __forceinline__ uint32_t word(uint32_t m) {
+    return sizeof(TI) == 2 ? ::max(m << 16, m & 0xffff0000u) : m;
   }
 };
 
@@ -118,16 +116,16 @@ __device__ __forceinline__ void tokens_to_lds(const TI* x, int64_t ldx, int rows
 #pragma unroll
     for (int i = 0; i < R; ++i)
       if (r0 + 4 * i < rows) {
-        float mx = 0.f;
+        uint32_t mx = 0;
 #pragma unroll
         for (int j = 0; j < NV; ++j) mx = v[i][j].max(mx);
-        const Quant to(wave_max_abs(mx));
+        const Quant to(wave_max_bits(Vec16<TI>::word(mx)));
         if (lane == 0) scales[r0 + 4 * i] = to.scale;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
           const int c = (j * 64 + lane) * V;
           uint32_t w[V / 4];
-          quantize(to, v[i][j].v, w);
+          to(v[i][j].v, w);
           if (c < cols) __builtin_memcpy(dst + (r0 + 4 * i) * (cols + 16) + c, w, V);
         }
       }

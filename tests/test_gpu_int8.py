@@ -124,12 +124,25 @@ def test_products(gpu_lib, M, N, K, precision):
     check_linear(q, w, xs, ws, None, TYPES[precision])
 
 
-def test_products_that_fill_the_chip(gpu_lib):
-    """The largest tiles: 256 of them and more, with ragged ends."""
-    g = torch.Generator().manual_seed(5)
-    M, N, K = 4100, 4000, 208
-    q, w = ints(M, K, g), ints(N, K, g)
-    check_linear(q, w, torch.rand(M, generator=g), torch.rand(N, generator=g), torch.randn(N, generator=g), torch.bfloat16)
+@pytest.mark.parametrize("precision", ["fp32", "bf16"])
+@pytest.mark.parametrize("M,N,K", [(4100, 4000, 208), (3900, 4001, 1040), (2000, 2310, 144), (1700, 1600, 80)])
+def test_products_that_fill_the_chip(gpu_lib, M, N, K, precision):
+    """Each size of tile with ragged ends; outputs whose rows no 16 bytes divide.  float64 products of these are exact."""
+    from paper_1907_05701_amd import binding as bd
+    t = TYPES[precision]
+    g = torch.Generator(device="cuda").manual_seed(M)
+    q = torch.randint(-127, 128, (M, K), generator=g, device="cuda", dtype=torch.int8)
+    w = torch.randint(-127, 128, (N, K), generator=g, device="cuda", dtype=torch.int8)
+    xs, ws = torch.rand(M, generator=g, device="cuda"), torch.rand(N, generator=g, device="cuda")
+    bias = torch.randn(N, generator=g, device="cuda")
+    s = (q.double() @ w.double().t().contiguous()).float()
+    for b in (bias, None):
+        want = s * (xs[:, None] * ws)
+        want = (want if b is None else want + b).to(t)
+        y = torch.full((M + 1, N), 7.0, dtype=t, device="cuda")
+        bd.int8_linear(q, xs, w, ws, y[:M], bias=b)
+        torch.cuda.synchronize()
+        assert torch.equal(y[:M], want) and bool((y[M] == 7.0).all())
 
 
 def test_the_largest_sums(gpu_lib):
