@@ -75,6 +75,7 @@ void int8_quantize(const TI* x, int64_t ldx, int64_t M, int32_t K, int8_t* q, in
   if (Kq <= 64 * V) launch(INT(64), INT(1));
   else if (Kq <= 2 * 64 * V) launch(INT(64), INT(2));
   else if (Kq <= 4 * 64 * V) launch(INT(64), INT(4));
+  else if (Kq <= 2 * 256 * V) launch(INT(256), INT(2));
   else if (Kq <= 4 * 256 * V) launch(INT(256), INT(4));
   else launch(INT(256), INT(0));
 #undef INT

@@ -16,7 +16,8 @@ __device__ __forceinline__ i32x4 mma_i8(i32x4 a, i32x4 b, i32x4 c) {
 // A token's integers: q = 127 x / max |x| to the nearest, ties to the even one,
 // scale = max |x| / 127.  x (127 / max) with a rounded quotient is off by less than
 // 127 * 2^-24 < 8e-6, so that only within that of a half the nearest one is in doubt; there
-// 127 x is compared with the half times max |x| in 64 bits, where both are exact (31 and 32 bits).
+// 127 x is compared with the half times max |x|, each as a product and its rounding error: as both
+// have at most 32 bits and are close, the difference is exact.
 // A token with a NaN or an infinite value has a NaN for its scale and integers of 0.
 // ---------------------------------------------------------------------------
 struct Quant {
@@ -31,10 +32,13 @@ struct Quant {
     scale = amax < INFINITY ? amax / 127.0f : NAN;
     inv = none || tiny ? 0.f : 127.0f / amax;
   }
-  __device__ __forceinline__ uint32_t nearest(float x) const {
-    const double a = (double)x * 127.0, q = a / (double)amax, lo = floor(q), b = (double)amax * (lo + 0.5);
-    const double n = a > b || (a == b && ((int)lo & 1)) ? lo + 1.0 : lo;
-    return (uint32_t)(int)n;
+  // am, quo: max |x| and 127 / it, both sides brought near 1 by `pre`, a power of 2
+  static __device__ __forceinline__ float nearest(float x, float pre, float am, float quo) {
+#pragma clang fp contract(off)
+    const float v = x * pre, t = v * quo, n = rintf(t), s = t < n ? -1.f : 1.f, h = n + 0.5f * s;
+    const float p = am * h, pl = __builtin_fmaf(am, h, -p), q = v * 127.0f, ql = __builtin_fmaf(v, 127.0f, -q);
+    const float d = ((q - p) + (ql - pl)) * s;   // beyond the half?
+    return d > 0.f || (d == 0.f && ((int)n & 1)) ? n + s : n;
   }
   // N adjacent values, 4 a word.  Most often none of them is in doubt: one branch for all.
   template <typename TI, int N>
@@ -48,8 +52,9 @@ struct Quant {
       q[i] = __float_as_uint(f);
     }
     if (far > NEAR && !none) {
+      const float pre = tiny ? 0x1p64f : amax > 1e30f ? 0x1p-64f : 1.f, am = amax * pre, quo = 127.0f / am;
 #pragma unroll
-      for (int i = 0; i < N; ++i) q[i] = nearest(to_f32(x[i]));
+      for (int i = 0; i < N; ++i) q[i] = (uint32_t)(int)nearest(to_f32(x[i]), pre, am, quo);
     }
 #pragma unroll
     for (int i = 0; i < N / 4; ++i) {
@@ -73,9 +78,14 @@ template <typename TI> struct Vec16 {
   __device__ __forceinline__ void load(const TI* row, int c, int K) {
     if (c + n <= K) {
       __builtin_memcpy(v, row + c, 16);
-    } else {
+      return;
+    }
 #pragma unroll
-      for (int j = 0; j < n; ++j) v[j] = c + j < K ? row[c + j] : from_f32<TI>(0.f);
+    for (int j = 0; j < n; ++j) v[j] = from_f32<TI>(0.f);
+    if (c < K) {
+#pragma unroll
+      for (int j = 0; j < n; ++j)
+        if (c + j < K) v[j] = row[c + j];
     }
   }
   // the largest magnitude so far: m in the type's own words (two of 16 bits side by side), word() as a float's

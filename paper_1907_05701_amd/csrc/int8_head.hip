@@ -426,16 +426,22 @@ __global__ __launch_bounds__(FT, 6) void int8_head_finish_kernel(const HeadP p, 
   }
   const int first = (1 - wave) * 16 + lane / 4;   // of the list: the first wave has the threshold to find
   int at = first < o.n ? o.ids[m * o.n + first] : -1;
+  // group maxima: up to NG quads a thread in registers, others read again
+  constexpr int NG = 8;
   const f32x4* gmax = (const f32x4*)(p.gmax + m * p.ngroup);
   const int quads = p.ngroup / 4;
-  f32x4 mx{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-  if (o.k) {
-#pragma unroll 8
-    for (int g = tid; g < quads; g += FT) {
-      const f32x4 v = gmax[g];
+  const f32x4 low{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+  f32x4 mx = low, gv[NG];
+  auto larger = [&](const f32x4& v) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) mx[j] = fmaxf(mx[j], v[j]);
-    }
+    for (int j = 0; j < 4; ++j) mx[j] = fmaxf(mx[j], v[j]);
+  };
+  if (o.k) {
+#pragma unroll
+    for (int i = 0; i < NG; ++i) gv[i] = tid + i * FT < quads ? gmax[tid + i * FT] : low;
+#pragma unroll
+    for (int i = 0; i < NG; ++i) larger(gv[i]);
+    for (int g = tid + NG * FT; g < quads; g += FT) larger(gmax[g]);
 #pragma unroll
     for (int j = 0; j < 4; ++j) h.l.tmax[j * FT + tid] = order_word(mx[j]);
   }
@@ -489,16 +495,17 @@ __global__ __launch_bounds__(FT, 6) void int8_head_finish_kernel(const HeadP p, 
     const uint32_t tw = max(same(h.l.thr), order_word(START));
     const float thr = order_value(tw);
     if (fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) >= thr) {
-#pragma unroll 4
-      for (int g = tid; g < quads; g += FT) {
-        const f32x4 v = gmax[g];
+      auto reach = [&](const f32x4& v, int g) {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
           if (v[j] >= thr) {
             const uint32_t at = atomicAdd(&h.ngroups, 1u);
             if (at < GROUPS) h.groups[at] = 4 * g + j;
           }
-      }
+      };
+#pragma unroll
+      for (int i = 0; i < NG; ++i) reach(gv[i], tid + i * FT);
+      for (int g = tid + NG * FT; g < quads; g += FT) reach(gmax[g], g);
     }
     __syncthreads();
     // a group's classes: 4 adjacent ones of every 16 that its wave has in a tile
@@ -555,7 +562,7 @@ static constexpr int HEAD_MAX_STEPS = 16;
 static HeadPlan head_plan(int64_t M, int32_t K, int32_t Kw) {
   HeadPlan h{};
   h.ks = (int)cdiv(Kw, 64);
-  h.fn = h.ks > 8 ? 1 : 2;
+  h.fn = h.ks > 8 || M <= 16 ? 1 : 2;
   const int frames = 16 * h.fn;
   h.fw = M <= frames ? 1 : M <= 2 * frames ? 2 : 4;
   h.nf = (int)cdiv(M, frames * h.fw);
@@ -614,10 +621,14 @@ int int8_head(const TI* x, int64_t ldx, int64_t M, int32_t P, const int8_t* w, i
     else if (h.fw == 2) launch(ks, fn, INT(2));
     else launch(ks, fn, INT(4));
   };
-  if (h.ks <= 1) waves(INT(1), INT(2));
-  else if (h.ks <= 2) waves(INT(2), INT(2));
-  else if (h.ks <= 4) waves(INT(4), INT(2));
-  else if (h.ks <= 8) waves(INT(8), INT(2));
+  auto columns = [&](auto ks) {
+    if (M <= 16) launch(ks, INT(1), INT(1));
+    else waves(ks, INT(2));
+  };
+  if (h.ks <= 1) columns(INT(1));
+  else if (h.ks <= 2) columns(INT(2));
+  else if (h.ks <= 4) columns(INT(4));
+  else if (h.ks <= 8) columns(INT(8));
   else waves(INT(16), INT(1));
 #undef INT
   const int rc = blstm_check_launch("int8_head");
