@@ -63,7 +63,7 @@ class SoftmaxTeacher(ctypes.Structure):
                 [("k", ctypes.c_int32)] + [(n, ctypes.c_float) for n in ("temperature", "soft", "hard")])
 
 
-class SoftmaxScores(ctypes.Structure):
+class SoftmaxScores(ctypes.Structure):   # (the calls pass its bytes)
     _fields_ = ([(n, ctypes.c_void_p) for n in ("ids", "logprob", "entropy", "top", "idx")] +
                 [("n", ctypes.c_int32), ("k", ctypes.c_int32), ("temperature", ctypes.c_float)])
 
@@ -129,7 +129,7 @@ def lib():
         L.softmax_head_ws_bytes.argtypes = [DP, ctypes.POINTER(S)]
         L.softmax_topk.argtypes = [DP, P, P, P, I, F, P, P, P, P, P]
         L.softmax_distill_fwd_bwd.argtypes = [DP, P, P, P, ST, F, P, P, P, P, P]
-        SS, SP = ctypes.POINTER(SoftmaxScores), ctypes.POINTER(SoftmaxScoreGrads)
+        SS = SP = P   # softmax_scores and softmax_score_grads by their bytes
         L.softmax_logprob_rows.argtypes = [P, I64, I64, I, I, SS, P]
         L.softmax_logprob_bwd_rows.argtypes = [P, I64, I64, I, I, SP, P, I64, P]
         L.softmax_logprob.argtypes = [DP, P, P, P, SS, P, P]
@@ -275,7 +275,7 @@ def _have(name, t, shape, dtype, dev, optional=False):
         if optional:
             return None
         raise ValueError(f"{name} is required")
-    if t.shape != shape or t.dtype != dtype or t.get_device() != dev or not t.is_contiguous():
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
         raise _wrong(name, f"a contiguous {dtype} tensor of shape {shape}", t, dev)
     return t.data_ptr()
 
@@ -309,7 +309,7 @@ def _call(fn, dev, stream, *args):
     on = getattr(stream, "device", None)
     if on is not None and on.index != dev:   # its kernels would reach for another device's memory
         raise ValueError(f"the stream is on {on}, the tensors are on cuda:{dev}")
-    if dev != torch.cuda.current_device():
+    if dev != torch._C._cuda_getDevice():   # (initialised: a tensor lies on it)
         with torch.cuda.device(dev):
             return _call(fn, dev, stream, *args)
     # the handle alone: a Stream object costs more than the launch's other arguments together
@@ -472,11 +472,7 @@ def ssm_scan_step(dims, x, dt, A, Bm, Cm, state, y, Dskip=None, z=None, dt_bias=
 
 # ---------------------------------------------------------------- distillation ---
 def _logits(logits):
-    if logits.dim() != 2 or logits.dtype not in (torch.bfloat16, torch.float32):
-        raise ValueError(f"logits must be bfloat16 or float32 rows [M][K]: got {logits.dtype} {tuple(logits.shape)}")
-    M, K = logits.shape
-    p, ld = _rows("logits", logits, (M, K), logits.dtype, _on(logits))
-    return p, ld, M, K, BLSTM_BF16 if logits.dtype == torch.bfloat16 else BLSTM_FP32
+    return _floats("logits", logits, _on(logits))
 
 
 def softmax_topk_rows(logits, top, idx, rest=None, temperature=1.0, stream=None):
@@ -545,24 +541,32 @@ def softmax_distill_fwd_bwd(dims, theta, theta_lp, y_top, top, idx, loss_scale, 
 
 
 # --------------------------------------------------------------------- scoring ---
+_SCORES, _SCORE_GRADS = struct.Struct("@5P2if4x"), struct.Struct("@3Pif")
+assert _SCORES.size == ctypes.sizeof(SoftmaxScores) and _SCORE_GRADS.size == ctypes.sizeof(SoftmaxScoreGrads)
+
+
+def _lists(M, dev, name, t, dtype, other, u, other_dtype):
+    """Addresses of two lists of rows of one width, and the width (zeros where neither is given)."""
+    if t is None and u is None:
+        return 0, 0, 0
+    if t is None or u is None:
+        raise ValueError(f"{name} and {other} belong together")
+    shape = t.shape
+    n = shape[-1] if shape else 0
+    return _have(name, t, (M, n), dtype, dev), _have(other, u, (M, n), other_dtype, dev), n
+
+
 def _scores(M, dev, ids, logprob, entropy, top, idx, temperature):
-    n = 0 if ids is None else ids.shape[-1]
-    k = 0 if top is None else top.shape[-1]
-    f, i = torch.float32, torch.int32
-    if (ids is None) != (logprob is None) or (top is None) != (idx is None):
-        raise ValueError("ids and logprob belong together, and top and idx")
-    return SoftmaxScores(_have("ids", ids, (M, n), i, dev, True), _have("logprob", logprob, (M, n), f, dev, True),
-                         _have("entropy", entropy, (M,), f, dev, True), _have("top", top, (M, k), f, dev, True),
-                         _have("idx", idx, (M, k), i, dev, True), n, k, temperature)
+    pi, pl, n = _lists(M, dev, "ids", ids, torch.int32, "logprob", logprob, torch.float32)
+    pt, px, k = _lists(M, dev, "top", top, torch.float32, "idx", idx, torch.int32)
+    pe = 0 if entropy is None else _have("entropy", entropy, (M,), torch.float32, dev)
+    return _SCORES.pack(pi, pl, pe, pt, px, n, k, temperature)
 
 
 def _score_grads(M, dev, ids, dlogprob, dentropy, temperature):
-    n = 0 if ids is None else ids.shape[-1]
-    if (ids is None) != (dlogprob is None):
-        raise ValueError("ids and dlogprob belong together")
-    return SoftmaxScoreGrads(_have("ids", ids, (M, n), torch.int32, dev, True),
-                             _have("dlogprob", dlogprob, (M, n), torch.float32, dev, True),
-                             _have("dentropy", dentropy, (M,), torch.float32, dev, True), n, temperature)
+    pi, pd, n = _lists(M, dev, "ids", ids, torch.int32, "dlogprob", dlogprob, torch.float32)
+    pe = 0 if dentropy is None else _have("dentropy", dentropy, (M,), torch.float32, dev)
+    return _SCORE_GRADS.pack(pi, pd, pe, n, temperature)
 
 
 def softmax_logprob_rows(logits, ids=None, logprob=None, entropy=None, top=None, idx=None, temperature=1.0,
@@ -571,7 +575,7 @@ def softmax_logprob_rows(logits, ids=None, logprob=None, entropy=None, top=None,
     p, ld, M, K, prec = _logits(logits)
     dev = logits.get_device()
     q = _scores(M, dev, ids, logprob, entropy, top, idx, temperature)
-    return _call("softmax_logprob_rows", dev, stream, p, ld, M, K, prec, ctypes.byref(q))
+    return _call("softmax_logprob_rows", dev, stream, p, ld, M, K, prec, q)
 
 
 def softmax_logprob_bwd_rows(logits, dlogits, ids=None, dlogprob=None, dentropy=None, temperature=1.0, stream=None):
@@ -579,7 +583,7 @@ def softmax_logprob_bwd_rows(logits, dlogits, ids=None, dlogprob=None, dentropy=
     dev = logits.get_device()
     g = _score_grads(M, dev, ids, dlogprob, dentropy, temperature)
     pd, ldd = _rows("dlogits", dlogits, (M, K), logits.dtype, dev)
-    return _call("softmax_logprob_bwd_rows", dev, stream, p, ld, M, K, prec, ctypes.byref(g), pd, ldd)
+    return _call("softmax_logprob_bwd_rows", dev, stream, p, ld, M, K, prec, g, pd, ldd)
 
 
 def softmax_logprob(dims, theta, theta_lp, y_top, ws, ids=None, logprob=None, entropy=None, top=None, idx=None,
@@ -588,7 +592,7 @@ def softmax_logprob(dims, theta, theta_lp, y_top, ws, ids=None, logprob=None, en
     dev = _on(y_top)
     pt, pl, py, pw = _head_args(dims, dev, theta, theta_lp, y_top, ws)
     q = _scores(dims.T * dims.B, dev, ids, logprob, entropy, top, idx, temperature)
-    return _call("softmax_logprob", dev, stream, ctypes.byref(dims), pt, pl, py, ctypes.byref(q), pw)
+    return _call("softmax_logprob", dev, stream, ctypes.byref(dims), pt, pl, py, q, pw)
 
 
 def softmax_logprob_bwd(dims, theta, theta_lp, y_top, dy_top, grad, ws, ids=None, dlogprob=None, dentropy=None,
@@ -596,26 +600,37 @@ def softmax_logprob_bwd(dims, theta, theta_lp, y_top, dy_top, grad, ws, ids=None
     dev = _on(y_top)
     pt, pl, py, pw = _head_args(dims, dev, theta, theta_lp, y_top, ws)
     g = _score_grads(dims.T * dims.B, dev, ids, dlogprob, dentropy, temperature)
-    return _call("softmax_logprob_bwd", dev, stream, ctypes.byref(dims), pt, pl, py, ctypes.byref(g),
+    return _call("softmax_logprob_bwd", dev, stream, ctypes.byref(dims), pt, pl, py, g,
                  _have("dy_top", dy_top, (dims.T, dims.B, 2 * dims.H), torch.float32, dev),
                  _have("grad", grad, tuple(theta.shape), torch.float32, dev), pw)
 
 
 # ----------------------------------------------------------------- 8-bit products ---
+def _matrix(name, t, shape, dtype, dev):
+    """_rows of a matrix."""
+    if t is not None and t.dtype is dtype and t.shape == shape and t.get_device() == dev:
+        ld, one = t.stride()
+        if one == 1 and ld >= shape[1]:
+            return t.data_ptr(), ld
+    return _rows(name, t, shape, dtype, dev)
+
+
 def _ints(name, q, rows, dev):
     """(address, row pitch, columns) of rows of 8-bit integers."""
-    if q is None or q.dim() != 2 or q.shape[0] != rows or q.dtype != torch.int8:
-        raise ValueError(f"{name} must be {rows} rows of int8" + ("" if q is None else f": got {q.dtype} {tuple(q.shape)}"))
-    p, ld = _rows(name, q, tuple(q.shape), torch.int8, dev)
-    return p, ld, q.shape[1]
+    shape = () if q is None else q.shape
+    if len(shape) != 2 or shape[0] != rows or q.dtype is not torch.int8:
+        raise ValueError(f"{name} must be {rows} rows of int8" + ("" if q is None else f": got {q.dtype} {tuple(shape)}"))
+    p, ld = _matrix(name, q, shape, torch.int8, dev)
+    return p, ld, shape[1]
 
 
 def _floats(name, x, dev):
     """(address, row pitch, rows, columns, precision) of rows of bfloat16 or float32."""
-    if x.dim() != 2 or x.dtype not in (torch.bfloat16, torch.float32):
-        raise ValueError(f"{name} must be bfloat16 or float32 rows: got {x.dtype} {tuple(x.shape)}")
-    p, ld = _rows(name, x, tuple(x.shape), x.dtype, dev)
-    return p, ld, x.shape[0], x.shape[1], BLSTM_BF16 if x.dtype == torch.bfloat16 else BLSTM_FP32
+    shape, t = x.shape, x.dtype
+    if len(shape) != 2 or (t is not torch.bfloat16 and t is not torch.float32):
+        raise ValueError(f"{name} must be bfloat16 or float32 rows: got {t} {tuple(shape)}")
+    p, ld = _matrix(name, x, shape, t, dev)
+    return p, ld, *shape, BLSTM_BF16 if t is torch.bfloat16 else BLSTM_FP32
 
 
 def int8_quantize_rows(x, q, scale, stream=None):
@@ -661,9 +676,9 @@ def int8_linear_rows(x, w, w_scale, y, ws, bias=None, stream=None):
     """x [M][K], w [N][Kw] integers with Kw >= K; y [M][N] of x's type."""
     dev, f = _on(x), torch.float32
     p, ld, M, K, prec = _floats("x", x, dev)
-    N = y.shape[-1]
+    N = w.shape[0]
     pw, ldw, Kw = _ints("w", w, N, dev)
-    py, ldy = _rows("y", y, (M, N), x.dtype, dev)
+    py, ldy = _matrix("y", y, (M, N), x.dtype, dev)
     return _call("int8_linear_rows", dev, stream, p, ld, M, K, prec, pw, ldw, _have("w_scale", w_scale, (N,), f, dev),
                  N, Kw, _have("bias", bias, (N,), f, dev, True), py, ldy,
                  _bytes("ws", ws, int8_linear_ws_bytes(M, Kw), dev))
@@ -683,4 +698,4 @@ def int8_logprob_rows(x, w, w_scale, ws, bias=None, ids=None, logprob=None, entr
     q = _scores(M, dev, ids, logprob, entropy, top, idx, temperature)
     return _call("int8_logprob_rows", dev, stream, p, ld, M, P, prec, pw, ldw,
                  _have("w_scale", w_scale, (K,), f, dev), K, Kw, _have("bias", bias, (K,), f, dev, True),
-                 ctypes.byref(q), _bytes("ws", ws, int8_logprob_ws_bytes(M, K, Kw), dev))
+                 q, _bytes("ws", ws, int8_logprob_ws_bytes(M, K, Kw), dev))

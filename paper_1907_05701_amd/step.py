@@ -20,6 +20,20 @@ def _given(teacher):
     return () if teacher is None else (teacher,)
 
 
+def new_scores(M, ids, k, entropy, device):
+    """Output tensors of the scoring calls for M rows, by argument name: those
+    that are asked for."""
+    out = {}
+    if ids is not None:
+        out["logprob"] = torch.empty(ids.shape, dtype=torch.float32, device=device)
+    if entropy:
+        out["entropy"] = torch.empty(M, dtype=torch.float32, device=device)
+    if k:
+        out["top"] = torch.empty((M, k), dtype=torch.float32, device=device)
+        out["idx"] = torch.empty((M, k), dtype=torch.int32, device=device)
+    return out
+
+
 class LearnerStep:
     def __init__(self, L, D, H, P, K, T, B, precision="bf16", device="cuda:0"):
         self.dims = bd.make_dims(L, D, H, P, K, T, B, precision)
@@ -91,6 +105,23 @@ class LearnerStep:
         bd.softmax_distill_fwd_bwd(self.dims, self.theta, self.theta_lp, self.y_top, top, idx, self.loss_scale,
                                    self.loss, self.dy_top, self.grad, self._distill_ws(), rest,
                                    self.labels.view(-1), weights, temperature, soft, hard)
+
+    def log_probs(self, ids=None, k=0, entropy=True, temperature=1.0):
+        """What this learner says of every frame, after forward(): the log
+        probabilities of the classes ids [T*B][n] (int32; outside the classes:
+        0), the entropy, and the log probabilities and classes of the k most
+        likely ones, as new tensors in a dict ("logprob", "entropy", "top", "idx")."""
+        out = new_scores(self.shape["T"] * self.shape["B"], ids, k, entropy, self.device)
+        bd.softmax_logprob(self.dims, self.theta, self.theta_lp, self.y_top, self._distill_ws(), ids=ids,
+                           temperature=temperature, **out)
+        return out
+
+    def score_head(self, ids=None, dlogprob=None, dentropy=None, temperature=1.0):
+        """head() from the loss gradients of log_probs()' outputs, for losses of
+        whole sequences: dy_top and the head's gradient, before backward()."""
+        bd.softmax_logprob_bwd(self.dims, self.theta, self.theta_lp, self.y_top, self.dy_top, self.grad,
+                               self._distill_ws(), ids=ids, dlogprob=dlogprob, dentropy=dentropy,
+                               temperature=temperature)
 
     def backward(self, dy_top=None):
         bd.blstm_bwd(self.dims, self.theta, self.theta_lp, self.act_ws, self.y_top,

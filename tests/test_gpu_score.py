@@ -130,7 +130,8 @@ def test_logits_far_from_zero(gpu_lib):
 @pytest.mark.parametrize("precision", ["fp32", "bf16"])
 @pytest.mark.parametrize("K", [130, 900, 9001, 33001])
 def test_views_and_what_is_not_asked_for(gpu_lib, K, precision):
-    """Rows of a wider matrix, at odd offsets; every subset of the outputs gives the same bits."""
+    """Rows of a wider matrix, at odd offsets.  A subset of the outputs may be another kernel's (short rows, by k), whose sums
+    add up in another order: both are within TOL of the exact values, and so within twice that of each other."""
     g = torch.Generator().manual_seed(K)
     wide = (torch.randn(6, K + 37, generator=g) * 3).to(TYPES[precision]).cuda()
     s, ids = wide[1:, 3:3 + K], some_ids(5, K, 5)
@@ -139,9 +140,10 @@ def test_views_and_what_is_not_asked_for(gpu_lib, K, precision):
     for n, k, e in ((0, 9, True), (5, 0, True), (5, 9, False), (0, 0, True), (5, 0, False), (0, 9, False)):
         part = run(s, ids if n else None, k, entropy=e)
         for name, v in part.items():
-            assert v is None or name == "top" or name == "logprob" or torch.equal(v, full[name])
-            if v is not None and name in ("top", "logprob"):
-                assert bool(((v - full[name]).abs() <= TOL * (1 + v.abs())).all())
+            if name == "idx":
+                assert v is None or torch.equal(v, full[name])
+            elif v is not None:
+                assert bool(((v - full[name]).abs() <= 2 * TOL * (1 + v.abs())).all())
 
 
 def grad(s, ids, g, h, tau=1.0, out=None, stream=None):
