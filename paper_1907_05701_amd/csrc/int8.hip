@@ -28,12 +28,21 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const TI* __restrict
   uint32_t mx = 0;
   if constexpr (NV > 0) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) v[i].load(s, (i * T + tid) * V, K);
+    for (int i = 0; i < NV; ++i) {
+      if (K >= V) v[i].load(s, (i * T + tid) * V, K);
+      else v[i].zero();
+    }
+    if (K % V) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) v[i].patch(s, (i * T + tid) * V, K);
+    }
 #pragma unroll
     for (int i = 0; i < NV; ++i) mx = v[i].max(mx);
-  } else {
+  } else {   // (a long row: K >= V)
+#pragma unroll 4
     for (int c = tid * V; c < K; c += T * V) {
       v[0].load(s, c, K);
+      v[0].patch(s, c, K);
       mx = v[0].max(mx);
     }
   }
@@ -57,6 +66,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const TI* __restrict
   } else {
     for (int c = tid * V; c < Kq; c += T * V) {
       v[0].load(s, c, K);
+      v[0].patch(s, c, K);
       store(c, v[0]);
     }
   }
@@ -86,61 +96,92 @@ template void int8_quantize<bf16>(const bf16*, int64_t, int64_t, int32_t, int8_t
 // ---------------------------------------------------------------------------
 // The product.
 // ---------------------------------------------------------------------------
-// The same for up to 16 tokens of floats (TO, also y's), quantised on the way by every workgroup for itself while its
-// weights are in flight.
+// The same for up to 16 FN tokens of floats (TO, also y's), quantised on the way by every workgroup for itself while
+// its weights are in flight; NW waves, each with every NW-th 64 of K.
 struct Int8FewP {
   Int8P p;
   const void* x;
   int64_t ldx;
   int K, cols;   // columns of x, p.K those of the weights; in LDS
 };
-static constexpr int FEW_COLS = 4096;   // of 16 tokens in LDS
-template <typename TO, int NV>
-__global__ __launch_bounds__(256) void int8_few_tokens_kernel(const Int8FewP a) {
+static constexpr int FEW_COLS = 4096;           // of a token in LDS
+// Of all tokens, whom every workgroup quantises: 64 tokens of 1024 take 13.4 us in one launch, and 4.5 + 5.9 in two.
+static constexpr int64_t FEW_VALUES = 1 << 15;
+template <typename TO, int FN, int NW, int NV>
+__global__ __launch_bounds__(NW * 64) void int8_few_tokens_kernel(const Int8FewP a) {
   const Int8P& p = a.p;
   constexpr int U = 4;
   extern __shared__ __attribute__((aligned(16))) char tokens[];
-  __shared__ i32x4 part[3][64];
-  __shared__ float xs[16];
+  __shared__ float xs[16 * FN];
   const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, fr = lane & 15, fc = lane >> 4;
   const int64_t n0 = (int64_t)blockIdx.x * 16;
   const int8_t* wr = p.w + min(n0 + fr, p.N - 1) * p.ldw;   // rows past the last: any, dropped at the end
   const int k0 = wid * 64 + fc * 16;
-  auto weights = [&](int k) { return k < p.K ? *(const i32x4*)(wr + k) : i32x4{0, 0, 0, 0}; };
   i32x4 w[U];
 #pragma unroll
-  for (int u = 0; u < U; ++u) w[u] = weights(k0 + u * 256);
-  tokens_to_lds<TO, NV < 8 ? 8 / NV : 1, NV>((const TO*)a.x, a.ldx, (int)p.M, a.K, a.cols, tokens, xs);
+  for (int u = 0; u < U; ++u) w[u] = ints16(wr, k0 + u * NW * 64, p.K);
+  tokens_to_lds<TO, NW, NV < 8 ? 8 / NV : 1, NV>((const TO*)a.x, a.ldx, (int)p.M, a.K, a.cols, tokens, xs);
   __syncthreads();
-  const char* xr = tokens + (fr < p.M ? fr : 0) * (a.cols + 16);   // columns past the last token: any
-  i32x4 acc{0, 0, 0, 0};
+  const char* xr[FN];
+#pragma unroll
+  for (int j = 0; j < FN; ++j) xr[j] = tokens + (j * 16 + fr < p.M ? j * 16 + fr : 0) * (a.cols + 16);   // past the last token: any
+  i32x4 acc[FN];
+#pragma unroll
+  for (int j = 0; j < FN; ++j) acc[j] = i32x4{0, 0, 0, 0};
+  auto add = [&](i32x4 v, int k) {
+#pragma unroll
+    for (int j = 0; j < FN; ++j) acc[j] = mma_i8(v, *(const i32x4*)(xr[j] + k), acc[j]);
+  };
 #pragma unroll
   for (int u = 0; u < U; ++u)
-    if (wid * 64 + u * 256 < a.cols) acc = mma_i8(w[u], *(const i32x4*)(xr + k0 + u * 256), acc);
-#pragma unroll 4
-  for (int k = wid * 64 + U * 256; k < a.cols; k += 256) acc = mma_i8(weights(k + fc * 16), *(const i32x4*)(xr + k + fc * 16), acc);
-  if (wid > 0) part[wid - 1][lane] = acc;
+    if (wid * 64 + u * NW * 64 < a.cols) add(w[u], k0 + u * NW * 64);
+  for (int k = U * NW * 64; k < a.cols; k += U * NW * 64) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) w[u] = ints16(wr, k0 + k + u * NW * 64, p.K);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (wid * 64 + k + u * NW * 64 < a.cols) add(w[u], k0 + k + u * NW * 64);
+  }
+  __syncthreads();   // the tokens are done with
+  i32x4* part = (i32x4*)tokens;
+#pragma unroll
+  for (int j = 0; j < FN; ++j) part[(wid * FN + j) * 64 + lane] = acc[j];
   __syncthreads();
-  if (wid > 0) return;
-  put4<TO>(p, fr, n0 + 4 * fc, acc + part[0][lane] + part[1][lane] + part[2][lane], xs[fr]);
+  if (wid >= FN) return;   // a wave for each 16 tokens
+  i32x4 sum{0, 0, 0, 0};
+#pragma unroll
+  for (int v = 0; v < NW; ++v) sum += part[(v * FN + wid) * 64 + lane];
+  put4<TO>(p, wid * 16 + fr, n0 + 4 * fc, sum, xs[wid * 16 + fr]);
+}
+static bool few_tokens_ok(int64_t M, int32_t Kw) {
+  return M <= 64 && Kw <= FEW_COLS && rup(M, 16) * rup(Kw, 64) <= FEW_VALUES;
 }
 template <typename TO>
 static void few_tokens(Int8FewP a, hipStream_t s) {
   constexpr int V = Vec16<TO>::n;
   a.cols = (int)rup(a.p.K, 64);
-  const size_t bytes = 16 * (size_t)(a.cols + 16);
-  auto launch = [&](auto nv) {
-    auto fn = int8_few_tokens_kernel<TO, decltype(nv)::value>;
-    static std::atomic<uint64_t> raised{0};
-    kc_raise_lds_limit((const void*)fn, 16 * (FEW_COLS + 16), raised);
-    BLSTM_LAUNCH("int8_linear_few", fn, dim3((unsigned)cdiv(a.p.N, 16)), dim3(256), bytes, s, a);
+  auto launch = [&](auto fn, auto nw, auto nv) {
+    constexpr int FN = decltype(fn)::value, NW = decltype(nw)::value, NV = decltype(nv)::value;
+    if constexpr (16 * FN * (NV / 2 + 1) * 64 * V <= FEW_VALUES) {   // sizes that a call can have
+      auto kernel = int8_few_tokens_kernel<TO, FN, NW, NV>;
+      constexpr size_t most = FEW_VALUES + 64 * 16;
+      const size_t bytes = std::max<size_t>((size_t)rup(a.p.M, 16) * (a.cols + 16), NW * FN * 1024);
+      static std::atomic<uint64_t> raised{0};
+      kc_raise_lds_limit((const void*)kernel, most, raised);
+      BLSTM_LAUNCH("int8_linear_few", kernel, dim3((unsigned)cdiv(a.p.N, 16)), dim3(NW * 64), bytes, s, a);
+    }
   };
 #define INT(n) std::integral_constant<int, n>{}
-  if (a.cols <= 64 * V) launch(INT(1));
-  else if (a.cols <= 2 * 64 * V) launch(INT(2));
-  else if (a.cols <= 4 * 64 * V) launch(INT(4));
-  else if (a.cols <= 8 * 64 * V) launch(INT(8));
-  else launch(INT(FEW_COLS / (64 * V)));
+  auto columns = [&](auto fn, auto nw) {
+    if (a.cols <= 64 * V) launch(fn, nw, INT(1));
+    else if (a.cols <= 2 * 64 * V) launch(fn, nw, INT(2));
+    else if (a.cols <= 4 * 64 * V) launch(fn, nw, INT(4));
+    else if (a.cols <= 8 * 64 * V) launch(fn, nw, INT(8));
+    else launch(fn, nw, INT(FEW_COLS / (64 * V)));
+  };
+  if (a.p.M <= 16) columns(INT(1), INT(4));
+  else if (a.p.M <= 32) columns(INT(2), INT(8));
+  else columns(INT(4), INT(8));
 #undef INT
 }
 
@@ -261,7 +302,7 @@ extern "C" int int8_linear_rows(const void* x, int64_t ldx, int64_t M, int32_t K
   if (rc) return rc;
   if (!y) return blstm_fail(BLSTM_EINVAL, "%s: NULL pointer", fn);
   if (ldy < N) return blstm_fail(BLSTM_EINVAL, "%s: a row pitch is below its row", fn);
-  if (M <= 16 && Kw <= FEW_COLS) {
+  if (few_tokens_ok(M, Kw)) {
     Int8FewP a{};
     a.p.w = w; a.p.ldw = ldw; a.p.ldy = ldy; a.p.M = M; a.p.N = N; a.p.K = Kw; a.p.ws = w_scale; a.p.bias = bias; a.p.y = y;
     a.x = x; a.ldx = ldx; a.K = K;

@@ -98,10 +98,10 @@ __global__ __launch_bounds__(256, head_per_cu<KS>()) void int8_head_kernel(const
   auto fetch = [&](int j) {
     const int c = j * CT + lane;
     if (wid == 0) next = c < rows ? p.ws[tile0 * CT + c] : 0.f;
-    if (wid == 1) next = c < rows ? (p.bias ? fmax_nan(p.bias[tile0 * CT + c], FLOOR) : 0.f) : FLOOR;
+    if (wid == 1) next = c < rows ? (p.bias ? p.bias[tile0 * CT + c] : 0.f) : FLOOR;
   };
   auto put = [&](int j) {
-    if (wid < 2) *(float*)(lds + (j & 1) * STAGE + TILE + wid * 256 + lane * 4) = next;
+    if (wid < 2) *(float*)(lds + (j & 1) * STAGE + TILE + wid * 256 + lane * 4) = wid ? fmax_nan(next, FLOOR) : next;
   };
   // a tile's rows end with the last class: what lies behind it, and behind a row's columns, reads as zeros
   uint32_t off[LOADS];
@@ -117,14 +117,20 @@ __global__ __launch_bounds__(256, head_per_cu<KS>()) void int8_head_kernel(const
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) dma16(r, off[i], st + (i * 4 + wid) * 1024);
   };
+  // both stages are on their way before anything is waited for
   issue(0);
   fetch(0);
+  const float first = next;
+  if (tiles > 1) {
+    issue(1);
+    fetch(1);
+  }
 
   const int own = (int)min((int64_t)16 * FN * FW, p.M - (f0 - wf * 16 * FN));   // frames of the workgroup
   float* scales = (float*)(lds + 2 * STAGE + 16 * FN * FW * (KS * 64 + 16));
   if constexpr (!std::is_void<TI>::value) {
     constexpr int V = 16 / sizeof(TI), NV = KS > V ? KS / V : 1;
-    tokens_to_lds<TI, NV < 4 ? 4 : 2, NV>((const TI*)p.x + (f0 - wf * 16 * FN) * p.ldx, p.ldx, own, p.P, KS * 64, lds + 2 * STAGE, scales);
+    tokens_to_lds<TI, 4, NV < 4 ? 4 : 2, NV>((const TI*)p.x + (f0 - wf * 16 * FN) * p.ldx, p.ldx, own, p.P, KS * 64, lds + 2 * STAGE, scales);
     __syncthreads();
   }
   i32x4 b[FN][KS];
@@ -137,7 +143,7 @@ __global__ __launch_bounds__(256, head_per_cu<KS>()) void int8_head_kernel(const
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
         const int k = ks * 64 + fc * 16;
-        b[j][ks] = k < p.Kw ? *(const i32x4*)(p.q + f * p.Kw + k) : i32x4{0, 0, 0, 0};
+        b[j][ks] = ints16(p.q + f * p.Kw, k, p.Kw);
       }
     } else {
       const int row = (wf * FN + j) * 16 + fr;
@@ -161,7 +167,13 @@ __global__ __launch_bounds__(256, head_per_cu<KS>()) void int8_head_kernel(const
     gm[j] = -INFINITY;
   }
   const float slack = SLACK / p.it2;
-  put(0);
+  {
+    const float second = next;
+    next = first;
+    put(0);
+    next = second;
+    if (tiles > 1) put(1);
+  }
   uint32_t at_k[KS];   // of a lane's piece in the first 16 rows of its wave (the slot depends on the row in 16 alone)
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) at_k[ks] = (wc * NI * 16 + fr) * (NCH * 16) + head_slot<NCH>(ks * 4 + fc, fr) * 16;
@@ -169,7 +181,8 @@ __global__ __launch_bounds__(256, head_per_cu<KS>()) void int8_head_kernel(const
   for (int it = 0; it < tiles; ++it) {
     int8_stage_wait();
     kc_barrier();
-    if (it + 1 < tiles) {
+    const bool more = it > 0 && it + 1 < tiles;
+    if (more) {
       issue(it + 1);
       fetch(it + 1);
     }
@@ -223,7 +236,7 @@ __global__ __launch_bounds__(256, head_per_cu<KS>()) void int8_head_kernel(const
         gm[j] = -INFINITY;
       }
     }
-    if (it + 1 < tiles) put(it + 1);
+    if (more) put(it + 1);
   }
   // a frame's lanes, then its waves
 #pragma unroll

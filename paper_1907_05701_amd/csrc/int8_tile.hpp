@@ -175,13 +175,20 @@ __global__ __launch_bounds__(256) void int8_few_kernel(const Int8P p) {
   i32x4 acc[FN];
 #pragma unroll
   for (int j = 0; j < FN; ++j) acc[j] = i32x4{0, 0, 0, 0};
-#pragma unroll 4
-  for (int k = wid * 64; k < p.K; k += 256) {
-    // behind K: any columns, of weights that count as zeros
-    const int at = min(k + fc * 16, p.K - 16);
-    const i32x4 v = *(const i32x4*)(wr + at), a = k + fc * 16 < p.K ? v : i32x4{0, 0, 0, 0};
+  constexpr int U = 4;   // steps whose loads go out together
+  for (int k = wid * 64; k < p.K; k += U * 256) {
+    i32x4 a[U], b[U][FN];
 #pragma unroll
-    for (int j = 0; j < FN; ++j) acc[j] = mma_i8(a, *(const i32x4*)(xr[j] + at), acc[j]);
+    for (int u = 0; u < U; ++u) {
+      const int at = k + u * 256 + fc * 16;
+      a[u] = ints16(wr, at, p.K);
+#pragma unroll
+      for (int j = 0; j < FN; ++j) b[u][j] = *(const i32x4*)(xr[j] + min(at, p.K - 16));   // behind K: any, times zeros
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int j = 0; j < FN; ++j) acc[j] = mma_i8(a[u], b[u][j], acc[j]);
   }
   if (wid > 0) {
 #pragma unroll
