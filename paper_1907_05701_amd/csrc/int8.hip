@@ -26,6 +26,11 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const TI* __restrict
   int8_t* d = q + m * ldq;
   Vec16<TI> v[NR];
   uint32_t mx = 0;
+  auto read = [&](Vec16<TI>& o, int c) {   // (q may have many more columns than a short row)
+    if (K >= V) o.load(s, c, K);
+    else o.zero();
+    if (K % V) o.patch(s, c, K);
+  };
   if constexpr (NV > 0) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -38,11 +43,9 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const TI* __restrict
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i) mx = v[i].max(mx);
-  } else {   // (a long row: K >= V)
-#pragma unroll 4
+  } else {
     for (int c = tid * V; c < K; c += T * V) {
-      v[0].load(s, c, K);
-      v[0].patch(s, c, K);
+      read(v[0], c);
       mx = v[0].max(mx);
     }
   }
@@ -65,8 +68,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const TI* __restrict
     for (int i = 0; i < NV; ++i) store((i * T + tid) * V, v[i]);
   } else {
     for (int c = tid * V; c < Kq; c += T * V) {
-      v[0].load(s, c, K);
-      v[0].patch(s, c, K);
+      read(v[0], c);
       store(c, v[0]);
     }
   }
@@ -153,8 +155,9 @@ __global__ __launch_bounds__(NW * 64) void int8_few_tokens_kernel(const Int8FewP
   for (int v = 0; v < NW; ++v) sum += part[(v * FN + wid) * 64 + lane];
   put4<TO>(p, wid * 16 + fr, n0 + 4 * fc, sum, xs[wid * 16 + fr]);
 }
+static int few_fragments(int64_t M) { return M <= 16 ? 1 : M <= 32 ? 2 : 4; }   // of 16 tokens
 static bool few_tokens_ok(int64_t M, int32_t Kw) {
-  return M <= 64 && Kw <= FEW_COLS && rup(M, 16) * rup(Kw, 64) <= FEW_VALUES;
+  return M <= 64 && Kw <= FEW_COLS && 16 * few_fragments(M) * rup(Kw, 64) <= FEW_VALUES;
 }
 template <typename TO>
 static void few_tokens(Int8FewP a, hipStream_t s) {
@@ -162,7 +165,7 @@ static void few_tokens(Int8FewP a, hipStream_t s) {
   a.cols = (int)rup(a.p.K, 64);
   auto launch = [&](auto fn, auto nw, auto nv) {
     constexpr int FN = decltype(fn)::value, NW = decltype(nw)::value, NV = decltype(nv)::value;
-    if constexpr (16 * FN * (NV / 2 + 1) * 64 * V <= FEW_VALUES) {   // sizes that a call can have
+    if constexpr (16 * FN * (NV / 2 * 64 * V + 64) <= FEW_VALUES) {   // (the fewest columns that come here)
       auto kernel = int8_few_tokens_kernel<TO, FN, NW, NV>;
       constexpr size_t most = FEW_VALUES + 64 * 16;
       const size_t bytes = std::max<size_t>((size_t)rup(a.p.M, 16) * (a.cols + 16), NW * FN * 1024);
@@ -179,9 +182,11 @@ static void few_tokens(Int8FewP a, hipStream_t s) {
     else if (a.cols <= 8 * 64 * V) launch(fn, nw, INT(8));
     else launch(fn, nw, INT(FEW_COLS / (64 * V)));
   };
-  if (a.p.M <= 16) columns(INT(1), INT(4));
-  else if (a.p.M <= 32) columns(INT(2), INT(8));
-  else columns(INT(4), INT(8));
+  switch (few_fragments(a.p.M)) {
+    case 1: return columns(INT(1), INT(4));
+    case 2: return columns(INT(2), INT(8));
+    default: return columns(INT(4), INT(8));
+  }
 #undef INT
 }
 

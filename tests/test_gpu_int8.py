@@ -53,6 +53,15 @@ def test_integers(gpu_lib, M, K, precision):
 
 
 @pytest.mark.parametrize("precision", ["fp32", "bf16"])
+@pytest.mark.parametrize("Kq", [16, 4096, 20000])
+def test_integers_of_short_rows_in_wide_ones(gpu_lib, Kq, precision):
+    """Fewer columns than 16 bytes hold, at the end of their memory, and integers' rows of any length."""
+    g = torch.Generator().manual_seed(Kq)
+    for K in (1, 3, 7, 9):
+        check_quantize(torch.randn(5, K, generator=g).to(TYPES[precision]).cuda(), Kq)
+
+
+@pytest.mark.parametrize("precision", ["fp32", "bf16"])
 def test_integers_at_borders(gpu_lib, precision):
     """Ties, values next to them, rows of zeros, the smallest and largest numbers, NaN and infinities."""
     t = TYPES[precision]
@@ -192,7 +201,9 @@ def linear_rows(x, w, ws, bias=None, stream=None, y=None, buf=None):
 
 @pytest.mark.parametrize("precision", ["fp32", "bf16"])
 @pytest.mark.parametrize("M,N,K", [(1, 1, 1), (1, 100, 260), (1, 4096, 1024), (3, 50, 1000), (16, 64, 4096), (17, 64, 1024),
-                                   (64, 128, 333), (65, 100, 260), (300, 520, 100), (2, 20, 12001), (9, 30, 2500)])
+                                   (64, 128, 333), (65, 100, 260), (300, 520, 100), (2, 20, 12001), (9, 30, 2500),
+                                   (40, 70, 600), (48, 33, 512), (33, 40, 50), (20, 40, 1024), (32, 33, 1025),
+                                   (5, 40, 2048), (16, 20, 2049), (1, 40, 5000)])
 def test_tokens_times_weights(gpu_lib, M, N, K, precision):
     """Rows of a wider matrix, one of zeros, one with a NaN."""
     t = TYPES[precision]
