@@ -397,6 +397,45 @@ def test_the_same_every_time_on_another_stream_and_in_graphs(gpu_lib):
                 assert torch.equal(y1, y) and all(torch.equal(first[n], o[n]) for n in first)
 
 
+@pytest.mark.parametrize("M", [3, 20, 40, 150])
+def test_head_of_views(gpu_lib, M):
+    """Tokens that are columns of a wider matrix at an odd offset, weights at a pitch, lists that are not all there."""
+    for precision in TYPES:
+        x, w, ws, bias, ids = head_case(M, 100, 700, 3, precision)
+        wide = torch.full((M + 2, 117), math.nan, dtype=x.dtype, device="cuda")
+        wide[1:M + 1, 5:105] = x
+        far = torch.full((700, 400), 55, dtype=torch.int8, device="cuda")
+        far[:, 32:144] = w
+        want = head(x, w, ws, bias, ids, 6)
+        got = head(wide[1:M + 1, 5:105], far[:, 32:144], ws, bias, ids, 6)
+        torch.cuda.synchronize()
+        assert all(torch.equal(got[n], want[n]) for n in want)
+
+
+def test_rows_past_32_bits(gpu_lib):
+    """Pitches of 2^22, so that the last rows lie past 2^32 bytes."""
+    from paper_1907_05701_amd import binding as bd
+    g = torch.Generator().manual_seed(1)
+    M, K, ld = 1100, 48, 1 << 22
+    far = torch.empty(M * ld, dtype=torch.int8, device="cuda")
+    rows = torch.as_strided(far, (M, K), (ld, 1))
+    small = ints(M, K, g).cuda()
+    rows.copy_(small)
+    xs, ys = torch.rand(M, generator=g).cuda(), torch.rand(40, generator=g).cuda()
+    few = ints(40, K, g).cuda()
+    for q, s, w, t in ((rows, xs, few, ys), (few, ys, rows, xs)):
+        a, b = (torch.empty(q.shape[0], w.shape[0], device="cuda") for _ in range(2))
+        bd.int8_linear(q, s, w, t, a)
+        bd.int8_linear(q.contiguous(), s, w.contiguous(), t, b)
+        torch.cuda.synchronize()
+        assert torch.equal(a, b)
+    x = torch.randn(5, K, generator=g).cuda()
+    ids = torch.randint(0, M, (5, 2), generator=g, dtype=torch.int32).cuda()
+    a, b = head(x, rows, xs, None, ids, 4), head(x, small, xs, None, ids, 4)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a[n], b[n]) for n in a)
+
+
 def test_refusals_of_tensors(gpu_lib):
     from paper_1907_05701_amd import binding as bd
     x, w, ws, bias, ids = head_case(4, 64, 100, 2, "fp32")

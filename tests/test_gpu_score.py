@@ -271,6 +271,38 @@ def test_the_same_every_time_on_another_stream_and_in_a_graph(gpu_lib):
             assert all(torch.equal(first[n], again[n]) for n in first) and torch.equal(dfirst, dagain)
 
 
+@pytest.mark.parametrize("K", [200, 3000])
+def test_rows_past_32_bits(gpu_lib, K):
+    """A pitch of 2^24 elements: the last rows lie past 2^32 bytes and 2^31 elements."""
+    M, ld = 140, 1 << 24
+    far = torch.empty(M * ld, dtype=torch.bfloat16, device="cuda")
+    rows = torch.as_strided(far, (M, K), (ld, 1))
+    g = torch.Generator(device="cuda").manual_seed(K)
+    small = torch.randn(M, K, generator=g, device="cuda").bfloat16()
+    rows.copy_(small)
+    ids, dl = some_ids(M, K, 2), torch.randn(M, 2, generator=g, device="cuda")
+    a, b = run(rows, ids, 3), run(small, ids, 3)
+    d = grad(small, ids, dl, None)
+    grad(rows, ids, dl, None, out=rows)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a[n], b[n]) for n in a) and torch.equal(rows, d)
+
+
+def test_many_rows_of_few_classes(gpu_lib):
+    """More rows than 16 bits count, each by a wave."""
+    M, K = 70001, 5
+    g = torch.Generator(device="cuda").manual_seed(2)
+    s = torch.randn(M, K, generator=g, device="cuda")
+    ids = torch.randint(0, K, (M, 1), generator=g, device="cuda", dtype=torch.int32)
+    o = run(s, ids, 2)
+    d = grad(s, ids, torch.ones(M, 1, device="cuda"), None)
+    lp = torch.log_softmax(s.double(), 1)
+    near(o["logprob"], lp.gather(1, ids.long()).cpu())
+    near(o["top"], lp.topk(2).values.cpu())
+    want = torch.zeros_like(lp).scatter_(1, ids.long(), 1.0) - lp.exp()
+    assert float((d - want).abs().max()) <= 2 * TOL
+
+
 def test_refusals_of_tensors(gpu_lib):
     from paper_1907_05701_amd import binding as bd
     s = torch.zeros(4, 50, device="cuda")
