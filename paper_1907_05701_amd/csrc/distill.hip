@@ -32,7 +32,7 @@ __global__ __launch_bounds__(T) void topk_long_kernel(const TI* __restrict__ log
   });
   if (nan) l.flag = 1;
   l.tmax[tid] = order_word(mx);
-  const float thr = order_value(max(kth_max<12, T>(l, p.k), LOWEST));
+  const float thr = order_value(max(kth_max<12>(l, p.k), LOWEST));
   if (same(l.flag)) {
     topk_any<TI, T, true>(l, s, m, p);
     return;
@@ -102,7 +102,7 @@ __global__ __launch_bounds__(T, (waves_of<TI, T, V, NV>())) void topk_rows_kerne
   l.tmax[tid] = order_word(mx);
   // bf16: the lower 16 bits of all order words are alike; float32: a threshold
   // rounded down to 11 bits lets a few more pass and takes a third fewer steps
-  const uint32_t tw = max(kth_max<std::is_same<TI, bf16>::value ? 16 : 12, T>(l, p.k), LOWEST);
+  const uint32_t tw = max(kth_max<std::is_same<TI, bf16>::value ? 16 : 12>(l, p.k), LOWEST);
   const float thr = order_value(tw);
   row.again();
   if (same(l.flag)) {

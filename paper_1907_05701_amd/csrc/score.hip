@@ -5,6 +5,10 @@
 //   log p_j = (s_j - max s) / tau - ln Z,   H = ln Z - ln 2 T / Z
 // Exponents are scaled differences of logits, so that a mask of -1e9 or of the
 // type's lowest value is a value like any other.  Sums are float32 in a fixed order.
+//
+// Memory bounds both: a row is read once, into registers.  2688 bf16 rows of 32000 logits with one listed class, the
+// entropy and 8 most likely classes in 39.8 us (172 MB, 4.3 TB/s; the vector unit issues 31 us of it), the gradient in
+// 70 us (344 MB, 4.9 TB/s).
 #include <cmath>
 
 #include "rows.hpp"
@@ -81,7 +85,8 @@ __device__ __forceinline__ void add_row(RowStats& r, Row<TI, V, NV, T>& row) {
 
 template <typename TI, int T, int V, int NV, bool TOP>
 __global__ __launch_bounds__(T, (waves_of<TI, T, V, NV>())) void score_rows_kernel(const TI* __restrict__ logits, const ScoreP p) {
-  __shared__ TopkLds<TOP ? T : 64> l;
+  constexpr int C = T == 64 ? 256 : CAND;   // (a one-wave workgroup's share of the LDS)
+  __shared__ TopkLds<TOP ? T : 64, TOP ? C : 64> l;
   __shared__ float buf[3][T / 64];
   const int64_t m = blockIdx.x;
   const TI* s = logits + m * p.ld;
@@ -106,7 +111,7 @@ __global__ __launch_bounds__(T, (waves_of<TI, T, V, NV>())) void score_rows_kern
     l.tmax[tid] = order_word(mx);
     // bf16: the lower 16 bits of all order words are alike; float32: a threshold
     // rounded down to 11 bits lets a few more pass and takes a third fewer steps
-    thr = order_value(max(kth_max<std::is_same<TI, bf16>::value ? 16 : 12, T>(l, p.k), LOWEST));
+    thr = order_value(max(kth_max<std::is_same<TI, bf16>::value ? 16 : 12>(l, p.k), LOWEST));
   } else {
     __syncthreads();
   }
@@ -157,94 +162,8 @@ __global__ __launch_bounds__(T, (waves_of<TI, T, V, NV>())) void score_rows_kern
   if constexpr (TOP) {
     TopkP tp{p.ld, K, p.k, p.it2, p.top, nullptr, p.idx};
     const int n = (int)same(l.count);
-    if (same(!r.good()) || n > CAND) topk_any<TI, T, true>(l, s, m, tp, lp);
+    if (same(!r.good()) || n > C) topk_any<TI, T, true>(l, s, m, tp, lp);
     else rank(l, n, m, tp, lp);
-  }
-}
-
-// ---------------------------------------------------------------------------
-// Short rows, a wave each: no barriers, and up to 16 most likely classes by as many searches for the largest.
-// (us, by a wave / by a workgroup of 256 threads a row: 20000 float32 rows of 100 classes 6.3 / 22.1, with 8 most
-// likely classes 13.7 / 38.3, the gradient 8.7 / 31.6; 5000 bf16 rows of 1000 with 8 classes 13.4 / 12.9, with 16 20 / -,
-// the gradient 8.4 / 12.6.)
-// ---------------------------------------------------------------------------
-static constexpr int WAVE_K = 1024, WAVE_TOP = 16, WAVE_SEARCH = 128, WAVE_LIST = 64;
-
-// Class i * 64 + lane of a row in registers, -inf behind the last.
-template <typename TI, int NV>
-__device__ __forceinline__ void wave_load(const TI* s, int K, float (&v)[NV]) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int i = 0; i < NV; ++i) v[i] = i * 64 + lane < K ? to_f32(s[i * 64 + lane]) : -INFINITY;
-}
-template <int NV>
-__device__ __forceinline__ RowStats wave_stats(const float (&v)[NV], float it2) {
-  float mx = -INFINITY;
-#pragma unroll
-  for (int i = 0; i < NV; ++i) mx = fmaxf(mx, v[i]);
-  RowStats r(wave_max(mx), it2);
-#pragma unroll
-  for (int i = 0; i < NV; ++i) r.add(v[i]);
-  r.z = wave_sum(r.z);
-  r.t = wave_sum(r.t);
-  return r;
-}
-
-// The largest word of a wave, by lanes moved within the vector unit: rows of 16, then across them.
-__device__ __forceinline__ uint32_t wave_largest(uint32_t v) {
-#define STEP(ctrl) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, ctrl, 0xf, 0xf, false))
-  STEP(0x111);   // row_shr:1, 2, 4, 8
-  STEP(0x112);
-  STEP(0x114);
-  STEP(0x118);
-  STEP(0x142);   // row_bcast:15, 31
-  STEP(0x143);
-#undef STEP
-  return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
-}
-
-template <typename TI, int NV>
-__global__ __launch_bounds__(256) void score_wave_kernel(const TI* __restrict__ logits, int64_t M, const ScoreP p) {
-  const int lane = threadIdx.x & 63, K = p.K;
-  const int64_t m = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (m >= M) return;
-  const TI* s = logits + m * p.ld;
-  float v[NV];
-  wave_load(s, K, v);
-  const RowStats r = wave_stats(v, p.it2);
-  const LogProb lp(r, p.itau);
-  for (int i = lane; i < p.n; i += 64) {
-    const int at = p.ids[m * p.n + i];
-    p.logprob[m * p.n + i] = at < 0 || at >= K ? 0.f : lp(to_f32(s[at]));
-  }
-  if (p.entropy && lane == 0) p.entropy[m] = lp.some ? lp.lz - r.t / r.z * LN2_F : 0.f;
-  if (!p.k) return;
-  uint32_t w[NV];
-#pragma unroll
-  for (int i = 0; i < NV; ++i) w[i] = i * 64 + lane < K ? order_word(v[i]) : 0;
-  float top = 0.f;
-  int idx = 0;
-  for (int j = 0; j < p.k; ++j) {
-    uint32_t b = 0, c = 0;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      c = w[i] > b ? i * 64 + lane : c;   // the lower class first
-      b = max(b, w[i]);
-    }
-    const uint32_t big = wave_largest(b);
-    uint64_t ties = __ballot(b == big);
-    int at = __builtin_amdgcn_readlane((int)c, __builtin_ctzll(ties));
-    for (ties &= ties - 1; ties; ties &= ties - 1) at = min(at, __builtin_amdgcn_readlane((int)c, __builtin_ctzll(ties)));
-    if (lane == j) {
-      top = lp(order_value(big));
-      idx = at;
-    }
-#pragma unroll
-    for (int i = 0; i < NV; ++i) w[i] = i * 64 + lane == at ? 0 : w[i];
-  }
-  if (lane < p.k) {
-    p.top[m * p.k + lane] = top;
-    p.idx[m * p.k + lane] = idx;
   }
 }
 
@@ -357,6 +276,29 @@ __global__ __launch_bounds__(T, (waves_of<TI, T, V, NV>())) void score_grad_kern
 }
 
 // Short rows, a wave each; a class's list entries are added where the class lies in registers.
+// (20000 float32 rows of 100 classes 8.7 us, by a workgroup of 256 threads each 31.6; 5000 bf16 rows of 1000 8.4 and 12.6.)
+static constexpr int WAVE_K = 1024, WAVE_LIST = 64;
+
+// Class i * 64 + lane of a row in registers, -inf behind the last.
+template <typename TI, int NV>
+__device__ __forceinline__ void wave_load(const TI* s, int K, float (&v)[NV]) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) v[i] = i * 64 + lane < K ? to_f32(s[i * 64 + lane]) : -INFINITY;
+}
+template <int NV>
+__device__ __forceinline__ RowStats wave_stats(const float (&v)[NV], float it2) {
+  float mx = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) mx = fmaxf(mx, v[i]);
+  RowStats r(wave_max(mx), it2);
+#pragma unroll
+  for (int i = 0; i < NV; ++i) r.add(v[i]);
+  r.z = wave_sum(r.z);
+  r.t = wave_sum(r.t);
+  return r;
+}
+
 template <typename TI, typename TO, int NV>
 __global__ __launch_bounds__(256) void score_grad_wave_kernel(const TI* logits, TO* dlogits, int64_t M, const ScoreGradP p) {
   const int lane = threadIdx.x & 63, K = p.K;
@@ -409,13 +351,6 @@ template <typename F> static void by_width(int32_t K, F f) {
 template <typename TI>
 int score_rows(const TI* logits, int64_t ld, int64_t M, int32_t K, const softmax_scores& q, hipStream_t stream) {
   const ScoreP p{ld, K, q.n, q.k, LOG2E_F / q.temperature, 1.f / q.temperature, q.ids, q.logprob, q.entropy, q.top, q.idx};
-  if (K <= WAVE_K && q.k <= WAVE_TOP && q.k * cdiv(K, 64) <= WAVE_SEARCH) {
-    by_width(K, [&](auto nv) {
-      BLSTM_LAUNCH("softmax_logprob_rows", (score_wave_kernel<TI, decltype(nv)::value>), dim3((unsigned)cdiv(M, 4)),
-                   dim3(256), 0, stream, logits, M, p);
-    });
-    return blstm_check_launch("softmax_logprob_rows");
-  }
   auto launch = [&](auto t, auto v, auto nv, auto top) {
     constexpr int T = decltype(t)::value, V = decltype(v)::value, NV = decltype(nv)::value;
     BLSTM_LAUNCH("softmax_logprob_rows", (score_rows_kernel<TI, T, V, NV, decltype(top)::value>), dim3((unsigned)M),
@@ -425,6 +360,21 @@ int score_rows(const TI* logits, int64_t ld, int64_t M, int32_t K, const softmax
     if (q.k) launch(t, v, nv, std::true_type{});
     else launch(t, v, nv, std::false_type{});
   };
+  // Rows that a wave holds are a workgroup of one wave each: its barriers wait for nobody, and a CU has 32 rows.  64 maxima
+  // give a threshold for up to 32 classes.  A few long rows are done sooner by more threads each.  (us, by a wave / by a
+  // workgroup of 256, 8 most likely classes: 20000 float32 rows of 100 13.1 / 38.3, 5000 bf16 rows of 1000 6.9 / 12.9, 12000
+  // of 1500 17.2 / 34.1, of 3500 27.4 / 31.4; one row of 3000 5.0 / 3.9.)
+  constexpr int V = Wide<TI>::n;
+  if (K <= 64 * 64 && q.k <= 32 && q.n <= 64 && (K <= 1024 || M >= 1024)) {
+#define INT(n) std::integral_constant<int, n>{}
+    if (K <= 4 * 64) with(INT(64), INT(1), INT(4));
+    else if (K <= 8 * 64) with(INT(64), INT(1), INT(8));
+    else if (K <= 16 * 64) with(INT(64), INT(V), INT(16 / V));
+    else if (K <= 32 * 64) with(INT(64), INT(V), INT(32 / V));
+    else with(INT(64), INT(V), INT(64 / V));
+#undef INT
+    return blstm_check_launch("softmax_logprob_rows");
+  }
   if (q.k <= 128) by_length<TI, 128 * 1024, true>(K, with);
   else by_length<TI, 128 * 1024, false>(K, with);
   return blstm_check_launch("softmax_logprob_rows");

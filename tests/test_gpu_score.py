@@ -44,9 +44,13 @@ def near(got, want):
     assert bool(((g - w).abs()[ok] <= TOL * (1 + w.abs()[ok])).all()), float(((g - w).abs()[ok]).max())
 
 
-def check(s, ids, k, tau=1.0):
+def check(s, ids, k, tau=1.0, only=None):
+    """`only`: the rows looked at."""
     o = run(s, ids, k, tau)
     torch.cuda.synchronize()
+    if only is not None:
+        o = {n: None if t is None else t[only] for n, t in o.items()}
+        s, ids = s[only], None if ids is None else ids[only]
     rows = s.double().cpu()
     lps = [sm.log_probs(r, tau) for r in rows]
     near(o["entropy"], torch.stack([sm.entropy(r, tau) for r in rows]))
@@ -117,6 +121,24 @@ def test_rows_that_masks_or_ties_bend(gpu_lib, K, precision):
     s = s.to(t).cuda()
     for k in (0, 1, 40, 80):
         check(s, some_ids(14, K, 6, seed=k), k)
+
+
+@pytest.mark.parametrize("precision", ["fp32", "bf16"])
+@pytest.mark.parametrize("K,k,n", [(200, 32, 64), (500, 33, 1), (1030, 32, 64), (2000, 5, 65), (2049, 0, 3), (4001, 32, 2), (4097, 7, 1)])
+def test_many_rows(gpu_lib, K, k, n, precision):
+    """Rows enough to fill the card: ties over all classes and over a part, rows with nothing left, infinities, NaN."""
+    t = TYPES[precision]
+    s = torch.randn(1100, K, generator=torch.Generator().manual_seed(K)) * 3
+    s[3] = 0.0
+    s[500, 10:K - 90] = 9.0
+    s[501] = torch.arange(K) / 64
+    s[700] = -math.inf
+    s[701] = torch.finfo(t).min
+    s[702, :K - 2] = -math.inf
+    s[900, K // 2] = math.nan
+    s[1098, 7] = math.inf
+    s[1099] = math.nan
+    check(s.to(t).cuda(), some_ids(1100, K, n), k, only=[*range(0, 1100, 37), 3, 500, 501, 700, 701, 702, 900, 1098, 1099])
 
 
 def test_logits_far_from_zero(gpu_lib):
