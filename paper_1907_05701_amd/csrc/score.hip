@@ -84,7 +84,8 @@ __device__ __forceinline__ void add_row(RowStats& r, Row<TI, V, NV, T>& row) {
 }
 
 template <typename TI, int T, int V, int NV, bool TOP>
-__global__ __launch_bounds__(T, (waves_of<TI, T, V, NV>())) void score_rows_kernel(const TI* __restrict__ logits, const ScoreP p) {
+__global__ __launch_bounds__(T, (waves_of<TI, T, V, NV>())) void score_rows_kernel(
+    const TI* __restrict__ logits, const ScoreP p) {
   constexpr int C = T == 64 ? 256 : CAND;   // (a one-wave workgroup's share of the LDS)
   __shared__ TopkLds<TOP ? T : 64, TOP ? C : 64> l;
   __shared__ float buf[3][T / 64];
@@ -275,9 +276,10 @@ __global__ __launch_bounds__(T, (waves_of<TI, T, V, NV>())) void score_grad_kern
   d[at] = from_f32<TO>(grad(sv) + own * p.itau);
 }
 
-// Short rows, a wave each; a class's list entries are added where the class lies in registers.
-// (20000 float32 rows of 100 classes 8.7 us, by a workgroup of 256 threads each 31.6; 5000 bf16 rows of 1000 8.4 and 12.6.)
-static constexpr int WAVE_K = 1024, WAVE_LIST = 64;
+// Short rows, four to a workgroup, a wave each without barriers; a class's list entries are added where the class lies in
+// registers.  (us, so / by a workgroup of one wave each: 20000 float32 rows of 100 classes 8.7 / 11.5, 20000 bf16 rows of
+// 300 12.3 / 15.2; 5000 bf16 rows of 1000 8.7 / 7.3.)
+static constexpr int WAVE_K = 512;
 
 // Class i * 64 + lane of a row in registers, -inf behind the last.
 template <typename TI, int NV>
@@ -341,11 +343,17 @@ __global__ __launch_bounds__(256) void score_grad_wave_kernel(const TI* logits, 
 // Host side.
 // ---------------------------------------------------------------------------
 // Values a lane of a wave that has a row.
-template <typename F> static void by_width(int32_t K, F f) {
-  if (K <= 2 * 64) f(std::integral_constant<int, 2>{});
-  else if (K <= 4 * 64) f(std::integral_constant<int, 4>{});
-  else if (K <= 8 * 64) f(std::integral_constant<int, 8>{});
-  else f(std::integral_constant<int, 16>{});
+// Rows that a wave holds are a workgroup of one wave each: its barriers wait for nobody, and a CU has 32 rows.  A few long
+// rows are done sooner by more threads each.  (us, by a wave / by a workgroup of 256; 8 most likely classes: 20000 float32
+// rows of 100 13.1 / 38.3, 5000 bf16 rows of 1000 6.9 / 12.9, 12000 of 1500 17.2 / 34.1, of 3500 27.4 / 31.4, one of 3000
+// 5.0 / 3.9; gradients: 5000 bf16 rows of 1000 7.3 / 12.6, 12000 of 1500 20.7 / 33.4, 1024 of 2000 4.8 / 5.4.)
+static bool one_wave(int64_t M, int32_t K) { return K <= 1024 || (K <= 64 * 64 && M >= 1024); }
+template <typename TI, typename F> static void by_wave(int32_t K, F f) {
+  constexpr int V = Wide<TI>::n;
+  constexpr std::integral_constant<int, 64> t{};
+  if (K <= 16 * 64) f(t, std::integral_constant<int, V>{}, std::integral_constant<int, 16 / V>{});
+  else if (K <= 32 * 64) f(t, std::integral_constant<int, V>{}, std::integral_constant<int, 32 / V>{});
+  else f(t, std::integral_constant<int, V>{}, std::integral_constant<int, 64 / V>{});
 }
 
 template <typename TI>
@@ -360,19 +368,12 @@ int score_rows(const TI* logits, int64_t ld, int64_t M, int32_t K, const softmax
     if (q.k) launch(t, v, nv, std::true_type{});
     else launch(t, v, nv, std::false_type{});
   };
-  // Rows that a wave holds are a workgroup of one wave each: its barriers wait for nobody, and a CU has 32 rows.  64 maxima
-  // give a threshold for up to 32 classes.  A few long rows are done sooner by more threads each.  (us, by a wave / by a
-  // workgroup of 256, 8 most likely classes: 20000 float32 rows of 100 13.1 / 38.3, 5000 bf16 rows of 1000 6.9 / 12.9, 12000
-  // of 1500 17.2 / 34.1, of 3500 27.4 / 31.4; one row of 3000 5.0 / 3.9.)
-  constexpr int V = Wide<TI>::n;
-  if (K <= 64 * 64 && q.k <= 32 && q.n <= 64 && (K <= 1024 || M >= 1024)) {
-#define INT(n) std::integral_constant<int, n>{}
-    if (K <= 4 * 64) with(INT(64), INT(1), INT(4));
-    else if (K <= 8 * 64) with(INT(64), INT(1), INT(8));
-    else if (K <= 16 * 64) with(INT(64), INT(V), INT(16 / V));
-    else if (K <= 32 * 64) with(INT(64), INT(V), INT(32 / V));
-    else with(INT(64), INT(V), INT(64 / V));
-#undef INT
+  // 64 maxima give a threshold for up to 32 classes
+  if (q.k <= 32 && q.n <= 64 && one_wave(M, K)) {
+    using One = std::integral_constant<int, 1>;
+    if (K <= 4 * 64) with(std::integral_constant<int, 64>{}, One{}, std::integral_constant<int, 4>{});
+    else if (K <= 8 * 64) with(std::integral_constant<int, 64>{}, One{}, std::integral_constant<int, 8>{});
+    else by_wave<TI>(K, with);
     return blstm_check_launch("softmax_logprob_rows");
   }
   if (q.k <= 128) by_length<TI, 128 * 1024, true>(K, with);
@@ -386,18 +387,26 @@ template <typename TI, typename TO>
 int score_grad_rows(const TI* logits, int64_t ld, int64_t M, int32_t K, const softmax_score_grads& q, TO* dlogits,
                     int64_t ldd, int32_t pad, hipStream_t stream) {
   const ScoreGradP p{ld, ldd, K, q.n, pad, LOG2E_F / q.temperature, 1.f / q.temperature, q.ids, q.dlogprob, q.dentropy};
-  if (K <= WAVE_K && q.n <= WAVE_LIST) {
-    by_width(K, [&](auto nv) {
+  if (K <= WAVE_K && q.n <= 64) {
+    auto wave = [&](auto nv) {
       BLSTM_LAUNCH("softmax_logprob_bwd_rows", (score_grad_wave_kernel<TI, TO, decltype(nv)::value>),
                    dim3((unsigned)cdiv(M, 4)), dim3(256), 0, stream, logits, dlogits, M, p);
-    });
+    };
+    if (K <= 2 * 64) wave(std::integral_constant<int, 2>{});
+    else if (K <= 4 * 64) wave(std::integral_constant<int, 4>{});
+    else wave(std::integral_constant<int, 8>{});
     return blstm_check_launch("softmax_logprob_bwd_rows");
   }
-  by_length<TI, 128 * 1024, true>(K, [&](auto t, auto v, auto nv) {
+  auto with = [&](auto t, auto v, auto nv) {
     constexpr int T = decltype(t)::value, V = decltype(v)::value, NV = decltype(nv)::value;
     BLSTM_LAUNCH("softmax_logprob_bwd_rows", (score_grad_kernel<TI, TO, T, V, NV>), dim3((unsigned)M), dim3(T), 0,
                  stream, logits, dlogits, p);
-  });
+  };
+  if (q.n <= 64 && one_wave(M, K)) {
+    by_wave<TI>(K, with);
+    return blstm_check_launch("softmax_logprob_bwd_rows");
+  }
+  by_length<TI, 128 * 1024, true>(K, with);
   return blstm_check_launch("softmax_logprob_bwd_rows");
 }
 template int score_grad_rows<float, float>(const float*, int64_t, int64_t, int32_t, const softmax_score_grads&, float*, int64_t, int32_t, hipStream_t);

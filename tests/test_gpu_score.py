@@ -310,6 +310,28 @@ def test_rows_past_32_bits(gpu_lib, K):
     assert all(torch.equal(a[n], b[n]) for n in a) and torch.equal(rows, d)
 
 
+@pytest.mark.parametrize("precision", ["fp32", "bf16"])
+@pytest.mark.parametrize("K,n", [(500, 64), (513, 65), (700, 64), (1030, 64), (2000, 3), (2049, 65), (4001, 1), (4097, 2)])
+def test_gradients_of_many_rows(gpu_lib, K, n, precision):
+    M, only = 1100, [*range(0, 1100, 37), 3, 500, 700, 702, 900, 1098]
+    g = torch.Generator().manual_seed(K)
+    s = torch.randn(M, K, generator=g) * 3
+    s[3] = 0.0
+    s[500] = torch.finfo(TYPES[precision]).min
+    s[700] = -math.inf
+    s[702, :K - 2] = -math.inf
+    s[1098, 5] = math.nan
+    s = s.to(TYPES[precision]).cuda()
+    dl, dh = torch.randn(M, n, generator=g), torch.randn(M, generator=g)
+    dl[900], dh[900] = 0.0, 0.0
+    ids = some_ids(M, K, n)
+    d = grad(s, ids, dl.cuda(), dh.cuda())
+    check_grad(s[only], ids[only], dl[only], dh[only], d=d[only])
+    assert not d[900].any()
+    over = s.clone()
+    assert torch.equal(grad(over, ids, dl.cuda(), dh.cuda(), out=over).nan_to_num(9.0), d.nan_to_num(9.0))
+
+
 def test_many_rows_of_few_classes(gpu_lib):
     """More rows than 16 bits count, each by a wave."""
     M, K = 70001, 5
