@@ -33,12 +33,14 @@ class Int8Head:
         self.w_s, self.scale_s = _quantized(w_s.view(K, P))
         self.b_l, self.b_s = b_l.clone(), b_s.clone()
         self.P, self.K, self.H2, self.device = P, K, H2, learner.device
-        self.ws = None
+        self.ws, self._older = None, []
 
     def _buffers(self, M):
-        """A workspace for M frames: one for both calls, which follow each other on a stream."""
+        """A workspace for M frames: one for both calls, which follow each other on a stream.
+        Smaller ones stay: a captured graph may hold them."""
         n = max(bd.int8_linear_ws_bytes(M, self.w_l.shape[1]), bd.int8_logprob_ws_bytes(M, self.K, self.w_s.shape[1]))
         if self.ws is None or self.ws.numel() < n:
+            self._older.append(self.ws)
             self.ws = torch.empty(n, dtype=torch.uint8, device=self.device)
         return self.ws
 

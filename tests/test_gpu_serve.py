@@ -137,3 +137,27 @@ def test_the_head_in_8_bits_takes_any_number_of_frames_in_turn(gpu_lib):
         torch.cuda.synchronize()
         assert torch.equal(part["idx"], whole["idx"][:n])
         assert float((part["entropy"] - whole["entropy"][:n]).abs().max()) <= 2 * TOL * 8
+
+
+def test_the_head_in_8_bits_in_a_graph_beside_larger_calls(gpu_lib):
+    """What a graph holds stays when a later call needs a larger workspace."""
+    from paper_1907_05701_amd.serve import Int8Head
+    st = learner("bf16")
+    head, H2 = Int8Head(st), 2 * SHAPE["H"]
+    y = st.y_top.view(-1, H2)
+    few = y[:2].clone()
+    want = head.log_probs(few, k=3)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = head.log_probs(few, k=3)
+    held = head.ws.data_ptr()
+    head.log_probs(y, k=3)
+    assert head.ws.data_ptr() != held
+    others = [torch.zeros(n, dtype=torch.uint8, device="cuda") for n in (512, 4096, 1 << 16, 1 << 20) for _ in range(8)]
+    for _ in range(3):
+        for t in got.values():
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(got[n], want[n]) for n in want)
+        assert not any(bool(t.any()) for t in others)
