@@ -367,7 +367,8 @@ int softmax_distill_fwd_bwd(const blstm_dims* dims, const float* theta, const vo
 
 /* ---------------------------------------------------------------------------
  * Scoring: what a model says of given classes, for alignment, rescoring and
- * confidences, and the gradient for training on sequences.
+ * confidences, and the gradient for training on sequences.  Outputs overlap
+ * neither each other nor an input, except where said.
  * ------------------------------------------------------------------------- */
 
 /* What is asked of every row.  With p = softmax(logits / temperature):
@@ -423,7 +424,7 @@ int softmax_logprob_bwd(const blstm_dims* dims, const float* theta, const void* 
  * channel (a row of the weights), for serving.
  * Integers lie in rows of K columns, K a multiple of 16 and at most 131056, at a row pitch
  * that 16 divides (at most 2^22), 16-byte aligned.  A matrix of fewer columns is padded with zeros,
- * as int8_quantize_rows does.
+ * as int8_quantize_rows does.  Outputs and workspaces overlap neither each other nor an input.
  * ------------------------------------------------------------------------- */
 
 /* Rows of x [M][K] (the precision's type, row pitch ldx) in integers:

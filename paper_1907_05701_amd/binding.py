@@ -616,12 +616,13 @@ def _matrix(name, t, shape, dtype, dev):
 
 
 def _ints(name, q, rows, dev):
-    """(address, row pitch, columns) of rows of 8-bit integers."""
+    """(address, row pitch, rows, columns) of rows of 8-bit integers; `rows` None: any."""
     shape = () if q is None else q.shape
-    if len(shape) != 2 or shape[0] != rows or q.dtype is not torch.int8:
-        raise ValueError(f"{name} must be {rows} rows of int8" + ("" if q is None else f": got {q.dtype} {tuple(shape)}"))
+    if len(shape) != 2 or (rows is not None and shape[0] != rows) or q.dtype is not torch.int8:
+        raise ValueError(f"{name} must be {'' if rows is None else f'{rows} '}rows of int8" +
+                         ("" if q is None else f": got {q.dtype} {tuple(shape)}"))
     p, ld = _matrix(name, q, shape, torch.int8, dev)
-    return p, ld, shape[1]
+    return p, ld, *shape
 
 
 def _floats(name, x, dev):
@@ -637,7 +638,7 @@ def int8_quantize_rows(x, q, scale, stream=None):
     """q [M][Kq], Kq at least x's columns and a multiple of 16; scale [M]."""
     dev = _on(x)
     p, ld, M, K, prec = _floats("x", x, dev)
-    pq, ldq, Kq = _ints("q", q, M, dev)
+    pq, ldq, _, Kq = _ints("q", q, M, dev)
     return _call("int8_quantize_rows", dev, stream, p, ld, M, K, prec, pq, ldq, Kq,
                  _have("scale", scale, (M,), torch.float32, dev))
 
@@ -646,8 +647,8 @@ def int8_linear(q, q_scale, w, w_scale, y, bias=None, stream=None):
     """q [M][K], w [N][K] integers; y [M][N] bfloat16 or float32."""
     dev, f = _on(q), torch.float32
     py, ldy, M, N, prec = _floats("y", y, dev)
-    pq, ldq, K = _ints("q", q, M, dev)
-    pw, ldw, Kw = _ints("w", w, N, dev)
+    pq, ldq, _, K = _ints("q", q, M, dev)
+    pw, ldw, _, Kw = _ints("w", w, N, dev)
     if K != Kw:
         raise ValueError(f"q has {K} columns, w {Kw}")
     return _call("int8_linear", dev, stream, pq, ldq, _have("q_scale", q_scale, (M,), f, dev), M, pw, ldw,
@@ -676,8 +677,7 @@ def int8_linear_rows(x, w, w_scale, y, ws, bias=None, stream=None):
     """x [M][K], w [N][Kw] integers with Kw >= K; y [M][N] of x's type."""
     dev, f = _on(x), torch.float32
     p, ld, M, K, prec = _floats("x", x, dev)
-    N = w.shape[0]
-    pw, ldw, Kw = _ints("w", w, N, dev)
+    pw, ldw, N, Kw = _ints("w", w, None, dev)
     py, ldy = _matrix("y", y, (M, N), x.dtype, dev)
     return _call("int8_linear_rows", dev, stream, p, ld, M, K, prec, pw, ldw, _have("w_scale", w_scale, (N,), f, dev),
                  N, Kw, _have("bias", bias, (N,), f, dev, True), py, ldy,
@@ -693,8 +693,7 @@ def int8_logprob_rows(x, w, w_scale, ws, bias=None, ids=None, logprob=None, entr
     """x [M][P], w [K][Kw] integers with Kw >= P, of K classes."""
     dev, f = _on(x), torch.float32
     p, ld, M, P, prec = _floats("x", x, dev)
-    K = w.shape[0]
-    pw, ldw, Kw = _ints("w", w, K, dev)
+    pw, ldw, K, Kw = _ints("w", w, None, dev)
     q = _scores(M, dev, ids, logprob, entropy, top, idx, temperature)
     return _call("int8_logprob_rows", dev, stream, p, ld, M, P, prec, pw, ldw,
                  _have("w_scale", w_scale, (K,), f, dev), K, Kw, _have("bias", bias, (K,), f, dev, True),

@@ -503,8 +503,9 @@ __global__ __launch_bounds__(FT, 6) void int8_head_finish_kernel(const HeadP p, 
   }
   __syncthreads();
   const float rc = h.buf[0][0], z = h.buf[0][1], t = h.buf[0][2];
-  // (a NaN fails both; a temperature beyond that would bring FLOOR's classes back in)
-  if (same(!(z > 0.f && z < INFINITY && p.it2 > 1e-15f))) {
+  // (a NaN fails all; a temperature beyond that would bring FLOOR's classes back in, and one below about 2e-9, where START's
+  // exponent is -inf, leaves t a NaN)
+  if (same(!(z > 0.f && z < INFINITY && fabsf(t) < INFINITY && p.it2 > 1e-15f))) {
     head_any(h, logit, p, o, m);
     return;
   }

@@ -350,6 +350,16 @@ def test_head_at_extreme_temperatures(gpu_lib):
     check_head(x, w, ws, bias, ids, 9, 2.0 ** -20)
 
 
+@pytest.mark.parametrize("M", [1, 20, 70])
+def test_head_next_to_no_temperature(gpu_lib, M):
+    """Exponents, and the sums' first reference, past what float32 holds."""
+    x, w, ws, bias, ids = head_case(M, 64, 900, 2, "fp32")
+    bias[::7] = -math.inf
+    for tau in (2.0 ** -29, 2.0 ** -31, 2.0 ** -60, 2.0 ** -100):
+        check_head(x, w, ws, bias, ids, 9, tau)
+        check_head(x, w, ws, None, ids, 0, tau)
+
+
 def test_head_asks_for_parts_and_leaves_the_rest(gpu_lib):
     x, w, ws, bias, ids = head_case(50, 256, 2000, 4, "bf16")
     full = head(x, w, ws, bias, ids, 6)
@@ -442,6 +452,11 @@ def test_refusals_of_tensors(gpu_lib):
     q, s = quantize(x)
     y = torch.empty(4, 100, device="cuda")
     buf = torch.empty(bd.int8_logprob_ws_bytes(4, 100, 64), dtype=torch.uint8, device="cuda")
+    for a in ((x, None, ws, y, buf), (x, w[0, 0], ws, y, buf), (x, w[0], ws, y, buf)):
+        with pytest.raises(ValueError):
+            bd.int8_linear_rows(*a)
+        with pytest.raises(ValueError):
+            bd.int8_logprob_rows(*a[:3], buf, entropy=torch.empty(4, device="cuda"))
     for a in ((q, s, w, ws, y.double()), (q, s, w, ws, y.t()), (q, s, w, ws, y[:3]), (q, s[:3], w, ws, y), (q, s, w[:99], ws, y),
               (q, s, w, ws[1:], y), (q.float(), s, w, ws, y), (q[:, :48], s, w, ws, y), (q.cpu(), s, w, ws, y),
               (q, s, w.t(), ws, y)):

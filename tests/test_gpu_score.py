@@ -332,6 +332,16 @@ def test_gradients_of_many_rows(gpu_lib, K, n, precision):
     assert torch.equal(grad(over, ids, dl.cuda(), dh.cuda(), out=over).nan_to_num(9.0), d.nan_to_num(9.0))
 
 
+@pytest.mark.parametrize("K", [90, 3000, 33000])
+def test_extreme_temperatures(gpu_lib, K):
+    s = torch.randn(5, K, generator=torch.Generator().manual_seed(K))
+    s[1, ::3] = -math.inf
+    s[2] = torch.finfo(torch.float32).min
+    s[3] = -math.inf
+    for tau in (2.0 ** 100, 2.0 ** 40, 2.0 ** -20, 2.0 ** -31, 2.0 ** -60, 2.0 ** -100):
+        check(s.cuda(), some_ids(5, K, 3), 5, tau)
+
+
 def test_many_rows_of_few_classes(gpu_lib):
     """More rows than 16 bits count, each by a wave."""
     M, K = 70001, 5
