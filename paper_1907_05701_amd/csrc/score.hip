@@ -184,10 +184,53 @@ struct ScoreGradP {
   const float *dlogprob, *dentropy;
 };
 
+// A row's list: all that is given to a class, for the class's first entry to write.  64 entries a wave; the ballots of each
+// bit of their classes say which of them a class equals, so that n entries take n / 64 steps a bit and not n.  (us, so / by
+// comparing each with each: 768 float32 rows of 9001 classes with 256 listed 16.3 / 51, 5000 of 700 with 64 8.9 / 24,
+// 2688 bf16 rows of 32000 with 256 75 / 154.)
+struct Listed {
+  bool first;
+  float sum;   // in the list's order
+};
+template <int N> struct ListLds {
+  static constexpr int BITS = 18;
+  float g[N];
+  uint64_t bit[N / 64][BITS], some[N / 64];
+  static __device__ __forceinline__ int bits(int K) { return 32 - __builtin_clz(K); }   // of every class, and of K
+  __device__ __forceinline__ void put(int at, float v, int n, int K) {
+    const int w = threadIdx.x >> 6;
+    if (n < 2 || w * 64 >= n) return;
+    g[threadIdx.x] = v;
+    const uint64_t there = __ballot(at >= 0);
+    if ((threadIdx.x & 63) == 0) some[w] = there;
+    const int nb = min(bits(K), BITS);
+    for (int b = 0; b < nb; ++b) {
+      const uint64_t set = __ballot(at >> b & 1);
+      if ((threadIdx.x & 63) == 0) bit[w][b] = set;
+    }
+  }
+  // behind a barrier
+  __device__ __forceinline__ Listed all_of(int at, float v, int n, int K) const {
+    const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    Listed o{at >= 0, v};
+    if (n < 2 || w * 64 >= n) return o;
+    o.sum = 0.f;
+    const int nb = min(bits(K), BITS);
+    for (int c = 0; c * 64 < n; ++c) {
+      uint64_t alike = some[c];
+#pragma unroll 4
+      for (int b = 0; b < nb; ++b) alike &= bit[c][b] ^ (uint64_t)((int64_t)(at >> b & 1) - 1);
+      const uint64_t before = c < w ? ~0ull : c == w ? (1ull << lane) - 1 : 0;
+      o.first &= !(alike & before);
+      for (; alike; alike &= alike - 1) o.sum += g[c * 64 + __builtin_ctzll(alike)];
+    }
+    return o;
+  }
+};
+
 template <typename TI, typename TO, int T, int V, int NV>
 __global__ __launch_bounds__(T, (waves_of<TI, T, V, NV>())) void score_grad_kernel(const TI* logits, TO* dlogits, const ScoreGradP p) {
-  __shared__ float gv[MAXK];
-  __shared__ int32_t iv[MAXK];
+  __shared__ ListLds<T == 64 ? 64 : MAXK> list;
   __shared__ float buf[4][T / 64];
   __shared__ uint32_t wanted;
   const int64_t m = blockIdx.x;
@@ -206,12 +249,12 @@ __global__ __launch_bounds__(T, (waves_of<TI, T, V, NV>())) void score_grad_kern
       sv = to_f32(s[at]);
       g = p.dlogprob[m * p.n + tid];
     }
-    iv[tid] = at;
-    gv[tid] = g;
   }
+  list.put(at, g, p.n, K);
   const float h = p.dentropy ? p.dentropy[m] : 0.f;
   for (int c = K + tid; c < K + p.pad; c += T) d[c] = from_f32<TO>(0.f);
   __syncthreads();
+  const Listed own = list.all_of(at, g, p.n, K);   // (the row is still on its way)
   float vm[NV ? NV : 1], mx = -INFINITY;
   if constexpr (NV > 0) mx = largest(row, vm);
   else each<TI, T>(s, K, [&](int, float v) { mx = fmaxf(mx, v); });
@@ -266,20 +309,14 @@ __global__ __launch_bounds__(T, (waves_of<TI, T, V, NV>())) void score_grad_kern
     if (c < K) d[c] = from_f32<TO>(grad(to_f32(s[c])));
   }
   __syncthreads();   // the dense part lies before what replaces the listed classes' values
-  if (at < 0) return;
-  float own = 0.f;   // all that is listed of the class, written by its first entry
-  for (int j = 0; j < p.n; ++j) {
-    if (iv[j] != at) continue;
-    if (j < tid) return;
-    own += gv[j];
-  }
-  d[at] = from_f32<TO>(grad(sv) + own * p.itau);
+  if (own.first) d[at] = from_f32<TO>(grad(sv) + own.sum * p.itau);
 }
 
 // Short rows, four to a workgroup, a wave each without barriers; a class's list entries are added where the class lies in
-// registers.  (us, so / by a workgroup of one wave each: 20000 float32 rows of 100 classes 8.7 / 11.5, 20000 bf16 rows of
-// 300 12.3 / 15.2; 5000 bf16 rows of 1000 8.7 / 7.3.)
-static constexpr int WAVE_K = 512;
+// registers, one after the other.  (us, so / by a workgroup of one wave each: 20000 bf16 rows of 100 classes with 4 listed
+// 8.4 / 16.6, with 16 11.7 / 16.8, with 64 26.8 / 17.3; 20000 of 500 with 4 19.0 / 20.0, with 8 20.3 / 19.4, with 12
+// 22.9 / 19.6; 5000 of 1000 with one 8.7 / 7.3.)
+static constexpr int WAVE_K = 512, WAVE_LIST = 64;   // most classes; most entries times values a lane
 
 // Class i * 64 + lane of a row in registers, -inf behind the last.
 template <typename TI, int NV>
@@ -387,7 +424,7 @@ template <typename TI, typename TO>
 int score_grad_rows(const TI* logits, int64_t ld, int64_t M, int32_t K, const softmax_score_grads& q, TO* dlogits,
                     int64_t ldd, int32_t pad, hipStream_t stream) {
   const ScoreGradP p{ld, ldd, K, q.n, pad, LOG2E_F / q.temperature, 1.f / q.temperature, q.ids, q.dlogprob, q.dentropy};
-  if (K <= WAVE_K && q.n <= 64) {
+  if (K <= WAVE_K && q.n * cdiv(K, 64) <= WAVE_LIST) {
     auto wave = [&](auto nv) {
       BLSTM_LAUNCH("softmax_logprob_bwd_rows", (score_grad_wave_kernel<TI, TO, decltype(nv)::value>),
                    dim3((unsigned)cdiv(M, 4)), dim3(256), 0, stream, logits, dlogits, M, p);

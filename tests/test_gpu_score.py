@@ -342,6 +342,25 @@ def test_extreme_temperatures(gpu_lib, K):
         check(s.cuda(), some_ids(5, K, 3), 5, tau)
 
 
+@pytest.mark.parametrize("precision", ["fp32", "bf16"])
+@pytest.mark.parametrize("K,n", [(2, 64), (40, 64), (64, 65), (200, 17), (512, 9), (700, 64), (3000, 256), (9001, 130), (32768, 256), (40007, 200)])
+def test_gradients_of_lists_that_repeat(gpu_lib, K, n, precision):
+    """Few classes listed many times, the same one throughout, classes a power of two apart, ids that are none."""
+    g = torch.Generator().manual_seed(n)
+    s = (torch.randn(7, K, generator=g) * 2).to(TYPES[precision]).cuda()
+    ids = torch.randint(0, K, (7, n), generator=g, dtype=torch.int32)
+    ids[0] = K - 1
+    ids[1] = torch.arange(n) % 3 * (K // 2) % K
+    ids[2] = torch.arange(n).flip(0) % K
+    ids[3] = (1 << torch.arange(n) % 18) % K
+    ids[4, ::2] = -1
+    ids[4, 1::2] = K - 1
+    ids[5] = torch.where(torch.arange(n) % 2 == 0, K, -5 - torch.arange(n))
+    ids[6, n // 2:] = -1
+    check_grad(s, ids.cuda(), torch.randn(7, n, generator=g).cuda(), torch.randn(7, generator=g).cuda())
+    check_grad(s, ids.cuda(), torch.randn(7, n, generator=g).cuda(), None, 0.7)
+
+
 def test_many_rows_of_few_classes(gpu_lib):
     """More rows than 16 bits count, each by a wave."""
     M, K = 70001, 5
