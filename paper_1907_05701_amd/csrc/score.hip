@@ -83,6 +83,49 @@ __device__ __forceinline__ void add_row(RowStats& r, Row<TI, V, NV, T>& row) {
   if constexpr (V > 1) r.add(row.tail);
 }
 
+// The most likely classes of a row whose candidates are too many, or that has a NaN or +inf, read again: all above the
+// k-th largest of the threads' maxima, and of those that equal it the first, which are found soon where they are many.
+// (175 bf16 rows of 32000 classes, one all at -inf: 22 us, 239 with a search bit by bit for the last of them.)
+template <typename TI, int T, int C, typename F>
+__device__ __forceinline__ void most_likely(TopkLds<T, C>& l, const TI* s, int64_t m, const TopkP& p, F value) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, K = p.K;
+  uint32_t mx = 0;
+  each<TI, T>(s, K, [&](int, float v) { mx = max(mx, order_word(v)); });
+  __syncthreads();
+  l.tmax[tid] = mx;
+  if (tid == 0) l.count = 0;
+  const uint32_t t = kth_max<0>(l, p.k);
+  each<TI, T>(s, K, [&](int c, float v) {
+    if (order_word(v) > t) push(l, v, c);
+  });
+  __syncthreads();
+  int taken = (int)same(l.count);
+  if (taken > C) {
+    topk_any<TI, T, true>(l, s, m, p, value);
+    return;
+  }
+  const int n = max(taken, p.k);
+  __syncthreads();
+  for (int c0 = 0, par = 0; taken < p.k && c0 < K; c0 += T, par ^= 1) {
+    const int c = c0 + tid;
+    const float v = c < K ? to_f32(s[c]) : 0.f;
+    const bool tie = c < K && order_word(v) == t;
+    const uint64_t ties = __ballot(tie);
+    if (lane == 0) l.cnt[par][wave] = __popcll(ties);
+    __syncthreads();
+    int before = taken + __popcll(ties & ((1ull << lane) - 1));
+#pragma unroll
+    for (int w = 0; w < T / 64; ++w) {
+      const int there = (int)l.cnt[par][w];
+      before += w < wave ? there : 0;
+      taken += there;
+    }
+    if (tie && before < p.k) push(l, v, c);
+  }
+  __syncthreads();
+  rank(l, n, m, p, value);
+}
+
 template <typename TI, int T, int V, int NV, bool TOP>
 __global__ __launch_bounds__(T, (waves_of<TI, T, V, NV>())) void score_rows_kernel(
     const TI* __restrict__ logits, const ScoreP p) {
@@ -163,7 +206,7 @@ __global__ __launch_bounds__(T, (waves_of<TI, T, V, NV>())) void score_rows_kern
   if constexpr (TOP) {
     TopkP tp{p.ld, K, p.k, p.it2, p.top, nullptr, p.idx};
     const int n = (int)same(l.count);
-    if (same(!r.good()) || n > C) topk_any<TI, T, true>(l, s, m, tp, lp);
+    if (same(!r.good()) || n > C) most_likely<TI, T>(l, s, m, tp, lp);
     else rank(l, n, m, tp, lp);
   }
 }

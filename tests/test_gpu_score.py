@@ -141,6 +141,28 @@ def test_many_rows(gpu_lib, K, k, n, precision):
     check(s.to(t).cuda(), some_ids(1100, K, n), k, only=[*range(0, 1100, 37), 3, 500, 501, 700, 701, 702, 900, 1098, 1099])
 
 
+@pytest.mark.parametrize("precision", ["fp32", "bf16"])
+@pytest.mark.parametrize("K,k", [(300, 32), (4000, 20), (9001, 130), (32000, 8), (140001, 32)])
+def test_rows_of_many_ties(gpu_lib, K, k, precision):
+    """Fewer classes above the ties than are asked for, ties at the end of a row alone, at any place, beside NaN and infinities,
+    several levels of them, and more than fit above the threshold."""
+    s = torch.full((9, K), -3.0)
+    s[0, torch.arange(k // 2) * 7 % K] = torch.linspace(1, 2, k // 2)
+    s[1] = torch.arange(K) % 2 * -1.0
+    s[2, :] = -50.0 - torch.arange(K) % 64
+    s[2, K - 3 * k // 2:] = 1.0
+    s[3, [5, K - 1, K // 2]] = math.nan
+    s[4, [6, K - 2]] = math.inf
+    s[4, 7] = math.nan
+    s[5] = torch.arange(K) % 5 * 1.0
+    s[6, : K // 3] = -math.inf
+    s[6, K // 3: K // 3 + 3] = 4.0
+    s[7, :K - k // 2] = -math.inf
+    s[8] = (torch.arange(K) // 16) * 0.0
+    s[8, torch.randperm(K, generator=torch.Generator().manual_seed(3))[:K // 2]] = -0.0
+    check(s.to(TYPES[precision]).cuda(), some_ids(9, K, 2), k)
+
+
 def test_logits_far_from_zero(gpu_lib):
     """Only differences count: the same rows 1e4 and 1e6 away, where float32 still holds them."""
     g = torch.Generator().manual_seed(4)
