@@ -104,41 +104,46 @@ void int8_tile_kernel(const Int8P p) {
   for (int j = 0; j < FN; ++j) xs[j] = p.xs[min(m0 + wn * (BN / WN) + j * 16 + fr, p.M - 1)];
   if constexpr (std::is_same<TO, bf16>::value && FM % 2 == 0) {
     // two fragments' 16 channels side by side: rows of 16 lanes trade places, so that a lane stores 8 adjacent channels
-    // and an instruction 64 bytes of each token
-    const bool whole = p.N % 8 == 0 && p.ldy % 8 == 0 && ((uintptr_t)p.y & 15) == 0;
-    if (whole) {
+    // and an instruction 64 bytes of each token (at any alignment: 3153 x 4268 x 1024 23.5 us, 29.9 by four channels; x 4267 29.0 and 31.7)
 #pragma unroll
-      for (int i = 0; i < FM; i += 2) {
-        const int64_t n = n0 + wm * (BM / WM) + i * 16;
-        f32x4 w[2], b[2];
+    for (int i = 0; i < FM; i += 2) {
+      const int64_t n = n0 + wm * (BM / WM) + i * 16;
+      f32x4 w[2], b[2];
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+      for (int u = 0; u < 2; ++u)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int64_t c = min(n + u * 16 + 4 * fc + r, p.N - 1);   // channels past the last: any, dropped
-            w[u][r] = p.ws[c];
-            b[u][r] = p.bias ? p.bias[c] : 0.f;
-          }
-        const int64_t c = n + (fc & 1) * 16 + (fc >> 1) * 8;
+        for (int r = 0; r < 4; ++r) {
+          const int64_t c = min(n + u * 16 + 4 * fc + r, p.N - 1);   // channels past the last: any, dropped
+          w[u][r] = p.ws[c];
+          b[u][r] = p.bias ? p.bias[c] : 0.f;
+        }
+      const int64_t c = n + (fc & 1) * 16 + (fc >> 1) * 8;
 #pragma unroll
-        for (int j = 0; j < FN; ++j) {
-          uint32_t o[2][2];
+      for (int j = 0; j < FN; ++j) {
+        uint32_t o[2][2];
 #pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            bf16 v[4];
+        for (int u = 0; u < 2; ++u) {
+          bf16 v[4];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) v[r] = (bf16)int8_value(acc[i + u][j][r], scale_of(xs[j], w[u][r]), b[u][r]);
-            __builtin_memcpy(o[u], v, 8);
-          }
-          const auto lo = __builtin_amdgcn_permlane16_swap(o[0][0], o[1][0], false, false);
-          const auto hi = __builtin_amdgcn_permlane16_swap(o[0][1], o[1][1], false, false);
-          const int64_t m = m0 + wn * (BN / WN) + j * 16 + fr;
-          const i32x4 out{(int)lo[0], (int)hi[0], (int)lo[1], (int)hi[1]};
-          if (m < p.M && c < p.N) *(i32x4*)((bf16*)p.y + m * p.ldy + c) = out;
+          for (int r = 0; r < 4; ++r) v[r] = (bf16)int8_value(acc[i + u][j][r], scale_of(xs[j], w[u][r]), b[u][r]);
+          __builtin_memcpy(o[u], v, 8);
+        }
+        const auto lo = __builtin_amdgcn_permlane16_swap(o[0][0], o[1][0], false, false);
+        const auto hi = __builtin_amdgcn_permlane16_swap(o[0][1], o[1][1], false, false);
+        const int64_t m = m0 + wn * (BN / WN) + j * 16 + fr;
+        const i32x4 out{(int)lo[0], (int)hi[0], (int)lo[1], (int)hi[1]};
+        bf16* y = (bf16*)p.y + m * p.ldy + c;
+        if (m < p.M && c + 8 <= p.N) __builtin_memcpy(y, &out, 16);
+        else if (m < p.M && c < p.N) {
+          bf16 v[8];
+          __builtin_memcpy(v, &out, 16);
+#pragma unroll
+          for (int r = 0; r < 8; ++r)
+            if (c + r < p.N) y[r] = v[r];
         }
       }
-      return;
     }
+    return;
   }
 #pragma unroll
   for (int i = 0; i < FM; ++i)
