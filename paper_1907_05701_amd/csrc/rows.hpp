@@ -206,16 +206,16 @@ __device__ __forceinline__ uint32_t kth_word(const uint32_t (&w)[NW], int k) {
   return t;
 }
 static constexpr int FOLD = 64;   // largest k for groups
-// (of one wave, behind a barrier)
+// (of one wave, behind a barrier; fold: largest k for groups here)
 template <int LOW, int T, int C, int N>
-__device__ __forceinline__ uint32_t kth_search(const TopkLds<T, C, N>& l, int k) {
+__device__ __forceinline__ uint32_t kth_search(const TopkLds<T, C, N>& l, int k, int fold = FOLD) {
   const int lane = threadIdx.x & 63;
   constexpr int NW = N / 64;
   uint32_t w[NW];
 #pragma unroll
   for (int i = 0; i < NW; ++i) w[i] = l.tmax[i * 64 + lane];
   if constexpr (NW > 2) {
-    if (k <= FOLD) {
+    if (k <= fold) {
       uint32_t g[2] = {w[0], w[1]};
 #pragma unroll
       for (int i = 2; i < NW; ++i) g[i & 1] = max(g[i & 1], w[i]);

@@ -289,6 +289,16 @@ def test_head(gpu_lib, M, P, K, n, k, tau, precision):
     check_head(x, w, ws, None, ids, k, tau)
 
 
+@pytest.mark.parametrize("M", [3, 40, 70])
+@pytest.mark.parametrize("K,k", [(319, 30), (319, 8), (512, 32), (513, 32), (1000, 30), (1000, 64), (1000, 200), (2100, 65), (8192, 64), (8300, 64)])
+def test_head_of_few_classes_and_many_of_them(gpu_lib, M, K, k):
+    """Groups of classes fewer than the likely ones, or hardly more; logits that tie."""
+    x, w, ws, bias, ids = head_case(M, 64, K, 2, "bf16")
+    check_head(x, w, ws, bias, ids, k)
+    w[:K // 2], ws[:K // 2] = w[:1], ws[0]
+    check_head(x, w, ws, None, None, k)
+
+
 def test_head_of_the_paper(gpu_lib):
     x, w, ws, bias, ids = head_case(40, 256, 32000, 2, "bf16")
     check_head(x, w, ws, bias, ids, 8)
