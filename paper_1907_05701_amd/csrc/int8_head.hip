@@ -32,6 +32,10 @@ static constexpr float FLOOR = -1e30f, START = 0.5f * FLOOR;
 // its branch in most tiles, one that follows far behind makes T large and its rounding with it (30: the entropy's
 // error 1.8e-6).
 static constexpr float SLACK = 4.f;
+// Largest reference, as an exponent, that the sums are good for: its rounding, at most 2 below that, shifts all of a frame's
+// exponents alike.  That of larger ones could reach float32's ends, and logits that large are no masks;
+// such frames are for the second pass alone.
+static constexpr float REF_MAX = 0x1p26f;
 
 struct HeadP {
   const void* x;           // tokens, where the first pass quantises them itself
@@ -344,13 +348,13 @@ struct HeadLds {
 struct HeadLogProb {
   float rc, l2z, it2, itau;
   __device__ __forceinline__ float operator()(float v) const {
-    // far out the exponent could overflow, and what it is compared with does not count
-    return fabsf(v) > 1e30f ? v * itau : (fmaf(v, it2, -rc) - l2z) * LN2_F;
+    // a mask's exponent could overflow; the reference, at most 2^26 / it2 <= 2^-24 of it, does not count beside it
+    return v < -1e30f ? v * itau : (fmaf(v, it2, -rc) - l2z) * LN2_F;
   }
 };
 
-// Any row, its logits computed again in every pass: one with a NaN or infinities, with fewer than k classes
-// above FLOOR, or with too many that reach the threshold.
+// Any row, its logits computed again in every pass: one with a NaN or infinities, with a reference beyond REF_MAX, with
+// fewer than k classes above FLOOR, or with too many that reach the threshold.
 __device__ __forceinline__ void head_any(HeadLds& h, const Logit& logit, const HeadP& p, const HeadOut& o, int64_t m) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, K = p.K;
   float mx = -INFINITY;
@@ -507,7 +511,7 @@ __global__ __launch_bounds__(FT, 6) void int8_head_finish_kernel(const HeadP p, 
   const float rc = h.buf[0][0], z = h.buf[0][1], t = h.buf[0][2];
   // (a NaN fails all; a temperature beyond that would bring FLOOR's classes back in, and one below about 2e-9, where START's
   // exponent is -inf, leaves t a NaN)
-  if (same(!(z > 0.f && z < INFINITY && fabsf(t) < INFINITY && p.it2 > 1e-15f))) {
+  if (same(!(z > 0.f && z < INFINITY && fabsf(t) < INFINITY && fabsf(rc) < REF_MAX && p.it2 > 1e-15f))) {
     head_any(h, logit, p, o, m);
     return;
   }
