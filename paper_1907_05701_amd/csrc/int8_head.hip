@@ -28,6 +28,9 @@ __host__ __device__ constexpr int group_tiles(int fw) { return fw == 4 ? 1 : 2; 
 // Biases below FLOOR count as FLOOR in the first pass, and sums start from a reference above it, so that such a class
 // adds 0; rows that have no other, or not k others, are for the second pass alone.
 static constexpr float FLOOR = -1e30f, START = 0.5f * FLOOR;
+// That holds as long as no product comes near FLOOR: with scales below SCALE_MAX it is at most 2^24 * 10^20.  A class of a
+// larger scale is a NaN in the first pass, and leaves every frame to the second; so does a frame's own scale its frame.
+static constexpr float SCALE_MAX = 1e10f;
 // How far above its reference a lane's largest exponent may get: a reference that follows every new maximum takes
 // its branch in most tiles, one that follows far behind makes T large and its rounding with it (30: the entropy's
 // error 1.8e-6).
@@ -110,7 +113,7 @@ __global__ __launch_bounds__(256, head_per_cu<KS>()) void int8_head_kernel(const
     if (wid == 1) next = c < rows ? (p.bias ? p.bias[tile0 * CT + c] : 0.f) : FLOOR;
   };
   auto put = [&](int j) {
-    if (wid < 2) *(float*)(lds + (j & 1) * STAGE + TILE + wid * 256 + lane * 4) = wid ? fmax_nan(next, FLOOR) : next;
+    if (wid < 2) *(float*)(lds + (j & 1) * STAGE + TILE + wid * 256 + lane * 4) = wid ? fmax_nan(next, FLOOR) : fabsf(next) < SCALE_MAX ? next : NAN;
   };
   // a tile's rows end with the last class: what lies behind it, and behind a row's columns, reads as zeros
   uint32_t off[LOADS];
@@ -353,8 +356,8 @@ struct HeadLogProb {
   }
 };
 
-// Any row, its logits computed again in every pass: one with a NaN or infinities, with a reference beyond REF_MAX, with
-// fewer than k classes above FLOOR, or with too many that reach the threshold.
+// Any row, its logits computed again in every pass: one with a NaN or infinities, with a scale beyond SCALE_MAX or a
+// reference beyond REF_MAX, with fewer than k classes above FLOOR, or with too many that reach the threshold.
 __device__ __forceinline__ void head_any(HeadLds& h, const Logit& logit, const HeadP& p, const HeadOut& o, int64_t m) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, K = p.K;
   float mx = -INFINITY;
@@ -495,7 +498,8 @@ __global__ __launch_bounds__(FT, 6) void int8_head_finish_kernel(const HeadP p, 
     z = wave_sum(z);
     t = wave_sum(t);
     if (lane == 0) {
-      h.buf[0][0] = rc;
+      // (as a term of the condition behind the barrier it costs 27 spilled registers: 2688 frames 73 us, 66 so)
+      h.buf[0][0] = logit.xs < SCALE_MAX ? rc : INFINITY;
       h.buf[0][1] = z;
       h.buf[0][2] = t;
     }

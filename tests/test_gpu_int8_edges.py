@@ -52,3 +52,26 @@ def test_head_of_masks_below_large_logits(gpu_lib, M, top):
     b[30:60], b[60:] = -1.1e30, torch.finfo(torch.float32).min / 4
     b[5] = top
     t8.check_head(x, w, ws, b, ids, 70)
+
+
+@pytest.mark.parametrize("M", [1, 6, 20, 40, 150])
+def test_head_of_masks_that_products_lift(gpu_lib, M):
+    """A bias of -2e30 with a product of exactly 10^30, or of more, or of -3e38, beside ordinary classes: the class is at
+    the sum of both."""
+    x, w, ws, bias, ids = t8.head_case(M, 64, 900, 2, "fp32")
+    x[:, 0], x[:, 1] = 127.0, 1.0                       # integers are the values themselves: a scale of 1
+    x[:, 2:] = torch.round(x[:, 2:])
+    ws = ws / 1000                                      # the others' logits are next to their biases
+    ids[:, 0] = 700
+    w[700] = 0
+    w[700, 1] = 1                                       # the sum is 1, the product the scale
+    assert bool((t8.quantize(x)[1] == 1.0).all())
+    for scale in (1e30, 1.0000001e30, 2e30, 1.7e38, -3e38, 1e10):
+        for mask in (-2e30, -1.0000001e30, -1e38, -1e30, float("-inf")):
+            s, b = ws.clone(), bias.clone()
+            s[700], b[700] = scale, mask
+            t8.check_head(x, w, s, b, ids, 9)
+    x = x * 1e12                                        # a scale of 10^12 for the tokens
+    s, b = ws * 1e-12, bias.clone()
+    s[700], b[700] = 1e18, -2e30                        # the product is 10^30 again
+    t8.check_head(x, w, s, b, ids, 9)
