@@ -37,10 +37,13 @@ class Int8Head:
 
     def _buffers(self, M):
         """A workspace for M frames: one for both calls, which follow each other on a stream.
-        Smaller ones stay: a captured graph may hold them."""
+        Smaller ones stay, since a captured graph may hold them; each is at least twice
+        the one before, so that they are less than the newest together."""
         n = max(bd.int8_linear_ws_bytes(M, self.w_l.shape[1]), bd.int8_logprob_ws_bytes(M, self.K, self.w_s.shape[1]))
         if self.ws is None or self.ws.numel() < n:
-            self._older.append(self.ws)
+            if self.ws is not None:
+                self._older.append(self.ws)
+                n = max(n, 2 * self.ws.numel())
             self.ws = torch.empty(n, dtype=torch.uint8, device=self.device)
         return self.ws
 
