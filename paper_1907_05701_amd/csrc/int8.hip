@@ -325,15 +325,25 @@ extern "C" int int8_linear_rows(const void* x, int64_t ldx, int64_t M, int32_t K
 // ---------------------------------------------------------------------------
 // The head (int8_head.hip); tokens of more columns than that holds: logits of rows at a time, scored.
 // ---------------------------------------------------------------------------
+// Frames that the head takes at a time: equal parts, of at most about 180 MB of group maxima (K / 4 bytes a frame) and tokens.
+static int64_t head_frames(int64_t M, int64_t K, int64_t Kw) {
+  const int64_t most = (180 << 20) / (Kw + 16 * cdiv(K, 64) + 64);
+  return cdiv(M, cdiv(M, most));
+}
 static int64_t logit_rows(int64_t M, int64_t K) { return std::min(M, std::max<int64_t>(64, (180 << 20) / (4 * rup(K, 4)))); }
 
 extern "C" int int8_logprob_ws_bytes(int64_t M, int32_t K, int32_t Kw, size_t* bytes) {
   const int rc = check_sizes("int8_logprob_ws_bytes", M, K, Kw);
   if (rc) return rc;
   if (K > SOFTMAX_MAX_CLASSES || Kw > INT8_MAX_K) return blstm_fail(BLSTM_EUNSUPPORTED, "int8_logprob_ws_bytes: too many classes or columns");
-  if (bytes)
-    *bytes = int8_head_fits(Kw) ? int8_head_bytes(M, K, (int32_t)rup(Kw, 16))
-                                : tokens_bytes(M, rup(Kw, 16)) + (size_t)logit_rows(M, K) * rup(K, 4) * 4;
+  if (!bytes) return BLSTM_OK;
+  const int32_t cols = (int32_t)rup(Kw, 16);
+  if (int8_head_fits(Kw)) {
+    const int64_t n = head_frames(M, K, cols);   // (the last part may be shorter, and its ranges of classes more)
+    *bytes = std::max(int8_head_bytes(n, K, cols), int8_head_bytes(M - (cdiv(M, n) - 1) * n, K, cols));
+  } else {
+    *bytes = tokens_bytes(M, cols) + (size_t)logit_rows(M, K) * rup(K, 4) * 4;
+  }
   return BLSTM_OK;
 }
 
@@ -347,10 +357,17 @@ extern "C" int int8_logprob_rows(const void* x, int64_t ldx, int64_t M, int32_t 
   int8_t* q = (int8_t*)ws;
   float* scale = (float*)((char*)ws + rup(M * Kw, 256));
   char* rest = (char*)ws + tokens_bytes(M, Kw);
-  if (int8_head_fits(Kw))
-    return precision == BLSTM_BF16
-               ? int8_head((const bf16*)x, ldx, M, P, w, ldw, w_scale, K, Kw, bias, *scores, (char*)ws, stream)
-               : int8_head((const float*)x, ldx, M, P, w, ldw, w_scale, K, Kw, bias, *scores, (char*)ws, stream);
+  if (int8_head_fits(Kw)) {
+    const int64_t step = head_frames(M, K, Kw);
+    for (int64_t r0 = 0; !rc && r0 < M; r0 += step) {
+      const int64_t n = std::min(step, M - r0);
+      const softmax_scores sc = scores_from(*scores, r0);
+      rc = precision == BLSTM_BF16
+               ? int8_head((const bf16*)x + r0 * ldx, ldx, n, P, w, ldw, w_scale, K, Kw, bias, sc, (char*)ws, stream)
+               : int8_head((const float*)x + r0 * ldx, ldx, n, P, w, ldw, w_scale, K, Kw, bias, sc, (char*)ws, stream);
+    }
+    return rc;
+  }
   rc = int8_quantize_rows(x, ldx, M, P, precision, q, Kw, Kw, scale, stream);
   float* logits = (float*)rest;
   const int64_t ld = rup(K, 4), step = logit_rows(M, K);

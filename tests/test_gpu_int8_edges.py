@@ -75,3 +75,39 @@ def test_head_of_masks_that_products_lift(gpu_lib, M):
     s, b = ws * 1e-12, bias.clone()
     s[700], b[700] = 1e18, -2e30                        # the product is 10^30 again
     t8.check_head(x, w, s, b, ids, 9)
+
+
+def rows_of(o, at):
+    return {n: v if v is None else v[at] for n, v in o.items()}
+
+
+def check_rows(o, at, x, w, ws, bias, ids, k):
+    """Rows `at` of the head's answers, as check_head does."""
+    o, x, ids = rows_of(o, at), x[at], ids[at]
+    q, xs = t8.sm.quantize(x.float().cpu().numpy())
+    rows = torch.from_numpy(t8.sm.linear(q, xs, w[:, :x.shape[1]].cpu().numpy(), ws.cpu().numpy(), bias.cpu().numpy())).double()
+    lps, orders = [t8.sm.log_probs(r, 1.0) for r in rows], [t8.sm.order(r)[:k] for r in rows]
+    t8.near(o["entropy"], torch.stack([t8.sm.entropy(r, 1.0) for r in rows]))
+    t8.near(o["logprob"], torch.stack([t8.sm.listed(lp, i) for lp, i in zip(lps, ids.cpu())]))
+    assert torch.equal(o["idx"].cpu().long(), torch.stack(orders))
+    t8.near(o["top"], torch.stack([lp[i] for lp, i in zip(lps, orders)]))
+
+
+@pytest.mark.parametrize("precision", ["fp32", "bf16"])
+def test_head_of_more_frames_than_a_part(gpu_lib, precision):
+    """Two parts, the second one shorter: every frame has its own list and answers.  (A part holds at most
+    180 * 2^20 / (32 + 16 * 4096 + 64) = 2875 frames of 262144 classes and 32 columns.)"""
+    from paper_1907_05701_amd import binding as bd
+    M, K, k = 5701, bd.SOFTMAX_MAX_CLASSES, 3
+    x, w, ws, bias, ids = t8.head_case(M, 20, K, 2, precision)
+    n = -(-M // 2)
+    assert bd.int8_logprob_ws_bytes(M, K, 32) < M * K // 4
+    wide = torch.full((M, 27), 1e9, dtype=x.dtype, device="cuda")
+    wide[:, 4:24] = x
+    o = t8.head(wide[:, 4:24], w, ws, bias, ids, k)
+    for r0 in range(0, M, n):
+        part = t8.head(x[r0:r0 + n], w, ws, bias, ids[r0:r0 + n], k)
+        torch.cuda.synchronize()
+        for name, v in part.items():
+            assert torch.equal(v, o[name][r0:r0 + n]), (name, r0)
+    check_rows(o, torch.tensor([0, n - 1, n, M - 1]), x, w, ws, bias, ids, k)

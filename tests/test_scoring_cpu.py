@@ -161,3 +161,13 @@ def test_tensors_have_to_be_on_the_gpu():
         bd.int8_linear(i, torch.zeros(4), i, torch.zeros(4), f)
     with pytest.raises(ValueError):
         bd.int8_linear_rows(f, i, torch.zeros(4), torch.zeros(4, 4), torch.zeros(1 << 16, dtype=torch.uint8))
+
+
+def test_head_workspaces_are_bounded():
+    """Frames past a part of about 180 MB are taken in turn."""
+    for M in (1, 2688, 30000, 1 << 20, (1 << 22) - 1):
+        for K in (100, 9001, 32000, 1 << 18):
+            if (M + 127) // 128 * ((K + 127) // 128) >= 1 << 22:
+                continue   # refused
+            for Kw in (16, 256, 1024):
+                assert bd.int8_logprob_ws_bytes(M, K, Kw) < 200 << 20, (M, K, Kw)
