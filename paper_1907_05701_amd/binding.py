@@ -258,6 +258,8 @@ def blstm_timing_end(cap: int = 64) -> dict:
 # to the library: a ValueError names the argument.
 def _on(x):
     """The device index the call runs on, from its first tensor."""
+    if x is None:
+        raise ValueError("the call's first tensor is required")
     dev = x.get_device()
     if dev < 0:
         raise ValueError("tensors must be on the GPU")
@@ -627,6 +629,8 @@ def _ints(name, q, rows, dev):
 
 def _floats(name, x, dev):
     """(address, row pitch, rows, columns, precision) of rows of bfloat16 or float32."""
+    if x is None:
+        raise ValueError(f"{name} is required")
     shape, t = x.shape, x.dtype
     if len(shape) != 2 or (t is not torch.bfloat16 and t is not torch.float32):
         raise ValueError(f"{name} must be bfloat16 or float32 rows: got {t} {tuple(shape)}")

@@ -111,3 +111,10 @@ def test_head_of_more_frames_than_a_part(gpu_lib, precision):
         for name, v in part.items():
             assert torch.equal(v, o[name][r0:r0 + n]), (name, r0)
     check_rows(o, torch.tensor([0, n - 1, n, M - 1]), x, w, ws, bias, ids, k)
+
+
+def test_a_product_needs_its_output(gpu_lib):
+    from paper_1907_05701_amd import binding as bd
+    q, s = torch.zeros(4, 64, dtype=torch.int8, device="cuda"), torch.zeros(4, device="cuda")
+    with pytest.raises(ValueError, match="y is required"):
+        bd.int8_linear(q, s, q, s, None)

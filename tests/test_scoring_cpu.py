@@ -171,3 +171,19 @@ def test_head_workspaces_are_bounded():
                 continue   # refused
             for Kw in (16, 256, 1024):
                 assert bd.int8_logprob_ws_bytes(M, K, Kw) < 200 << 20, (M, K, Kw)
+
+
+@pytest.mark.parametrize("call", ["softmax_logprob_rows", "softmax_logprob_bwd_rows", "int8_quantize_rows", "int8_linear",
+                                  "int8_linear_rows", "int8_logprob_rows", "softmax_topk_rows"])
+def test_the_first_tensor_is_required(call):
+    n = {"softmax_logprob_rows": 0, "softmax_logprob_bwd_rows": 1, "int8_quantize_rows": 2, "int8_linear": 4,
+         "int8_linear_rows": 4, "int8_logprob_rows": 3, "softmax_topk_rows": 2}[call]
+    with pytest.raises(ValueError, match="required"):
+        getattr(bd, call)(None, *[None] * n)
+
+
+def test_rows_that_are_not_there():
+    """int8_linear takes its sizes from y."""
+    for name in ("x", "y", "logits"):
+        with pytest.raises(ValueError, match=f"{name} is required"):
+            bd._floats(name, None, 0)
