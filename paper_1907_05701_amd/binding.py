@@ -311,7 +311,7 @@ def _call(fn, dev, stream, *args):
     on = getattr(stream, "device", None)
     if on is not None and on.index != dev:   # its kernels would reach for another device's memory
         raise ValueError(f"the stream is on {on}, the tensors are on cuda:{dev}")
-    if dev != torch._C._cuda_getDevice():   # (initialised: a tensor lies on it)
+    if dev != torch.cuda.current_device():
         with torch.cuda.device(dev):
             return _call(fn, dev, stream, *args)
     # the handle alone: a Stream object costs more than the launch's other arguments together

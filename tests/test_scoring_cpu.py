@@ -187,3 +187,12 @@ def test_rows_that_are_not_there():
     for name in ("x", "y", "logits"):
         with pytest.raises(ValueError, match=f"{name} is required"):
             bd._floats(name, None, 0)
+
+
+def test_calls_ask_for_the_device_by_torch_s_public_name(monkeypatch):
+    """With nothing private to find it by, a call reaches the library, which refuses these arguments."""
+    monkeypatch.delattr(torch._C, "_cuda_getDevice", raising=False)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    stream = type("Stream", (), {"cuda_stream": 0, "device": torch.device("cuda", 0)})()
+    with pytest.raises(bd.BlstmError):
+        bd._call("int8_quantize_rows", 0, stream, None, 64, 4, 64, 1, PTR, 64, 64, PTR)
