@@ -106,7 +106,6 @@ struct Int8FewP {
   int64_t ldx;
   int K, cols;   // columns of x, p.K those of the weights; in LDS
 };
-static constexpr int FEW_COLS = 4096;           // of a token in LDS
 // Of all tokens, whom every workgroup quantises: 64 tokens of 1024 take 13.4 us in one launch, and 4.5 + 5.9 in two.
 static constexpr int64_t FEW_VALUES = 1 << 15;
 template <typename TO, int FN, int NW, int NV>
@@ -157,37 +156,30 @@ __global__ __launch_bounds__(NW * 64) void int8_few_tokens_kernel(const Int8FewP
 }
 static int few_fragments(int64_t M) { return M <= 16 ? 1 : M <= 32 ? 2 : 4; }   // of 16 tokens
 static bool few_tokens_ok(int64_t M, int32_t Kw) {
-  return M <= 64 && Kw <= FEW_COLS && 16 * few_fragments(M) * rup(Kw, 64) <= FEW_VALUES;
+  return M <= 64 && 16 * few_fragments(M) * rup(Kw, 64) <= FEW_VALUES;
+}
+// NV vectors a lane hold a token; longer ones take twice as many, up to the longest that few_tokens_ok lets pass.
+template <typename TO, int FN, int NW, int NV = 1>
+static void few_tokens(const Int8FewP& a, hipStream_t s) {
+  constexpr int COLS = NV * 64 * Vec16<TO>::n, MOST = FEW_VALUES / (16 * FN);
+  if constexpr (COLS < MOST) {
+    if (a.cols > COLS) return few_tokens<TO, FN, NW, 2 * NV>(a, s);
+  }
+  auto kernel = int8_few_tokens_kernel<TO, FN, NW, NV>;
+  constexpr size_t most = FEW_VALUES + 64 * 16;
+  const size_t bytes = std::max<size_t>((size_t)rup(a.p.M, 16) * (a.cols + 16), NW * FN * 1024);
+  static std::atomic<uint64_t> raised{0};
+  kc_raise_lds_limit((const void*)kernel, most, raised);
+  BLSTM_LAUNCH("int8_linear_few", kernel, dim3((unsigned)cdiv(a.p.N, 16)), dim3(NW * 64), bytes, s, a);
 }
 template <typename TO>
-static void few_tokens(Int8FewP a, hipStream_t s) {
-  constexpr int V = Vec16<TO>::n;
+static void few_tokens_rows(Int8FewP a, hipStream_t s) {
   a.cols = (int)rup(a.p.K, 64);
-  auto launch = [&](auto fn, auto nw, auto nv) {
-    constexpr int FN = decltype(fn)::value, NW = decltype(nw)::value, NV = decltype(nv)::value;
-    if constexpr (16 * FN * (NV / 2 * 64 * V + 64) <= FEW_VALUES) {   // (the fewest columns that come here)
-      auto kernel = int8_few_tokens_kernel<TO, FN, NW, NV>;
-      constexpr size_t most = FEW_VALUES + 64 * 16;
-      const size_t bytes = std::max<size_t>((size_t)rup(a.p.M, 16) * (a.cols + 16), NW * FN * 1024);
-      static std::atomic<uint64_t> raised{0};
-      kc_raise_lds_limit((const void*)kernel, most, raised);
-      BLSTM_LAUNCH("int8_linear_few", kernel, dim3((unsigned)cdiv(a.p.N, 16)), dim3(NW * 64), bytes, s, a);
-    }
-  };
-#define INT(n) std::integral_constant<int, n>{}
-  auto columns = [&](auto fn, auto nw) {
-    if (a.cols <= 64 * V) launch(fn, nw, INT(1));
-    else if (a.cols <= 2 * 64 * V) launch(fn, nw, INT(2));
-    else if (a.cols <= 4 * 64 * V) launch(fn, nw, INT(4));
-    else if (a.cols <= 8 * 64 * V) launch(fn, nw, INT(8));
-    else launch(fn, nw, INT(FEW_COLS / (64 * V)));
-  };
   switch (few_fragments(a.p.M)) {
-    case 1: return columns(INT(1), INT(4));
-    case 2: return columns(INT(2), INT(8));
-    default: return columns(INT(4), INT(8));
+    case 1: return few_tokens<TO, 1, 4>(a, s);
+    case 2: return few_tokens<TO, 2, 8>(a, s);
+    default: return few_tokens<TO, 4, 8>(a, s);
   }
-#undef INT
 }
 
 template <typename TO>
@@ -311,8 +303,8 @@ extern "C" int int8_linear_rows(const void* x, int64_t ldx, int64_t M, int32_t K
     Int8FewP a{};
     a.p.w = w; a.p.ldw = ldw; a.p.ldy = ldy; a.p.M = M; a.p.N = N; a.p.K = Kw; a.p.ws = w_scale; a.p.bias = bias; a.p.y = y;
     a.x = x; a.ldx = ldx; a.K = K;
-    if (precision == BLSTM_BF16) few_tokens<bf16>(a, stream);
-    else few_tokens<float>(a, stream);
+    if (precision == BLSTM_BF16) few_tokens_rows<bf16>(a, stream);
+    else few_tokens_rows<float>(a, stream);
     return blstm_check_launch(fn);
   }
   int8_t* q = (int8_t*)ws;
