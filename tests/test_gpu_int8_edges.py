@@ -118,3 +118,20 @@ def test_a_product_needs_its_output(gpu_lib):
     q, s = torch.zeros(4, 64, dtype=torch.int8, device="cuda"), torch.zeros(4, device="cuda")
     with pytest.raises(ValueError, match="y is required"):
         bd.int8_linear(q, s, q, s, None)
+
+
+@pytest.mark.parametrize("precision", ["fp32", "bf16"])
+def test_head_of_long_tokens_in_parts(gpu_lib, precision):
+    """More than 1024 columns, whose logits go through memory, 180 * 2^20 / 400000 = 471 frames of 100000 classes at a
+    time: bit by bit what the product and the rows' operator give in turn."""
+    from paper_1907_05701_amd import binding as bd
+    M, K, k = 500, 100000, 4
+    x, w, ws, bias, ids = t8.head_case(M, 1030, K, 2, precision)
+    o = t8.head(x, w, ws, bias, ids, k)
+    logits = t8.linear_rows(x.float(), w, ws, bias)
+    want = {n: torch.empty_like(v) for n, v in o.items()}
+    bd.softmax_logprob_rows(logits, ids=ids, **want)
+    torch.cuda.synchronize()
+    for name, v in want.items():
+        assert torch.equal(v, o[name]), name
+    check_rows(o, torch.tensor([0, 470, 471, M - 1]), x, w, ws, bias, ids, k)
