@@ -88,9 +88,9 @@ __device__ __forceinline__ int head_slot(int c, int r) {
 // KS: most 64-column steps; 16 FN frames a wave; FW waves side by side along the
 // frames, the other 4 / FW along the classes of a tile.  TI: tokens of this type are quantised here, by every workgroup
 // for itself (a launch less), and left for the second pass by the first range's; void: their integers lie in memory.
-template <int KS> constexpr int head_per_cu() { return KS > 8 ? 1 : KS > 4 ? 2 : 3; }   // workgroups
+constexpr int head_per_cu(int ks) { return ks > 8 ? 1 : ks > 4 ? 2 : 3; }   // workgroups, by their registers
 template <int KS, int FN, int FW, typename TI>
-__global__ __launch_bounds__(256, head_per_cu<KS>()) void int8_head_kernel(const HeadP p) {
+__global__ __launch_bounds__(256, head_per_cu(KS)) void int8_head_kernel(const HeadP p) {
   constexpr int WC = 4 / FW, NI = 4 / WC, TG = group_tiles(FW), NCH = KS * 4, TILE = CT * KS * 64, STAGE = TILE + 512;
   constexpr int LOADS = TILE / 1024 / 4;   // of a wave
   extern __shared__ __attribute__((aligned(1024))) char lds[];
@@ -608,21 +608,33 @@ __global__ __launch_bounds__(FT, 6) void int8_head_finish_kernel(const HeadP p, 
 // Host side.
 // ---------------------------------------------------------------------------
 struct HeadPlan {
-  int fn, fw, ks;                 // frames / 16 of a wave, waves along the frames, column steps
+  int fn, fw, ks;                 // frames / 16 of a wave, waves along the frames, most column steps
   int nf, ranges, per, ngroup;
   size_t stats, gmax, bytes;      // behind the tokens
 };
 static constexpr int HEAD_MAX_STEPS = 16;
 
+// Whether the first pass quantises its tokens itself: where they are few, and beside two stages of long rows there is room.
+static constexpr bool quantised_here(int fw, int ks) { return fw == 1 || (fw == 2 && ks <= 8); }
+static constexpr size_t head_lds(int fn, int fw, int ks) {
+  return 2 * (CT * ks * 64 + 512) + (quantised_here(fw, ks) ? 16 * fn * fw * (ks * 64 + 16 + 4) : 0);
+}
+// Workgroups of the first pass that run at a time.  (512 columns of 17 to 64 frames have LDS for one a CU.  us, planned for
+// one / for the two that the registers hold: 17 frames of 45000 classes 28.0 / 34.6, of 131072 43.0 / 50.8; 64 frames 40.2 / 53.3
+// and 50.0 / 65.8.)
+static int head_slots(int fn, int fw, int ks) {
+  return 256 * (int)std::min<size_t>(head_per_cu(ks), 160 * 1024 / head_lds(fn, fw, ks));
+}
+
 static HeadPlan head_plan(int64_t M, int32_t K, int32_t Kw) {
   HeadPlan h{};
-  h.ks = (int)cdiv(Kw, 64);
+  h.ks = Kw <= 64 ? 1 : Kw <= 128 ? 2 : Kw <= 256 ? 4 : Kw <= 512 ? 8 : HEAD_MAX_STEPS;
   h.fn = h.ks > 8 || M <= 16 ? 1 : 2;
   const int frames = 16 * h.fn;
   h.fw = M <= frames ? 1 : M <= 2 * frames ? 2 : 4;
   h.nf = (int)cdiv(M, frames * h.fw);
   const int tg = group_tiles(h.fw);
-  const int64_t units = cdiv(K, CT * tg), slots = 256 * (h.ks > 8 ? 1 : h.ks > 4 ? 2 : 3);
+  const int64_t units = cdiv(K, CT * tg), slots = head_slots(h.fn, h.fw, h.ks);
   // as many ranges as take least: whole rounds of the chip, each as long as a range and its start
   int64_t best = -1, per = 1;
   for (int64_t r = 1; r <= units && r <= std::max<int64_t>(1, 2 * slots / h.nf); ++r) {
@@ -641,8 +653,6 @@ static HeadPlan head_plan(int64_t M, int32_t K, int32_t Kw) {
   return h;
 }
 
-// Whether the first pass quantises its tokens itself: where they are few, and beside two stages of long rows there is room.
-static constexpr bool quantised_here(int fw, int ks) { return fw == 1 || (fw == 2 && ks <= 8); }
 bool int8_head_fits(int32_t Kw) { return cdiv(Kw, 64) <= HEAD_MAX_STEPS; }
 static size_t ints_bytes(int64_t M, int32_t Kw) { return (size_t)(rup(M * Kw, 256) + rup(M * 4, 256)); }
 size_t int8_head_bytes(int64_t M, int32_t K, int32_t Kw) { return ints_bytes(M, Kw) + head_plan(M, K, Kw).bytes; }
@@ -662,7 +672,7 @@ int int8_head(const TI* x, int64_t ldx, int64_t M, int32_t P, const int8_t* w, i
   auto launch = [&](auto ks, auto fn, auto fw) {
     constexpr int KS = decltype(ks)::value, FN = decltype(fn)::value, FW = decltype(fw)::value;
     constexpr bool here = quantised_here(FW, KS);
-    constexpr size_t bytes = 2 * (CT * KS * 64 + 512) + (here ? 16 * FN * FW * (KS * 64 + 16 + 4) : 0);
+    constexpr size_t bytes = head_lds(FN, FW, KS);
     auto kernel = int8_head_kernel<KS, FN, FW, typename std::conditional<here, TI, void>::type>;
     static_assert(bytes <= 160 * 1024, "LDS");
     if (!here) int8_quantize(x, ldx, M, P, p.q, Kw, Kw, p.xs, s);
@@ -680,11 +690,13 @@ int int8_head(const TI* x, int64_t ldx, int64_t M, int32_t P, const int8_t* w, i
     if (M <= 16) launch(ks, INT(1), INT(1));
     else waves(ks, INT(2));
   };
-  if (h.ks <= 1) columns(INT(1));
-  else if (h.ks <= 2) columns(INT(2));
-  else if (h.ks <= 4) columns(INT(4));
-  else if (h.ks <= 8) columns(INT(8));
-  else waves(INT(16), INT(1));
+  switch (h.ks) {
+    case 1: columns(INT(1)); break;
+    case 2: columns(INT(2)); break;
+    case 4: columns(INT(4)); break;
+    case 8: columns(INT(8)); break;
+    default: waves(INT(HEAD_MAX_STEPS), INT(1));
+  }
 #undef INT
   const int rc = blstm_check_launch("int8_head");
   if (rc) return rc;

@@ -135,3 +135,11 @@ def test_head_of_long_tokens_in_parts(gpu_lib, precision):
     for name, v in want.items():
         assert torch.equal(v, o[name]), name
     check_rows(o, torch.tensor([0, 470, 471, M - 1]), x, w, ws, bias, ids, k)
+
+
+@pytest.mark.parametrize("M,P", [(17, 512), (40, 300), (64, 512)])
+def test_head_of_some_frames_and_many_classes(gpu_lib, M, P):
+    x, w, ws, bias, ids = t8.head_case(M, P, 45000, 2, "bf16")
+    o = t8.head(x, w, ws, bias, ids, 7)
+    torch.cuda.synchronize()
+    check_rows(o, torch.tensor([0, 15, 16, M - 1]), x, w, ws, bias, ids, 7)

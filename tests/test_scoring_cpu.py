@@ -196,3 +196,13 @@ def test_calls_ask_for_the_device_by_torch_s_public_name(monkeypatch):
     stream = type("Stream", (), {"cuda_stream": 0, "device": torch.device("cuda", 0)})()
     with pytest.raises(bd.BlstmError):
         bd._call("int8_quantize_rows", 0, stream, None, 64, 4, 64, 1, PTR, 64, 64, PTR)
+
+
+@pytest.mark.parametrize("M", [17, 32, 64])
+def test_head_plans_for_the_workgroups_that_run_at_a_time(M):
+    """512 columns of few frames leave LDS for one workgroup a CU: 256 ranges of 131072 classes, 16 bytes a frame each,
+    beside tokens and group maxima (1024 pairs of tiles, 4 a wave along the classes)."""
+    waves = 4 if M <= 32 else 2
+    up = lambda n: -(-n // 256) * 256  # noqa: E731
+    most = up(M * 512) + up(M * 4) + up(M * 256 * 16) + up(M * 1024 * waves * 4 * 4)
+    assert bd.int8_logprob_ws_bytes(M, 131072, 512) <= most
