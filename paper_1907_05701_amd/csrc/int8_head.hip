@@ -35,10 +35,10 @@ static constexpr float SCALE_MAX = 1e10f;
 // its branch in most tiles, one that follows far behind makes T large and its rounding with it (30: the entropy's
 // error 1.8e-6).
 static constexpr float SLACK = 4.f;
-// Largest reference, as an exponent, that the sums are good for: its rounding, at most 2 below that, shifts all of a frame's
-// exponents alike.  That of larger ones could reach float32's ends, and logits that large are no masks;
-// such frames are for the second pass alone.
-static constexpr float REF_MAX = 0x1p26f;
+// Largest reference, as an exponent, that the sums are good for: its rounding, at most 8 below that, shifts all of a frame's
+// exponents alike.  That of larger ones could reach float32's ends, and logits that large are no masks; such
+// frames are for the second pass alone.
+static constexpr float REF_MAX = 0x1p28f;
 
 struct HeadP {
   const void* x;           // tokens, where the first pass quantises them itself
@@ -351,7 +351,7 @@ struct HeadLds {
 struct HeadLogProb {
   float rc, l2z, it2, itau;
   __device__ __forceinline__ float operator()(float v) const {
-    // a mask's exponent could overflow; the reference, at most 2^26 / it2 <= 2^-24 of it, does not count beside it
+    // a mask's exponent could overflow; the reference, at most 2^28 / it2 <= 2^-21.8 of it, does not count beside it
     return v < -1e30f ? v * itau : (fmaf(v, it2, -rc) - l2z) * LN2_F;
   }
 };

@@ -143,3 +143,22 @@ def test_head_of_some_frames_and_many_classes(gpu_lib, M, P):
     o = t8.head(x, w, ws, bias, ids, 7)
     torch.cuda.synchronize()
     check_rows(o, torch.tensor([0, 15, 16, M - 1]), x, w, ws, bias, ids, 7)
+
+
+@pytest.mark.parametrize("M", [1, 20, 40, 150])
+def test_head_on_either_side_of_the_largest_reference(gpu_lib, M):
+    """Largest exponents from 2^25 to 2^29, of one class, of many that tie, of all by their scales, and of ordinary logits at
+    small temperatures."""
+    x, w, ws, bias, ids = t8.head_case(M, 64, 900, 2, "fp32")
+    for top in (2.5e7, 6e7, 1.2e8, 1.8e8, 1.9e8, 3e8, -1.2e8, -1.9e8):
+        b = bias.clone()
+        b[:] = top
+        t8.check_head(x, w, ws, b, ids, 9)
+        t8.check_head(x, w * 0, ws, b, ids, 9)
+        if top > 0:
+            b[:-2] = -top
+            t8.check_head(x, w, ws, b, ids, 9)
+    for size in (1e6, 4e6, 1e7, 3e7):
+        t8.check_head(x, w, ws * size, bias, ids, 9)
+    for tau in (2.0 ** -19, 2.0 ** -21, 2.0 ** -23, 2.0 ** -25):
+        t8.check_head(x, w, ws, bias, ids, 9, tau)
