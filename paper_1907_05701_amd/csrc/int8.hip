@@ -106,7 +106,7 @@ struct Int8FewP {
   int64_t ldx;
   int K, cols;   // columns of x, p.K those of the weights; in LDS
 };
-// Of all tokens, whom every workgroup quantises: 64 tokens of 1024 take 13.4 us in one launch, and 4.5 + 5.9 in two.
+// Of all tokens, whom every workgroup quantises: 64 tokens of 1024 take 13.4 us in one launch, and 3.2 + 6.2 in two.
 static constexpr int64_t FEW_VALUES = 1 << 15;
 template <typename TO, int FN, int NW, int NV>
 __global__ __launch_bounds__(NW * 64) void int8_few_tokens_kernel(const Int8FewP a) {
@@ -194,11 +194,11 @@ static void product(Int8P p, hipStream_t s) {
   }
   // 256x256 blocks stage and read the fewest bytes a product, one a CU: where they fill whole rounds of the chip and
   // their start and end count little.  128x192 ones, two a CU, where they leave few CUs idle; else 64x64 ones, with a
-  // deeper ring where two a CU hold them all.  (us, 256x256 / 128x192 / 64x64 with two stages / with four.
-  // 16384 x 4096 x 4096 217 / 238 / 346 / -, 8192 x 4096 x 1024 39 / 42 / 59 / -, 5000 x 4096 x 1024 34 / 28.6 / 38 / -,
-  // 2688 x 32000 x 256 56 / 53 / 63 / -, 2688 x 4096 x 1024 19.7 / 16.6 / 20.8 / 26, 2688 x 2048 x 1024 - / 10.6 / 12.2 /
-  // 14.5, 2688 x 1024 x 4096 49 / 26.5 / 19.7 / 22.9, 1000 x 1000 x 8192 83 / 49 / 31.7 / 20.5, 1000 x 2048 x 1024
-  // - / 9.8 / 5.7 / 5.9.)
+  // deeper ring where two a CU hold them all.  (us on uniform integers, 256x256 / 128x192 / 64x64 with two stages / with four.
+  // 16384 x 4096 x 4096 237 / 264 / 407 / 440, 8192 x 4096 x 1024 44 / 48 / 66 / 74, 5000 x 4096 x 1024 37 / 32 / 43 / 47,
+  // 2688 x 32000 x 256 61 / 59 / 74 / 93, 2688 x 4096 x 1024 20.7 / 18.2 / 22.3 / 26.9, 2688 x 2048 x 1024 18.5 / 11.3 / 13.5 /
+  // 15.3, 2688 x 1024 x 4096 46 / 27.0 / 21.1 / 24.6, 1000 x 1000 x 8192 81 / 47 / 31.9 / 20.2, 1000 x 2048 x 1024
+  // 17.5 / 10.2 / 6.3 / 6.4.  The values decide the clock: the first takes 191 on zeros.)
   const int64_t big = cdiv(p.M, 256) * cdiv(p.N, 256), rounds = cdiv(big, 256) * 256;
   if (p.K >= 1024 && 5 * big >= 4 * rounds) int8_tile_launch<TO, 256, 256, 4, 4, 128, 2>(p, s);
   else if (cdiv(p.M, 192) * cdiv(p.N, 128) >= 192) int8_tile_launch<TO, 128, 192, 2, 4, 128, 2>(p, s);

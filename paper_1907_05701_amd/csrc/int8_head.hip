@@ -357,7 +357,8 @@ struct HeadLogProb {
 };
 
 // Any row, its logits computed again in every pass: one with a NaN or infinities, with a scale beyond SCALE_MAX or a
-// reference beyond REF_MAX, with fewer than k classes above FLOOR, or with too many that reach the threshold.
+// reference beyond REF_MAX, with fewer than k classes above FLOOR, or with too many that reach the threshold.  (3.0 ms for up
+// to 16 frames of 32000 classes and 256 columns, 17.5 for 2688: a lane computes a class, seven times.)
 __device__ __forceinline__ void head_any(HeadLds& h, const Logit& logit, const HeadP& p, const HeadOut& o, int64_t m) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, K = p.K;
   float mx = -INFINITY;

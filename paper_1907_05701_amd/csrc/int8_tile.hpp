@@ -104,7 +104,8 @@ void int8_tile_kernel(const Int8P p) {
   for (int j = 0; j < FN; ++j) xs[j] = p.xs[min(m0 + wn * (BN / WN) + j * 16 + fr, p.M - 1)];
   if constexpr (std::is_same<TO, bf16>::value && FM % 2 == 0) {
     // two fragments' 16 channels side by side: rows of 16 lanes trade places, so that a lane stores 8 adjacent channels
-    // and an instruction 64 bytes of each token (at any alignment: 3153 x 4268 x 1024 23.5 us, 29.9 by four channels; x 4267 29.0 and 31.7)
+    // and an instruction 64 bytes of each token (at any alignment; us, so / by four channels: 16384 x 4096 x 4096
+    // 238 / 265, 3153 x 4268 x 1024 22.8 / 30.9, x 4267 28.3 / 30.3)
 #pragma unroll
     for (int i = 0; i < FM; i += 2) {
       const int64_t n = n0 + wm * (BM / WM) + i * 16;

@@ -422,7 +422,6 @@ __global__ __launch_bounds__(256) void score_grad_wave_kernel(const TI* logits, 
 // ---------------------------------------------------------------------------
 // Host side.
 // ---------------------------------------------------------------------------
-// Values a lane of a wave that has a row.
 // Rows that a wave holds are a workgroup of one wave each: its barriers wait for nobody, and a CU has 32 rows.  A few long
 // rows are done sooner by more threads each.  (us, by a wave / by a workgroup of 256; 8 most likely classes: 20000 float32
 // rows of 100 13.1 / 38.3, 5000 bf16 rows of 1000 6.9 / 12.9, 12000 of 1500 17.2 / 34.1, of 3500 27.4 / 31.4, one of 3000
