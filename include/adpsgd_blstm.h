@@ -456,7 +456,7 @@ int int8_linear_rows(const void* x, int64_t ldx, int64_t M, int32_t K, int32_t p
  * x [M][P] and weights w [K][Kw] of K classes.  The logits are the same bits as there.  Frames with fewer than k
  * classes above -1e30, or with more than 512 next to the k-th (k near K / 16 and above, K > 512), are computed in several
  * passes over all classes, some 3 ms and more for 32000: the two calls in turn are faster for those.
- *   ws  int8_logprob_ws_bytes(M, K, Kw) bytes, as above. */
+ *   ws  int8_logprob_ws_bytes(M, K, Kw) bytes, as above.  Either size is enough for fewer rows too. */
 int int8_logprob_ws_bytes(int64_t M, int32_t K, int32_t Kw, size_t* bytes);
 int int8_logprob_rows(const void* x, int64_t ldx, int64_t M, int32_t P, int32_t precision, const int8_t* w, int64_t ldw,
                       const float* w_scale, int32_t K, int32_t Kw, const float* bias, const softmax_scores* scores,

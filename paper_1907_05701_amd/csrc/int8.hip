@@ -318,10 +318,8 @@ extern "C" int int8_linear_rows(const void* x, int64_t ldx, int64_t M, int32_t K
 // The head (int8_head.hip); tokens of more columns than that holds: logits of rows at a time, scored.
 // ---------------------------------------------------------------------------
 // Frames that the head takes at a time: equal parts, of at most about 180 MB of group maxima (K / 4 bytes a frame) and tokens.
-static int64_t head_frames(int64_t M, int64_t K, int64_t Kw) {
-  const int64_t most = (180 << 20) / (Kw + 16 * cdiv(K, 64) + 64);
-  return cdiv(M, cdiv(M, most));
-}
+static int64_t head_most(int64_t K, int64_t Kw) { return (180 << 20) / (Kw + 16 * cdiv(K, 64) + 64); }
+static int64_t head_frames(int64_t M, int64_t K, int64_t Kw) { return cdiv(M, cdiv(M, head_most(K, Kw))); }
 static int64_t logit_rows(int64_t M, int64_t K) { return std::min(M, std::max<int64_t>(64, (180 << 20) / (4 * rup(K, 4)))); }
 
 extern "C" int int8_logprob_ws_bytes(int64_t M, int32_t K, int32_t Kw, size_t* bytes) {
@@ -330,12 +328,8 @@ extern "C" int int8_logprob_ws_bytes(int64_t M, int32_t K, int32_t Kw, size_t* b
   if (K > SOFTMAX_MAX_CLASSES || Kw > INT8_MAX_K) return blstm_fail(BLSTM_EUNSUPPORTED, "int8_logprob_ws_bytes: too many classes or columns");
   if (!bytes) return BLSTM_OK;
   const int32_t cols = (int32_t)rup(Kw, 16);
-  if (int8_head_fits(Kw)) {
-    const int64_t n = head_frames(M, K, cols);   // (the last part may be shorter, and its ranges of classes more)
-    *bytes = std::max(int8_head_bytes(n, K, cols), int8_head_bytes(M - (cdiv(M, n) - 1) * n, K, cols));
-  } else {
-    *bytes = tokens_bytes(M, cols) + (size_t)logit_rows(M, K) * rup(K, 4) * 4;
-  }
+  *bytes = int8_head_fits(Kw) ? int8_head_bytes(std::min(M, head_most(K, cols)), K, cols)
+                              : tokens_bytes(M, cols) + (size_t)logit_rows(M, K) * rup(K, 4) * 4;
   return BLSTM_OK;
 }
 

@@ -204,7 +204,7 @@ template <typename TI>
 void int8_quantize(const TI* x, int64_t ldx, int64_t M, int32_t K, int8_t* q, int64_t ldq, int32_t Kq, float* scale,
                    hipStream_t stream);
 
-// Log probabilities of a head of K classes from tokens x [M][P] (int8_head.hip); buf: int8_head_bytes.  For up to
+// Log probabilities of a head of K classes from tokens x [M][P] (int8_head.hip); buf: int8_head_bytes of as many frames or more.  For up to
 // so many columns:
 bool int8_head_fits(int32_t Kw);
 size_t int8_head_bytes(int64_t M, int32_t K, int32_t Kw);

@@ -610,8 +610,9 @@ __global__ __launch_bounds__(FT, 6) void int8_head_finish_kernel(const HeadP p, 
 // ---------------------------------------------------------------------------
 struct HeadPlan {
   int fn, fw, ks;                 // frames / 16 of a wave, waves along the frames, most column steps
-  int nf, ranges, per, ngroup;
-  size_t stats, gmax, bytes;      // behind the tokens
+  int nf, ngroup, ranges, per;
+  int64_t units, slots, most;     // runs of classes that may not be parted; workgroups at a time; most ranges
+  size_t stats, gmax;             // behind the tokens
 };
 static constexpr int HEAD_MAX_STEPS = 16;
 
@@ -627,7 +628,7 @@ static int head_slots(int fn, int fw, int ks) {
   return 256 * (int)std::min<size_t>(head_per_cu(ks), 160 * 1024 / head_lds(fn, fw, ks));
 }
 
-static HeadPlan head_plan(int64_t M, int32_t K, int32_t Kw) {
+static HeadPlan head_shape(int64_t M, int32_t K, int32_t Kw) {
   HeadPlan h{};
   h.ks = Kw <= 64 ? 1 : Kw <= 128 ? 2 : Kw <= 256 ? 4 : Kw <= 512 ? 8 : HEAD_MAX_STEPS;
   h.fn = h.ks > 8 || M <= 16 ? 1 : 2;
@@ -635,28 +636,47 @@ static HeadPlan head_plan(int64_t M, int32_t K, int32_t Kw) {
   h.fw = M <= frames ? 1 : M <= 2 * frames ? 2 : 4;
   h.nf = (int)cdiv(M, frames * h.fw);
   const int tg = group_tiles(h.fw);
-  const int64_t units = cdiv(K, CT * tg), slots = head_slots(h.fn, h.fw, h.ks);
+  h.units = cdiv(K, CT * tg);
+  h.slots = head_slots(h.fn, h.fw, h.ks);
+  h.ngroup = (int)h.units * (4 / h.fw) * 4;
+  // (of one tile of frames, two rounds are never shorter than one of ranges twice as long)
+  h.most = std::min(h.units, std::max<int64_t>(1, (h.nf == 1 ? 1 : 2) * h.slots / h.nf));
+  return h;
+}
+static HeadPlan head_plan(int64_t M, int32_t K, int32_t Kw) {
+  HeadPlan h = head_shape(M, K, Kw);
+  const int tg = group_tiles(h.fw);
   // as many ranges as take least: whole rounds of the chip, each as long as a range and its start
   int64_t best = -1, per = 1;
-  for (int64_t r = 1; r <= units && r <= std::max<int64_t>(1, 2 * slots / h.nf); ++r) {
-    const int64_t u = cdiv(units, r), t = cdiv(cdiv(units, u) * h.nf, slots) * (u * tg + 1);
+  for (int64_t r = 1; r <= h.most; ++r) {
+    const int64_t u = cdiv(h.units, r), t = cdiv(cdiv(h.units, u) * h.nf, h.slots) * (u * tg + 1);
     if (best < 0 || t < best) {
       best = t;
       per = u;
     }
   }
   h.per = (int)per * tg;
-  h.ranges = (int)cdiv(units, per);
-  h.ngroup = (int)units * (4 / h.fw) * 4;
+  h.ranges = (int)cdiv(h.units, per);
   h.stats = 0;
   h.gmax = (size_t)rup(M * h.ranges * 16, 256);
-  h.bytes = h.gmax + (size_t)rup(M * h.ngroup * 4, 256);
   return h;
 }
 
 bool int8_head_fits(int32_t Kw) { return cdiv(Kw, 64) <= HEAD_MAX_STEPS; }
 static size_t ints_bytes(int64_t M, int32_t Kw) { return (size_t)(rup(M * Kw, 256) + rup(M * 4, 256)); }
-size_t int8_head_bytes(int64_t M, int32_t K, int32_t Kw) { return ints_bytes(M, Kw) + head_plan(M, K, Kw).bytes; }
+// For every number of frames up to M: the shapes change behind 16, 32 and 64 frames, and of one shape more frames have more
+// tokens and maxima; their statistics, M times ranges, are at most M times `units`, and at most those of whole tiles in
+// two rounds (one round of one tile) or of one range.
+size_t int8_head_bytes(int64_t M, int32_t K, int32_t Kw) {
+  size_t bytes = 0;
+  for (const int64_t end : {(int64_t)16, (int64_t)32, (int64_t)64, M}) {
+    const int64_t m = std::min(end, M);
+    const HeadPlan h = head_shape(m, K, Kw);
+    const int64_t stats = h.nf == 1 ? m * h.most : std::min(m * h.units, std::max(m, 2 * h.slots * 16 * h.fn * h.fw));
+    bytes = std::max(bytes, ints_bytes(m, Kw) + (size_t)rup(stats * 16, 256) + (size_t)rup(m * h.ngroup * 4, 256));
+  }
+  return bytes;
+}
 
 template <typename TI>
 int int8_head(const TI* x, int64_t ldx, int64_t M, int32_t P, const int8_t* w, int64_t ldw, const float* ws, int32_t K,

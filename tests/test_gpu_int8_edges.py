@@ -162,3 +162,20 @@ def test_head_on_either_side_of_the_largest_reference(gpu_lib, M):
         t8.check_head(x, w, ws * size, bias, ids, 9)
     for tau in (2.0 ** -19, 2.0 ** -21, 2.0 ** -23, 2.0 ** -25):
         t8.check_head(x, w, ws, bias, ids, 9, tau)
+
+
+@pytest.mark.parametrize("P,K", [(64, 900), (256, 9001), (500, 40000), (900, 700), (1100, 300)])
+def test_one_workspace_for_batches_of_every_size(gpu_lib, P, K):
+    """A workspace of the largest batch serves the smaller ones with the same bits, and no call writes behind its own size."""
+    from paper_1907_05701_amd import binding as bd
+    most = 150
+    x, w, ws, bias, ids = t8.head_case(most, P, K, 2, "bf16")
+    kept = torch.empty(bd.int8_logprob_ws_bytes(most, *w.shape), dtype=torch.uint8, device="cuda")
+    for M in (most, 1, 16, 17, 32, 33, 64, 65, 129, 2):
+        need = bd.int8_logprob_ws_bytes(M, *w.shape)
+        own = torch.full((need + 4096,), 77, dtype=torch.uint8, device="cuda")
+        a = t8.head(x[:M], w, ws, bias, ids[:M], 5, buf=own[:need])
+        b = t8.head(x[:M], w, ws, bias, ids[:M], 5, buf=kept)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a[n], b[n]) for n in a), M
+        assert bool((own[need:] == 77).all()), M

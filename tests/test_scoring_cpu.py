@@ -206,3 +206,12 @@ def test_head_plans_for_the_workgroups_that_run_at_a_time(M):
     up = lambda n: -(-n // 256) * 256  # noqa: E731
     most = up(M * 512) + up(M * 4) + up(M * 256 * 16) + up(M * 1024 * waves * 4 * 4)
     assert bd.int8_logprob_ws_bytes(M, 131072, 512) <= most
+
+
+@pytest.mark.parametrize("K,Kw", [(100, 16), (1000, 256), (9001, 512), (32000, 256), (32000, 1024), (131072, 512), (1 << 18, 32), (5000, 1040)])
+def test_a_workspace_for_some_frames_is_enough_for_fewer(K, Kw):
+    """As a program keeps it that calls with batches of several sizes."""
+    sizes = [bd.int8_logprob_ws_bytes(M, K, Kw) for M in (*range(1, 400), *range(400, 6000, 37), 20000, 100000)]
+    assert sizes == sorted(sizes)
+    sizes = [bd.int8_linear_ws_bytes(M, Kw) for M in range(1, 400)]
+    assert sizes == sorted(sizes)
